@@ -404,6 +404,205 @@ jacap_status jacap_select_compact_inplace(const jacap_layout* layout, const floa
                                           int32_t preserve_order, void* ws, size_t ws_bytes, void* stream);
 
 /*
+ * Rotary positions: the first rot_dim channels of every head, as rot_dim / 2
+ * pairs (a, b), turned by the angle p f_i of the token's position p,
+ *   (a, b) -> amplitude (a cos - b sin, b cos + a sin),
+ * the other channels copied. Keys go into a cache turned, and queries meet
+ * them turned, so a loop calls this before jacap_append and jacap_attend.
+ *
+ * jacap_rope
+ *   head_dim     128 (else JACAP_ERR_UNSUPPORTED)
+ *   rot_dim      even, 2 to 128
+ *   interleaved  0: pair i is channels (i, i + rot_dim / 2); 1: (2 i, 2 i + 1)
+ *   amplitude    factor on sine and cosine (1; more with some scalings)
+ *   turns        device uint64 [rot_dim / 2]: f_i as a fraction of a turn,
+ *                round(2^64 f_i / 2 pi) modulo 2^64, so that p f_i is exact
+ *                modulo one turn for every int32 p. A scaling for long contexts
+ *                changes the f_i.
+ * jacap_rope_tensor
+ *   x, y         device; element (s, t, h, c) at s strides[0] + t strides[1] +
+ *                h strides[2] + c (elements). y == x works in place (with equal
+ *                strides); x and y must not overlap otherwise. Rows of 16-byte
+ *                aligned addresses and strides whose pairs no 16-byte piece
+ *                splits are read and written in 16-byte pieces.
+ *
+ * positions: device int32, token (s, t) at s position_strides[0] + t
+ * position_strides[1]; negative positions turn backwards. inverse = 1 turns
+ * back (by the negative angle), which is the gradient with respect to x. q or k
+ * may be NULL (one of them is given). Zero requests or tokens are no work.
+ */
+typedef struct {
+  int32_t head_dim, rot_dim, interleaved;
+  float amplitude;
+  const uint64_t* turns;
+} jacap_rope;
+typedef struct {
+  const void* x;
+  void* y;
+  int32_t heads;
+  int64_t x_strides[3], y_strides[3]; /* request, token, head */
+} jacap_rope_tensor;
+jacap_status jacap_rotate(const jacap_rope* rope, jacap_dtype dtype, int32_t num_seqs, int32_t tokens,
+                          const int32_t* positions, const int64_t* position_strides, int32_t inverse,
+                          const jacap_rope_tensor* q, const jacap_rope_tensor* k, void* stream);
+
+/*
+ * Attention of each request's last queries over its cached tokens and, if given,
+ * over drafted tokens that are not in the cache yet: one token (a decode step),
+ * a chain, or a tree whose tokens see their ancestors.
+ *
+ * The layout is that of the cache; `window` (T, at most 64, else
+ * JACAP_ERR_UNSUPPORTED) is the number of queries per request and head, and the
+ * q strides are those of q. Row (s, l, h, t) sees the first lengths[s] tokens of
+ * its request and the drafted tokens j of its mask:
+ *   logit = scale q . k,  o = sum softmax(logit) v,  lse = ln sum exp(logit).
+ * A row that sees nothing has o = 0 and lse = -inf. What a row does not see has
+ * no effect on it, NaN and infinities included.
+ *
+ *   scale          > 0 (1 / sqrt(128) for plain attention)
+ *   lengths        device int32 [num_seqs] (cached tokens of each request, the
+ *                  first ones of its range, 0 up to min(n_s, max_seqlen)), or
+ *                  NULL: all n_s. Read when the kernels run: a captured graph
+ *                  follows what the array holds.
+ *   draft_lens     device int32 [num_seqs], 0 to T, or NULL: T. Queries (and
+ *                  drafted tokens) of each request; rows of o and lse from there
+ *                  on are left as they were.
+ *   k_draft, v_draft  device, the layout's dtype: row (s, l, g, j), j < T, at s
+ *                  draft_strides[0] + l [1] + g [2] + j [3] of k_draft ([4 .. 7] of
+ *                  v_draft), strides of at least 128 and multiples of 16 bytes; both
+ *                  NULL: cached tokens only
+ *   tree           device uint64 [num_seqs][T]: bit j of entry (s, t): token t
+ *                  sees drafted token j (its ancestors and itself); bits from
+ *                  draft_lens[s] on are ignored. NULL: a chain, j <= t.
+ *   o_strides      of o, as those of q (request, layer, head, query)
+ *   lse            device float32 [num_seqs][num_layers][num_q_heads][T] or NULL
+ *   ws             device, 256-byte aligned, jacap_attend_workspace() bytes (0 for
+ *                  a layout that is refused), whose first 64 bytes were zeroed once:
+ *                  the status word. A length outside its range is clamped and
+ *                  reported there (JACAP_ERR_INVALID_ARG); the word stays set until
+ *                  it is zeroed again.
+ * o must not overlap an input. Sums are float32; with bf16 caches the softmax
+ * weights are rounded to bf16 for their product with V.
+ */
+typedef struct {
+  float scale;
+  const int32_t* lengths;
+  const int32_t* draft_lens;
+  const void* k_draft;
+  const void* v_draft;
+  int64_t draft_strides[8];
+  const uint64_t* tree;
+  int64_t o_strides[4];
+} jacap_attention;
+size_t jacap_attend_workspace(const jacap_layout* layout);
+jacap_status jacap_attend(const jacap_layout* layout, const jacap_attention* attn, const void* q,
+                          const void* k, const void* v, void* o, float* lse,
+                          void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * The attention weight that every cached token received from the last queries of
+ * its request: of n cached tokens and w queries, query j is that of token
+ * n - w + j and sees the tokens up to its own,
+ *   weights_i = [before_i] + sum over the group's heads and queries of
+ *               exp(scale q . k_i - lse),
+ * lse being the logarithm of each row's sum of exponentials. The scores of an
+ * eviction by accumulated attention: over a prompt's window after its prefill
+ * (before = NULL), or added up step by step while decoding.
+ *
+ * The layout is that of the cache with Q_win as for jacap_score; num_q_heads /
+ * num_kv_heads times window is at most 512 (else JACAP_ERR_UNSUPPORTED).
+ *   scale      > 0
+ *   lengths    device int32 [num_seqs] or NULL, as in jacap_attend (the device
+ *              reports a length outside [0, n_s] and does nothing)
+ *   q_lens     device int32 [num_seqs] or NULL: queries of each request, clamped
+ *              to [0, window]; w above
+ *   q_rows     device int32 [num_seqs][window] or NULL: which of the window's
+ *              queries is the j-th (the accepted path of a drafted tree); an entry
+ *              outside [0, window) is no query
+ *   lse_given  1: lse is an input, as jacap_attend wrote it for these queries (K is
+ *              then read once); 0: it is computed, and written unless NULL
+ *   lse        device float32 [num_seqs][num_layers][num_q_heads][window], indexed
+ *              like the queries (before q_rows); rows without a query are left alone.
+ *              A row that sees nothing has -inf and gives no weight.
+ *   before     device float32 [num_layers][num_kv_heads][total_tokens] or NULL; it
+ *              counts for tokens before the w queries' own (those are new: their
+ *              weights start from zero). May be `weights` itself.
+ *   weights    device float32, the same shape; rows past a request's length are left
+ *              as they were
+ *   ws         device, 256-byte aligned, jacap_weigh_workspace() bytes (0 for a
+ *              layout that is refused); the call resets its status word. A weight
+ *              that is not finite is reported there (JACAP_ERR_NONFINITE).
+ */
+typedef struct {
+  float scale;
+  const int32_t* lengths;
+  const int32_t* q_lens;
+  const int32_t* q_rows;
+  int32_t lse_given;
+} jacap_weighing;
+size_t jacap_weigh_workspace(const jacap_layout* layout);
+jacap_status jacap_weigh(const jacap_layout* layout, const jacap_weighing* how, const void* q_win,
+                         const void* k, float* lse, const float* before, float* weights,
+                         void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * jacap_select_compact by attention weights: per unit the first `sinks` and the
+ * last `recent` tokens stay, and of the others those of the largest weights (ties
+ * to the lower index), `budget` tokens in all (all n_s of them if there are no
+ * more).
+ *   weights      device float32 [num_layers][num_kv_heads][total_tokens], finite
+ *                and not negative (else JACAP_ERR_NONFINITE in the status word and
+ *                nothing is selected)
+ *   pos          NULL: first and last by row; or the tokens' tags (laid out as in
+ *                jacap_compact_inplace): a token stays if its tag is below `sinks`
+ *                or above the unit's largest tag less `recent`
+ *   sinks, recent  >= 0, together at most `budget`
+ *   weights_out  device float32 [num_layers][num_kv_heads][num_seqs][budget] or
+ *                NULL: the kept tokens' weights (0 where idx is -1)
+ *   keys         device float32, the shape of weights, not overlapping it: scratch
+ *   ws           device, 256-byte aligned, at least 64 bytes: the status word, zero
+ *                at first (a workspace of jacap_weigh serves; one that holds an error
+ *                selects nothing)
+ * The other arguments and results are those of jacap_select_compact.
+ */
+jacap_status jacap_select_weights(const jacap_layout* layout, const float* weights, const int32_t* pos,
+                                  int32_t sinks, int32_t recent, int32_t budget, int32_t* idx,
+                                  int32_t* kept, const void* k, const void* v, void* k_out, void* v_out,
+                                  float* weights_out, float* keys, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * The same selection with the retained cache in place, as
+ * jacap_select_compact_inplace leaves it: k, v, pos (unless NULL) and the weights
+ * move together. Here the weights are laid out as pos is (for a dense K as above; K's
+ * layer and head strides must be multiples of its token stride); those of rows from
+ * kept on are left as they were.
+ */
+jacap_status jacap_evict_weights(const jacap_layout* layout, float* weights, int32_t* pos, int32_t sinks,
+                                 int32_t recent, int32_t budget, int32_t* idx, int32_t* kept, void* k,
+                                 void* v, int32_t preserve_order, float* keys, void* ws, size_t ws_bytes,
+                                 void* stream);
+
+/*
+ * jacap_append for the accepted path of a drafted tree (or chain): of request s's
+ * drafted tokens the path[s][0 .. taken[s] - 1]-th go to rows lengths[s],
+ * lengths[s] + 1, ... of its slot, tagged ids[s], ids[s] + 1, ..., and their queries
+ * are merged into the running statistics in that order (unless stats and counts are
+ * NULL; q_new may be then).
+ *   window         of the layout: drafted tokens per request (its q strides are those
+ *                  of q_new)
+ *   strides        eight: request, layer, head, token of k_new, then of v_new
+ *   path           HOST int32 [num_seqs][depth], entries in [0, window)
+ *   taken          HOST int32 [num_seqs], 0 to depth; lengths[s] + taken[s] <= max_seqlen
+ * One launch per token of the longest path. The other arguments are those of
+ * jacap_append.
+ */
+jacap_status jacap_append_path(const jacap_layout* layout, const void* k_new, const void* v_new,
+                               const int64_t* strides, const void* q_new, const int32_t* path,
+                               int32_t depth, const int32_t* taken, const int32_t* lengths,
+                               const int32_t* ids, void* k, void* v, int32_t* pos, float* stats,
+                               int32_t* counts, void* stream);
+
+/*
  * Eviction of a cache held in host memory (an offloaded KV cache, Sec. 3.1):
  * the whole pass of jacap_score + jacap_select (+ jacap_compact) on caches that
  * stay in host memory, with the kept positions (and optionally the retained

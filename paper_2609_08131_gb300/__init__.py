@@ -85,6 +85,55 @@ class jacap_ws_offsets(ctypes.Structure):
     ]
 
 
+class jacap_rope(ctypes.Structure):
+    """Mirror of ``jacap_rope`` (include/jacap.h)."""
+
+    _fields_ = [
+        ("head_dim", ctypes.c_int32),
+        ("rot_dim", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32),
+        ("amplitude", ctypes.c_float),
+        ("turns", ctypes.c_void_p),
+    ]
+
+
+class jacap_rope_tensor(ctypes.Structure):
+    _fields_ = [
+        ("x", ctypes.c_void_p),
+        ("y", ctypes.c_void_p),
+        ("heads", ctypes.c_int32),
+        ("x_strides", ctypes.c_int64 * 3),
+        ("y_strides", ctypes.c_int64 * 3),
+    ]
+
+
+class jacap_attention(ctypes.Structure):
+    """Mirror of ``jacap_attention`` (include/jacap.h)."""
+
+    _fields_ = [
+        ("scale", ctypes.c_float),
+        ("lengths", ctypes.c_void_p),
+        ("draft_lens", ctypes.c_void_p),
+        ("k_draft", ctypes.c_void_p),
+        ("v_draft", ctypes.c_void_p),
+        ("draft_strides", ctypes.c_int64 * 8),
+        ("tree", ctypes.c_void_p),
+        ("o_strides", ctypes.c_int64 * 4),
+    ]
+
+
+class jacap_weighing(ctypes.Structure):
+    """Mirror of ``jacap_weighing`` (include/jacap.h)."""
+
+    _fields_ = [
+        ("scale", ctypes.c_float),
+        ("lengths", ctypes.c_void_p),
+        ("q_lens", ctypes.c_void_p),
+        ("q_rows", ctypes.c_void_p),
+        ("lse_given", ctypes.c_int32),
+    ]
+
+
 _P = ctypes.c_void_p
 _SIGS = {
     "jacap_workspace_size": (ctypes.c_size_t, [ctypes.POINTER(jacap_layout), ctypes.c_int32]),
@@ -118,6 +167,24 @@ _SIGS = {
                                                  ctypes.c_int32]),
     "jacap_evict_host": (ctypes.c_int, [ctypes.POINTER(jacap_layout), ctypes.POINTER(jacap_params), ctypes.c_int32,
                                         ctypes.c_int32, _P, _P, _P, _P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P, _P]),
+    "jacap_rotate": (ctypes.c_int, [ctypes.POINTER(jacap_rope), ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _P,
+                                    ctypes.POINTER(ctypes.c_int64), ctypes.c_int32,
+                                    ctypes.POINTER(jacap_rope_tensor), ctypes.POINTER(jacap_rope_tensor), _P]),
+    "jacap_attend_workspace": (ctypes.c_size_t, [ctypes.POINTER(jacap_layout)]),
+    "jacap_attend": (ctypes.c_int, [ctypes.POINTER(jacap_layout), ctypes.POINTER(jacap_attention), _P, _P, _P, _P, _P,
+                                    _P, ctypes.c_size_t, _P]),
+    "jacap_weigh_workspace": (ctypes.c_size_t, [ctypes.POINTER(jacap_layout)]),
+    "jacap_weigh": (ctypes.c_int, [ctypes.POINTER(jacap_layout), ctypes.POINTER(jacap_weighing), _P, _P, _P, _P, _P,
+                                   _P, ctypes.c_size_t, _P]),
+    "jacap_select_weights": (ctypes.c_int, [ctypes.POINTER(jacap_layout), _P, _P, ctypes.c_int32, ctypes.c_int32,
+                                            ctypes.c_int32, _P, _P, _P, _P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P]),
+    "jacap_evict_weights": (ctypes.c_int, [ctypes.POINTER(jacap_layout), _P, _P, ctypes.c_int32, ctypes.c_int32,
+                                           ctypes.c_int32, _P, _P, _P, _P, ctypes.c_int32, _P, _P, ctypes.c_size_t,
+                                           _P]),
+    "jacap_append_path": (ctypes.c_int, [ctypes.POINTER(jacap_layout), _P, _P, ctypes.POINTER(ctypes.c_int64), _P,
+                                         ctypes.POINTER(ctypes.c_int32), ctypes.c_int32,
+                                         ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(ctypes.c_int32),
+                                         ctypes.POINTER(ctypes.c_int32), _P, _P, _P, _P, _P, _P]),
     "jacap_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     "jacap_schedule_info": (ctypes.c_int32, [ctypes.POINTER(jacap_layout), ctypes.POINTER(jacap_params),
                                              ctypes.POINTER(ctypes.c_int32)]),
@@ -242,6 +309,56 @@ def jacap_evict_host(layout, params, budget, group_layers, q_win_host, k_host, v
     return lib().jacap_evict_host(ctypes.byref(layout), ctypes.byref(params), budget, group_layers, q_win_host,
                                   k_host, v_host, out_factor, idx_host, kept_host, k_out_host, v_out_host, dev_buf,
                                   dev_bytes, stream, copy_stream)
+
+
+def jacap_rotate(rope, dtype, num_seqs, tokens, positions, position_strides, inverse, q, k, stream) -> int:
+    """``q``, ``k``: ``jacap_rope_tensor`` or None; ``position_strides``: two element strides."""
+    return lib().jacap_rotate(ctypes.byref(rope), dtype, num_seqs, tokens, positions,
+                              (ctypes.c_int64 * 2)(*position_strides), int(inverse),
+                              None if q is None else ctypes.byref(q), None if k is None else ctypes.byref(k), stream)
+
+
+def jacap_attend_workspace(layout: jacap_layout) -> int:
+    return lib().jacap_attend_workspace(ctypes.byref(layout))
+
+
+def jacap_attend(layout, attn: jacap_attention, q, k, v, o, lse, ws, ws_bytes, stream) -> int:
+    return lib().jacap_attend(ctypes.byref(layout), ctypes.byref(attn), q, k, v, o, lse, ws, ws_bytes, stream)
+
+
+def jacap_weigh_workspace(layout: jacap_layout) -> int:
+    return lib().jacap_weigh_workspace(ctypes.byref(layout))
+
+
+def jacap_weigh(layout, how: jacap_weighing, q_win, k, lse, before, weights, ws, ws_bytes, stream) -> int:
+    return lib().jacap_weigh(ctypes.byref(layout), ctypes.byref(how), q_win, k, lse, before, weights, ws, ws_bytes,
+                             stream)
+
+
+def jacap_select_weights(layout, weights, pos, sinks, recent, budget, idx, kept, k, v, k_out, v_out, weights_out, keys,
+                         ws, ws_bytes, stream) -> int:
+    return lib().jacap_select_weights(ctypes.byref(layout), weights, pos, sinks, recent, budget, idx, kept, k, v, k_out,
+                                      v_out, weights_out, keys, ws, ws_bytes, stream)
+
+
+def jacap_evict_weights(layout, weights, pos, sinks, recent, budget, idx, kept, k, v, preserve_order, keys, ws,
+                        ws_bytes, stream) -> int:
+    return lib().jacap_evict_weights(ctypes.byref(layout), weights, pos, sinks, recent, budget, idx, kept, k, v,
+                                     int(preserve_order), keys, ws, ws_bytes, stream)
+
+
+def jacap_append_path(layout, k_new, v_new, strides, q_new, path, depth, taken, lengths, ids, k, v, pos, stats, counts,
+                      stream) -> int:
+    """``strides``: eight element strides (request, layer, head, token of k_new, then of v_new); ``path``: a sequence
+    of ``depth`` drafted tokens per request; ``taken``, ``lengths``, ``ids``: sequences of ints, one per request."""
+    n = len(lengths)
+    flat = [int(t) for p in path for t in p]
+    if len(path) != n or len(taken) != n or len(ids) != n or any(len(p) != depth for p in path):
+        raise ValueError("one path of `depth` tokens, count, length and id per request")
+    ints = ctypes.c_int32 * n
+    return lib().jacap_append_path(ctypes.byref(layout), k_new, v_new, (ctypes.c_int64 * 8)(*strides), q_new,
+                                   (ctypes.c_int32 * max(1, len(flat)))(*flat), depth, ints(*map(int, taken)),
+                                   ints(*map(int, lengths)), ints(*map(int, ids)), k, v, pos, stats, counts, stream)
 
 
 def jacap_device_status(ws, stream) -> int:

@@ -23,7 +23,8 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libjacap.so")
 
 SOURCES = ["jacap_api.cu", "k_stream.cu", "k_kpass.cu", "k_gram.cu", "k_factor.cu", "k_score.cu", "k_select.cu",
-           "jacap_static.cu", "k_kfull.cu", "k_decode.cu", "jacap_host.cu", "k_fused.cu"]
+           "jacap_static.cu", "k_kfull.cu", "k_decode.cu", "jacap_host.cu", "k_fused.cu", "jacap_attn.cu", "k_attend.cu",
+           "k_weigh.cu", "k_rope.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 CFLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr",
           "-I" + INCLUDE, "-I" + CSRC]
@@ -134,4 +135,12 @@ EXPORTS = [
     "jacap_workspace_offsets",
     "jacap_host_buffer_size",
     "jacap_evict_host",
+    "jacap_rotate",
+    "jacap_attend_workspace",
+    "jacap_attend",
+    "jacap_weigh_workspace",
+    "jacap_weigh",
+    "jacap_select_weights",
+    "jacap_evict_weights",
+    "jacap_append_path",
 ]

@@ -6,7 +6,9 @@ libjacap's kernels. Errors from the library raise ``JacapError``.
 
 from __future__ import annotations
 
+import contextlib
 import ctypes
+import math
 from dataclasses import dataclass
 
 import torch
@@ -16,12 +18,20 @@ from . import (
     JACAP_F32,
     JACAP_OK,
     jacap_append,
+    jacap_append_path,
+    jacap_attend,
+    jacap_attend_workspace,
+    jacap_attention,
     jacap_compact,
     jacap_device_status,
     jacap_evict_host,
+    jacap_evict_weights,
     jacap_host_buffer_size,
     jacap_layout,
     jacap_params,
+    jacap_rope,
+    jacap_rope_tensor,
+    jacap_rotate,
     jacap_schedule_info,
     jacap_score,
     jacap_score_timed,
@@ -30,8 +40,12 @@ from . import (
     jacap_select,
     jacap_select_compact,
     jacap_select_compact_inplace,
+    jacap_select_weights,
     jacap_stats_update,
     jacap_status_string,
+    jacap_weigh,
+    jacap_weigh_workspace,
+    jacap_weighing,
     jacap_workspace_offsets,
     jacap_workspace_size,
 )
@@ -98,6 +112,317 @@ class Cache:
         lay.q_stride_seq, lay.q_stride_layer, lay.q_stride_head, lay.q_stride_pos = (
             q.stride(0), q.stride(1), q.stride(2), q.stride(3))
         return lay
+
+
+@contextlib.contextmanager
+def _on(device, stream):
+    """The device current, and `stream` (the device's current one if None) for what is
+    allocated and enqueued inside; yields the stream's handle."""
+    with torch.cuda.device(device):
+        if stream is None:
+            yield _stream(torch.cuda.current_stream(device))
+        else:
+            if stream.device != device:
+                raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
+            with torch.cuda.stream(stream):
+                yield _stream(stream)
+
+
+def _tensor(name, t, device, dtype, shape, contiguous=False):
+    """Checks a tensor argument; None passes."""
+    if t is None:
+        return
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on {device}")
+    if torch.is_grad_enabled() and t.requires_grad:
+        raise ValueError(f"{name} requires a gradient, which this call does not give")
+    if contiguous and not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if not contiguous and len(shape) > 1 and shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"the last axis of {name} must be contiguous")
+
+
+def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling=None):
+    """(frequencies, amplitude): the rot_dim / 2 angles per position in 64 bits,
+    base^(-2 i / rot_dim), changed for long contexts by ``scaling``:
+
+      None
+      ("linear", factor)    positions divided by factor
+      ("ntk", factor)       base multiplied by factor^(rot_dim / (rot_dim - 2))
+      ("llama3", factor, low, high, length)   pairs that turn fewer than `low` times over
+                            the original `length` divided by factor, those that turn more
+                            than `high` times kept, a ramp in the turns between
+      ("yarn", factor, length, fast, slow)    pairs that turn `fast` times or more over
+                            `length` kept, `slow` times or fewer divided by factor, a ramp
+                            in the pair's number between; amplitude 0.1 ln(factor) + 1
+    """
+    if rot_dim < 2 or rot_dim > 128 or rot_dim % 2:
+        raise ValueError("rot_dim must be even, 2 to 128")
+    if not (base > 0 and math.isfinite(base)):
+        raise ValueError("base must be positive")
+    kind, args = (None, ()) if scaling is None else (scaling[0], tuple(scaling[1:]))
+    wanted = {None: 0, "linear": 1, "ntk": 1, "llama3": 4, "yarn": 4}
+    if kind not in wanted or len(args) != wanted[kind]:
+        raise ValueError(f"unknown scaling {scaling!r}")
+    if args and not args[0] > 0:
+        raise ValueError("the scaling factor must be positive")
+    half = rot_dim // 2
+    if kind == "ntk":
+        if rot_dim == 2:
+            raise ValueError("ntk scaling needs more than one pair")
+        base = base * args[0] ** (rot_dim / (rot_dim - 2))
+    f = [base ** (-2.0 * i / rot_dim) for i in range(half)]
+    if kind == "linear":
+        f = [x / args[0] for x in f]
+    elif kind == "llama3":
+        factor, low, high, length = args
+        if not high > low:
+            raise ValueError("llama3 scaling needs low < high")
+        keep = [min(max((length * x / (2 * math.pi) - low) / (high - low), 0.0), 1.0) for x in f]
+        f = [x * (k + (1 - k) / factor) for x, k in zip(f, keep)]
+    elif kind == "yarn":
+        factor, length, fast, slow = args
+        if not fast > slow > 0:
+            raise ValueError("yarn scaling needs fast > slow > 0")
+        at = [rot_dim * math.log(length / (turns * 2 * math.pi)) / (2 * math.log(base)) for turns in (fast, slow)]
+        lo, hi = max(math.floor(at[0]), 0), min(math.ceil(at[1]), rot_dim - 1)
+        keep = [1 - min(max((i - lo) / max(hi - lo, 0.001), 0.0), 1.0) for i in range(half)]
+        f = [x * (k + (1 - k) / factor) for x, k in zip(f, keep)]
+        return f, 0.1 * math.log(factor) + 1.0 if factor > 1 else 1.0
+    return f, 1.0
+
+
+class Rope:
+    """Rotary positions (``jacap_rotate``): the first ``rot_dim`` channels of every
+    head, in pairs (i, i + rot_dim / 2) or, interleaved, (2 i, 2 i + 1), turned by
+    position times the pair's frequency (``rope_frequencies``). Keeps the frequencies on
+    the device; exact to float32 for every int32 position."""
+
+    def __init__(self, rot_dim: int = 128, base: float = 10000.0, interleaved: bool = False, scaling=None,
+                 device="cuda"):
+        freq, amplitude = rope_frequencies(rot_dim, base, scaling)
+        self.rot_dim, self.amplitude, self.interleaved = int(rot_dim), float(amplitude), bool(interleaved)
+        turns = [round(f / (2 * math.pi) * 2.0 ** 64) % (1 << 64) for f in freq]
+        self.turns = torch.tensor([t - (1 << 64) if t >> 63 else t for t in turns], dtype=torch.int64, device=device)
+        self.device = self.turns.device
+        self._c = jacap_rope()
+        self._c.head_dim, self._c.rot_dim, self._c.interleaved = 128, self.rot_dim, int(self.interleaved)
+        self._c.amplitude, self._c.turns = self.amplitude, self.turns.data_ptr()
+
+    def apply(self, q, k, positions, inverse: bool = False, inplace: bool = False, stream=None):
+        """q, k: [..., heads, 128] (one of them may be None) with one or two leading axes,
+        of any strides but the last axis' (float32 or bfloat16); positions: int32 of the
+        leading axes' shape. Returns the turned (q, k): new tensors, or the same ones
+        with ``inplace``. ``inverse`` turns back (and is the gradient)."""
+        given = [(n, t) for n, t in (("q", q), ("k", k)) if t is not None]
+        if not given:
+            raise ValueError("q or k must be given")
+        lead, dtype = tuple(given[0][1].shape[:-2]), given[0][1].dtype
+        if len(lead) not in (1, 2) or dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError("q and k must be float32 or bfloat16 [tokens, heads, 128] or [requests, tokens, heads, 128]")
+        for name, t in given:
+            _tensor(name, t, self.device, dtype, lead + (t.shape[-2], 128))
+            if t.shape[-2] < 1:
+                raise ValueError(f"{name} has no heads")
+        if (not isinstance(positions, torch.Tensor) or positions.dtype != torch.int32 or positions.device != self.device
+                or tuple(positions.shape) != lead):
+            raise ValueError(f"positions must be an int32 tensor of shape {lead} on {self.device}")
+        S, T = lead if len(lead) == 2 else (1, lead[0])
+        ps = positions.stride() if len(lead) == 2 else (0, positions.stride(0))
+        with _on(self.device, stream) as st:
+            out, args = [None, None], [None, None]
+            for i, t in enumerate((q, k)):
+                if t is None:
+                    continue
+                y = t if inplace else torch.empty_like(t)
+                x = jacap_rope_tensor()
+                x.x, x.y, x.heads = t.data_ptr(), y.data_ptr(), t.shape[-2]
+                for into, src in ((x.x_strides, t), (x.y_strides, y)):
+                    into[:] = src.stride()[:-1] if len(lead) == 2 else (0,) + src.stride()[:-1]
+                out[i], args[i] = y, x
+            if S and T:
+                _check(jacap_rotate(self._c, JACAP_BF16 if dtype == torch.bfloat16 else JACAP_F32, S, T,
+                                    _ptr(positions), ps, inverse, args[0], args[1], st), "jacap_rotate")
+        return out[0], out[1]
+
+
+def tree_masks(parents):
+    """The masks of drafted trees for ``CacheAttention``: ``parents[s][t]`` is the drafted
+    token that token t of request s follows (before t), or -1 for the cached ones. Returns
+    int64 [S, T] on the host: bit j of entry (s, t) says that token t sees token j."""
+    rows = []
+    for p in parents:
+        row = []
+        for t, at in enumerate(p):
+            if not -1 <= at < t or t >= 64:
+                raise ValueError("a token's parent is -1 or an earlier token, of at most 64")
+            row.append((row[at] if at >= 0 else 0) | 1 << t)
+        rows.append([m - (1 << 64) if m >> 63 else m for m in row])
+    return torch.tensor(rows, dtype=torch.int64)
+
+
+def _query_strides(lay, q):
+    """q's strides into the layout (that of an axis of one entry means nothing and may be anything)."""
+    lay.q_stride_seq, lay.q_stride_layer, lay.q_stride_head, lay.q_stride_pos = [
+        st if n > 1 else 128 for n, st in zip(q.shape[:4], q.stride()[:4])]
+    return lay
+
+
+class CacheAttention:
+    """Attention of each request's last queries over its cached tokens and, if given, over
+    drafted tokens that are not in the cache yet (``jacap_attend``): one token, a chain, or
+    a tree (``tree_masks``). ``cache.q_win`` [S, L, Hq, T, 128] gives the shape of the
+    queries (T at most 64) and the default ones. Owns the workspace and the outputs
+    ``o`` [S, L, Hq, T, 128] and ``lse`` [S, L, Hq, T] (float32), which each run overwrites."""
+
+    def __init__(self, cache: Cache, scale: float | None = None):
+        self.cache = cache
+        self.device, self.dtype = cache.k.device, cache.k.dtype
+        q = cache.q_win
+        if q.dim() != 5 or q.shape != (len(cache.seqlens), cache.k.shape[0], cache.num_q_heads, q.shape[3], 128):
+            raise ValueError("q_win must be [S, L, Hq, T, 128]")
+        S, L, Hq, T = q.shape[:4]
+        self.lay = _query_strides(cache.layout(), q)
+        nbytes = jacap_attend_workspace(self.lay)
+        if nbytes == 0:
+            raise JacapError(2 if T > 64 else 1, "jacap_attend_workspace")
+        self.ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        self.ws[:64].zero_()
+        self.o = torch.empty((S, L, Hq, T, 128), dtype=self.dtype, device=self.device)
+        self.lse = torch.empty((S, L, Hq, T), dtype=torch.float32, device=self.device)
+        self._attn = jacap_attention()
+        self._attn.scale = 1.0 / math.sqrt(128.0) if scale is None else float(scale)
+        self._attn.o_strides[:] = self.o.stride()[:4]
+
+    def run(self, q=None, k_draft=None, v_draft=None, tree=None, lengths=None, draft_lens=None, stream=None):
+        """q: [S, L, Hq, T, 128] (the cache's q_win if None); k_draft, v_draft: [S, L, Hkv,
+        T, 128]; tree: int64 [S, T] masks (None: a chain); lengths: int32
+        [S] cached tokens of each request (None: all); draft_lens: int32 [S] queries of
+        each request (None: T; rows behind are left as they were). Returns (o, lse)."""
+        c, a, dev = self.cache, self._attn, self.device
+        S, L, Hq, T = self.lse.shape
+        q = c.q_win if q is None else q
+        _tensor("q", q, dev, self.dtype, (S, L, Hq, T, 128))
+        _tensor("lengths", lengths, dev, torch.int32, (S,), True)
+        _tensor("draft_lens", draft_lens, dev, torch.int32, (S,), True)
+        _tensor("tree", tree, dev, torch.int64, (S, T), True)
+        if (k_draft is None) != (v_draft is None) or (tree is not None and k_draft is None):
+            raise ValueError("k_draft and v_draft come together, and a tree with them")
+        for name, t in (("k_draft", k_draft), ("v_draft", v_draft)):
+            _tensor(name, t, dev, self.dtype, (S, L, c.k.shape[1], T, 128))
+        if k_draft is not None:
+            # (the stride of an axis of one entry means nothing and may be anything)
+            a.draft_strides[:] = [st if n > 1 else 128 for t in (k_draft, v_draft)
+                                  for n, st in zip(t.shape[:4], t.stride()[:4])]
+        for name, t in (("lengths", lengths), ("draft_lens", draft_lens), ("tree", tree), ("k_draft", k_draft),
+                        ("v_draft", v_draft)):
+            setattr(a, name, None if t is None else t.data_ptr())
+        lay = _query_strides(self.lay, q)
+        with _on(dev, stream) as st:
+            _check(jacap_attend(lay, a, _ptr(q), _ptr(c.k), _ptr(c.v), _ptr(self.o), _ptr(self.lse), _ptr(self.ws),
+                                self.ws.numel(), st), "jacap_attend")
+        return self.o, self.lse
+
+    def check(self, stream=None):
+        _check_and_clear(self.ws, self.device, stream)
+
+
+def _check_and_clear(ws, device, stream):
+    """Raises what the status word holds, clearing it: a later call starts anew."""
+    with _on(device, stream) as st:
+        status = jacap_device_status(_ptr(ws), st)
+        if status != JACAP_OK:
+            ws[:64].zero_()
+    _check(status, "device status")
+
+
+class WeightEvictor:
+    """Eviction by accumulated attention: the tokens that received the most attention
+    weight from the last queries stay, beside the first ``sinks`` and the last ``recent``
+    ones (together at most ``budget``). ``cache.q_win`` [S, L, Hq, w, 128] are those
+    queries (Hq / Hkv times w at most 512), the last w tokens' own.
+
+    ``run()`` enqueues ``score()`` and ``select_compact()``. Buffers: ``weights``
+    [L, Hkv, N] and ``lse`` [S, L, Hq, w] (float32); ``idx``, ``kept``, ``k_out``,
+    ``v_out`` as ``Evictor``'s, and ``weights_out`` [L, Hkv, S, budget]."""
+
+    def __init__(self, cache: Cache, budget: int, sinks: int = 0, recent: int = 0, scale: float | None = None):
+        self.cache, self.budget = cache, int(budget)
+        self.sinks, self.recent = int(sinks), int(recent)
+        if self.budget < 1 or self.sinks < 0 or self.recent < 0 or self.sinks + self.recent > self.budget:
+            raise ValueError("the budget must be positive and hold the sinks and the recent tokens")
+        self.device = cache.k.device
+        L, Hkv, N, d = cache.k.shape
+        S, q = len(cache.seqlens), cache.q_win
+        if q.dim() != 5 or q.shape != (S, L, cache.num_q_heads, q.shape[3], 128):
+            raise ValueError("q_win must be [S, L, Hq, w, 128]")
+        w = q.shape[3]
+        self.lay = _query_strides(cache.layout(), q)
+        nbytes = jacap_weigh_workspace(self.lay)
+        if nbytes == 0:
+            raise JacapError(2 if cache.num_q_heads // Hkv * w > 512 else 1, "jacap_weigh_workspace")
+        self.ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        self.ws[:64].zero_()
+        self._how = jacap_weighing()
+        self._how.scale = 1.0 / math.sqrt(128.0) if scale is None else float(scale)
+        new = lambda shape, dtype: torch.empty(shape, dtype=dtype, device=self.device)  # noqa: E731
+        self.weights = new((L, Hkv, N), torch.float32)
+        self.lse = new((S, L, cache.num_q_heads, w), torch.float32)
+        self.keys = new((L, Hkv, N), torch.float32)
+        self.idx = new((L, Hkv, S, self.budget), torch.int32)
+        self.kept = new((S,), torch.int32)
+        self.k_out = new((L, Hkv, S, self.budget, d), cache.k.dtype)
+        self.v_out = torch.empty_like(self.k_out)
+        self.weights_out = new((L, Hkv, S, self.budget), torch.float32)
+
+    def score(self, q=None, lse=None, before=None, lengths=None, q_lens=None, q_rows=None, stream=None):
+        """The weights (``jacap_weigh``) into ``weights``; returns (weights, lse).
+        q: other queries of q_win's shape; lse: the rows' normalisers, as
+        ``CacheAttention`` returned them for these queries (computed into ``lse`` if None);
+        before: earlier weights to add to (``weights`` itself works); lengths, q_lens: int32
+        [S] live tokens and queries of each request; q_rows: int32 [S, w] which query is
+        the j-th."""
+        c, h, dev = self.cache, self._how, self.device
+        q = c.q_win if q is None else q
+        S, L, Hq, w = self.lse.shape
+        _tensor("q", q, dev, c.k.dtype, (S, L, Hq, w, 128))
+        _tensor("lse", lse, dev, torch.float32, self.lse.shape, True)
+        _tensor("before", before, dev, torch.float32, self.weights.shape, True)
+        _tensor("lengths", lengths, dev, torch.int32, (S,), True)
+        _tensor("q_lens", q_lens, dev, torch.int32, (S,), True)
+        _tensor("q_rows", q_rows, dev, torch.int32, (S, w), True)
+        h.lse_given = int(lse is not None)
+        for name, t in (("lengths", lengths), ("q_lens", q_lens), ("q_rows", q_rows)):
+            setattr(h, name, None if t is None else t.data_ptr())
+        lay = _query_strides(self.lay, q)
+        lse = self.lse if lse is None else lse
+        with _on(dev, stream) as st:
+            _check(jacap_weigh(lay, h, _ptr(q), _ptr(c.k), _ptr(lse), _ptr(before), _ptr(self.weights), _ptr(self.ws),
+                               self.ws.numel(), st), "jacap_weigh")
+        return self.weights, lse
+
+    def select_compact(self, weights=None, pos=None, stream=None):
+        """The selection by ``weights`` (None: those of ``score()``) and the retained
+        cache (``jacap_select_weights``). ``pos``: int32 [L, Hkv, N] tags by which the
+        first and the last tokens are told (None: by row)."""
+        c, dev = self.cache, self.device
+        weights = self.weights if weights is None else weights
+        _tensor("weights", weights, dev, torch.float32, self.weights.shape, True)
+        _tensor("pos", pos, dev, torch.int32, self.weights.shape, True)
+        if pos is not None and not c.k.is_contiguous():
+            raise ValueError("tags need a dense cache")
+        with _on(dev, stream) as st:
+            _check(jacap_select_weights(self.lay, _ptr(weights), _ptr(pos), self.sinks, self.recent, self.budget,
+                                        _ptr(self.idx), _ptr(self.kept), _ptr(c.k), _ptr(c.v), _ptr(self.k_out),
+                                        _ptr(self.v_out), _ptr(self.weights_out), _ptr(self.keys), _ptr(self.ws),
+                                        self.ws.numel(), st), "jacap_select_weights")
+
+    def run(self, stream=None):
+        self.score(stream=stream)
+        self.select_compact(stream=stream)
+
+    def check(self, stream=None):
+        _check_and_clear(self.ws, self.device, stream)
 
 
 class Evictor:

@@ -29,10 +29,10 @@ struct Carve {
   size_t units, trace, trace_cta, base, runs, sched, seqs;
 };
 
-bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+}  // namespace
 
 // Argument checks that need no GPU. Returns JACAP_OK or the error.
-jacap_status check_layout(const jacap_layout* L) {
+jacap_status jacap::check_layout(const jacap_layout* L) {
   if (L == nullptr || L->cu_seqlens == nullptr) return JACAP_ERR_INVALID_ARG;
   if (L->num_seqs < 1 || L->num_layers < 1 || L->num_kv_heads < 1 || L->num_q_heads < 1) return JACAP_ERR_INVALID_ARG;
   if (L->total_tokens < 1 || L->total_tokens >= ((int64_t)1 << 31)) return JACAP_ERR_INVALID_ARG;
@@ -57,6 +57,8 @@ jacap_status check_layout(const jacap_layout* L) {
   return JACAP_OK;
 }
 
+namespace {
+
 // Tokens per work item: the largest of 16384..128 that still yields 4096
 // items (independent of the device so the workspace size is a pure function
 // of the layout): ~27 per CTA on 152 SMs. The K pass and the scores take runs of
@@ -75,7 +77,9 @@ int pick_chunk(const jacap_layout* L) {
   return TILE;
 }
 
-void make_dims(const jacap_layout* L, const jacap_params* P, Dims& dm) {
+}  // namespace
+
+void jacap::make_dims(const jacap_layout* L, const jacap_params* P, Dims& dm) {
   memset(&dm, 0, sizeof(dm));
   dm.pdl = 1;
   dm.S = L->num_seqs;
@@ -103,6 +107,8 @@ void make_dims(const jacap_layout* L, const jacap_params* P, Dims& dm) {
     if (dm.full_cov && L->dtype == JACAP_BF16) dm.kf_rp = kfull_rows_padded(dm.G, dm.window);
   }
 }
+
+namespace {
 
 Carve carve(const Dims& dm) {
   Carve c;
@@ -185,8 +191,10 @@ Ws make_ws(void* base, const Carve& c) {
   return ws;
 }
 
+}  // namespace
+
 // Current device must be sm_103 (GB300). Returns its SM count via *sms.
-jacap_status check_device(int* sms) {
+jacap_status jacap::check_device(int* sms) {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return JACAP_ERR_CUDA;
   int major = 0, minor = 0;
@@ -197,6 +205,8 @@ jacap_status check_device(int* sms) {
   if (major != 10 || minor != 3) return JACAP_ERR_UNSUPPORTED;
   return JACAP_OK;
 }
+
+namespace {
 
 PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
   static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
@@ -211,9 +221,11 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
   return fn;
 }
 
-// 4-D map over (channel, token, kv head, layer) with {128 B, 128 tokens} boxes
+}  // namespace
+
+// 4-D map over (channel, token, kv head, layer) with {128 B, box_tokens tokens} boxes
 // and the 128-byte swizzle; out-of-range tokens read as zero.
-bool encode_kv_map(CUtensorMap* map, const jacap_layout* L, const void* base) {
+bool jacap::encode_kv_map(CUtensorMap* map, const jacap_layout* L, const void* base, int box_tokens) {
   PFN_cuTensorMapEncodeTiled_v12000 fn = encode_fn();
   if (fn == nullptr) return false;
   const bool bf = L->dtype == JACAP_BF16;
@@ -222,7 +234,7 @@ bool encode_kv_map(CUtensorMap* map, const jacap_layout* L, const void* base) {
                               (cuuint64_t)L->num_layers};
   const cuuint64_t strides[3] = {(cuuint64_t)L->kv_stride_token * es, (cuuint64_t)L->kv_stride_head * es,
                                  (cuuint64_t)L->kv_stride_layer * es};
-  const cuuint32_t box[4] = {(cuuint32_t)(128 / es), (cuuint32_t)TILE, 1, 1};
+  const cuuint32_t box[4] = {(cuuint32_t)(128 / es), (cuuint32_t)box_tokens, 1, 1};
   const cuuint32_t estr[4] = {1, 1, 1, 1};
   const CUresult r = fn(map, bf ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4,
                         const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
@@ -231,7 +243,25 @@ bool encode_kv_map(CUtensorMap* map, const jacap_layout* L, const void* base) {
   return r == CUDA_SUCCESS;
 }
 
-jacap_status map_cuda(cudaError_t e) { return e == cudaSuccess ? JACAP_OK : JACAP_ERR_CUDA; }
+// 5-D map over (channel, drafted token, kv head, layer, request) of bf16 rows at
+// `strides` (request, layer, head, token; elements) with {64 channels, 64 tokens}
+// boxes; tokens past `tokens` read as zero.
+bool jacap::encode_draft_map(CUtensorMap* map, const jacap_layout* L, const void* base, const int64_t* strides,
+                             int tokens) {
+  PFN_cuTensorMapEncodeTiled_v12000 fn = encode_fn();
+  if (fn == nullptr) return false;
+  const cuuint64_t dims[5] = {(cuuint64_t)D, (cuuint64_t)tokens, (cuuint64_t)L->num_kv_heads,
+                              (cuuint64_t)L->num_layers, (cuuint64_t)L->num_seqs};
+  const cuuint64_t str[4] = {(cuuint64_t)strides[3] * 2, (cuuint64_t)strides[2] * 2, (cuuint64_t)strides[1] * 2,
+                             (cuuint64_t)strides[0] * 2};
+  const cuuint32_t box[5] = {64, 64, 1, 1, 1};
+  const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(base), dims, str, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+namespace {
 
 // The per-token tags `pos` follow K's layer and head strides in units of its
 // token stride, which must therefore divide them.
@@ -363,6 +393,12 @@ int64_t pass_items(const jacap_layout* L, const Dims& dm) {
 }
 
 }  // namespace
+
+void jacap::plan_runs(Dims& dm, int64_t items, int sms) { pick_runs(dm, items, sms); }
+
+int64_t jacap::plan_items(const jacap_layout* L, const Dims& dm) { return pass_items(L, dm); }
+
+int jacap::plan_grid(int64_t items, int sms) { return persistent_grid(items, sms, 1); }
 
 size_t jacap::workspace_base(const jacap_layout* layout) {
   if (check_layout(layout) != JACAP_OK) return 0;
@@ -608,6 +644,122 @@ jacap_status jacap_append(const jacap_layout* layout, const void* k_new, const v
   a.slot_rows = layout->max_seqlen;
   a.k = k, a.v = v, a.pos = pos, a.stats = stats, a.counts = counts;
   return map_cuda(launch_append(dm, layout->dtype == JACAP_BF16 ? 1 : 0, a, lengths, ids, (cudaStream_t)stream));
+}
+
+jacap_status jacap_append_path(const jacap_layout* layout, const void* k_new, const void* v_new,
+                               const int64_t* strides, const void* q_new, const int32_t* path, int32_t depth,
+                               const int32_t* taken, const int32_t* lengths, const int32_t* ids, void* k, void* v,
+                               int32_t* pos, float* stats, int32_t* counts, void* stream) {
+  jacap_status st = check_layout(layout);
+  if (st != JACAP_OK) return st;
+  if (k_new == nullptr || v_new == nullptr || strides == nullptr || path == nullptr || taken == nullptr ||
+      lengths == nullptr || ids == nullptr || k == nullptr || v == nullptr || depth < 1 || depth > layout->window)
+    return JACAP_ERR_INVALID_ARG;
+  if ((stats == nullptr) != (counts == nullptr) || (stats != nullptr && q_new == nullptr)) return JACAP_ERR_INVALID_ARG;
+  if (layout->total_tokens != (int64_t)layout->num_seqs * layout->max_seqlen) return JACAP_ERR_INVALID_ARG;
+  if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(q_new) || !aligned16(k) || !aligned16(v) ||
+      !aligned16(stats) || ((uintptr_t)counts & 3u) != 0 || ((uintptr_t)pos & 3u) != 0 || !pos_layout_ok(layout, pos))
+    return JACAP_ERR_INVALID_ARG;
+  const int64_t el16 = layout->dtype == JACAP_BF16 ? 8 : 4;  // elements per 16 bytes
+  AppendArgs a = {};
+  for (int i = 0; i < 8; ++i) {
+    if (strides[i] < 0 || strides[i] % el16 != 0) return JACAP_ERR_INVALID_ARG;
+    (i == 3 ? a.tok_stride_k : i == 7 ? a.tok_stride_v : a.strides[i < 3 ? i : i - 1]) = strides[i];
+  }
+  int32_t most = 0;
+  for (int s = 0; s < layout->num_seqs; ++s) {
+    if (lengths[s] < 0 || taken[s] < 0 || taken[s] > depth || (int64_t)lengths[s] + taken[s] > layout->max_seqlen)
+      return JACAP_ERR_INVALID_ARG;
+    for (int j = 0; j < taken[s]; ++j)
+      if (path[(int64_t)s * depth + j] < 0 || path[(int64_t)s * depth + j] >= layout->window)
+        return JACAP_ERR_INVALID_ARG;
+    most = std::max(most, taken[s]);
+  }
+  if ((int64_t)layout->num_layers * layout->num_q_heads * 256 >= ((int64_t)1 << 31)) return JACAP_ERR_INVALID_ARG;
+  int sms = 0;
+  if ((st = check_device(&sms)) != JACAP_OK) return st;
+  Dims dm;
+  make_dims(layout, nullptr, dm);
+  a.k_new = k_new, a.v_new = v_new, a.q_new = q_new;
+  a.slot_rows = layout->max_seqlen;
+  a.k = k, a.v = v, a.pos = pos, a.stats = stats, a.counts = counts;
+  const TraceRange trace("jacap/append_path");
+  for (int j = 0; j < most; ++j)
+    if ((st = map_cuda(launch_append(dm, layout->dtype == JACAP_BF16 ? 1 : 0, a, lengths, ids, (cudaStream_t)stream, path,
+                                     depth, taken, j))) != JACAP_OK)
+      return st;
+  return JACAP_OK;
+}
+
+namespace {
+
+// Checks shared by the selections by attention weights.
+jacap_status check_weights(const jacap_layout* layout, const float* weights, const int32_t* pos, int32_t sinks,
+                           int32_t recent, int32_t budget, const int32_t* idx, const int32_t* kept, const void* k,
+                           const void* v, const float* keys, void* ws, size_t ws_bytes, Ws* w, Dims* dm) {
+  jacap_status st = check_layout(layout);
+  if (st != JACAP_OK) return st;
+  if (weights == nullptr || idx == nullptr || kept == nullptr || k == nullptr || v == nullptr || keys == nullptr ||
+      ws == nullptr || budget < 1 || sinks < 0 || recent < 0 || (int64_t)sinks + recent > budget || keys == weights)
+    return JACAP_ERR_INVALID_ARG;
+  if (((uintptr_t)weights & 3u) != 0 || ((uintptr_t)keys & 3u) != 0 || ((uintptr_t)idx & 3u) != 0 ||
+      ((uintptr_t)kept & 3u) != 0 || ((uintptr_t)pos & 3u) != 0 || !aligned16(k) || !aligned16(v))
+    return JACAP_ERR_INVALID_ARG;
+  if (!pos_layout_ok(layout, pos)) return JACAP_ERR_INVALID_ARG;
+  make_dims(layout, nullptr, *dm);
+  if (((uintptr_t)ws & 255u) != 0 || ws_bytes < 64) return JACAP_ERR_WORKSPACE;
+  memset(w, 0, sizeof(*w));
+  w->status = (uint32_t*)ws;  // all that the selection needs
+  int sms = 0;
+  return check_device(&sms);
+}
+
+}  // namespace
+
+jacap_status jacap_select_weights(const jacap_layout* layout, const float* weights, const int32_t* pos, int32_t sinks,
+                                  int32_t recent, int32_t budget, int32_t* idx, int32_t* kept, const void* k,
+                                  const void* v, void* k_out, void* v_out, float* weights_out, float* keys, void* ws,
+                                  size_t ws_bytes, void* stream) {
+  Ws w;
+  Dims dm;
+  jacap_status st = check_weights(layout, weights, pos, sinks, recent, budget, idx, kept, k, v, keys, ws, ws_bytes, &w, &dm);
+  if (st != JACAP_OK) return st;
+  if (k_out == nullptr || v_out == nullptr || !aligned16(k_out) || !aligned16(v_out) || ((uintptr_t)weights_out & 3u) != 0)
+    return JACAP_ERR_INVALID_ARG;
+  const cudaStream_t s = (cudaStream_t)stream;
+  const TraceRange trace("jacap/select_weights");
+  WeightRef wr = {const_cast<float*>(weights), (int64_t)dm.Hkv * dm.Ntot, dm.Ntot};
+  if ((st = map_cuda(launch_protect(dm, w, layout->cu_seqlens, wr, pos, sinks, recent, keys, layout->max_seqlen, s))) !=
+      JACAP_OK)
+    return st;
+  if (weights_out == nullptr) wr.p = nullptr;
+  return map_cuda(launch_select(dm, w, layout->cu_seqlens, keys, budget, idx, kept, layout->max_seqlen, s,
+                                layout->dtype == JACAP_BF16 ? 1 : 0, k, v, k_out, v_out, nullptr, nullptr, nullptr, wr,
+                                weights_out));
+}
+
+jacap_status jacap_evict_weights(const jacap_layout* layout, float* weights, int32_t* pos, int32_t sinks, int32_t recent,
+                                 int32_t budget, int32_t* idx, int32_t* kept, void* k, void* v, int32_t preserve_order,
+                                 float* keys, void* ws, size_t ws_bytes, void* stream) {
+  Ws w;
+  Dims dm;
+  jacap_status st = check_weights(layout, weights, pos, sinks, recent, budget, idx, kept, k, v, keys, ws, ws_bytes, &w, &dm);
+  if (st != JACAP_OK) return st;
+  if (preserve_order != 0 && preserve_order != 1) return JACAP_ERR_INVALID_ARG;
+  if (dm.kv_sl % dm.kv_st != 0 || dm.kv_sh % dm.kv_st != 0) return JACAP_ERR_INVALID_ARG;
+  const WeightRef wr = {weights, dm.kv_sl / dm.kv_st, dm.kv_sh / dm.kv_st};
+  const int dt = layout->dtype == JACAP_BF16 ? 1 : 0;
+  const cudaStream_t s = (cudaStream_t)stream;
+  const TraceRange trace("jacap/evict_weights");
+  if ((st = map_cuda(launch_protect(dm, w, layout->cu_seqlens, wr, pos, sinks, recent, keys, layout->max_seqlen, s))) !=
+      JACAP_OK)
+    return st;
+  if (!preserve_order)
+    return map_cuda(launch_select(dm, w, layout->cu_seqlens, keys, budget, idx, kept, layout->max_seqlen, s, dt, nullptr,
+                                  nullptr, nullptr, nullptr, k, v, pos, wr));
+  if ((st = map_cuda(launch_select(dm, w, layout->cu_seqlens, keys, budget, idx, kept, layout->max_seqlen, s))) != JACAP_OK)
+    return st;
+  return map_cuda(launch_compact_inplace(dm, w, dt, layout->cu_seqlens, k, v, pos, idx, budget, 1, s, wr));
 }
 
 jacap_status jacap_compact_inplace(const jacap_layout* layout, void* k, void* v, int32_t* pos, const int32_t* idx,

@@ -108,6 +108,15 @@ enum { TR_GRAM0 = 0, TR_GRAM1, TR_FAC0, TR_FAC1, TR_SC_IMG, TR_SC1, TR_SC_MMA, T
 enum { TR_K_GRAM = 0, TR_K_SCORE = 1, TR_K_KPASS = 2, TR_K_FACTOR = 3, TR_K_SELECT = 4, TR_KERNELS = 5, TR_CTAS = 1024,
        TR_CTA_SLOTS = 16 };
 
+// One float per token beside a cache: that of token t of plane (l, g) at l sl + g sh + t.
+struct WeightRef {
+  float* p;  // or null
+  int64_t sl, sh;
+  __device__ __forceinline__ float* unit(int l, int g, int64_t t0) const {
+    return p != nullptr ? p + l * sl + g * sh + t0 : nullptr;
+  }
+};
+
 // A unit is (plane p = l*Hkv + g, request s); its index is p*S + s.
 struct Item {
   int plane, seq;         // plane and request

@@ -12,12 +12,14 @@ namespace jacap {
 
 constexpr int CI_CHUNK_BYTES = 16384;  // per tensor and chunk
 
+// `wt`: the weights of the unit's tokens (WeightRef::unit), moved with the rows, or null.
+//
 // Ascending order: row r receives row ix[r]. Rows move in chunks that are
 // read whole (a barrier) before any of them is written; since ix[r] >= r, a
 // chunk's writes never touch a row that a later chunk still has to read.
 template <typename T, int NT>
 __device__ __forceinline__ void compact_ordered_unit(const Dims& dm, int plane, int64_t t0, int kept, T* k, T* v,
-                                                     int32_t* pos, const int32_t* ix) {
+                                                     int32_t* pos, const int32_t* ix, float* wt) {
   constexpr int RB = D * (int)sizeof(T) / 16;  // 16-byte pieces per row
   constexpr int CH = CI_CHUNK_BYTES / (D * (int)sizeof(T));
   constexpr int PER = CH * RB / NT;            // pieces per thread and tensor
@@ -33,6 +35,7 @@ __device__ __forceinline__ void compact_ordered_unit(const Dims& dm, int plane, 
   for (int c0 = 0; c0 < kept; c0 += CH) {
     uint4 kr[PER], vr[PER];
     int32_t pr = 0;
+    float wr = 0.f;
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
       const int q = e * NT + tid, r = c0 + q / RB, piece = q % RB;
@@ -45,6 +48,7 @@ __device__ __forceinline__ void compact_ordered_unit(const Dims& dm, int plane, 
       }
     }
     if (pb != nullptr && tid < CH && c0 + tid < kept) pr = pb[t0 + ix[c0 + tid]];
+    if (wt != nullptr && tid < CH && c0 + tid < kept) wr = wt[ix[c0 + tid]];
     __syncthreads();  // the whole chunk is read before any of it is written
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
@@ -55,6 +59,7 @@ __device__ __forceinline__ void compact_ordered_unit(const Dims& dm, int plane, 
       }
     }
     if (pb != nullptr && tid < CH && c0 + tid < kept) pb[t0 + c0 + tid] = pr;
+    if (wt != nullptr && tid < CH && c0 + tid < kept) wt[c0 + tid] = wr;
   }
 }
 
@@ -67,7 +72,8 @@ __device__ __forceinline__ void compact_ordered_unit(const Dims& dm, int plane, 
 // Part `part` of `parts` of the holes.
 template <typename T, int NT>
 __device__ __forceinline__ void fill_holes_unit(const Dims& dm, int plane, int64_t t0, int kept, int f, int part,
-                                                int parts, T* k, T* v, int32_t* pos, const int32_t* ix) {
+                                                int parts, T* k, T* v, int32_t* pos, const int32_t* ix,
+                                                float* wt) {
   constexpr int RB = D * (int)sizeof(T) / 16;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int holes = kept - f;
@@ -90,6 +96,7 @@ __device__ __forceinline__ void fill_holes_unit(const Dims& dm, int plane, int64
       vb[dst * st16 + piece] = vb[src * st16 + piece];
     }
     if (pb != nullptr && lane == 0) pb[dst] = pb[src];
+    if (wt != nullptr && lane == 1) wt[dst - t0] = wt[src - t0];
   }
 }
 

@@ -12,6 +12,21 @@ namespace jacap {
 // an invalid layout).
 size_t workspace_base(const jacap_layout* layout);
 
+// Shared by the entry points (jacap_api.cu). check_layout needs no GPU; check_device
+// gives the SM count of the current device, which must be a GB300.
+jacap_status check_layout(const jacap_layout* L);
+jacap_status check_device(int* sms);
+void make_dims(const jacap_layout* L, const jacap_params* P, Dims& dm);
+bool encode_kv_map(CUtensorMap* map, const jacap_layout* L, const void* base, int box_tokens = TILE);
+bool encode_draft_map(CUtensorMap* map, const jacap_layout* L, const void* base, const int64_t* strides, int tokens);
+// The work plan's choices: work items of a pass over `L`, runs of the streaming
+// kernels, CTAs of a persistent grid.
+int64_t plan_items(const jacap_layout* L, const Dims& dm);
+void plan_runs(Dims& dm, int64_t items, int sms);
+int plan_grid(int64_t items, int sms);
+inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+inline jacap_status map_cuda(cudaError_t e) { return e == cudaSuccess ? JACAP_OK : JACAP_ERR_CUDA; }
+
 // Tracing: built with -DJACAP_NVTX (JACAP_NVTX=1 in the environment of the
 // build), the host side marks each kernel's launch with an NVTX range named
 // "jacap/<step>" so a profiler timeline groups the GPU work by step of the
@@ -57,7 +72,9 @@ cudaError_t launch_pdl(bool pdl, void (*kernel)(KArgs...), dim3 grid, dim3 block
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
 }
 
-cudaError_t launch_plan(const Dims& dm, const Ws& ws, const int32_t* cu, cudaStream_t st);
+// lengths: tokens of each request (the first ones of its range), or null: all.
+cudaError_t launch_plan(const Dims& dm, const Ws& ws, const int32_t* cu, cudaStream_t st,
+                        const int32_t* lengths = nullptr);
 cudaError_t launch_window_stats(const Dims& dm, const Ws& ws, int dtype, const void* q, cudaStream_t st);
 cudaError_t launch_kpass(const CUtensorMap& kmap, const Dims& dm, const Ws& ws, int dtype, const int32_t* cu,
                          int grid, cudaStream_t st);
@@ -94,32 +111,99 @@ cudaError_t launch_fused(const CUtensorMap& vmap, const Dims& dm, const Ws& ws, 
                          cudaStream_t st);
 // Selection only when k and kio are null. With k: the kept rows of k and v
 // (dtype 1 = bf16, 0 = float32) are also copied into k_out and v_out, as
-// launch_compact does. With kio: the holes of kio, vio (and pos) are filled in
-// place, as launch_compact_inplace does without preserve_order.
+// launch_compact does (and the kept tokens' weights wt into wt_out, unless null).
+// With kio: the holes of kio, vio (and pos, wt) are filled in place, as
+// launch_compact_inplace does without preserve_order.
 cudaError_t launch_select(const Dims& dm, const Ws& ws, const int32_t* cu, const float* scores, int budget,
                           int32_t* idx, int32_t* kept, int max_seqlen, cudaStream_t st, int dtype = 1,
                           const void* k = nullptr, const void* v = nullptr, void* k_out = nullptr,
-                          void* v_out = nullptr, void* kio = nullptr, void* vio = nullptr, int32_t* pos = nullptr);
+                          void* v_out = nullptr, void* kio = nullptr, void* vio = nullptr, int32_t* pos = nullptr,
+                          const WeightRef& wt = WeightRef{}, float* wt_out = nullptr);
+// Selection keys from attention weights: +inf for the first `sinks` and the last
+// `recent` tokens of every unit.
+cudaError_t launch_protect(const Dims& dm, const Ws& ws, const int32_t* cu, const WeightRef& weights,
+                           const int32_t* pos, int sinks, int recent, float* keys, int max_seqlen, cudaStream_t st);
 cudaError_t launch_compact(const Dims& dm, int dtype, const int32_t* cu, const void* k, const void* v,
                            const int32_t* idx, int budget, void* k_out, void* v_out, cudaStream_t st);
 cudaError_t launch_stats_update(const Dims& dm, int dtype, const void* q, float* stats, int32_t* counts, int reset,
                                 cudaStream_t st);
-// One decode step (jacap_append): new rows, slots and running statistics.
+// One decode step (jacap_append): new rows, slots and running statistics (unless
+// stats is null).
 struct AppendArgs {
   const void *k_new, *v_new, *q_new;
   int64_t strides[6];
+  int64_t tok_stride_k, tok_stride_v;  // between a request's new tokens (jacap_append_path)
   int64_t slot_rows;
   void *k, *v;
   int32_t* pos;
   float* stats;
   int32_t* counts;
 };
+// With `path` (host, [S][depth]): request s's new token path[s][step] to row
+// lengths[s] + step, where step < taken[s].
 cudaError_t launch_append(const Dims& dm, int dtype, const AppendArgs& a, const int32_t* lengths, const int32_t* ids,
-                          cudaStream_t st);
+                          cudaStream_t st, const int32_t* path = nullptr, int depth = 0,
+                          const int32_t* taken = nullptr, int step = 0);
 cudaError_t launch_stats_moments(const Dims& dm, const Ws& ws, const float* stats, const int32_t* counts,
                                  cudaStream_t st);
 cudaError_t launch_compact_inplace(const Dims& dm, const Ws& ws, int dtype, const int32_t* cu, void* k, void* v,
                                    int32_t* pos, const int32_t* idx, int budget, int preserve_order,
-                                   cudaStream_t st);
+                                   cudaStream_t st, const WeightRef& wt = WeightRef{});
+
+// Rotary positions (k_rope.cu): token j of request s is row s, j of x and y.
+struct RopeTensor {
+  const void* x;
+  void* y;
+  int heads;
+  int64_t xs[3], ys[3];  // request, token, head (elements)
+};
+struct RopeArgs {
+  RopeTensor q, k;
+  const int32_t* pos;
+  int64_t ps[2];  // request, token
+  const uint64_t* turns;
+  int seqs, tokens, rot, interleaved, inverse;
+  float amplitude;
+};
+// `vec`: every row of x and y starts on 16 bytes and no 16-byte piece splits a pair.
+cudaError_t launch_rope(const RopeArgs& a, int dtype, bool vec, int sms, cudaStream_t st);
+
+// Attention of a request's queries over its cached and drafted tokens (k_attend.cu);
+// the layout's window is the number of queries.
+struct AttendArgs {
+  const void *q, *k, *v;
+  const void *kd, *vd;        // drafted K and V, or null
+  void* o;
+  float* lse;                 // or null
+  const int32_t* lengths;     // live tokens of each request, or null: all
+  const int32_t* draft_lens;  // queries (and drafted tokens) of each request, or null: all
+  const uint64_t* tree;       // [S][window] masks, or null: a chain
+  int64_t os[4], kds[4], vds[4];  // strides of o and of the drafted K and V: request, layer, head, token
+  float scale;
+  int chunk, nsplit, nrb, max_seqlen;  // tokens per split, splits of the longest request, row blocks
+  float *opart, *mlpart;      // [units][nsplit][G window][128], [..][2]: the splits' sums, (maximum, sum)
+  uint32_t* status;
+};
+int attend_row_block(int dtype, int rows);  // rows of a CTA
+// maps: K, V, drafted K, drafted V (bf16)
+cudaError_t launch_attend(const CUtensorMap* maps, const Dims& dm, int dtype, const AttendArgs& a, const int32_t* cu,
+                          cudaStream_t st);
+
+// Attention weights that tokens received from a window of queries (k_weigh.cu).
+struct WeighArgs {
+  const void *q, *k;
+  const int32_t* lengths;  // live tokens of each request, or null: all
+  const int32_t* q_lens;   // queries of each request, or null: the window
+  const int32_t* q_rows;   // [S][window] which query is the j-th, or null: j
+  float* lse;              // [S][L][Hq][window]
+  int given;               // 1: lse is an input
+  const float* before;     // earlier weights, or null
+  float* weights;          // [L*Hkv][Ntot]
+  float scale;
+  float2* stat;            // [L*Hkv][c_cap][2][row blocks][128] (maximum, sum) of a run (float32: a chunk)
+};
+constexpr int WEIGH_ROWS_MAX = 512;  // query rows per KV head
+cudaError_t launch_weigh(const CUtensorMap& kmap, const Dims& dm, const Ws& ws, int dtype, const WeighArgs& a,
+                         const int32_t* cu, int grid, cudaStream_t st);
 
 }  // namespace jacap

@@ -92,7 +92,8 @@ __global__ void __launch_bounds__(D)
 // longer wait for the device.
 constexpr int AP_MAX = 256;
 struct AppendRows {
-  int32_t row[AP_MAX], id[AP_MAX];
+  int32_t row[AP_MAX], id[AP_MAX];  // slot row (negative: this request has no token here) and tag
+  int32_t tok[AP_MAX];              // which of the request's new tokens
 };
 
 template <typename T>
@@ -101,11 +102,18 @@ __global__ void __launch_bounds__(D)
   pdl_wait();
   const int b = blockIdx.x, tid = threadIdx.x;
   const int hq = b % dm.Hq, l = (b / dm.Hq) % dm.L, sl = b / (dm.Hq * dm.L), s = s0 + sl;
+  if (rows.row[sl] < 0) return;
+  const int64_t tok = rows.tok[sl];
   const int64_t sb = ((int64_t)s * dm.L + l) * dm.Hq + hq;
+  const bool merge = a.stats != nullptr;
   float* st = a.stats + sb * 2 * D;
-  const float x = q_elem((const T*)a.q_new + s * dm.q_ss + l * dm.q_sl + hq * dm.q_sh + tid);
-  const float ma = st[tid], sa = st[D + tid];
-  int na = a.counts[sb];
+  float x = 0.f, ma = 0.f, sa = 0.f;
+  int na = 0;
+  if (merge) {
+    x = q_elem((const T*)a.q_new + s * dm.q_ss + l * dm.q_sl + hq * dm.q_sh + tok * dm.q_sp + tid);
+    ma = st[tid], sa = st[D + tid];
+    na = a.counts[sb];
+  }
   if (hq % dm.G == 0) {
     constexpr int CH = D * (int)sizeof(T) / 16;  // 16-byte pieces of a row
     const int g = hq / dm.G;
@@ -114,13 +122,15 @@ __global__ void __launch_bounds__(D)
       const bool isv = tid >= CH;
       const int p = isv ? tid - CH : tid;
       const int64_t* str = a.strides + (isv ? 3 : 0);
-      const T* src = (const T*)(isv ? a.v_new : a.k_new) + s * str[0] + l * str[1] + g * str[2];
+      const T* src = (const T*)(isv ? a.v_new : a.k_new) + s * str[0] + l * str[1] + g * str[2] +
+                     tok * (isv ? a.tok_stride_v : a.tok_stride_k);
       T* dst = (T*)(isv ? a.v : a.k) + (int64_t)l * dm.kv_sl + (int64_t)g * dm.kv_sh + row * dm.kv_st;
       ((uint4*)dst)[p] = ((const uint4*)src)[p];
     } else if (tid == 2 * CH && a.pos != nullptr) {
       a.pos[(int64_t)l * (dm.kv_sl / dm.kv_st) + (int64_t)g * (dm.kv_sh / dm.kv_st) + row] = rows.id[sl];
     }
   }
+  if (!merge) return;
   if (na < 0) na = 0;
   float mean = x, m2 = 0.f;
   if (na > 0) {
@@ -162,7 +172,7 @@ constexpr int CI_THREADS = 256;
 template <typename T>
 __global__ void __launch_bounds__(CI_THREADS)
     compact_inplace_kernel(Dims dm, Ws ws, const int32_t* __restrict__ cu, T* k, T* v, int32_t* pos,
-                           const int32_t* __restrict__ idx, int budget) {
+                           const int32_t* __restrict__ idx, int budget, WeightRef wt) {
   pdl_wait();
   // together, as a block of this launch may set the word (a unit's positions)
   if (__syncthreads_or(status_failed(ws) ? 1 : 0)) return;
@@ -182,7 +192,8 @@ __global__ void __launch_bounds__(CI_THREADS)
     if (tid == 0) flag(ws, ST_INVALID);
     return;
   }
-  compact_ordered_unit<T, CI_THREADS>(dm, plane, t0, kept, k, v, pos, ix);
+  compact_ordered_unit<T, CI_THREADS>(dm, plane, t0, kept, k, v, pos, ix,
+                                      wt.unit(plane / dm.Hkv, plane % dm.Hkv, t0));
 }
 
 template <typename T>
@@ -212,7 +223,7 @@ __global__ void __launch_bounds__(CI_THREADS)
     if (tid == 0) flag(ws, ST_INVALID);
     return;
   }
-  fill_holes_unit<T, CI_THREADS>(dm, plane, t0, kept, s_f, 0, 1, k, v, pos, ix);
+  fill_holes_unit<T, CI_THREADS>(dm, plane, t0, kept, s_f, 0, 1, k, v, pos, ix, nullptr);
 }
 
 template <typename T>
@@ -230,13 +241,15 @@ cudaError_t launch_stats_update(const Dims& dm, int dtype, const void* q, float*
 }
 
 cudaError_t launch_append(const Dims& dm, int dtype, const AppendArgs& a, const int32_t* lengths, const int32_t* ids,
-                          cudaStream_t st) {
+                          cudaStream_t st, const int32_t* path, int depth, const int32_t* taken, int step) {
   for (int s0 = 0; s0 < dm.S; s0 += AP_MAX) {
     const int n = dm.S - s0 < AP_MAX ? dm.S - s0 : AP_MAX;
     AppendRows rows;
     for (int i = 0; i < AP_MAX; ++i) {
-      rows.row[i] = i < n ? lengths[s0 + i] : 0;
-      rows.id[i] = i < n ? ids[s0 + i] : 0;
+      const bool on = i < n && (path == nullptr || step < taken[s0 + i]);
+      rows.row[i] = on ? lengths[s0 + i] + step : -1;
+      rows.id[i] = on ? ids[s0 + i] + step : 0;
+      rows.tok[i] = on && path != nullptr ? path[(int64_t)(s0 + i) * depth + step] : 0;
     }
     const int blocks = n * dm.L * dm.Hq;
     if (dtype == 1)
@@ -255,7 +268,7 @@ cudaError_t launch_stats_moments(const Dims& dm, const Ws& ws, const float* stat
 
 cudaError_t launch_compact_inplace(const Dims& dm, const Ws& ws, int dtype, const int32_t* cu, void* k, void* v,
                                    int32_t* pos, const int32_t* idx, int budget, int preserve_order,
-                                   cudaStream_t st) {
+                                   cudaStream_t st, const WeightRef& wt) {
   const int units = dm.L * dm.Hkv * dm.S;
   if (!preserve_order) {
     if (dtype == 1)
@@ -268,10 +281,10 @@ cudaError_t launch_compact_inplace(const Dims& dm, const Ws& ws, int dtype, cons
   }
   if (dtype == 1)
     JACAP_TRY(launch_pdl(dm.pdl != 0, compact_inplace_kernel<__nv_bfloat16>, units, CI_THREADS, 0, st, dm, ws, cu,
-                         (__nv_bfloat16*)k, (__nv_bfloat16*)v, pos, idx, budget));
+                         (__nv_bfloat16*)k, (__nv_bfloat16*)v, pos, idx, budget, wt));
   else
     JACAP_TRY(launch_pdl(dm.pdl != 0, compact_inplace_kernel<float>, units, CI_THREADS, 0, st, dm, ws, cu, (float*)k,
-                         (float*)v, pos, idx, budget));
+                         (float*)v, pos, idx, budget, wt));
   return cudaGetLastError();
 }
 

@@ -98,7 +98,8 @@ template <typename T, int NT>
 __device__ __forceinline__ void gather_unit(const Dims& dm, int plane, int64_t start, int64_t end, bool valid,
                                             const T* __restrict__ k, const T* __restrict__ v,
                                             const int32_t* out, const int32_t* sidx, int B, int64_t u, int part,
-                                            int parts, T* __restrict__ k_out, T* __restrict__ v_out) {
+                                            int parts, T* __restrict__ k_out, T* __restrict__ v_out,
+                                            const WeightRef wt, float* wt_out) {
   constexpr int CH = D * (int)sizeof(T) / 16;  // 16-byte chunks per row
   const int l = plane / dm.Hkv, g = plane % dm.Hkv;
   const int64_t base = (int64_t)l * dm.kv_sl + (int64_t)g * dm.kv_sh;
@@ -116,6 +117,13 @@ __device__ __forceinline__ void gather_unit(const Dims& dm, int plane, int64_t s
     }
     ko[e] = kk;
     vo[e] = vv;
+  }
+  if (wt.p != nullptr) {
+    const float* w = wt.unit(l, g, start);
+    for (int r = part * NT + threadIdx.x; r < B; r += parts * NT) {
+      const int32_t src = sidx != nullptr && r < SE_IDX ? sidx[r] : out[r];
+      wt_out[u * B + r] = valid && src >= 0 && start + src < end ? w[src] : 0.f;
+    }
   }
 }
 
@@ -163,7 +171,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT)
     select_kernel(Dims dm, Ws ws, const int32_t* __restrict__ cu, const float* __restrict__ scores, int B,
                   int32_t* __restrict__ idx, int32_t* __restrict__ kept, const E* __restrict__ k,
                   const E* __restrict__ v, E* __restrict__ k_out, E* __restrict__ v_out, E* kio, E* vio,
-                  int32_t* pos, int parts) {
+                  int32_t* pos, int parts, WeightRef wt, float* wt_out) {
   constexpr bool GATHER = MODE == 1;
   pdl_wait();
   constexpr int SLAB = NT * KPT;  // warp w holds positions 32 KPT w .. + 32 KPT - 1 of a slab
@@ -196,7 +204,8 @@ __global__ void __launch_bounds__(NT, 1024 / NT)
     for (int r = tid; r < B; r += NT) out[r] = r < n ? r : -1;
     if constexpr (GATHER) {
       __syncthreads();
-      gather_unit<E, NT>(dm, plane, start, end, valid, k, v, out, nullptr, B, u, part, parts, k_out, v_out);
+      gather_unit<E, NT>(dm, plane, start, end, valid, k, v, out, nullptr, B, u, part, parts, k_out, v_out, wt,
+                         wt_out);
     }
     return;
   }
@@ -377,7 +386,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT)
   TRC_ADD(2, tr_e);
   TRC_T(tr_g);
   if constexpr (GATHER) gather_unit<E, NT>(dm, plane, start, end, true, k, v, out, sm.idx, B, u, part, parts, k_out,
-                                          v_out);
+                                          v_out, wt, wt_out);
   TRC_ADD(3, tr_g);
   if constexpr (MODE == 2) {
     // f = the kept positions below B (they ascend: a binary search)
@@ -386,10 +395,55 @@ __global__ void __launch_bounds__(NT, 1024 / NT)
       const int mid = (lo + hi) >> 1;
       if ((mid < SE_IDX ? sm.idx[mid] : out[mid]) < B) lo = mid + 1; else hi = mid;
     }
-    fill_holes_unit<E, NT>(dm, plane, start, B, lo, part, parts, kio, vio, pos, out);
+    fill_holes_unit<E, NT>(dm, plane, start, B, lo, part, parts, kio, vio, pos, out,
+                           wt.unit(plane / dm.Hkv, plane % dm.Hkv, start));
   }
   TRC_ADD(5, tr_u);
   if (tid == 0) TRC_PUT(ws, TR_K_SELECT, 6);
+}
+
+// Selection keys from attention weights: a weight where the token may go, +inf (above
+// every weight) where it must stay: the unit's first `sinks` tokens and its last
+// `recent` ones, by the tags of `pos` (counted from the largest tag of the unit; tags
+// below `sinks` are the first ones) or, without tags, by row. A weight that is
+// negative or not finite ends the selection (ST_NONFINITE). One block per PK_PART
+// tokens of a unit (with tags, per unit: the largest tag comes first).
+constexpr int PK_THREADS = 256, PK_PART = 4096;
+
+__global__ void __launch_bounds__(PK_THREADS)
+    protect_kernel(Dims dm, Ws ws, const int32_t* __restrict__ cu, WeightRef weights, const int32_t* __restrict__ pos, int sinks, int recent, float* __restrict__ keys, int parts) {
+  pdl_wait();
+  __shared__ int32_t s_max[PK_THREADS / 32];
+  const int tid = threadIdx.x, u = blockIdx.x / parts, part = blockIdx.x % parts;
+  const int s = u % dm.S, plane = u / dm.S;
+  const int64_t start = cu[s], end = cu[s + 1];
+  if (start < 0 || end < start || end > dm.Ntot) return;  // the selection reports it
+  const int64_t n = end - start, per = parts == 1 ? n : PK_PART;
+  const int64_t a = part * per, b = part + 1 < parts ? a + per : n;  // (n may pass max_seqlen)
+  const int l = plane / dm.Hkv, g = plane % dm.Hkv;
+  const float* wt = weights.unit(l, g, start);
+  float* key = keys + (int64_t)plane * dm.Ntot + start;
+  const int32_t* tag = nullptr;
+  int64_t last = n - 1;
+  if (pos != nullptr) {
+    tag = pos + (int64_t)l * (dm.kv_sl / dm.kv_st) + (int64_t)g * (dm.kv_sh / dm.kv_st) + start;
+    int32_t m = INT32_MIN;
+    for (int64_t i = tid; i < n; i += PK_THREADS) m = max(m, tag[i]);
+    m = __reduce_max_sync(0xffffffffu, m);
+    if ((tid & 31) == 0) s_max[tid >> 5] = m;
+    __syncthreads();
+    for (int w = 0; w < PK_THREADS / 32; ++w) m = max(m, s_max[w]);
+    last = m;
+  }
+  bool bad = false;
+#pragma unroll 4
+  for (int64_t i = a + tid; i < b; i += PK_THREADS) {  // (no work where a > n)
+    const int64_t p = tag != nullptr ? (int64_t)tag[i] : i;
+    const float w = wt[i];
+    bad |= !(w >= 0.f && w < INFINITY);
+    key[i] = p < sinks || p > last - recent ? INFINITY : w + 0.f;  // (-0 -> 0)
+  }
+  if (bad) flag(ws, ST_NONFINITE);
 }
 
 template <typename T>
@@ -424,37 +478,37 @@ template <int KPT, int NT>
 static cudaError_t launch_select_kpt(const Dims& dm, const Ws& ws, const int32_t* cu, const float* scores, int budget,
                                      int32_t* idx, int32_t* kept, int dtype, const void* k, const void* v,
                                      void* k_out, void* v_out, void* kio, void* vio, int32_t* pos, int grid, int parts,
-                                     cudaStream_t st) {
+                                     const WeightRef& wt, float* wt_out, cudaStream_t st) {
   using bf = __nv_bfloat16;
   if (kio != nullptr) {  // hole filling in place
     if (dtype == 1)
       return launch_pdl(dm.pdl != 0, select_kernel<KPT, bf, 2, NT>, grid, NT, 0, st, dm, ws, cu, scores, budget,
                         idx, kept, (const bf*)nullptr, (const bf*)nullptr, (bf*)nullptr, (bf*)nullptr, (bf*)kio,
-                        (bf*)vio, pos, parts);
+                        (bf*)vio, pos, parts, wt, (float*)nullptr);
     return launch_pdl(dm.pdl != 0, select_kernel<KPT, float, 2, NT>, grid, NT, 0, st, dm, ws, cu, scores, budget,
                       idx, kept, (const float*)nullptr, (const float*)nullptr, (float*)nullptr, (float*)nullptr,
-                      (float*)kio, (float*)vio, pos, parts);
+                      (float*)kio, (float*)vio, pos, parts, wt, (float*)nullptr);
   }
   if (k == nullptr)
     return launch_pdl(dm.pdl != 0, select_kernel<KPT, bf, 0, NT>, grid, NT, 0, st, dm, ws, cu, scores, budget,
                       idx, kept, (const bf*)nullptr, (const bf*)nullptr, (bf*)nullptr, (bf*)nullptr, (bf*)nullptr,
-                      (bf*)nullptr, (int32_t*)nullptr, parts);
+                      (bf*)nullptr, (int32_t*)nullptr, parts, WeightRef{}, (float*)nullptr);
   if (dtype == 1)
     return launch_pdl(dm.pdl != 0, select_kernel<KPT, bf, 1, NT>, grid, NT, 0, st, dm, ws, cu, scores, budget,
                       idx, kept, (const bf*)k, (const bf*)v, (bf*)k_out, (bf*)v_out, (bf*)nullptr, (bf*)nullptr,
-                      (int32_t*)nullptr, parts);
+                      (int32_t*)nullptr, parts, wt, wt_out);
   return launch_pdl(dm.pdl != 0, select_kernel<KPT, float, 1, NT>, grid, NT, 0, st, dm, ws, cu, scores, budget,
                     idx, kept, (const float*)k, (const float*)v, (float*)k_out, (float*)v_out, (float*)nullptr,
-                    (float*)nullptr, (int32_t*)nullptr, parts);
+                    (float*)nullptr, (int32_t*)nullptr, parts, wt, wt_out);
 }
 
 cudaError_t launch_select(const Dims& dm, const Ws& ws, const int32_t* cu, const float* scores, int budget,
                           int32_t* idx, int32_t* kept, int max_seqlen, cudaStream_t st, int dtype,
                           const void* k, const void* v, void* k_out, void* v_out, void* kio, void* vio,
-                          int32_t* pos) {
+                          int32_t* pos, const WeightRef& wt, float* wt_out) {
 #define JACAP_SELECT(KPT, NT)                                                                                   \
   JACAP_TRY((launch_select_kpt<KPT, NT>(dm, ws, cu, scores, budget, idx, kept, dtype, k, v, k_out, v_out, kio, vio, \
-                                        pos, grid, parts, st)))
+                                        pos, grid, parts, wt, wt_out, st)))
   // More units than SMs: CTAs of 256 threads (four per SM) while they hold the
   // longest request in one slab, of 512 (two per SM) beyond that (256 units of 32768
   // tokens: 42 us, 46 with 1024 threads; of 131072: 119 and 120). Otherwise CTAs of
@@ -481,6 +535,15 @@ cudaError_t launch_select(const Dims& dm, const Ws& ws, const int32_t* cu, const
   else JACAP_SELECT(32, 1024);
 #undef JACAP_SELECT
   return cudaGetLastError();
+}
+
+cudaError_t launch_protect(const Dims& dm, const Ws& ws, const int32_t* cu, const WeightRef& weights,
+                           const int32_t* pos, int sinks, int recent, float* keys, int max_seqlen, cudaStream_t st) {
+  const int parts = pos != nullptr ? 1 : (max_seqlen - 1) / PK_PART + 1;
+  const int64_t blocks = (int64_t)dm.L * dm.Hkv * dm.S * parts;
+  if (blocks > INT32_MAX) return cudaErrorInvalidValue;
+  return launch_pdl(dm.pdl != 0, protect_kernel, dim3((unsigned)blocks), PK_THREADS, 0, st, dm, ws, cu, weights, pos,
+                    sinks, recent, keys, parts);
 }
 
 cudaError_t launch_compact(const Dims& dm, int dtype, const int32_t* cu, const void* k, const void* v,

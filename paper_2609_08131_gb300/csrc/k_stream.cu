@@ -23,8 +23,11 @@ namespace jacap {
 // the chunk table, record r = {t0, t1, request, r} for the C_tot chunks of a
 // plane, its two lists of runs, {t0, t1, request, first chunk} each, and the Gram's
 // shares of the items.
-__global__ void __launch_bounds__(256) plan_kernel(Dims dm, Ws ws, const int32_t* __restrict__ cu) {
+__global__ void __launch_bounds__(256) plan_kernel(Dims dm, Ws ws, const int32_t* __restrict__ cu,
+                                                    const int32_t* __restrict__ lengths) {
   pdl_wait();
+  // tokens of request s: the first ones of its range, all unless `lengths` says
+  const auto tokens = [&](int s) { return lengths != nullptr ? lengths[s] : cu[s + 1] - cu[s]; };
   __shared__ int s_ctot, s_rtot[2], s_ttot;
   if (threadIdx.x < 16) ws.status[threadIdx.x] = 0u;
   if (threadIdx.x < 8) ws.sched[threadIdx.x] = 0;
@@ -36,8 +39,8 @@ __global__ void __launch_bounds__(256) plan_kernel(Dims dm, Ws ws, const int32_t
     int32_t cacc = 0, racc[2] = {0, 0}, tacc = 0;
     for (int s0 = 0; s0 < dm.S; s0 += 32) {
       const int s = s0 + lane;
-      const int32_t n = s < dm.S ? cu[s + 1] - cu[s] : 0;
-      if (n < 0) ok = false;
+      const int32_t n = s < dm.S ? tokens(s) : 0;
+      if (n < 0 || (s < dm.S && n > cu[s + 1] - cu[s])) ok = false;
       const int32_t c = n > 0 ? (n - 1) / dm.chunk + 1 : 0;
       int32_t v[4] = {c, (c + dm.run_chunks[0] - 1) / dm.run_chunks[0], (c + dm.run_chunks[1] - 1) / dm.run_chunks[1],
                       n > 0 ? (n - 1) / TILE + 1 : 0};
@@ -96,7 +99,7 @@ __global__ void __launch_bounds__(256) plan_kernel(Dims dm, Ws ws, const int32_t
   for (int r = threadIdx.x; r < ctot; r += blockDim.x) {
     const int s = request_of(cpre, r);
     const int64_t t0 = (int64_t)cu[s] + (int64_t)(r - cpre[s]) * dm.chunk;
-    const int64_t t1 = min((int64_t)cu[s + 1], t0 + (int64_t)dm.chunk);
+    const int64_t t1 = min((int64_t)cu[s] + tokens(s), t0 + (int64_t)dm.chunk);
     ws.chunks[r] = make_int4((int)t0, (int)t1, s, r);
   }
   // a request's chunks in as few runs of at most run_chunks as hold them, of nearly equal lengths
@@ -107,7 +110,7 @@ __global__ void __launch_bounds__(256) plan_kernel(Dims dm, Ws ws, const int32_t
     const int64_t nc = cpre[s + 1] - cpre[s], k = rpre[s + 1] - rpre[s], j = r - rpre[s];
     const int64_t c0 = j * nc / k, c1 = (j + 1) * nc / k;
     const int64_t t0 = (int64_t)cu[s] + c0 * dm.chunk;
-    const int64_t t1 = min((int64_t)cu[s + 1], (int64_t)cu[s] + c1 * dm.chunk);
+    const int64_t t1 = min((int64_t)cu[s] + tokens(s), (int64_t)cu[s] + c1 * dm.chunk);
     ws.runs[m * dm.c_cap + r] = make_int4((int)t0, (int)t1, s, cpre[s] + (int)c0);
   }
   // the Gram's shares: the first item of each, at the chunk boundary nearest to an
@@ -474,8 +477,8 @@ static cudaError_t launch_window_stats_t(const Dims& dm, const Ws& ws, const voi
   return cudaGetLastError();
 }
 
-cudaError_t launch_plan(const Dims& dm, const Ws& ws, const int32_t* cu, cudaStream_t st) {
-  JACAP_TRY(launch_pdl(dm.pdl != 0, plan_kernel, 1, 256, 0, st, dm, ws, cu));
+cudaError_t launch_plan(const Dims& dm, const Ws& ws, const int32_t* cu, cudaStream_t st, const int32_t* lengths) {
+  JACAP_TRY(launch_pdl(dm.pdl != 0, plan_kernel, 1, 256, 0, st, dm, ws, cu, lengths));
   return cudaGetLastError();
 }
 

@@ -1,0 +1,580 @@
+"""GPU tests of the decoding loop's operators (rotary positions, attention of drafted tokens, weights received,
+eviction by weights) against plain implementations in 64 bits.
+
+Tolerances are bounds, from the roundings of each path (a rounding is off by half a step: 2^-24 relative in float32,
+2^-8 in bf16):
+
+* a logit is a sum of 128 products: |error| <= 136 2^-24 scale sum_c |q_c k_c| (the products, the additions - the
+  tensor cores' truncate, a whole step each, but in blocks of 16 - and the scaling), so a softmax weight is off by
+  twice that relative, plus 2^-20 for the exponential at its argument and the sums (float32, a few hundred terms at a
+  time);
+* an output adds the weights' roundings to bf16 (bf16 caches), 2^-8 of sum p |v|, and its own.
+"""
+
+import math
+
+import pytest
+import torch
+
+import paper_2609_08131_gb300.api as api
+from paper_2609_08131_gb300 import JACAP_ERR_INVALID_ARG, JACAP_ERR_NONFINITE
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+D = 128
+F32, BF16 = torch.float32, torch.bfloat16
+HALF = {F32: 2.0 ** -24, BF16: 2.0 ** -8}
+SCALE = 1 / math.sqrt(D)
+
+
+def gen(seed):
+    return torch.Generator(device=DEV).manual_seed(seed)
+
+
+def randn(g, *shape, dtype=F32):
+    return torch.randn(*shape, generator=g, device=DEV).to(dtype)
+
+
+def within(got, want, tol, what):
+    got, tol = got.double(), torch.as_tensor(tol, dtype=torch.float64, device=got.device)
+    assert got.shape == want.shape, what
+    assert torch.equal(got.isnan(), want.isnan()), f"{what}: NaN in other places"
+    inf = want.isinf()
+    assert torch.equal(got[inf], want[inf]) and not got[~inf].isinf().any(), f"{what}: infinities in other places"
+    fine = want.isfinite()
+    off = ((got - want).abs() - tol)[fine]
+    assert off.numel() == 0 or off.max() <= 0, f"{what}: {(off > 0).sum()} of {off.numel()} out of bounds, by {off.max():.3e}"
+
+
+# ------------------------------------------------------------------- rope ----
+def rope_plain(x, positions, freq, amplitude, rot, interleaved, inverse):
+    """The turned x in 64 bits and its bound."""
+    angle = positions.double()[..., None] * torch.tensor(freq, dtype=torch.float64, device=x.device)
+    if inverse:
+        angle = -angle
+    c, s = (amplitude * angle.cos())[..., None, :], (amplitude * angle.sin())[..., None, :]
+    y, tol = x.double().clone(), torch.zeros(x.shape, dtype=torch.float64, device=x.device)
+    at = (slice(0, rot, 2), slice(1, rot, 2)) if interleaved else (slice(0, rot // 2), slice(rot // 2, rot))
+    a, b = x.double()[..., at[0]], x.double()[..., at[1]]
+    y[..., at[0]], y[..., at[1]] = a * c - b * s, b * c + a * s
+    # sine and cosine: 2^-23 by sincospif, 2^-25 by the turn's rounding, 2^-24 by the amplitude; 2^-24 for each product
+    # and the sum
+    tol[..., at[0]] = tol[..., at[1]] = (a.abs() + b.abs()) * amplitude * 2.0 ** -21.5
+    return y, tol + y.abs() * (HALF[x.dtype] if x.dtype == BF16 else 0.0)
+
+
+ROPES = [(128, False, None), (128, True, None), (64, False, ("linear", 4.0)), (96, True, ("ntk", 2.0)), (2, True, None),
+         (50, False, ("llama3", 8.0, 1.0, 4.0, 8192)), (20, True, ("yarn", 4.0, 32768, 32.0, 1.0)), (6, False, None),
+         (32, False, ("yarn", 16.0, 4096, 32.0, 1.0)), (16, False, None), (8, True, None)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rot,interleaved,scaling", ROPES)
+def test_rope_against_64_bits(rot, interleaved, scaling, dtype):
+    rope = api.Rope(rot, base=10000.0, interleaved=interleaved, scaling=scaling, device=DEV)
+    freq, amplitude = api.rope_frequencies(rot, 10000.0, scaling)
+    g = gen(rot)
+    for lead, hq, hkv in (((1,), 1, 1), ((3, 7), 8, 2), ((2, 130), 5, 5), ((1300,), 28, 4), ((0, 4), 2, 2)):
+        q, k = randn(g, *lead, hq, D, dtype=dtype), randn(g, *lead, hkv, D, dtype=dtype)
+        positions = torch.randint(-5, 1 << 20, lead, generator=g, device=DEV, dtype=torch.int32)
+        if positions.numel():
+            positions.view(-1)[0] = 2 ** 31 - 1
+            positions.view(-1)[-1] = 0
+        for inverse in (False, True):
+            for got, x in zip(rope.apply(q, k, positions, inverse=inverse), (q, k)):
+                want, tol = rope_plain(x, positions, freq, amplitude, rot, interleaved, inverse)
+                within(got, want, tol, f"rope {lead}")
+                assert torch.equal(got[..., rot:], x[..., rot:])
+
+
+def test_rope_strides_in_place_and_one_tensor():
+    g, rope = gen(5), api.Rope(64, device=DEV)
+    freq, amplitude = api.rope_frequencies(64)
+    wide = randn(g, 3, 6, 9, 2 * D + 8, dtype=BF16)
+    positions = torch.arange(27, device=DEV, dtype=torch.int32).view(9, 3).t()
+    # [requests, heads, tokens, 128] turned around, rows inside wider ones; aligned and not
+    for x in (wide[..., :D].transpose(1, 2), wide[..., 1:D + 1].transpose(1, 2), wide[:, :, :, 8:8 + D].transpose(1, 2)):
+        want, tol = rope_plain(x, positions, freq, amplitude, 64, False, False)
+        q, k = rope.apply(x, None, positions)
+        assert k is None
+        within(q, want, tol, "strided")
+        within(rope.apply(None, x, positions)[1], want, tol, "strided keys")
+    before = wide.clone()
+    x = wide[..., 1:D + 1].transpose(1, 2)
+    assert rope.apply(x, None, positions, inplace=True)[0] is x
+    within(x, want_of(before, positions, freq, amplitude), tol_of(before, positions, freq, amplitude), "in place")
+    outside = torch.ones_like(wide, dtype=torch.bool)
+    outside[..., 1:D + 1] = False
+    assert torch.equal(wide[outside], before[outside])
+    # a key head shared by every query head: read with stride 0
+    shared = randn(g, 5, 1, D).expand(5, 4, D)
+    at = torch.arange(5, device=DEV, dtype=torch.int32)
+    want, tol = rope_plain(shared, at, freq, amplitude, 64, False, False)
+    within(rope.apply(shared, None, at)[0], want, tol, "shared head")
+    with pytest.raises(api.JacapError):
+        rope.apply(shared, None, at, inplace=True)
+
+
+def want_of(before, positions, freq, amplitude):
+    return rope_plain(before[..., 1:D + 1].transpose(1, 2), positions, freq, amplitude, 64, False, False)[0]
+
+
+def tol_of(before, positions, freq, amplitude):
+    return rope_plain(before[..., 1:D + 1].transpose(1, 2), positions, freq, amplitude, 64, False, False)[1]
+
+
+def test_rope_turns_back_and_is_its_own_gradient():
+    g, rope = gen(6), api.Rope(128, interleaved=True, device=DEV)
+    x, y = randn(g, 50, 3, D), randn(g, 50, 3, D)
+    at = torch.randint(0, 1 << 17, (50,), generator=g, device=DEV, dtype=torch.int32)
+    there = rope.apply(x, None, at)[0]
+    back = rope.apply(there, None, at, inverse=True)[0]
+    assert (back - x).abs().max() <= 4 * x.abs().max() * 2.0 ** -21.5
+    # d/dx <turn(x), y> = turn back(y): the map is linear, so a difference of any size is exact but for rounding
+    step = randn(g, 50, 3, D)
+    lhs = ((rope.apply(x + step, None, at)[0].double() - there.double()) * y.double()).sum()
+    rhs = (step.double() * rope.apply(y, None, at, inverse=True)[0].double()).sum()
+    bound = 2.0 ** -20 * ((x.abs() + step.abs()).double().sum() * y.abs().max())
+    assert (lhs - rhs).abs() <= bound
+
+
+# ----------------------------------------------------------------- attend ----
+def make_cache(g, S, L, Hq, Hkv, T, lens, dtype, spread=1.0):
+    N = max(1, sum(lens))
+    k, v = (randn(g, L, Hkv, N, D, dtype=dtype) for _ in range(2))
+    q = (spread * randn(g, S, L, Hq, T, D)).to(dtype)
+    cu = torch.tensor([sum(lens[:i]) for i in range(S + 1)], dtype=torch.int32, device=DEV)
+    return api.Cache(q, k, v, cu, list(lens), Hq)
+
+
+def attend_plain(q, k, v, seen, dtype):
+    """q [rows, D], k and v [n, D], seen [rows, n]: (o, lse, bounds) in 64 bits; what is not seen is left out."""
+    q, k, v = q.double(), k.double(), v.double()
+    x = torch.where(seen, q @ torch.where(seen.any(0)[:, None], k, 0).T * SCALE, -math.inf)
+    size = torch.where(seen, (q.abs() @ k.abs().T) * SCALE, 0.0)
+    size = torch.nan_to_num(size, 0.0, 0.0).amax(1, keepdim=True) if x.shape[1] else x.sum(1, keepdim=True)
+    p = torch.exp(x - x.amax(1, keepdim=True)) if x.shape[1] else x
+    p = torch.where(seen, p, 0.0)
+    z = p.sum(1, keepdim=True)
+    rows = []
+    for r in range(q.shape[0]):
+        at = seen[r]
+        rows.append((p[r, at][:, None] * v[at]).sum(0) / z[r] if at.any() else torch.zeros(D, dtype=torch.float64, device=q.device))
+    o = torch.stack(rows)
+    lse = torch.where(seen.any(1), torch.logsumexp(torch.where(seen.any(1)[:, None], x, 0.0), 1) if x.shape[1] else 0.0, -math.inf)
+    mass = torch.nan_to_num((p / z.clamp_min(1e-300)) @ torch.nan_to_num(v.abs(), 0.0, 0.0))
+    logit = 136 * 2.0 ** -24 * size
+    tol = (2 * logit + 2.0 ** -20 + (HALF[BF16] if dtype == BF16 else 0.0)) * mass + HALF[dtype] * torch.nan_to_num(o.abs())
+    return o, lse, tol, (logit[:, 0] + 2.0 ** -20 + 2.0 ** -23 * torch.nan_to_num(lse.abs(), 0, 0, 0))
+
+
+def check_attend(cache, o, lse, kd=None, vd=None, tree=None, lengths=None, draft_lens=None, untouched=None):
+    S, L, Hq, T = lse.shape
+    Hkv, cu = cache.k.shape[1], cache.cu_seqlens.tolist()
+    G = Hq // Hkv
+    for s in range(S):
+        n = cache.seqlens[s] if lengths is None else lengths[s]
+        rows = T if draft_lens is None else draft_lens[s]
+        nd = 0 if kd is None else rows
+        seen = torch.ones(rows, n + nd, dtype=torch.bool, device=DEV)
+        if kd is not None:
+            bits = torch.arange(nd, device=DEV)
+            seen[:, n:] = bits <= bits[:, None] if tree is None else (tree[s, :rows, None] >> bits & 1).bool()
+        for l in range(L):
+            for h in range(Hq):
+                g = h // G
+                k, v = cache.k[l, g, cu[s]:cu[s] + n], cache.v[l, g, cu[s]:cu[s] + n]
+                if kd is not None:
+                    k, v = torch.cat([k, kd[s, l, g, :nd]]), torch.cat([v, vd[s, l, g, :nd]])
+                if rows:
+                    wo, wl, to, tl = attend_plain(cache_q(cache, s, l, h)[:rows], k, v, seen, cache.k.dtype)
+                    within(o[s, l, h, :rows], wo, to, f"o of request {s}, head {h}")
+                    within(lse[s, l, h, :rows], wl, tl, f"lse of request {s}, head {h}")
+                if untouched is not None:
+                    assert (o[s, l, h, rows:] == untouched).all() and (lse[s, l, h, rows:] == untouched).all()
+
+
+def cache_q(cache, s, l, h):
+    return cache.q_win[s, l, h]
+
+
+def random_tree(seed, S, T):
+    r = torch.Generator().manual_seed(seed)
+    return [[int(torch.randint(-1, t, (1,), generator=r)) if t else -1 for t in range(T)] for _ in range(S)]
+
+
+ATTEND = [
+    # (L, Hq, Hkv, T, lens, drafted: None, "chain", "tree")
+    (1, 4, 1, 1, (37,), "chain"),
+    (1, 1, 1, 1, (1,), None),
+    (1, 8, 8, 1, (64, 65, 63), "chain"),
+    (2, 8, 2, 3, (128, 1, 129, 200), "tree"),
+    (1, 28, 4, 5, (640, 17), "tree"),       # 35 rows
+    (1, 32, 8, 8, (700,), "chain"),         # 32 rows
+    (1, 16, 2, 8, (301,), "tree"),          # 64 rows
+    (1, 10, 2, 13, (1000, 60), "tree"),     # 65 rows
+    (1, 8, 1, 16, (500,), "chain"),         # 128 rows
+    (1, 5, 1, 64, (257, 5), "tree"),        # 320 rows
+    (1, 8, 1, 64, (130,), "tree"),          # 512 rows
+    (1, 4, 4, 2, (2500, 900), "tree"),      # several splits
+    (1, 2, 1, 33, (70,), None),
+    (3, 3, 1, 1, (5, 2, 9), "chain"),
+]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("case", range(len(ATTEND)))
+def test_attend_against_64_bits(case, dtype):
+    L, Hq, Hkv, T, lens, drafted = ATTEND[case]
+    S, g = len(lens), gen(100 + case)
+    cache = make_cache(g, S, L, Hq, Hkv, T, lens, dtype, spread=2.0)
+    att = api.CacheAttention(cache)
+    kd = vd = tree = None
+    if drafted:
+        kd, vd = (randn(g, S, L, Hkv, T, D, dtype=dtype) for _ in range(2))
+    if drafted == "tree":
+        tree = api.tree_masks(random_tree(case, S, T)).to(DEV)
+    o, lse = att.run(k_draft=kd, v_draft=vd, tree=tree)
+    att.check()
+    check_attend(cache, o, lse, kd, vd, tree)
+    first = (o.clone(), lse.clone())
+    att.run(k_draft=kd, v_draft=vd, tree=tree)
+    assert torch.equal(first[0], o) and torch.equal(first[1], lse)  # the order of every sum is fixed
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_attend_live_lengths_masks_and_rows_left_alone(dtype):
+    S, L, Hq, Hkv, T, cap = 5, 2, 6, 2, 9, 200
+    g = gen(7)
+    cache = make_cache(g, S, L, Hq, Hkv, T, (cap,) * S, dtype)
+    lengths, draft_lens = [0, 200, 64, 1, 0], [9, 0, 4, 1, 3]
+    # what lies behind the live tokens and behind the drafted ones may be anything
+    for s, n in enumerate(lengths):
+        for t in (cache.k, cache.v):
+            t[:, :, s * cap + n:(s + 1) * cap] = math.nan
+    kd, vd = (randn(g, S, L, Hkv, T, D, dtype=dtype) for _ in range(2))
+    for s, n in enumerate(draft_lens):
+        kd[s, :, :, n:] = math.inf
+        vd[s, :, :, n:] = math.nan
+    tree = api.tree_masks(random_tree(3, S, T)).to(DEV)
+    tree[0, 4] = 0           # sees nothing at all
+    tree[2, 1] = 0           # cached tokens only
+    tree[3, 0] = -1          # bits of tokens that are not there
+    att = api.CacheAttention(cache)
+    att.o.fill_(77.0)
+    att.lse.fill_(77.0)
+    dev = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    o, lse = att.run(k_draft=kd, v_draft=vd, tree=tree, lengths=dev(lengths), draft_lens=dev(draft_lens))
+    att.check()
+    check_attend(cache, o, lse, kd, vd, tree, lengths, draft_lens, untouched=77.0)
+    assert (lse[0, :, :, 4] == -math.inf).all() and (o[0, :, :, 4] == 0).all()
+    o, lse = att.run(lengths=dev(lengths))  # no drafted tokens
+    check_attend(cache, o, lse, lengths=lengths)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_attend_drafted_values_that_are_not_finite(dtype):
+    S, Hq, Hkv, T = 1, 8, 2, 6
+    g = gen(8)
+    cache = make_cache(g, S, 1, Hq, Hkv, T, (100,), dtype)
+    kd, vd = (randn(g, S, 1, Hkv, T, D, dtype=dtype) for _ in range(2))
+    tree = api.tree_masks([[-1, 0, 0, 1, 2, -1]]).to(DEV)
+    vd[0, 0, 0, 1, 5] = math.nan    # seen by tokens 1 and 3
+    vd[0, 0, 1, 2, 7] = -math.inf   # seen by tokens 2 and 4
+    kd[0, 0, 1, 5, 0] = math.nan    # seen by token 5 only
+    o, lse = api.CacheAttention(cache).run(k_draft=kd, v_draft=vd, tree=tree)
+    check_attend(cache, o, lse, kd, vd, tree)
+
+
+def test_attend_strides():
+    g, S, L, Hq, Hkv, T, cap = gen(9), 3, 2, 8, 2, 4, 90
+    # slots as [tokens, heads] rows (a head's rows apart), queries and drafts as [S, T, H, D]
+    kv = randn(g, 2, L, S * cap, Hkv, D, dtype=BF16).transpose(2, 3)
+    q = randn(g, S, L, T, Hq, D, dtype=BF16).transpose(2, 3)
+    drafts = randn(g, 2, S, L, T, Hkv, D + 8, dtype=BF16)[..., :D].transpose(3, 4)
+    cu = torch.arange(0, S * cap + 1, cap, dtype=torch.int32, device=DEV)
+    cache = api.Cache(q, kv[0], kv[1], cu, [cap] * S, Hq)
+    o, lse = api.CacheAttention(cache).run(k_draft=drafts[0], v_draft=drafts[1])
+    check_attend(cache, o, lse, drafts[0], drafts[1])
+
+
+def test_attend_large_logits():
+    """Maxima that rise by far more than the lazy rescaling allows, and logits whose exponentials underflow."""
+    g = gen(10)
+    for dtype in (BF16, F32):
+        cache = make_cache(g, 1, 1, 4, 1, 2, (900,), dtype, spread=4.0)
+        cache.k[:, :, ::7] *= 6.0
+        cache.k[:, :, 500] *= 20.0
+        o, lse = api.CacheAttention(cache).run()
+        check_attend(cache, o, lse)
+
+
+def test_attend_reports_lengths_out_of_range():
+    g = gen(11)
+    cache = make_cache(g, 2, 1, 4, 1, 1, (50, 60), BF16)
+    att = api.CacheAttention(cache)
+    bad = torch.tensor([50, 61], dtype=torch.int32, device=DEV)
+    o, lse = att.run(lengths=bad)  # clamped
+    with pytest.raises(api.JacapError) as e:
+        att.check()
+    assert e.value.status == JACAP_ERR_INVALID_ARG
+    check_attend(cache, o, lse)
+    att.run()
+    att.check()  # the word was cleared
+
+
+# ------------------------------------------------------------------ weigh ----
+def weigh_plain(cache, lengths=None, q_lens=None, q_rows=None, lse=None, before=None):
+    """weights and lse of every unit in 64 bits, with their bounds; NaN where nothing is written."""
+    S, L, Hq, w, _ = cache.q_win.shape
+    Hkv, N = cache.k.shape[1:3]
+    G, cu = Hq // Hkv, cache.cu_seqlens.tolist()
+    weights = torch.full((L, Hkv, N), math.nan, dtype=torch.float64, device=DEV)
+    tol, out, tol_lse = weights.clone(), torch.full((S, L, Hq, w), math.nan, dtype=torch.float64, device=DEV), None
+    tol_lse = out.clone()
+    for s in range(S):
+        n = cache.seqlens[s] if lengths is None else lengths[s]
+        ql = w if q_lens is None else q_lens[s]
+        rows = list(range(ql)) if q_rows is None else [int(x) for x in q_rows[s, :ql]]
+        for l in range(L):
+            for g in range(Hkv):
+                k = cache.k[l, g, cu[s]:cu[s] + n].double()
+                sums, bound = torch.zeros(n, dtype=torch.float64, device=DEV), torch.zeros(n, dtype=torch.float64, device=DEV)
+                for h in range(g * G, (g + 1) * G):
+                    for j, r in enumerate(rows):
+                        if r < 0 or r >= w:
+                            continue
+                        last = n - ql + j
+                        q = cache.q_win[s, l, h, r].double()
+                        x = k[:max(0, last + 1)] @ q * SCALE
+                        size = (k.abs() @ q.abs()).amax() * SCALE if n else torch.zeros(())
+                        e = torch.logsumexp(x, 0) if x.numel() else torch.tensor(-math.inf, dtype=torch.float64)
+                        d = 136 * 2.0 ** -24 * float(size) + 2.0 ** -20
+                        out[s, l, h, r], tol_lse[s, l, h, r] = e, d + 2.0 ** -23 * (abs(float(e)) if x.numel() else 0.0)
+                        if lse is not None:
+                            e = lse[s, l, h, r].double()
+                        if x.numel() and e > -math.inf:
+                            p = torch.exp(x - e)
+                            sums[:x.numel()] += p
+                            # with e given its own rounding to float32 is the input's; e log2 e rounds again
+                            bound[:x.numel()] += p * (2 * d + 2.0 ** -23 * abs(float(e)) + 2.0 ** -22 * x.abs())
+                if before is not None:
+                    old = max(0, n - ql)
+                    sums[:old] += before[l, g, cu[s]:cu[s] + old].double()
+                weights[l, g, cu[s]:cu[s] + n] = sums
+                tol[l, g, cu[s]:cu[s] + n] = bound + sums * 2.0 ** -22
+    return weights, tol, out, tol_lse
+
+
+def check_weigh(cache, got, lse, want, filler=None):
+    weights, tol, e, tol_e = want
+    written = ~weights.isnan()
+    within(got[written], weights[written], tol[written], "weights")
+    if lse is not None:
+        rows = ~e.isnan()
+        within(lse[rows], e[rows], tol_e[rows], "lse")
+    if filler is not None:
+        assert (got[~written] == filler).all()
+        if lse is not None:
+            assert (lse[e.isnan()] == filler).all()
+
+
+WEIGH = [  # (L, Hq, Hkv, w, lens)
+    (1, 4, 1, 8, (300,)), (1, 1, 1, 1, (1,)), (2, 8, 2, 16, (129, 5, 128)), (1, 4, 4, 32, (20, 33, 32)),
+    (1, 5, 1, 32, (400,)), (1, 7, 1, 32, (700, 40)), (1, 6, 1, 64, (300,)), (1, 8, 1, 64, (257,)), (1, 8, 1, 40, (150,)),
+    (1, 3, 1, 3, (1100, 2, 1)), (1, 8, 2, 20, (513,)),
+]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("case", range(len(WEIGH)))
+def test_weigh_against_64_bits(case, dtype):
+    L, Hq, Hkv, w, lens = WEIGH[case]
+    cache = make_cache(gen(200 + case), len(lens), L, Hq, Hkv, w, lens, dtype, spread=2.0)
+    ev = api.WeightEvictor(cache, 1)
+    got, lse = ev.score()
+    ev.check()
+    want = weigh_plain(cache)
+    check_weigh(cache, got, lse, want)
+    first = got.clone()
+    ev.score()
+    assert torch.equal(first, got)
+    # the same with the normalisers given, on top of earlier weights, into the same array
+    before = torch.rand(got.shape, generator=gen(1), device=DEV)
+    given = lse.clone()
+    got.copy_(before)
+    ev.score(lse=given, before=got)
+    ev.check()
+    check_weigh(cache, got, None, weigh_plain(cache, lse=given, before=before))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_weigh_slots_queries_and_paths(dtype):
+    S, L, Hq, Hkv, w, cap = 6, 2, 6, 2, 7, 300
+    g = gen(13)
+    cache = make_cache(g, S, L, Hq, Hkv, w, (cap,) * S, dtype)
+    lengths, q_lens = [300, 0, 5, 130, 1, 200], [7, 3, 7, 0, 1, 4]
+    for s, n in enumerate(lengths):
+        cache.k[:, :, s * cap + n:(s + 1) * cap] = math.nan
+    rows = torch.tensor([[6, 5, 4, 3, 2, 1, 0], [0, 1, 2, 3, 4, 5, 6], [0, 2, 4, 6, 1, 3, 5], [1] * 7, [3] + [-1] * 6,
+                         [0, -1, 9, 2, 5, 5, 5]], dtype=torch.int32)
+    dev = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    ev = api.WeightEvictor(cache, 1)
+    ev.weights.fill_(55.0)
+    ev.lse.fill_(55.0)
+    before = torch.rand(ev.weights.shape, generator=g, device=DEV)
+    got, lse = ev.score(lengths=dev(lengths), q_lens=dev(q_lens), q_rows=rows.to(DEV), before=before)
+    ev.check()
+    check_weigh(cache, got, lse, weigh_plain(cache, lengths, q_lens, rows, before=before), filler=55.0)
+
+
+def test_weigh_many_runs_and_requests():
+    """Enough tokens that a unit's statistics come from several runs of several CTAs."""
+    for dtype, lens in ((BF16, (30000, 17, 9000, 4097)), (F32, (9000, 100))):
+        cache = make_cache(gen(14), len(lens), 1, 2, 1, 4, lens, dtype, spread=2.0)
+        ev = api.WeightEvictor(cache, 1)
+        got, lse = ev.score()
+        ev.check()
+        check_weigh(cache, got, lse, weigh_plain(cache))
+
+
+def test_weigh_reports_what_is_not_finite_and_bad_lengths():
+    cache = make_cache(gen(15), 1, 1, 4, 1, 4, (200,), BF16)
+    cache.k[0, 0, 100, 3] = math.nan
+    ev = api.WeightEvictor(cache, 8)
+    ev.run()
+    with pytest.raises(api.JacapError) as e:
+        ev.check()
+    assert e.value.status == JACAP_ERR_NONFINITE
+    cache.k[0, 0, 100, 3] = 0.0
+    ev.run()
+    ev.check()
+    for n in (-1, 201):
+        ev.score(lengths=torch.tensor([n], dtype=torch.int32, device=DEV))
+        with pytest.raises(api.JacapError) as e:
+            ev.check()
+        assert e.value.status == JACAP_ERR_INVALID_ARG
+
+
+# ------------------------------------------------------------------ evict ----
+def select_plain(weights, n, budget, sinks, recent, tags=None):
+    tag = torch.arange(n) if tags is None else tags.cpu().long()
+    w = weights.double().cpu().clone()
+    if n:
+        w[(tag < sinks) | (tag > tag.max() - recent)] = math.inf
+    order = sorted(range(n), key=lambda i: (-w[i].item(), i))
+    return sorted(order[:budget])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("L,Hkv,lens,budget,sinks,recent", [
+    (1, 1, (1,), 1, 0, 0), (2, 3, (100, 7, 33), 16, 2, 5), (1, 2, (4000, 900), 700, 4, 64), (1, 1, (5000,), 96, 96, 0),
+    (1, 1, (40000,), 300, 0, 300), (3, 60, (50, 60), 20, 1, 1), (1, 2, (64, 64), 64, 3, 3)])
+def test_select_by_weights(L, Hkv, lens, budget, sinks, recent, dtype):
+    g = gen(16)
+    cache = make_cache(g, len(lens), L, Hkv, Hkv, 1, lens, dtype)
+    ev = api.WeightEvictor(cache, budget, sinks=sinks, recent=recent)
+    weights = torch.exp(2 * randn(g, L, Hkv, sum(lens)))
+    weights[torch.rand(weights.shape, generator=g, device=DEV) < 0.3] = 0.0   # many ties
+    weights[torch.rand(weights.shape, generator=g, device=DEV) < 0.1] = 1e-30
+    kept_weights = weights.clone()
+    ev.select_compact(weights)
+    ev.check()
+    assert torch.equal(weights, kept_weights)
+    at = 0
+    for s, n in enumerate(lens):
+        for l in range(L):
+            for h in range(Hkv):
+                want = select_plain(weights[l, h, at:at + n], n, budget, sinks, recent)
+                got = ev.idx[l, h, s].tolist()
+                assert got == want + [-1] * (budget - len(want))
+                rows = torch.tensor(want, device=DEV, dtype=torch.long) + at
+                for out, src in ((ev.k_out, cache.k), (ev.v_out, cache.v)):
+                    assert torch.equal(out[l, h, s, :len(want)], src[l, h, rows]) and (out[l, h, s, len(want):] == 0).all()
+                assert torch.equal(ev.weights_out[l, h, s, :len(want)], weights[l, h, rows])
+                assert (ev.weights_out[l, h, s, len(want):] == 0).all()
+        assert ev.kept[s] == min(n, budget)
+        at += n
+
+
+def test_select_by_weights_and_tags():
+    g, n = gen(17), 500
+    cache = make_cache(g, 1, 2, 2, 2, 1, (n,), BF16)
+    ev = api.WeightEvictor(cache, 50, sinks=3, recent=20)
+    weights = torch.rand((2, 2, n), generator=g, device=DEV)
+    tags = torch.stack([torch.randperm(2 * n, generator=g, device=DEV)[:n] for _ in range(4)]).view(2, 2, n).to(torch.int32)
+    ev.select_compact(weights, pos=tags)
+    ev.check()
+    for l in range(2):
+        for h in range(2):
+            assert ev.idx[l, h, 0].tolist() == select_plain(weights[l, h], n, 50, 3, 20, tags[l, h])
+
+
+@pytest.mark.parametrize("bad", [math.nan, -1.0, math.inf])
+def test_select_refuses_weights_that_are_none(bad):
+    cache = make_cache(gen(18), 1, 1, 1, 1, 1, (100,), BF16)
+    ev = api.WeightEvictor(cache, 10)
+    ev.idx.fill_(-7)
+    weights = torch.rand((1, 1, 100), device=DEV)
+    weights[0, 0, 42] = bad
+    ev.select_compact(weights)
+    with pytest.raises(api.JacapError) as e:
+        ev.check()
+    assert e.value.status == JACAP_ERR_NONFINITE and (ev.idx == -7).all()
+    weights[0, 0, 42] = 0.5
+    ev.select_compact(weights)
+    ev.check()
+    assert ev.idx[0, 0, 0].tolist() == select_plain(weights[0, 0], 100, 10, 0, 0)
+
+
+# --------------------------------------------------- streams, graphs, refusals ----
+def test_operators_on_another_stream_and_in_graphs():
+    g, S, L, Hq, Hkv, T = gen(19), 2, 1, 8, 2, 3
+    cache = make_cache(g, S, L, Hq, Hkv, T, (900, 1500), BF16)
+    kd, vd = (randn(g, S, L, Hkv, T, D, dtype=BF16) for _ in range(2))
+    lengths = torch.tensor([900, 1500], dtype=torch.int32, device=DEV)
+    at = torch.arange(S * T, dtype=torch.int32, device=DEV).view(S, T)
+    rope = api.Rope(device=DEV)
+    att, ev = api.CacheAttention(cache), api.WeightEvictor(cache, 100, sinks=2, recent=10)
+
+    def loop(stream=None):
+        q, k = rope.apply(cache.q_win[:, 0].transpose(1, 2), kd[:, 0].transpose(1, 2), at, stream=stream)
+        q, k = q.transpose(1, 2).unsqueeze(1), k.transpose(1, 2).unsqueeze(1)
+        o, lse = att.run(q, k_draft=k, v_draft=vd_like, lengths=lengths, stream=stream)
+        ev.score(q, lse=lse, lengths=lengths, stream=stream)
+        ev.select_compact(stream=stream)
+        return [t.clone() for t in (q, o, lse, ev.weights, ev.idx, ev.k_out)]
+
+    vd_like = vd.transpose(2, 3).contiguous().transpose(2, 3)
+    ref = loop()
+    side = torch.cuda.Stream(device=DEV)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        out = loop()
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(ref, out))
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(torch.cuda.current_stream()):
+        loop(side)
+    side.synchronize()
+    # two graphs that share the workspaces, replayed one after the other with other lengths
+    graphs, results = [], []
+    torch.cuda.synchronize()
+    for _ in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            results.append(loop())
+        graphs.append(graph)
+    for n in ([900, 1500], [1, 700], [450, 0]):
+        lengths.copy_(torch.tensor(n, dtype=torch.int32))
+        want = loop()
+        for graph, got in zip(graphs, results):
+            graph.replay()
+        torch.cuda.synchronize()
+        for got in results:
+            for a, b in zip(want[:3], got[:3]):
+                assert torch.equal(a, b)
+            for s in range(2):
+                a0 = 900 * s
+                assert torch.equal(want[3][:, :, a0:a0 + n[s]], got[3][:, :, a0:a0 + n[s]])
