@@ -475,7 +475,9 @@ jacap_status jacap_rotate(const jacap_rope* rope, jacap_dtype dtype, int32_t num
  *                  sees drafted token j (its ancestors and itself); bits from
  *                  draft_lens[s] on are ignored. NULL: a chain, j <= t.
  *   o_strides      of o, as those of q (request, layer, head, query)
- *   lse            device float32 [num_seqs][num_layers][num_q_heads][T] or NULL
+ *   lse            device float32 or NULL: row (s, l, h, t) at s lse_strides[0] + l [1]
+ *                  + h [2] + t (elements; a layer's call can write its part of an
+ *                  array over all layers)
  *   ws             device, 256-byte aligned, jacap_attend_workspace() bytes (0 for
  *                  a layout that is refused), whose first 64 bytes were zeroed once:
  *                  the status word. A length outside its range is clamped and
@@ -493,6 +495,7 @@ typedef struct {
   int64_t draft_strides[8];
   const uint64_t* tree;
   int64_t o_strides[4];
+  int64_t lse_strides[3];
 } jacap_attention;
 size_t jacap_attend_workspace(const jacap_layout* layout);
 jacap_status jacap_attend(const jacap_layout* layout, const jacap_attention* attn, const void* q,
@@ -521,7 +524,7 @@ jacap_status jacap_attend(const jacap_layout* layout, const jacap_attention* att
  *              outside [0, window) is no query
  *   lse_given  1: lse is an input, as jacap_attend wrote it for these queries (K is
  *              then read once); 0: it is computed, and written unless NULL
- *   lse        device float32 [num_seqs][num_layers][num_q_heads][window], indexed
+ *   lse        device float32 [num_seqs][num_layers][num_q_heads][window], dense, indexed
  *              like the queries (before q_rows); rows without a query are left alone.
  *              A row that sees nothing has -inf and gives no weight.
  *   before     device float32 [num_layers][num_kv_heads][total_tokens] or NULL; it

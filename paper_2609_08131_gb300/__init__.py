@@ -119,6 +119,7 @@ class jacap_attention(ctypes.Structure):
         ("draft_strides", ctypes.c_int64 * 8),
         ("tree", ctypes.c_void_p),
         ("o_strides", ctypes.c_int64 * 4),
+        ("lse_strides", ctypes.c_int64 * 3),
     ]
 
 
@@ -193,16 +194,20 @@ _SIGS = {
 }
 
 
+_typed = None
+
+
 def lib() -> ctypes.CDLL:
     """The loaded C library with argument types declared."""
-    h = _lib.load(build_if_missing=True)
-    if not getattr(h, "_jacap_typed", False):
+    global _typed
+    if _typed is None:
+        h = _lib.load(build_if_missing=True)
         for name, (res, args) in _SIGS.items():
             fn = getattr(h, name)
             fn.restype = res
             fn.argtypes = args
-        h._jacap_typed = True
-    return h
+        _typed = h
+    return _typed
 
 
 def jacap_schedule_info(layout: jacap_layout, params: jacap_params):

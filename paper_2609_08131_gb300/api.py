@@ -6,7 +6,6 @@ libjacap's kernels. Errors from the library raise ``JacapError``.
 
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import math
 from dataclasses import dataclass
@@ -114,32 +113,34 @@ class Cache:
         return lay
 
 
-@contextlib.contextmanager
-def _on(device, stream):
-    """The device current, and `stream` (the device's current one if None) for what is
-    allocated and enqueued inside; yields the stream's handle."""
+def _enqueue(device, stream, call):
+    """call(handle of the stream) with the device current and the stream (the device's current one
+    if None) current for what is allocated inside."""
+    if stream is None and device.index == torch.cuda.current_device():
+        return call(torch._C._cuda_getCurrentRawStream(device.index))
     with torch.cuda.device(device):
         if stream is None:
-            yield _stream(torch.cuda.current_stream(device))
-        else:
-            if stream.device != device:
-                raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
-            with torch.cuda.stream(stream):
-                yield _stream(stream)
+            stream = torch.cuda.current_stream(device)
+        elif stream.device != device:
+            raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
+        with torch.cuda.stream(stream):
+            return call(stream.cuda_stream)
 
 
 def _tensor(name, t, device, dtype, shape, contiguous=False):
-    """Checks a tensor argument; None passes."""
+    """Checks a tensor argument; its address. None passes, as None."""
     if t is None:
-        return
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device or tuple(t.shape) != tuple(shape):
+        return None
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device or t.shape != shape:
         raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on {device}")
-    if torch.is_grad_enabled() and t.requires_grad:
+    if t.requires_grad and torch.is_grad_enabled():
         raise ValueError(f"{name} requires a gradient, which this call does not give")
-    if contiguous and not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    if not contiguous and len(shape) > 1 and shape[-1] > 1 and t.stride(-1) != 1:
+    if contiguous:
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+    elif t.stride(-1) != 1:
         raise ValueError(f"the last axis of {name} must be contiguous")
+    return t.data_ptr()
 
 
 def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling=None):
@@ -214,36 +215,38 @@ class Rope:
         of any strides but the last axis' (float32 or bfloat16); positions: int32 of the
         leading axes' shape. Returns the turned (q, k): new tensors, or the same ones
         with ``inplace``. ``inverse`` turns back (and is the gradient)."""
-        given = [(n, t) for n, t in (("q", q), ("k", k)) if t is not None]
-        if not given:
+        first = q if q is not None else k
+        if first is None:
             raise ValueError("q or k must be given")
-        lead, dtype = tuple(given[0][1].shape[:-2]), given[0][1].dtype
+        lead, dtype, dev = first.shape[:-2], first.dtype, self.device
         if len(lead) not in (1, 2) or dtype not in (torch.float32, torch.bfloat16):
             raise ValueError("q and k must be float32 or bfloat16 [tokens, heads, 128] or [requests, tokens, heads, 128]")
-        for name, t in given:
-            _tensor(name, t, self.device, dtype, lead + (t.shape[-2], 128))
-            if t.shape[-2] < 1:
-                raise ValueError(f"{name} has no heads")
-        if (not isinstance(positions, torch.Tensor) or positions.dtype != torch.int32 or positions.device != self.device
-                or tuple(positions.shape) != lead):
-            raise ValueError(f"positions must be an int32 tensor of shape {lead} on {self.device}")
-        S, T = lead if len(lead) == 2 else (1, lead[0])
-        ps = positions.stride() if len(lead) == 2 else (0, positions.stride(0))
-        with _on(self.device, stream) as st:
+        for name, t in (("q", q), ("k", k)):
+            if t is not None:
+                _tensor(name, t, dev, dtype, (*lead, t.shape[-2], 128))
+                if t.shape[-2] < 1:
+                    raise ValueError(f"{name} has no heads")
+        if (not isinstance(positions, torch.Tensor) or positions.dtype != torch.int32 or positions.device != dev
+                or positions.shape != lead):
+            raise ValueError(f"positions must be an int32 tensor of shape {tuple(lead)} on {dev}")
+        two = len(lead) == 2
+        S, T = lead if two else (1, lead[0])
+
+        def turn(st):
             out, args = [None, None], [None, None]
             for i, t in enumerate((q, k)):
-                if t is None:
-                    continue
-                y = t if inplace else torch.empty_like(t)
-                x = jacap_rope_tensor()
-                x.x, x.y, x.heads = t.data_ptr(), y.data_ptr(), t.shape[-2]
-                for into, src in ((x.x_strides, t), (x.y_strides, y)):
-                    into[:] = src.stride()[:-1] if len(lead) == 2 else (0,) + src.stride()[:-1]
-                out[i], args[i] = y, x
+                if t is not None:
+                    y = out[i] = t if inplace else torch.empty_like(t)
+                    xs, ys = t.stride()[:-1], y.stride()[:-1]
+                    args[i] = jacap_rope_tensor(t.data_ptr(), y.data_ptr(), t.shape[-2], xs if two else (0, *xs),
+                                                ys if two else (0, *ys))
             if S and T:
                 _check(jacap_rotate(self._c, JACAP_BF16 if dtype == torch.bfloat16 else JACAP_F32, S, T,
-                                    _ptr(positions), ps, inverse, args[0], args[1], st), "jacap_rotate")
-        return out[0], out[1]
+                                    positions.data_ptr(), positions.stride() if two else (0, positions.stride(0)),
+                                    inverse, args[0], args[1], st), "jacap_rotate")
+            return out[0], out[1]
+
+        return _enqueue(dev, stream, turn)
 
 
 def tree_masks(parents):
@@ -261,10 +264,14 @@ def tree_masks(parents):
     return torch.tensor(rows, dtype=torch.int64)
 
 
+def _strides(t):
+    """The strides of the four leading axes (that of an axis of one entry means nothing and may be anything)."""
+    st, shape = t.stride(), t.shape
+    return [st[i] if shape[i] > 1 else 128 for i in range(4)]
+
+
 def _query_strides(lay, q):
-    """q's strides into the layout (that of an axis of one entry means nothing and may be anything)."""
-    lay.q_stride_seq, lay.q_stride_layer, lay.q_stride_head, lay.q_stride_pos = [
-        st if n > 1 else 128 for n, st in zip(q.shape[:4], q.stride()[:4])]
+    lay.q_stride_seq, lay.q_stride_layer, lay.q_stride_head, lay.q_stride_pos = _strides(q)
     return lay
 
 
@@ -293,35 +300,36 @@ class CacheAttention:
         self._attn = jacap_attention()
         self._attn.scale = 1.0 / math.sqrt(128.0) if scale is None else float(scale)
         self._attn.o_strides[:] = self.o.stride()[:4]
+        self._attn.lse_strides[:] = self.lse.stride()[:3]
 
     def run(self, q=None, k_draft=None, v_draft=None, tree=None, lengths=None, draft_lens=None, stream=None):
         """q: [S, L, Hq, T, 128] (the cache's q_win if None); k_draft, v_draft: [S, L, Hkv,
         T, 128]; tree: int64 [S, T] masks (None: a chain); lengths: int32
         [S] cached tokens of each request (None: all); draft_lens: int32 [S] queries of
         each request (None: T; rows behind are left as they were). Returns (o, lse)."""
-        c, a, dev = self.cache, self._attn, self.device
+        c, a, dev, dt = self.cache, self._attn, self.device, self.dtype
         S, L, Hq, T = self.lse.shape
-        q = c.q_win if q is None else q
-        _tensor("q", q, dev, self.dtype, (S, L, Hq, T, 128))
-        _tensor("lengths", lengths, dev, torch.int32, (S,), True)
-        _tensor("draft_lens", draft_lens, dev, torch.int32, (S,), True)
-        _tensor("tree", tree, dev, torch.int64, (S, T), True)
+        if q is None:
+            q = c.q_win
+        qp = _tensor("q", q, dev, dt, (S, L, Hq, T, 128))
+        a.lengths = _tensor("lengths", lengths, dev, torch.int32, (S,), True)
+        a.draft_lens = _tensor("draft_lens", draft_lens, dev, torch.int32, (S,), True)
+        a.tree = _tensor("tree", tree, dev, torch.int64, (S, T), True)
         if (k_draft is None) != (v_draft is None) or (tree is not None and k_draft is None):
             raise ValueError("k_draft and v_draft come together, and a tree with them")
-        for name, t in (("k_draft", k_draft), ("v_draft", v_draft)):
-            _tensor(name, t, dev, self.dtype, (S, L, c.k.shape[1], T, 128))
+        shape = (S, L, c.k.shape[1], T, 128)
+        a.k_draft = _tensor("k_draft", k_draft, dev, dt, shape)
+        a.v_draft = _tensor("v_draft", v_draft, dev, dt, shape)
         if k_draft is not None:
-            # (the stride of an axis of one entry means nothing and may be anything)
-            a.draft_strides[:] = [st if n > 1 else 128 for t in (k_draft, v_draft)
-                                  for n, st in zip(t.shape[:4], t.stride()[:4])]
-        for name, t in (("lengths", lengths), ("draft_lens", draft_lens), ("tree", tree), ("k_draft", k_draft),
-                        ("v_draft", v_draft)):
-            setattr(a, name, None if t is None else t.data_ptr())
+            a.draft_strides[:] = _strides(k_draft) + _strides(v_draft)
         lay = _query_strides(self.lay, q)
-        with _on(dev, stream) as st:
-            _check(jacap_attend(lay, a, _ptr(q), _ptr(c.k), _ptr(c.v), _ptr(self.o), _ptr(self.lse), _ptr(self.ws),
-                                self.ws.numel(), st), "jacap_attend")
-        return self.o, self.lse
+
+        def attend(st):
+            _check(jacap_attend(lay, a, qp, c.k.data_ptr(), c.v.data_ptr(), self.o.data_ptr(), self.lse.data_ptr(),
+                                self.ws.data_ptr(), self.ws.numel(), st), "jacap_attend")
+            return self.o, self.lse
+
+        return _enqueue(dev, stream, attend)
 
     def check(self, stream=None):
         _check_and_clear(self.ws, self.device, stream)
@@ -329,11 +337,13 @@ class CacheAttention:
 
 def _check_and_clear(ws, device, stream):
     """Raises what the status word holds, clearing it: a later call starts anew."""
-    with _on(device, stream) as st:
-        status = jacap_device_status(_ptr(ws), st)
+    def read(st):
+        status = jacap_device_status(ws.data_ptr(), st)
         if status != JACAP_OK:
             ws[:64].zero_()
-    _check(status, "device status")
+        return status
+
+    _check(_enqueue(device, stream, read), "device status")
 
 
 class WeightEvictor:
@@ -383,39 +393,46 @@ class WeightEvictor:
         [S] live tokens and queries of each request; q_rows: int32 [S, w] which query is
         the j-th."""
         c, h, dev = self.cache, self._how, self.device
-        q = c.q_win if q is None else q
+        if q is None:
+            q = c.q_win
         S, L, Hq, w = self.lse.shape
-        _tensor("q", q, dev, c.k.dtype, (S, L, Hq, w, 128))
-        _tensor("lse", lse, dev, torch.float32, self.lse.shape, True)
-        _tensor("before", before, dev, torch.float32, self.weights.shape, True)
-        _tensor("lengths", lengths, dev, torch.int32, (S,), True)
-        _tensor("q_lens", q_lens, dev, torch.int32, (S,), True)
-        _tensor("q_rows", q_rows, dev, torch.int32, (S, w), True)
+        qp = _tensor("q", q, dev, c.k.dtype, (S, L, Hq, w, 128))
         h.lse_given = int(lse is not None)
-        for name, t in (("lengths", lengths), ("q_lens", q_lens), ("q_rows", q_rows)):
-            setattr(h, name, None if t is None else t.data_ptr())
+        if lse is None:
+            lse = self.lse
+        lp = _tensor("lse", lse, dev, torch.float32, self.lse.shape, True)
+        bp = _tensor("before", before, dev, torch.float32, self.weights.shape, True)
+        h.lengths = _tensor("lengths", lengths, dev, torch.int32, (S,), True)
+        h.q_lens = _tensor("q_lens", q_lens, dev, torch.int32, (S,), True)
+        h.q_rows = _tensor("q_rows", q_rows, dev, torch.int32, (S, w), True)
         lay = _query_strides(self.lay, q)
-        lse = self.lse if lse is None else lse
-        with _on(dev, stream) as st:
-            _check(jacap_weigh(lay, h, _ptr(q), _ptr(c.k), _ptr(lse), _ptr(before), _ptr(self.weights), _ptr(self.ws),
+
+        def weigh(st):
+            _check(jacap_weigh(lay, h, qp, c.k.data_ptr(), lp, bp, self.weights.data_ptr(), self.ws.data_ptr(),
                                self.ws.numel(), st), "jacap_weigh")
-        return self.weights, lse
+            return self.weights, lse
+
+        return _enqueue(dev, stream, weigh)
 
     def select_compact(self, weights=None, pos=None, stream=None):
         """The selection by ``weights`` (None: those of ``score()``) and the retained
         cache (``jacap_select_weights``). ``pos``: int32 [L, Hkv, N] tags by which the
         first and the last tokens are told (None: by row)."""
         c, dev = self.cache, self.device
-        weights = self.weights if weights is None else weights
-        _tensor("weights", weights, dev, torch.float32, self.weights.shape, True)
-        _tensor("pos", pos, dev, torch.int32, self.weights.shape, True)
+        if weights is None:
+            weights = self.weights
+        wp = _tensor("weights", weights, dev, torch.float32, self.weights.shape, True)
+        pp = _tensor("pos", pos, dev, torch.int32, self.weights.shape, True)
         if pos is not None and not c.k.is_contiguous():
             raise ValueError("tags need a dense cache")
-        with _on(dev, stream) as st:
-            _check(jacap_select_weights(self.lay, _ptr(weights), _ptr(pos), self.sinks, self.recent, self.budget,
-                                        _ptr(self.idx), _ptr(self.kept), _ptr(c.k), _ptr(c.v), _ptr(self.k_out),
-                                        _ptr(self.v_out), _ptr(self.weights_out), _ptr(self.keys), _ptr(self.ws),
-                                        self.ws.numel(), st), "jacap_select_weights")
+
+        def select(st):
+            _check(jacap_select_weights(self.lay, wp, pp, self.sinks, self.recent, self.budget, self.idx.data_ptr(),
+                                        self.kept.data_ptr(), c.k.data_ptr(), c.v.data_ptr(), self.k_out.data_ptr(),
+                                        self.v_out.data_ptr(), self.weights_out.data_ptr(), self.keys.data_ptr(),
+                                        self.ws.data_ptr(), self.ws.numel(), st), "jacap_select_weights")
+
+        _enqueue(dev, stream, select)
 
     def run(self, stream=None):
         self.score(stream=stream)
@@ -684,15 +701,28 @@ class DecodeEvictor:
     launch (jacap_append; indexed copies and jacap_stats_update where that takes
     no such tensors); the scoring pass, the selection and the compaction run in
     libjacap's kernels too.
+
+    A model's step reads the slots with ``attend`` (layer by layer, the step's own
+    tokens passed as drafted ones: one, a chain, or a tree), with queries and keys turned
+    by ``rotate`` where it uses rotary positions, and then enters its token with
+    ``step`` or the accepted drafted tokens with ``accept``.
     """
 
     def __init__(self, num_seqs: int, num_layers: int, num_q_heads: int, num_kv_heads: int, budget: int,
                  interval: int, dtype=torch.bfloat16, params: jacap_params | None = None, device="cuda",
-                 preserve_order: bool = False):
+                 preserve_order: bool = False, rule: str = "jacap", sinks: int = 0, recent: int = 0,
+                 scale: float | None = None):
         """``preserve_order``: keep the retained rows in ascending slot order
         (moves up to ``budget`` rows per eviction) instead of filling the
         evicted rows with the kept rows from past the budget (moves at most
-        ``interval`` rows)."""
+        ``interval`` rows).
+
+        ``rule``: "jacap", or "weight": the tokens that received the most attention so far
+        stay, beside those with ids below ``sinks`` and the last ``recent`` ones. Every
+        query adds its softmax weights (``scale``, 1 / sqrt(128) if None, in this rule and
+        in ``attend``) to ``weights`` [S, L, Hkv, cap], which move with the rows; no query
+        statistics are kept, and after an eviction ``scores`` holds the selection's keys
+        (infinite for tokens that stay anyway)."""
         if budget < 1 or interval < 1:
             raise ValueError("budget and interval must be >= 1")
         if dtype not in (torch.bfloat16, torch.float32):
@@ -703,6 +733,12 @@ class DecodeEvictor:
         self.dtype = dtype
         self.params = params if params is not None else jacap_params()
         self.preserve_order = bool(preserve_order)
+        if rule not in ("jacap", "weight"):
+            raise ValueError('rule must be "jacap" or "weight"')
+        self.rule, self.sinks, self.recent = rule, int(sinks), int(recent)
+        if self.sinks < 0 or self.recent < 0 or self.sinks + self.recent > (self.budget if rule == "weight" else 0):
+            raise ValueError("sinks and recent tokens belong to the weight rule, and the budget must hold them")
+        self.scale = 1.0 / math.sqrt(128.0) if scale is None else float(scale)
         dev = torch.device(device)
         S, L, Hq, Hkv, cap, d = self.S, self.L, self.Hq, self.Hkv, self.cap, 128
         self._k = torch.zeros((L, Hkv, S, cap, d), dtype=dtype, device=dev)
@@ -711,8 +747,18 @@ class DecodeEvictor:
         self.k = self._k.permute(2, 0, 1, 3, 4)
         self.v = self._v.permute(2, 0, 1, 3, 4)
         self.pos = self._pos.permute(2, 0, 1, 3)
-        self.stats = torch.zeros((S, L, Hq, 2, d), dtype=torch.float32, device=dev)
-        self.counts = torch.zeros((S, L, Hq), dtype=torch.int32, device=dev)
+        self.device = self._k.device
+        self.stats = self.counts = None
+        if rule == "jacap":
+            self.stats = torch.zeros((S, L, Hq, 2, d), dtype=torch.float32, device=dev)
+            self.counts = torch.zeros((S, L, Hq), dtype=torch.int32, device=dev)
+        else:
+            self._w = torch.zeros((L, Hkv, S, cap), dtype=torch.float32, device=dev)
+            self.weights = self._w.permute(2, 0, 1, 3)
+        self._ints = {}        # small int32 arrays on the device and what they hold
+        self._attention = {}   # per number of drafted tokens: layout, workspace, normalisers
+        self._attended = (0, set())
+        self._weigh_ws = {}
         self.lengths = [0] * S
         self.next_id = [0] * S
         self.events = 0   # request evictions
@@ -723,12 +769,15 @@ class DecodeEvictor:
         self.slot = self._group_layout(1)
         # one query per (request, layer, head), [S, L, Hq, 128] contiguous
         self.step_layout = self._layout(S, window=1, q_strides=(L * Hq * d, Hq * d, d, d))
-        # one workspace serves every group size (the work-item size depends on it)
+        # one workspace serves every group size (the work-item size depends on it); the selection by
+        # weights needs a status word
         sizes = [jacap_workspace_size(self._group_layout(n), self.budget) for n in range(1, S + 1)]
         if min(sizes) == 0:
             raise JacapError(1, "jacap_workspace_size")
-        nbytes = max(sizes)
+        nbytes = max(sizes) if rule == "jacap" else 1024
         self.ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        if rule == "weight":
+            self.ws.zero_()
         self._scores = torch.empty(L * Hkv * S * cap, dtype=torch.float32, device=dev)
         self._idx = torch.empty(L * Hkv * S * self.budget, dtype=torch.int32, device=dev)
         self._kept = torch.empty((S,), dtype=torch.int32, device=dev)
@@ -784,6 +833,10 @@ class DecodeEvictor:
                        .expand_as(self.pos))
         self.lengths = list(lengths)
         self.next_id = list(lengths)
+        if self.rule == "weight":
+            self._w.zero_()
+            self._weigh(q_win, None, None, stream)
+            return
         self._merge(q_win, reset=True, stream=stream)
 
     def append(self, k_new, v_new, q_new, stream=None):
@@ -793,6 +846,10 @@ class DecodeEvictor:
         full = [s for s in range(self.S) if self.lengths[s] >= self.cap]
         if full:
             raise RuntimeError(f"request {full[0]} is full; evict it first")
+        if self.rule == "weight":
+            self._take(k_new.unsqueeze(3), v_new.unsqueeze(3), q_new.unsqueeze(3), [[0]] * self.S, stream)
+            self._attended = (0, set())  # the next step's normalisers are others
+            return [s for s in range(self.S) if self.lengths[s] >= self.cap]
         if self._one_launch(k_new, v_new, q_new, stream):
             _check(jacap_append(self.step_layout, _ptr(k_new), _ptr(v_new), k_new.stride()[:3] + v_new.stride()[:3],
                                 _ptr(q_new), self.lengths, self.next_id, _ptr(self._k), _ptr(self._v),
@@ -858,7 +915,7 @@ class DecodeEvictor:
         return [tuple(g) for g in groups]
 
     def schedule_info(self, requests: int | None = None):
-        """(schedule, roles) of the scoring pass over ``requests`` slots evicted together
+        """(schedule, roles) of the scoring pass (of the rule "jacap") over ``requests`` slots evicted together
         (default: all), as jacap_schedule_info reports it."""
         lay = self._group_layout(self.S if requests is None else int(requests))
         sched, roles = jacap_schedule_info(lay, self.params)
@@ -872,6 +929,16 @@ class DecodeEvictor:
         n = b - a
         lay, st = self._group_layout(n), _stream(stream)
         handles = [e.cuda_event for e in events] if events is not None else []
+        if self.rule == "weight":
+            if events is not None:
+                raise ValueError("there are no scoring kernels to time: the weights are kept up step by step")
+            self._views(n)
+            _check(jacap_evict_weights(lay, _ptr(self._w[0, 0, a]), _ptr(self._pos[0, 0, a]), self.sinks, self.recent,
+                                       self.budget, _ptr(self.idx), _ptr(self.kept), _ptr(self._k[0, 0, a]),
+                                       _ptr(self._v[0, 0, a]), self.preserve_order, _ptr(self.scores), _ptr(self.ws),
+                                       self.ws.numel(), st), "jacap_evict_weights")
+            self._evicted(a, b, stream, tail)
+            return
         stats = ctypes.c_void_p(self.stats[a].data_ptr())
         counts = ctypes.c_void_p(self.counts[a].data_ptr())
         k, v, pos = _ptr(self._k[0, 0, a]), _ptr(self._v[0, 0, a]), _ptr(self._pos[0, 0, a])
@@ -881,11 +948,14 @@ class DecodeEvictor:
         _check(jacap_select_compact_inplace(lay, _ptr(self.scores), self.budget, _ptr(self.idx), _ptr(self.kept), k,
                                             v, pos, self.preserve_order, _ptr(self.ws), self.ws.numel(), st),
                "jacap_select_compact_inplace")
+        self._evicted(a, b, stream, tail)
+
+    def _evicted(self, a, b, stream, tail):
         if tail is not None:
             tail[0].record(stream)
         for s in range(a, b):
             self.lengths[s] = self.budget
-        self.events += n
+        self.events += b - a
         self.passes += 1
 
     def step(self, k_new, v_new, q_new, stream=None):
@@ -894,8 +964,174 @@ class DecodeEvictor:
         self.evict_many(full, stream)
         return full
 
+    def _int32(self, name, values):
+        """The int32 array `name` on the device, holding `values` (copied when they changed)."""
+        held, t = self._ints.get(name, (None, None))
+        if held != values:
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError(f"{name} changed: a graph would hold the old ones")
+            host = torch.tensor(values, dtype=torch.int32)
+            if t is None or t.shape != host.shape:
+                t = torch.empty(host.shape, dtype=torch.int32, device=self.device)
+            t.copy_(host, non_blocking=True)
+            self._ints[name] = ([list(v) if isinstance(v, (list, tuple)) else v for v in values], t)
+        return t
+
+    def positions(self, tokens: int, depth=None):
+        """int32 [S, tokens]: the ids that drafted tokens get if accepted; ``depth``: int32
+        [S, tokens] how many drafted tokens come before each (a tree; None: a chain)."""
+        first = self._int32("next ids", self.next_id)[:, None]
+        if depth is None:
+            depth = torch.arange(tokens, dtype=torch.int32, device=self.device)[None]
+        return first + depth
+
+    def rotate(self, rope: Rope, q, k, depth=None, stream=None):
+        """q [S, Hq, T, 128] and k [S, Hkv, T, 128] of one layer's drafted tokens turned by
+        their positions; returns new tensors."""
+        T = (q if q is not None else k).shape[2]
+
+        def turn(_):
+            at = self.positions(T, depth)
+            out = rope.apply(*(None if t is None else t.transpose(1, 2) for t in (q, k)), at)
+            return tuple(None if t is None else t.transpose(1, 2) for t in out)
+
+        return _enqueue(self.device, stream, turn)
+
+    def attend(self, layer: int, q, k_draft=None, v_draft=None, tree=None, draft_lens=None, stream=None):
+        """Attention of one layer's drafted tokens over the slots and over themselves:
+        q [S, Hq, T, 128], k_draft and v_draft [S, Hkv, T, 128], tree int64 [S, T]
+        (``tree_masks``; None: a chain; T = 1: the step's own token), draft_lens int32 [S] (rows
+        behind are not written). Returns (o [S, Hq, T, 128], lse [S, Hq, T], a view of what the
+        next call with as many tokens overwrites). Under the weight rule the normalisers are kept for ``step``,
+        ``append`` or ``accept``."""
+        if not 0 <= layer < self.L:
+            raise ValueError(f"layer must be 0 to {self.L - 1}")
+        if not isinstance(q, torch.Tensor) or q.dim() != 4:
+            raise ValueError("q must be [S, Hq, T, 128]")
+        T = q.shape[2]
+        if T not in self._attention:
+            lay = self._layout(self.S, max(T, 1), (128, 128, 128, 128))
+            lay.num_layers = 1
+            nbytes = jacap_attend_workspace(lay)
+            if nbytes == 0 or T == 0:
+                raise JacapError(2 if T > 64 else 1, "jacap_attend_workspace")
+            ws = torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
+            lse = torch.full((self.S, self.L, self.Hq, T), -math.inf, dtype=torch.float32, device=self.device)
+            self._attention[T] = (lay, ws, lse, jacap_attention())
+        lay, ws, lse, a = self._attention[T]
+        dev, S, Hq = self.device, self.S, self.Hq
+        qp = _tensor("q", q, dev, self.dtype, (S, Hq, T, 128))
+        if (k_draft is None) != (v_draft is None) or (tree is not None and k_draft is None):
+            raise ValueError("k_draft and v_draft come together, and a tree with them")
+        a.k_draft = _tensor("k_draft", k_draft, dev, self.dtype, (S, self.Hkv, T, 128))
+        a.v_draft = _tensor("v_draft", v_draft, dev, self.dtype, (S, self.Hkv, T, 128))
+        a.tree = _tensor("tree", tree, dev, torch.int64, (S, T), True)
+        a.draft_lens = _tensor("draft_lens", draft_lens, dev, torch.int32, (S,), True)
+        a.scale = self.scale
+        if k_draft is not None:
+            a.draft_strides[:] = _strides(k_draft.unsqueeze(1)) + _strides(v_draft.unsqueeze(1))
+        _query_strides(lay, q.unsqueeze(1))
+        part = lse[:, layer]
+        a.lse_strides[:] = (lse.stride(0), lse.stride(1), lse.stride(2))
+
+        def attend(st):
+            o = torch.empty((S, Hq, T, 128), dtype=self.dtype, device=dev)
+            a.o_strides[:] = (o.stride(0), 0, o.stride(1), o.stride(2))
+            a.lengths = self._int32("lengths", self.lengths).data_ptr()
+            _check(jacap_attend(lay, a, qp, self._k[layer].data_ptr(), self._v[layer].data_ptr(), o.data_ptr(),
+                                part.data_ptr(), ws.data_ptr(), ws.numel(), st), "jacap_attend")
+            if self._attended[0] != T:
+                self._attended = (T, set())
+            self._attended[1].add(layer)
+            return o, part
+
+        return _enqueue(dev, stream, attend)
+
+    def accept(self, k_draft, v_draft, q_draft, path, stream=None):
+        """Enter the accepted drafted tokens of a step: k_draft, v_draft [S, L, Hkv, T, 128],
+        q_draft [S, L, Hq, T, 128] (turned, as ``attend`` took them), path[s]: which drafted
+        tokens of request s, in order (none: an empty list). As in ``step`` a request whose
+        slot becomes full is evicted, here in the middle of its path where that happens; returns the
+        requests that were evicted."""
+        if len(path) != self.S:
+            raise ValueError("one path per request")
+        T = k_draft.shape[3]
+        left = [[int(t) for t in p] for p in path]
+        if any(len(p) > T or any(not 0 <= t < T for t in p) for p in left):
+            raise ValueError(f"a path holds at most {T} tokens, 0 to {T - 1}")
+        if any(n >= self.cap for n in self.lengths):
+            raise RuntimeError("a request is full; evict it first")
+        gone = set()
+        while True:
+            now = [p[:self.cap - n] for p, n in zip(left, self.lengths)]
+            left = [p[len(x):] for p, x in zip(left, now)]
+            self._take(k_draft, v_draft, q_draft, now, stream)
+            full = [s for s in range(self.S) if self.lengths[s] >= self.cap]
+            self.evict_many(full, stream)
+            gone.update(full)
+            if not any(left):
+                self._attended = (0, set())  # the next step's normalisers are others
+                return sorted(gone)
+
+    def _take(self, k, v, q, path, stream):
+        """The drafted tokens `path` into the slots, and their queries into the statistics or weights."""
+        S, L, Hq, Hkv, T = self.S, self.L, self.Hq, self.Hkv, k.shape[3]
+        for name, t, heads in (("k", k, Hkv), ("v", v, Hkv), ("q", q, Hq)):
+            _tensor(name, t, self.device, self.dtype, (S, L, heads, T, 128))
+        if torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("the rows' numbers would be frozen in the graph")
+        depth = max(len(p) for p in path)
+        if depth == 0:
+            return
+        lay = self._layout(S, T, _strides(q))
+
+        def append(st):
+            _check(jacap_append_path(lay, _ptr(k), _ptr(v), _strides(k) + _strides(v), _ptr(q),
+                                     [p + [0] * (depth - len(p)) for p in path], depth, [len(p) for p in path],
+                                     self.lengths, self.next_id, _ptr(self._k), _ptr(self._v), _ptr(self._pos),
+                                     _ptr(self.stats), _ptr(self.counts), st), "jacap_append_path")
+
+        _enqueue(self.device, stream, append)
+        self.lengths = [n + len(p) for n, p in zip(self.lengths, path)]
+        self.next_id = [n + len(p) for n, p in zip(self.next_id, path)]
+        if self.rule == "weight":
+            known = self._attended[0] == T and len(self._attended[1]) == L
+            self._weigh(q, self._attention[T][2] if known else None, path, stream)
+
+    def _weigh(self, q, lse, path, stream):
+        """Add the weights of the queries q [S, L, Hq, w, 128] (of `path` of them; None: the window of a
+        prompt) to the slots' tokens; lse: their normalisers, or None."""
+        w = q.shape[3]
+        if q.dtype != self.dtype or q.stride(-1) != 1 or tuple(q.shape) != (self.S, self.L, self.Hq, w, 128):
+            raise ValueError("queries must be [S, L, Hq, w, 128] in the cache dtype")
+        lay = self._layout(self.S, w, _strides(q))
+        if w not in self._weigh_ws:
+            nbytes = jacap_weigh_workspace(lay)
+            if nbytes == 0:
+                raise JacapError(2 if self.Hq // self.Hkv * w > 512 else 1, "jacap_weigh_workspace")
+            self._weigh_ws[w] = torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
+        ws, how = self._weigh_ws[w], jacap_weighing()
+        how.scale, how.lse_given = self.scale, int(lse is not None)
+
+        def weigh(st):
+            how.lengths = self._int32("lengths", self.lengths).data_ptr()
+            if path is not None and (w > 1 or any(not p for p in path)):
+                how.q_lens = self._int32("taken", [len(p) for p in path]).data_ptr()
+                how.q_rows = self._int32("path", [p + [-1] * (w - len(p)) for p in path]).data_ptr()
+            wp = self._w.data_ptr()
+            _check(jacap_weigh(lay, how, _ptr(q), _ptr(self._k), _ptr(lse), None if path is None else wp, wp, _ptr(ws),
+                               ws.numel(), st), "jacap_weigh")
+
+        _enqueue(self.device, stream, weigh)
+
     def check(self, stream=None):
-        _check(jacap_device_status(_ptr(self.ws), _stream(stream)), "device status")
+        """Raises what the kernels reported so far."""
+        if self.rule == "jacap":
+            _check(jacap_device_status(_ptr(self.ws), _stream(stream)), "device status")
+        else:
+            _check_and_clear(self.ws, self.device, stream)
+        for ws in [x[1] for x in self._attention.values()] + list(self._weigh_ws.values()):
+            _check_and_clear(ws, self.device, stream)
 
 
 class HostEvictor:

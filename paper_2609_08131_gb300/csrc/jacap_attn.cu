@@ -185,6 +185,8 @@ jacap_status jacap_attend(const jacap_layout* layout, const jacap_attention* att
   for (int i = 0; i < 4; ++i) {
     if (attn->o_strides[i] % el16 != 0 || attn->o_strides[i] < (count[i] > 1 ? D : 0)) return JACAP_ERR_INVALID_ARG;
   }
+  for (int i = 0; lse != nullptr && i < 3; ++i)
+    if (attn->lse_strides[i] < (count[i] > 1 ? layout->window : 0)) return JACAP_ERR_INVALID_ARG;
   for (int i = 0; attn->k_draft != nullptr && i < 8; ++i)
     if (attn->draft_strides[i] % el16 != 0 || attn->draft_strides[i] < D || attn->draft_strides[i] >= (1ll << 38))
       return JACAP_ERR_INVALID_ARG;
@@ -205,6 +207,7 @@ jacap_status jacap_attend(const jacap_layout* layout, const jacap_attention* att
     a.kds[i] = attn->k_draft != nullptr ? attn->draft_strides[i] : 0;
     a.vds[i] = attn->k_draft != nullptr ? attn->draft_strides[4 + i] : 0;
   }
+  for (int i = 0; i < 3; ++i) a.ls[i] = attn->lse_strides[i];
   a.scale = attn->scale;
   a.chunk = p.chunk, a.nsplit = p.nsplit, a.nrb = p.nrb, a.max_seqlen = layout->max_seqlen;
   uint8_t* b = (uint8_t*)ws;

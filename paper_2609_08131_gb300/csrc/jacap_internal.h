@@ -179,6 +179,7 @@ struct AttendArgs {
   const int32_t* draft_lens;  // queries (and drafted tokens) of each request, or null: all
   const uint64_t* tree;       // [S][window] masks, or null: a chain
   int64_t os[4], kds[4], vds[4];  // strides of o and of the drafted K and V: request, layer, head, token
+  int64_t ls[3];              // of lse: request, layer, head
   float scale;
   int chunk, nsplit, nrb, max_seqlen;  // tokens per split, splits of the longest request, row blocks
   float *opart, *mlpart;      // [units][nsplit][G window][128], [..][2]: the splits' sums, (maximum, sum)

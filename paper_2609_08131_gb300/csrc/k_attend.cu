@@ -126,7 +126,7 @@ __device__ __forceinline__ void at_put(const Dims& dm, const AttendArgs& a, cons
   else
     *(float4*)o = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
   if (lane == 0 && a.lse != nullptr)
-    a.lse[(((int64_t)x.s * dm.L + x.l) * dm.Hq + x.g * dm.G + h) * dm.window + t] =
+    a.lse[x.s * a.ls[0] + x.l * a.ls[1] + (x.g * dm.G + h) * a.ls[2] + t] =
         z == 0.f ? -INFINITY : m * a.scale + logf(z);
 }
 

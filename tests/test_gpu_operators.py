@@ -541,12 +541,11 @@ def test_operators_on_another_stream_and_in_graphs():
     def loop(stream=None):
         q, k = rope.apply(cache.q_win[:, 0].transpose(1, 2), kd[:, 0].transpose(1, 2), at, stream=stream)
         q, k = q.transpose(1, 2).unsqueeze(1), k.transpose(1, 2).unsqueeze(1)
-        o, lse = att.run(q, k_draft=k, v_draft=vd_like, lengths=lengths, stream=stream)
+        o, lse = att.run(q, k_draft=k, v_draft=vd, lengths=lengths, stream=stream)
         ev.score(q, lse=lse, lengths=lengths, stream=stream)
         ev.select_compact(stream=stream)
         return [t.clone() for t in (q, o, lse, ev.weights, ev.idx, ev.k_out)]
 
-    vd_like = vd.transpose(2, 3).contiguous().transpose(2, 3)
     ref = loop()
     side = torch.cuda.Stream(device=DEV)
     side.wait_stream(torch.cuda.current_stream())
@@ -578,3 +577,189 @@ def test_operators_on_another_stream_and_in_graphs():
             for s in range(2):
                 a0 = 900 * s
                 assert torch.equal(want[3][:, :, a0:a0 + n[s]], got[3][:, :, a0:a0 + n[s]])
+
+
+# ------------------------------------------------------- the decoding loop ----
+def _slot(ev, s, l, g):
+    """{id: (k bits, v bits, weight)} of a slot."""
+    n = ev.lengths[s]
+    ids = ev.pos[s, l, g, :n].tolist()
+    assert len(set(ids)) == n
+    k, v = ev.k[s, l, g, :n].float().cpu(), ev.v[s, l, g, :n].float().cpu()
+    w = ev.weights[s, l, g, :n].double().cpu() if ev.rule == "weight" else torch.zeros(n)
+    return {i: (k[r], v[r], w[r].item()) for r, i in enumerate(ids)}
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("ordered", [False, True])
+@pytest.mark.parametrize("drafts", [1, 5])
+def test_decoding_loop_by_weights(drafts, ordered, dtype):
+    """Rotary positions, attention over the slots, the accepted path, weights and evictions together, against a plain
+    simulation in 64 bits that keeps every request's tokens in dictionaries."""
+    S, L, Hq, Hkv, B, I, T, w0 = 3, 2, 4, 2, 40, 6, drafts, 8
+    G, g, lens = Hq // Hkv, gen(21 + drafts), [30, 45, 12]
+    rope = api.Rope(64, base=1000.0, device=DEV)
+    ev = api.DecodeEvictor(S, L, Hq, Hkv, B, I, dtype=dtype, device=DEV, preserve_order=ordered, rule="weight", sinks=2,
+                           recent=4)
+    k0, v0 = (randn(g, S, L, Hkv, max(lens), D, dtype=dtype) for _ in range(2))
+    qw = randn(g, S, L, Hq, w0, D, dtype=dtype)
+    ev.start(k0, v0, qw, lens)
+    sim = {}
+    for s, n in enumerate(lens):
+        for l in range(L):
+            for h in range(Hkv):
+                rows = [[k0[s, l, h, i].double(), v0[s, l, h, i].double(), 0.0] for i in range(n)]
+                for hq in range(h * G, (h + 1) * G):
+                    for j in range(w0):
+                        at = n - w0 + j
+                        x = torch.stack([r[0] for r in rows[:at + 1]]) @ qw[s, l, hq, j].double() * SCALE
+                        for r, p in zip(rows, torch.softmax(x, 0).tolist()):
+                            r[2] += p
+                sim[s, l, h] = dict(enumerate(rows))
+
+    def same():
+        for (s, l, h), rows in sim.items():
+            got = _slot(ev, s, l, h)
+            assert got.keys() == rows.keys(), (s, l, h)
+            for i, (k, v, w) in got.items():
+                assert torch.equal(k.double(), rows[i][0].cpu()) and torch.equal(v.double(), rows[i][1].cpu())
+                # 2 (136 2^-24 size + 2^-20) of each weight added, sizes below 16: under 2.6e-4
+                assert abs(w - rows[i][2]) <= 2.6e-4 * rows[i][2] + 1e-9
+
+    same()
+    r = torch.Generator().manual_seed(5)
+    ids, evictions = list(lens), 0
+    for step in range(14):
+        parents = random_tree(step, S, T)
+        tree = api.tree_masks(parents).to(DEV)
+        depth = [[0] * T for _ in range(S)]
+        for s in range(S):
+            for t in range(T):
+                depth[s][t] = 0 if parents[s][t] < 0 else depth[s][parents[s][t]] + 1
+        depth = torch.tensor(depth, dtype=torch.int32, device=DEV)
+        q, k, v = (randn(g, S, L, n, T, D, dtype=dtype) for n in (Hq, Hkv, Hkv))
+        for l in range(L):
+            q[:, l], k[:, l] = ev.rotate(rope, q[:, l], k[:, l], depth)
+            o, lse = ev.attend(l, q[:, l], k[:, l], v[:, l], tree)
+            for s in range(S):
+                seen = torch.ones(T, ev.lengths[s] + T, dtype=torch.bool, device=DEV)
+                seen[:, ev.lengths[s]:] = (tree[s, :, None] >> torch.arange(T, device=DEV) & 1).bool()
+                for h in range(Hq):
+                    n = ev.lengths[s]
+                    kk = torch.cat([ev.k[s, l, h // G, :n], k[s, l, h // G]])
+                    vv = torch.cat([ev.v[s, l, h // G, :n], v[s, l, h // G]])
+                    wo, wl, to, tl = attend_plain(q[s, l, h], kk, vv, seen, dtype)
+                    within(o[s, h], wo, to, "o")
+                    within(lse[s, h], wl, tl, "lse")
+        assert ev.next_id == ids
+        # a path from the root: some requests take nothing, some all of a branch
+        path = []
+        for s in range(S):
+            t = int(torch.randint(-1, T, (1,), generator=r))
+            p = []
+            while t >= 0:
+                p.insert(0, t)
+                t = parents[s][t]
+            path.append(p)
+        if T == 1:
+            path = [[0]] * S
+            gone = ev.step(k[:, :, :, 0], v[:, :, :, 0], q[:, :, :, 0])
+        else:
+            gone = ev.accept(k, v, q, path)
+        ev.check()
+        # the plain loop: rounds that end where a slot is full
+        left, want_gone = [list(p) for p in path], set()
+        seen_lse = {}
+        for (s, l, h), rows in sim.items():
+            for hq in range(h * G, (h + 1) * G):
+                for t in path[s]:
+                    chain = [t]
+                    while parents[s][chain[0]] >= 0:
+                        chain.insert(0, parents[s][chain[0]])
+                    keys = torch.stack([x[0] for x in rows.values()] + [k[s, l, h, c].double() for c in chain])
+                    seen_lse[s, l, hq, t] = torch.logsumexp(keys @ q[s, l, hq, t].double() * SCALE, 0)
+        count = {s: len(sim[s, 0, 0]) for s in range(S)}
+        for s in range(S):
+            while left[s]:
+                now = left[s][:B + I - count[s]]
+                left[s] = left[s][len(now):]
+                for l in range(L):
+                    for h in range(Hkv):
+                        rows = sim[s, l, h]
+                        for i, t in enumerate(now):
+                            rows[ids[s] + i] = [k[s, l, h, t].double(), v[s, l, h, t].double(), 0.0]
+                        order = sorted(rows)
+                        for hq in range(h * G, (h + 1) * G):
+                            for i, t in enumerate(now):
+                                see = [x for x in order if x <= ids[s] + i]
+                                p = torch.exp(torch.stack([rows[x][0] for x in see]) @ q[s, l, hq, t].double() * SCALE
+                                              - seen_lse[s, l, hq, t])
+                                for x, e in zip(see, p.tolist()):
+                                    rows[x][2] += e
+                count[s] += len(now)
+                ids[s] += len(now)
+                if count[s] == B + I:
+                    want_gone.add(s)
+                    count[s] = B
+                    for l in range(L):
+                        for h in range(Hkv):
+                            rows, last = sim[s, l, h], ids[s] - 1
+                            stay = [x for x in rows if x < 2 or x > last - 4]
+                            rest = sorted((x for x in rows if x not in stay), key=lambda x: -rows[x][2])
+                            sim[s, l, h] = {x: rows[x] for x in stay + rest[:B - len(stay)]}
+        assert sorted(want_gone) == list(gone)
+        evictions += len(gone)
+        same()
+    assert evictions >= 3
+
+
+def test_accepted_paths_keep_the_query_statistics():
+    """The rule "jacap" with accepted paths: rows, ids and running statistics as one step at a time leaves them."""
+    S, L, Hq, Hkv, T = 2, 2, 4, 2, 4
+    g = gen(23)
+    one = api.DecodeEvictor(S, L, Hq, Hkv, 20, 30, device=DEV)
+    two = api.DecodeEvictor(S, L, Hq, Hkv, 20, 30, device=DEV)
+    k0, v0 = (randn(g, S, L, Hkv, 10, D, dtype=BF16) for _ in range(2))
+    qw = randn(g, S, L, Hq, 4, D, dtype=BF16)
+    for ev in (one, two):
+        ev.start(k0, v0, qw, [10, 10])
+    for path in ([[0, 2, 3], [1, 2, 3]], [[], []], [[3, 0], [2, 2]]):
+        k, v = (randn(g, S, L, T, Hkv, D, dtype=BF16).transpose(2, 3) for _ in range(2))
+        q = randn(g, S, L, Hq, T, D, dtype=BF16)
+        assert two.accept(k, v, q, path) == []
+        for i in range(len(path[0])):
+            pick = lambda x: torch.stack([x[s, :, :, path[s][i]] for s in range(S)]).contiguous()  # noqa: E731
+            one.append(pick(k), pick(v), pick(q))
+    assert one.lengths == two.lengths and one.next_id == two.next_id
+    for a, b in ((one.k, two.k), (one.v, two.v), (one.pos, two.pos), (one.stats, two.stats), (one.counts, two.counts)):
+        assert torch.equal(a, b)
+
+
+def test_loop_refusals_on_the_device_side():
+    ev = api.DecodeEvictor(2, 1, 4, 2, 8, 2, device=DEV, rule="weight")
+    g = gen(24)
+    k0 = randn(g, 2, 1, 2, 8, D, dtype=BF16)
+    ev.start(k0, k0, randn(g, 2, 1, 4, 2, D, dtype=BF16), [8, 8])
+    k, q = randn(g, 2, 1, 2, 3, D, dtype=BF16), randn(g, 2, 1, 4, 3, D, dtype=BF16)
+    for path in ([[0]], [[0, 1, 2, 0], []], [[3], []], [[-1], []]):
+        with pytest.raises(ValueError):
+            ev.accept(k, k, q, path)
+    with pytest.raises(ValueError):
+        ev.attend(1, q[:, 0], k[:, 0], k[:, 0])
+    with pytest.raises(ValueError):
+        ev.attend(0, q[:, 0].float(), k[:, 0], k[:, 0])
+    with pytest.raises(ValueError):
+        ev.attend(0, q[:, 0], k[:, 0], None)
+    with pytest.raises(api.JacapError):
+        ev.attend(0, randn(g, 2, 4, 65, D, dtype=BF16))
+    x = q[:, 0].clone().requires_grad_()
+    with pytest.raises(ValueError):
+        ev.attend(0, x, k[:, 0], k[:, 0])
+    with pytest.raises(ValueError):
+        api.Rope(device=DEV).apply(x, None, torch.zeros((2, 4), dtype=torch.int32, device=DEV))
+    graph = torch.cuda.CUDAGraph()
+    ev.attend(0, q[:, 0], k[:, 0], k[:, 0])
+    torch.cuda.synchronize()
+    with pytest.raises(RuntimeError):
+        with torch.cuda.graph(graph):
+            ev.accept(k, k, q, [[0], [1]])
