@@ -479,10 +479,11 @@ jacap_status jacap_rotate(const jacap_rope* rope, jacap_dtype dtype, int32_t num
  *                  + h [2] + t (elements; a layer's call can write its part of an
  *                  array over all layers)
  *   ws             device, 256-byte aligned, jacap_attend_workspace() bytes (0 for
- *                  a layout that is refused), whose first 64 bytes were zeroed once:
- *                  the status word. A length outside its range is clamped and
- *                  reported there (JACAP_ERR_INVALID_ARG); the word stays set until
- *                  it is zeroed again.
+ *                  a layout that is refused), zeroed once before its first call: it
+ *                  starts with the status word and holds counters that every call
+ *                  leaves at zero. A length outside its range is clamped and reported
+ *                  in the word (JACAP_ERR_INVALID_ARG), which stays set until the
+ *                  workspace is zeroed again.
  * o must not overlap an input. Sums are float32; with bf16 caches the softmax
  * weights are rounded to bf16 for their product with V.
  */

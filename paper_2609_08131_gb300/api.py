@@ -293,8 +293,7 @@ class CacheAttention:
         nbytes = jacap_attend_workspace(self.lay)
         if nbytes == 0:
             raise JacapError(2 if T > 64 else 1, "jacap_attend_workspace")
-        self.ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
-        self.ws[:64].zero_()
+        self.ws = torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
         self.o = torch.empty((S, L, Hq, T, 128), dtype=self.dtype, device=self.device)
         self.lse = torch.empty((S, L, Hq, T), dtype=torch.float32, device=self.device)
         self._attn = jacap_attention()
@@ -340,7 +339,7 @@ def _check_and_clear(ws, device, stream):
     def read(st):
         status = jacap_device_status(ws.data_ptr(), st)
         if status != JACAP_OK:
-            ws[:64].zero_()
+            ws.zero_()
         return status
 
     _check(_enqueue(device, stream, read), "device status")

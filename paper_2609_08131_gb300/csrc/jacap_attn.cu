@@ -25,7 +25,7 @@ constexpr int AT_DRAFTS_MAX = 64;
 // workspace does.
 struct AttendPlan {
   int chunk, nsplit, nrb;
-  size_t status, opart, mlpart, total;
+  size_t status, counts, opart, mlpart, total;
 };
 AttendPlan attend_plan(const jacap_layout* L) {
   AttendPlan p;
@@ -33,22 +33,26 @@ AttendPlan attend_plan(const jacap_layout* L) {
   const int block = attend_row_block(bf, rows);
   p.nrb = (rows + block - 1) / block;
   const int64_t units = (int64_t)L->num_seqs * L->num_layers * L->num_kv_heads, ctas = units * p.nrb;
-  const int64_t slots = bf ? 304 : 152;
-  // about three CTAs per place where that leaves each 1024 tokens or more, at least one
-  // where it leaves 128; a split's sums (written, and read by the join) stay an eighth of
-  // the K and V that it reads
   const int64_t most = L->max_seqlen;
-  int64_t chunk = most * ctas / (3 * slots);
-  if (chunk < 1024) chunk = std::min<int64_t>(1024, (most * ctas + slots - 1) / slots);
-  chunk = std::max<int64_t>(chunk, std::max(128, std::min(rows, block) * 16));
+  // float32: about three CTAs per SM where that leaves each 1024 tokens or more, at least one
+  // where it leaves 128. bf16: the least that a split may have (the kernel chooses from the live
+  // lengths). A split's sums, written and read by the join, stay an eighth of its K and V.
+  int64_t chunk = 256;
+  if (!bf) {
+    chunk = most * ctas / (3 * 152);
+    if (chunk < 1024) chunk = std::min<int64_t>(1024, (most * ctas + 151) / 152);
+    chunk = std::max<int64_t>(chunk, 128);
+  }
+  chunk = std::max<int64_t>(chunk, std::min(rows, block) * 16);
   chunk = std::min<int64_t>((chunk + 63) / 64 * 64, (most + 63) / 64 * 64);
   p.chunk = (int)chunk;
   p.nsplit = (int)((most + chunk - 1) / chunk);
   size_t o = 0;
-  p.status = o; o = align_up(o + 64);
-  const size_t parts = p.nsplit > 1 ? (size_t)units * p.nsplit * rows : 0;
-  p.opart = o; o = align_up(o + parts * D * 4);
-  p.mlpart = o; o = align_up(o + parts * 8);
+  p.status = o; o += 64;
+  p.counts = o; o = align_up(o + (p.nsplit > 1 ? (size_t)units * 4 : 0));
+  const size_t parts = p.nsplit > 1 ? (size_t)units * p.nsplit : 0, prows = attend_part_rows(rows);
+  p.opart = o; o = align_up(o + parts * ((rows + prows - 1) / prows * prows) * D * 4);
+  p.mlpart = o; o = align_up(o + parts * rows * 8);
   p.total = o;
   return p;
 }
@@ -209,9 +213,12 @@ jacap_status jacap_attend(const jacap_layout* layout, const jacap_attention* att
   }
   for (int i = 0; i < 3; ++i) a.ls[i] = attn->lse_strides[i];
   a.scale = attn->scale;
+  a.prows = attend_part_rows(dm.G * dm.window);
+  a.tdiv = dm.window > 1 ? 0xffffffffu / (uint32_t)dm.window + 1u : 0u;
   a.chunk = p.chunk, a.nsplit = p.nsplit, a.nrb = p.nrb, a.max_seqlen = layout->max_seqlen;
   uint8_t* b = (uint8_t*)ws;
   a.status = (uint32_t*)(b + p.status);
+  a.counts = (int32_t*)(b + p.counts);
   a.opart = (float*)(b + p.opart);
   a.mlpart = (float*)(b + p.mlpart);
   CUtensorMap maps[4];
@@ -223,7 +230,7 @@ jacap_status jacap_attend(const jacap_layout* layout, const jacap_attention* att
       return JACAP_ERR_CUDA;
   }
   const TraceRange trace("jacap/attend");
-  return map_cuda(launch_attend(maps, dm, bf ? 1 : 0, a, layout->cu_seqlens, (cudaStream_t)stream));
+  return map_cuda(launch_attend(maps, dm, bf ? 1 : 0, a, layout->cu_seqlens, sms, (cudaStream_t)stream));
 }
 
 size_t jacap_weigh_workspace(const jacap_layout* layout) {

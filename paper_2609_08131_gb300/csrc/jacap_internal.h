@@ -181,14 +181,20 @@ struct AttendArgs {
   int64_t os[4], kds[4], vds[4];  // strides of o and of the drafted K and V: request, layer, head, token
   int64_t ls[3];              // of lse: request, layer, head
   float scale;
-  int chunk, nsplit, nrb, max_seqlen;  // tokens per split, splits of the longest request, row blocks
-  float *opart, *mlpart;      // [units][nsplit][G window][128], [..][2]: the splits' sums, (maximum, sum)
+  int chunk, nsplit, nrb, max_seqlen;  // tokens per split (bf16: at least), splits of the longest request, row blocks
+  int places;                 // CTAs that the SMs hold at a time (bf16)
+  int prows;                  // rows of a block of the splits' sums (attend_part_rows)
+  uint32_t tdiv;              // 2^32 / window, rounded up (window > 1)
+  float *opart, *mlpart;      // the splits' sums [units][nsplit][row blocks][32][prows][4], and their
+                              // [units][nsplit][G window][2] (maximum, sum)
+  int32_t* counts;            // [units] splits done, where the last one joins them (zero between calls)
   uint32_t* status;
 };
 int attend_row_block(int dtype, int rows);  // rows of a CTA
+int attend_part_rows(int rows);
 // maps: K, V, drafted K, drafted V (bf16)
 cudaError_t launch_attend(const CUtensorMap* maps, const Dims& dm, int dtype, const AttendArgs& a, const int32_t* cu,
-                          cudaStream_t st);
+                          int sms, cudaStream_t st);
 
 // Attention weights that tokens received from a window of queries (k_weigh.cu).
 struct WeighArgs {

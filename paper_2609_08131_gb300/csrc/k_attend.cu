@@ -40,13 +40,16 @@ namespace jacap {
 constexpr int AT_TOK = 64;             // tokens per tile
 constexpr int AT_BOX = AT_TOK * 128;   // {64 channels, 64 tokens} bf16
 constexpr int AT_TILE = 2 * AT_BOX;
-constexpr int AT_STAGES = 2;
-constexpr int AT_Q_BYTES = 128 * D * 2;
-constexpr int AT_THREADS = 192;
-constexpr uint32_t AT_COLS = 256;      // S (and P over it): 2 x 64, O: 128
-constexpr uint32_t AT_O = 128;
-constexpr size_t AT_SMEM = 1024 + AT_Q_BYTES + 2 * AT_STAGES * AT_TILE;
-static_assert(2 * AT_STAGES * AT_TILE >= 128 * D * 4, "the ring holds the accumulators on their way out");
+// A CTA of NB blocks of 128 rows (that share its tiles): warps 0 TMA producer, 1 MMA, then 4 NB
+// softmax and 2 NB row warps. Two CTAs of one block share an SM, a CTA of two blocks has one.
+constexpr int AT_QUEUE = 3;            // items published and not yet taken by all
+template <int NB>
+struct AtCfg {
+  static constexpr int RING = 5 * NB;  // tiles of K and of V in flight, in the order K0 V0 K1 V1 ...
+  static constexpr int Q_BYTES = NB * 128 * D * 2;
+  static constexpr int LOADERS = 2 * NB, LOAD0 = 2 + 4 * NB, THREADS = 32 * (LOAD0 + LOADERS);
+  static constexpr uint32_t COLS = 256 * NB;  // tensor memory: per block S (and P over it) 2 x 64, O 128
+};
 constexpr float AT_LAZY = 8.f;         // log2 of how far a logit may pass the maximum
 
 __device__ __forceinline__ float ex2(float x) {
@@ -71,32 +74,71 @@ struct AtUnit {
   int64_t u, t0;
   int n, rows, nd, nsp;
   int tok0, tok1, ncache, nt;  // this split's tokens, its tiles of cached tokens and in all (`tile` tokens each)
+  int r0;                      // the CTA's first row
 };
-__device__ __forceinline__ AtUnit at_unit(const Dims& dm, const AttendArgs& a, const int32_t* cu, int64_t u, int split,
-                                          int tile) {
+__device__ __forceinline__ AtUnit at_unit(const Dims& dm, const AttendArgs& a, const int32_t* cu, uint32_t u, int split,
+                                          int tile, int chunk) {  // (32-bit divisions: a 64-bit one takes ~300 cycles)
   AtUnit x;
   x.u = u;
   x.split = split;
-  x.s = (int)(u % dm.S);
-  const int plane = (int)(u / dm.S);
-  x.l = plane / dm.Hkv;
-  x.g = plane % dm.Hkv;
+  const uint32_t plane = u / (uint32_t)dm.S;
+  x.s = (int)(u - plane * dm.S);
+  x.l = (int)(plane / (uint32_t)dm.Hkv);
+  x.g = (int)(plane - x.l * dm.Hkv);
   const int64_t start = cu[x.s], end = cu[x.s + 1];
+  const int given = a.lengths != nullptr ? a.lengths[x.s] : 0;
+  const int want = a.draft_lens != nullptr ? a.draft_lens[x.s] : dm.window;
   const bool ok = start >= 0 && end >= start && end <= dm.Ntot;
   const int64_t room = ok ? (end - start < a.max_seqlen ? end - start : a.max_seqlen) : 0;
-  const int64_t live = a.lengths != nullptr ? a.lengths[x.s] : end - start;
-  const int want = a.draft_lens != nullptr ? a.draft_lens[x.s] : dm.window;
+  const int64_t live = a.lengths != nullptr ? (int64_t)given : end - start;
   x.t0 = ok ? start : 0;
   x.n = (int)(live < 0 ? 0 : (live < room ? live : room));
   x.rows = want < 0 ? 0 : (want < dm.window ? want : dm.window);
   if (!ok || live != x.n || want != x.rows) atomicOr(a.status, (uint32_t)ST_INVALID);
   x.nd = a.kd != nullptr ? x.rows : 0;
-  x.nsp = x.n > a.chunk ? (x.n - 1) / a.chunk + 1 : 1;
-  x.tok0 = split * a.chunk;
-  x.tok1 = x.tok0 + a.chunk < x.n ? x.tok0 + a.chunk : x.n;
+  x.nsp = x.n > chunk ? (x.n - 1) / chunk + 1 : 1;
+  x.tok0 = split * chunk;
+  x.tok1 = x.tok0 + chunk < x.n ? x.tok0 + chunk : x.n;
   x.ncache = x.tok1 > x.tok0 ? (x.tok1 - x.tok0 - 1) / tile + 1 : 0;
   x.nt = x.ncache + (split == x.nsp - 1 && x.nd > 0 ? (x.nd - 1) / tile + 1 : 0);
   return x;
+}
+
+// Two CTAs share an SM's 228 KB (1 KB of each is the system's). There are no static
+// variables, so the dynamic ones start on the 1024 bytes that the swizzle needs; the rest up
+// to AT_SMEM makes up for a start that does not.
+template <int NB>
+struct AtSmem {
+  uint64_t full[AtCfg<NB>::RING], empty[AtCfg<NB>::RING], sfull[2], pready[2];
+  uint64_t pvdone[2];  // by a tile's parity: a wait for tile i knows that tile i - 2's product is done (S of tile i follows it)
+  uint64_t qfull[AT_QUEUE], qempty[AT_QUEUE];
+  uint64_t rowsready, rowsfree, rowsasked, ofree;
+  AtUnit queue[AT_QUEUE];
+  uint32_t tmem, bad[2];
+  int abort, last;
+};
+template <int NB>
+constexpr size_t at_used() { return AtCfg<NB>::Q_BYTES + AtCfg<NB>::RING * AT_TILE + sizeof(AtSmem<NB>); }
+template <int NB>
+constexpr size_t at_smem() { return 233472 / (3 - NB) - 1024; }
+static_assert(at_used<1>() <= at_smem<1>() && at_used<2>() <= at_smem<2>(), "shared memory");
+static_assert(128 * D * 2 >= 128 * 64 * 4, "the rows' space holds half the channels of the accumulators (copies)");
+// words beside the status word (zero between calls): items dealt beyond the first of each CTA,
+// CTAs that stopped claiming
+enum { AT_NEXT = 4, AT_DONE = 5 };
+// and the tokens per split that the call chose (for the joining kernel)
+enum { AT_CHUNK = 6 };
+
+// The head of a unit's row r (r / window, exact for r below 2^16).
+__device__ __forceinline__ int at_head(const Dims& dm, const AttendArgs& a, int r) {
+  return dm.window == 1 ? r : (int)__umulhi((uint32_t)r, a.tdiv);
+}
+
+// A split's unnormalised sums of row r: channels 4 c .. + 3 at [c prows] (the rows of a block lie
+// next to each other, as a warp's lanes have them).
+__device__ __forceinline__ float4* at_part(const Dims& dm, const AttendArgs& a, int64_t u, int split, int r) {
+  const int rows = a.prows, blocks = (dm.G * dm.window - 1) / rows + 1, b = r / rows;
+  return (float4*)a.opart + ((u * a.nsplit + split) * blocks + b) * (32 * rows) + (r - b * rows);
 }
 
 // Drafted tokens that drafted token t of request s sees (bit j: token j).
@@ -111,11 +153,11 @@ __device__ __forceinline__ uint64_t at_mask(const Dims& dm, const AttendArgs& a,
 template <typename T>
 __device__ __forceinline__ void at_put(const Dims& dm, const AttendArgs& a, const AtUnit& x, int r, float4 acc, float m,
                                        float z, int lane) {
-  const int h = r / dm.window, t = r - h * dm.window;
+  const int h = at_head(dm, a, r), t = r - h * dm.window;
   if (t >= x.rows) return;
   if (x.nsp > 1) {
     const int64_t p = (x.u * a.nsplit + x.split) * ((int64_t)dm.G * dm.window) + r;
-    *(float4*)(a.opart + p * D + 4 * lane) = acc;
+    at_part(dm, a, x.u, x.split, r)[lane * a.prows] = acc;
     if (lane == 0) *(float2*)(a.mlpart + 2 * p) = make_float2(m, z);
     return;
   }
@@ -130,121 +172,285 @@ __device__ __forceinline__ void at_put(const Dims& dm, const AttendArgs& a, cons
         z == 0.f ? -INFINITY : m * a.scale + logf(z);
 }
 
-template <int REP>
-__global__ void __launch_bounds__(AT_THREADS, 2)
+// Few rows in few splits (bf16) are joined by the CTA that finishes the unit's last split; the others by a
+// kernel of their own, which has more reads in flight.
+__host__ __device__ __forceinline__ bool at_joins_inside(int nsp, int R) { return R <= 32 && nsp <= 16; }
+
+// Rows r0 .. r0 + NR - 1 (4 or 8) of unit x from its splits' sums, scaled to the largest maximum and added in the
+// splits' order. W warps share the work (warp `part` takes every W-th split, and part 0 adds the
+// others' sums in order, from s_o and s_z, the warp's own shared memory, the warps' next to each
+// other; with a barrier of the whole block, which all its warps reach); one warp needs none. A lane
+// has channels 4 lane .. + 3 of all the rows.
+template <typename T, int W, int NR>
+__device__ __forceinline__ void at_join(const Dims& dm, const AttendArgs& a, const AtUnit& x, int r0, int part, float4* s_o,
+                                        float* s_z) {
+  const int R = dm.G * dm.window, lane = threadIdx.x & 31, rl = lane % NR;
+  const float scale2 = a.scale * 1.4426950408889634f;
+  const bool on = r0 < R && x.nsp > 1;
+  float m = -INFINITY, z = 0.f;  // of row r0 + rl
+  float4 s[NR];
+#pragma unroll
+  for (int i = 0; i < NR; ++i) s[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (on) {
+    const int r = r0 + rl < R ? r0 + rl : R - 1;
+    const float2* ml = (const float2*)a.mlpart + x.u * a.nsplit * R + r;
+    const float4* o = at_part(dm, a, x.u, 0, r0) + lane * a.prows;
+    const int64_t step = at_part(dm, a, x.u, 1, r0) - at_part(dm, a, x.u, 0, r0);
+    for (int j = lane / NR; j < x.nsp; j += 32 / NR) m = fmaxf(m, ml[(int64_t)j * R].x);
+#pragma unroll
+    for (int off = NR; off < 32; off <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+#pragma unroll (NR == 8 ? 2 : 4)
+    for (int j = part; j < x.nsp; j += W) {
+      const float2 w = ml[(int64_t)j * R];
+      float4 v[NR];
+#pragma unroll
+      for (int i = 0; i < NR; ++i) v[i] = o[j * step + i];  // (rows behind the last lie in the block too)
+      // (a split that saw nothing has the maximum -inf and the sum 0, one of NaN only -inf and NaN)
+      const float f = w.x == m ? 1.f : ex2((w.x - m) * scale2);
+      const bool none = w.x == -INFINITY && w.y == 0.f;
+      z += none ? 0.f : w.y * f;
+#pragma unroll
+      for (int i = 0; i < NR; ++i) {
+        const float fi = __shfl_sync(0xffffffffu, none ? 0.f : f, i);
+        const bool skip = __shfl_sync(0xffffffffu, none ? 1 : 0, i);
+        s[i].x += skip ? 0.f : v[i].x * fi;
+        s[i].y += skip ? 0.f : v[i].y * fi;
+        s[i].z += skip ? 0.f : v[i].z * fi;
+        s[i].w += skip ? 0.f : v[i].w * fi;
+      }
+    }
+  }
+  if constexpr (W > 1) {
+#pragma unroll
+    for (int i = 0; i < NR; ++i) s_o[i * 32 + lane] = s[i];
+    if (lane < NR) s_z[lane] = z;
+    __syncthreads();
+    if (part != 0) return;
+    for (int k = 1; k < W; ++k) {
+#pragma unroll
+      for (int i = 0; i < NR; ++i) {
+        const float4 v = s_o[(k * NR + i) * 32 + lane];
+        s[i].x += v.x, s[i].y += v.y, s[i].z += v.z, s[i].w += v.w;
+      }
+      z += s_z[k * NR + rl];
+    }
+  }
+  if (!on) return;
+  AtUnit whole = x;
+  whole.nsp = 1;  // straight to the output
+#pragma unroll
+  for (int i = 0; i < NR; ++i) {
+    const float mi = __shfl_sync(0xffffffffu, m, i), zi = __shfl_sync(0xffffffffu, z, i);
+    if (r0 + i < R) at_put<T>(dm, a, whole, r0 + i, s[i], mi, zi, lane);
+  }
+}
+
+// acc, the sums of channels c .. c + 3 of drafted token t's row, with the drafted values that are
+// not finite (of the tokens `bad`, zeroed in the product) added where the row sees them.
+__device__ __forceinline__ void at_bad(const Dims& dm, const AttendArgs& a, const AtUnit& x, uint64_t bad, int t, int c,
+                                       float* acc) {
+  uint64_t seen = bad & at_mask(dm, a, x, t);
+  const __nv_bfloat16* vd = (const __nv_bfloat16*)a.vd + x.s * a.vds[0] + x.l * a.vds[1] + x.g * a.vds[2] + c;
+  for (; seen != 0; seen &= seen - 1) {
+    const uint2 w = *(const uint2*)(vd + (__ffsll((long long)seen) - 1) * a.vds[3]);
+    const float e[4] = {bf16lo(w.x), bf16hi(w.x), bf16lo(w.y), bf16hi(w.y)};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (!isfinite(e[i])) acc[i] += e[i];
+  }
+}
+
+// Tokens per split (a warp; every CTA finds the same from the live lengths): of 32 sizes around an
+// even share of a place (two CTAs on an SM, or one), at least a.chunk (the smallest that the workspace
+// has room for), the one that finishes first by a simple account: items that all run at once take the
+// largest one's tokens, more than that the places' mean share and half an item at the end, and each
+// `extra` tokens' time to change over to.
+// Measured, 8 units of 131011 tokens: 38 splits of 3456 tokens 88 us, 114 of 1152 103 us; 128 units of about
+// 2100: two splits 33 us, four 40 us.
+__device__ __forceinline__ int at_chunk(const Dims& dm, const AttendArgs& a, const int32_t* cu, int lane, float extra,
+                                        int* longest_out) {
+  const auto tokens_of = [&](int s) {
+    const int64_t room = (int64_t)cu[s + 1] - cu[s], live = a.lengths != nullptr ? (int64_t)a.lengths[s] : room;
+    return (int)max((int64_t)0, min(live, min(room, (int64_t)a.max_seqlen)));
+  };
+  const int mine = lane < dm.S ? tokens_of(lane) : 0;  // of the first 32 requests
+  int longest = mine;
+  float tokens = (float)mine;
+  for (int s = lane + 32; s < dm.S; s += 32) {
+    const int n = tokens_of(s);
+    longest = max(longest, n);
+    tokens += (float)n;
+  }
+  longest = __reduce_max_sync(0xffffffffu, longest);
+  *longest_out = longest;
+#pragma unroll
+  for (int off = 16; off >= 1; off >>= 1) tokens += __shfl_xor_sync(0xffffffffu, tokens, off);
+  if (longest <= a.chunk) return a.chunk;
+  const float same = (float)(dm.L * dm.Hkv * a.nrb), work = tokens * same, share = work / (float)a.places;
+  // (sizes from an eighth of the share to 27 times it)
+  int c = (int)fminf(share * exp2f(0.25f * (float)(lane - 12)), (float)longest) / AT_TOK * AT_TOK + AT_TOK;
+  c = max(c, a.chunk);
+  const float per = 1.f / (float)c;
+  float items = 0.f;
+  for (int s0 = 0; s0 < dm.S; s0 += 32) {
+    const int n32 = s0 == 0 ? mine : (s0 + lane < dm.S ? tokens_of(s0 + lane) : 0);
+    const int left = min(32, dm.S - s0);
+    for (int k = 0; k < left; ++k) items += fmaxf(1.f, ceilf((float)__shfl_sync(0xffffffffu, n32, k) * per));
+  }
+  items *= same;
+  const float most = (float)min(c, longest), places = (float)a.places;
+  const float time = items <= places ? most + extra : (work + items * extra) / places + 0.5f * most + extra;
+  const uint32_t best = __reduce_min_sync(0xffffffffu, (__float_as_uint(time) & ~31u) | (uint32_t)lane);
+  return __shfl_sync(0xffffffffu, c, (int)(best & 31u));
+}
+
+template <int REP, int NB>
+__global__ void __launch_bounds__(AtCfg<NB>::THREADS, 3 - NB)
     attend_bf16_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
                        const __grid_constant__ CUtensorMap kdmap, const __grid_constant__ CUtensorMap vdmap, Dims dm,
                        const __grid_constant__ AttendArgs a, const int32_t* __restrict__ cu) {
-  constexpr int ROWS = 128 / REP;      // rows per copy
+  using C = AtCfg<NB>;
+  static_assert(NB == 1 || REP == 1, "copies are for few rows");
+  constexpr int AT_RING = C::RING, AT_LOAD0 = C::LOAD0, AT_LOADERS = C::LOADERS;
+  constexpr uint32_t AT_O = 128 * NB;  // columns [0, AT_O): S of block j at 128 j + 64 (tile % 2); O of block j at AT_O + 128 j
+  constexpr int ROWS = 128 / REP;      // rows per copy (and block)
   constexpr int NC = AT_TOK / REP;     // columns per softmax warp
-  extern __shared__ uint8_t smem_raw[];
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   uint8_t* qs = smem;
-  uint8_t* ks = qs + AT_Q_BYTES;
-  uint8_t* vs = ks + AT_STAGES * AT_TILE;
-  __shared__ uint64_t kfull[AT_STAGES], kempty[AT_STAGES], vfull[AT_STAGES], vempty[AT_STAGES], sfull[2], pready[2],
-      pvdone[2];  // by a tile's parity: a wait for tile i knows that tile i - 2's product is done (S of tile i follows it)
-  __shared__ uint32_t s_tmem, s_bad[2];
-  __shared__ int s_abort;
-  __shared__ float s_m[128], s_z[128];
+  uint8_t* ring = qs + C::Q_BYTES;
+  AtSmem<NB>& sh = *(AtSmem<NB>*)(ring + AT_RING * AT_TILE);
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  pdl_wait();
-  const int rb = blockIdx.x % a.nrb, rest = blockIdx.x / a.nrb;
-  const AtUnit x = at_unit(dm, a, cu, rest / a.nsplit, rest % a.nsplit, AT_TOK);
-  if (x.split >= x.nsp) return;
-  const int R = dm.G * dm.window, r0 = rb * 128;
-  const int nrow = R - r0 < ROWS ? R - r0 : ROWS;
-  if (x.nt == 0) {  // nothing to see
-    for (int r = warp; r < nrow; r += AT_THREADS / 32)
-      at_put<__nv_bfloat16>(dm, a, x, r0 + r, make_float4(0.f, 0.f, 0.f, 0.f), -INFINITY, 0.f, lane);
+  const int R = dm.G * dm.window;
+  if (smem + at_used<NB>() > smem_raw + at_smem<NB>()) {  // (the start was not on 1024 bytes)
+    pdl_wait();
+    if (tid == 0) atomicOr(a.status, (uint32_t)ST_INVALID);
     return;
   }
   if (tid == 0) {
-    s_abort = 0;
-    s_bad[0] = s_bad[1] = 0;
-    for (int i = 0; i < AT_STAGES; ++i) {
-      mbar_init(smem_u32(&kfull[i]), 1);
-      mbar_init(smem_u32(&kempty[i]), 1);
-      mbar_init(smem_u32(&vfull[i]), 1);
-      mbar_init(smem_u32(&vempty[i]), 1);
+    sh.abort = 0;
+    sh.bad[0] = sh.bad[1] = 0;
+    for (int i = 0; i < AT_RING; ++i) {
+      mbar_init(smem_u32(&sh.full[i]), 1);
+      mbar_init(smem_u32(&sh.empty[i]), 1);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(smem_u32(&sfull[i]), 1);
-      mbar_init(smem_u32(&pready[i]), 4);
-      mbar_init(smem_u32(&pvdone[i]), 1);
+      mbar_init(smem_u32(&sh.sfull[i]), 1);
+      mbar_init(smem_u32(&sh.pready[i]), 4 * NB);
+      mbar_init(smem_u32(&sh.pvdone[i]), 1);
     }
+    for (int i = 0; i < AT_QUEUE; ++i) {
+      mbar_init(smem_u32(&sh.qfull[i]), 1);
+      mbar_init(smem_u32(&sh.qempty[i]), 1 + 4 * NB + AT_LOADERS);  // MMA, softmax and row warps
+    }
+    mbar_init(smem_u32(&sh.rowsready), AT_LOADERS);
+    mbar_init(smem_u32(&sh.rowsasked), AT_LOADERS);
+    mbar_init(smem_u32(&sh.rowsfree), REP == 1 ? 1 : 4);
+    mbar_init(smem_u32(&sh.ofree), 4 * NB);
     fence_mbar_init();
   }
   if (warp == 1) {
-    tmem_alloc(smem_u32(&s_tmem), AT_COLS);
+    tmem_alloc(smem_u32(&sh.tmem), C::COLS);
     tmem_relinquish();
   }
-  __syncthreads();
-  Ws ws;
-  ws.status = a.status;
-  volatile int* abort = &s_abort;
-
-  auto load = [&](int i, bool values) {  // tile i of K or V into its stage
-    const int st = i % AT_STAGES;
-    const uint32_t dst = smem_u32((values ? vs : ks) + st * AT_TILE), bar = smem_u32(&(values ? vfull : kfull)[st]);
-    mbar_arrive_expect_tx(bar, AT_TILE);
-    if (i < x.ncache) {
-      const CUtensorMap* map = values ? &vmap : &kmap;
-      const int t = (int)x.t0 + x.tok0 + i * AT_TOK;
-      tma_load_4d(dst, map, 0, t, x.g, x.l, bar);
-      tma_load_4d(dst + AT_BOX, map, 64, t, x.g, x.l, bar);
-    } else {
-      const CUtensorMap* map = values ? &vdmap : &kdmap;
-      tma_load_5d(dst, map, 0, 0, x.g, x.l, x.s, bar);
-      tma_load_5d(dst + AT_BOX, map, 64, 0, x.g, x.l, x.s, bar);
-    }
-  };
   if (tid == 0) {
-    for (int i = 0; i < AT_STAGES && i < x.nt; ++i) {
-      load(i, false);
-      load(i, true);
-    }
+    prefetch_tmap(&kmap);
+    prefetch_tmap(&vmap);
   }
-  // the rows, K-major with the 128-byte swizzle; a copy for each group of lane quarters
-  {
-    const __nv_bfloat16* q = (const __nv_bfloat16*)a.q + x.s * dm.q_ss + x.l * dm.q_sl + (int64_t)x.g * dm.G * dm.q_sh;
-#pragma unroll 4
-    for (int e = tid; e < 128 * 16; e += AT_THREADS) {
-      const int y = e >> 4, c = e & 15, r = y % ROWS;
-      uint4 v = make_uint4(0, 0, 0, 0);
-      if (r < nrow) {
-        const int h = (r0 + r) / dm.window, t = r0 + r - h * dm.window;
-        v = *((const uint4*)(q + h * dm.q_sh + t * dm.q_sp) + c);
-      }
-      *(uint4*)(qs + (c >> 3) * 16384 + sw128_off(y, c & 7)) = v;
-    }
-  }
-  fence_proxy_async_smem();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = s_tmem;
+  pdl_wait();  // nothing before it touches global memory
+  const uint32_t tmem = sh.tmem;
+  Ws ws;
+  ws.status = a.status;
+  volatile int* abort = &sh.abort;
+  // item `k` of this CTA, as the producer published it; the caller's warp (or thread) takes it once
+  auto take = [&](uint32_t k, AtUnit& x, bool whole) {
+    const int q = k % AT_QUEUE;
+    if (!mbar_wait(smem_u32(&sh.qfull[q]), (k / AT_QUEUE) & 1, ws, abort)) return false;
+    x = sh.queue[q];
+    if (whole) __syncwarp();
+    if (!whole || lane == 0) mbar_arrive(smem_u32(&sh.qempty[q]));
+    return x.nt >= 0;
+  };
 
   if (warp == 0) {
     // ------------------------------------------------ TMA producer --------
+    const uint32_t units = (uint32_t)dm.L * dm.Hkv * dm.S;
+    int longest;
+    const int chunk = at_chunk(dm, a, cu, lane, NB == 1 ? 192.f : 400.f, &longest);
     if (lane == 0) {
-      int i = AT_STAGES;
-      for (; i < x.nt; ++i) {
-        const int st = i % AT_STAGES;
-        const uint32_t par = ((i / AT_STAGES) & 1) ^ 1;
-        if (!mbar_wait(smem_u32(&kempty[st]), par, ws, abort)) break;
-        load(i, false);
-        if (!mbar_wait(smem_u32(&vempty[st]), par, ws, abort)) {  // K of this tile is under way alone
-          mbar_wait(smem_u32(&kfull[st]), (i / AT_STAGES) & 1, ws, nullptr);
-          break;
+      const uint32_t most = longest > chunk ? (longest - 1) / chunk + 1 : 1;
+      const uint32_t total = units * a.nrb * most;  // (fewer than 2^31)
+      if (blockIdx.x == 0) a.status[AT_CHUNK] = (uint32_t)chunk;
+      uint32_t n = 0, published = 0;  // loads, items
+      bool ok = true;
+      AtUnit next;
+      uint32_t at = blockIdx.x;
+      // The next item that is not behind its request's last split, into `next` and the queue.
+      // Items are dealt as CTAs become free; row blocks of the same tokens follow each other.
+      auto publish = [&]() {
+        for (;; at = gridDim.x + atomicAdd(a.status + AT_NEXT, 1u)) {
+          if (at >= total) {
+            next.nt = -1;
+            break;
+          }
+          const uint32_t rest = a.nrb == 1 ? at : at / (uint32_t)a.nrb, split = most == 1 ? 0u : rest / units;
+          next = at_unit(dm, a, cu, rest - split * units, (int)split, AT_TOK, chunk);
+          next.r0 = (int)(at - rest * a.nrb) * (128 * NB);
+          if (next.split < next.nsp) break;
         }
-        load(i, true);
+        const int q = published % AT_QUEUE;
+        if (published >= AT_QUEUE && !mbar_wait(smem_u32(&sh.qempty[q]), ((published / AT_QUEUE) & 1) ^ 1, ws, abort))
+          return false;
+        sh.queue[q] = next;
+        mbar_arrive(smem_u32(&sh.qfull[q]));
+        ++published;
+        return true;
+      };
+      ok = publish();
+      // the first rows are asked for before the tiles, which would be ahead of them in memory's queues
+      if (ok && next.nt > 0) ok = mbar_wait(smem_u32(&sh.rowsasked), 0, ws, abort);
+      while (ok && next.nt >= 0) {
+        const AtUnit x = next;
+        // the item after it, a few loads later: its rows are on their way long before they are needed
+        const int when = 2 * x.nt < 4 ? 2 * x.nt : 4;
+        auto claim = [&]() {
+          at = gridDim.x + atomicAdd(a.status + AT_NEXT, 1u);
+          return publish();
+        };
+        for (int i = 0; ok && i < 2 * x.nt; ++i, ++n) {  // K and V of each tile
+          if (i == when && !(ok = claim())) break;
+          const int st = n % AT_RING;
+          if (n >= AT_RING && !mbar_wait(smem_u32(&sh.empty[st]), ((n / AT_RING) & 1) ^ 1, ws, abort)) {
+            ok = false;
+            break;
+          }
+          const uint32_t dst = smem_u32(ring + st * AT_TILE), bar = smem_u32(&sh.full[st]);
+          mbar_arrive_expect_tx(bar, AT_TILE);
+          if ((i >> 1) < x.ncache) {
+            const CUtensorMap* map = i & 1 ? &vmap : &kmap;
+            const int t = (int)x.t0 + x.tok0 + (i >> 1) * AT_TOK;
+            tma_load_4d(dst, map, 0, t, x.g, x.l, bar);
+            tma_load_4d(dst + AT_BOX, map, 64, t, x.g, x.l, bar);
+          } else {
+            const CUtensorMap* map = i & 1 ? &vdmap : &kdmap;
+            tma_load_5d(dst, map, 0, 0, x.g, x.l, x.s, bar);
+            tma_load_5d(dst + AT_BOX, map, 64, 0, x.g, x.l, x.s, bar);
+          }
+        }
+        if (ok && when == 2 * x.nt) ok = claim();
       }
-      const int loaded = i < x.nt ? i : x.nt;  // what is under way lands before the CTA leaves
-      for (int k = loaded > AT_STAGES ? loaded - AT_STAGES : 0; k < loaded; ++k) {
-        mbar_wait(smem_u32(&kfull[k % AT_STAGES]), (k / AT_STAGES) & 1, ws, nullptr);
-        mbar_wait(smem_u32(&vfull[k % AT_STAGES]), (k / AT_STAGES) & 1, ws, nullptr);
+      // what is under way lands before the CTA leaves
+      for (uint32_t k = n > AT_RING ? n - AT_RING : 0; k < n; ++k)
+        mbar_wait(smem_u32(&sh.full[k % AT_RING]), (k / AT_RING) & 1, ws, nullptr);
+      // the last CTA to stop claiming leaves the counters as it found them
+      __threadfence();
+      if (atomicAdd(a.status + AT_DONE, 1u) == gridDim.x - 1) {
+        a.status[AT_NEXT] = 0u;
+        a.status[AT_DONE] = 0u;
       }
     }
   } else if (warp == 1) {
@@ -252,213 +458,378 @@ __global__ void __launch_bounds__(AT_THREADS, 2)
     if (elect_one()) {
       constexpr uint32_t IDESC_S = idesc_bf16_f32(128, AT_TOK, 0, 0), IDESC_O = idesc_bf16_f32(128, D, 0, 1);
       const uint64_t qd = smem_desc_sw128(smem_u32(qs), 16, 1024);
-      int issued = 0;  // second products
-      auto second = [&](int i) {  // O += P V of tile i
-        const int b = i & 1, st = i % AT_STAGES;
-        if (!mbar_wait(smem_u32(&pready[b]), (i >> 1) & 1, ws, abort) ||
-            !mbar_wait(smem_u32(&vfull[st]), (i / AT_STAGES) & 1, ws, abort))
+      uint32_t it = 0, n = 0, busy = 0;  // tiles whose S was issued, loads, items with tiles
+      uint32_t issued = 0;               // second products
+      bool ok = true;
+      int nb = NB;                       // blocks that hold rows
+      AtUnit x;
+      auto second = [&](uint32_t t, uint32_t load, bool first) {  // O (+)= P V of tile t
+        const uint32_t b = t & 1, st = load % AT_RING;
+        // the first of an item: the accumulators of the item before are read out
+        if (first && busy > 1 && !mbar_wait(smem_u32(&sh.ofree), busy & 1, ws, abort)) return false;
+        if (!mbar_wait(smem_u32(&sh.pready[b]), (t >> 1) & 1, ws, abort) ||
+            !mbar_wait(smem_u32(&sh.full[st]), (load / AT_RING) & 1, ws, abort))
           return false;
         tc_fence_after();
-        const uint64_t vd = smem_desc_sw128(smem_u32(vs + st * AT_TILE), AT_BOX, 1024);
+        const uint64_t vd = smem_desc_sw128(smem_u32(ring + st * AT_TILE), AT_BOX, 1024);
 #pragma unroll
-        for (int k = 0; k < AT_TOK / 16; ++k)
-          umma_f16_ts(tmem + AT_O, tmem + 64 * b + 8 * k, vd + (uint64_t)((k * 2048) >> 4), IDESC_O,
-                      i > 0 || k > 0 ? 1u : 0u);
-        umma_commit(smem_u32(&vempty[st]));
-        umma_commit(smem_u32(&pvdone[b]));
+        for (int j = 0; j < NB; ++j) {
+          if (j >= nb) break;
+#pragma unroll
+          for (int k = 0; k < AT_TOK / 16; ++k)
+            umma_f16_ts(tmem + AT_O + 128 * j, tmem + 128 * j + 64 * b + 8 * k, vd + (uint64_t)((k * 2048) >> 4), IDESC_O,
+                        !first || k > 0 ? 1u : 0u);
+        }
+        umma_commit(smem_u32(&sh.empty[st]));
+        umma_commit(smem_u32(&sh.pvdone[b]));
         ++issued;
         return true;
       };
-      bool ok = true;
-      int firsts = 0;
-      for (int i = 0; ok && i < x.nt; ++i) {
-        const int b = i & 1, st = i % AT_STAGES;
-        if (!mbar_wait(smem_u32(&kfull[st]), (i / AT_STAGES) & 1, ws, abort)) {
-          ok = false;
-          break;
-        }
-        tc_fence_after();
-        // S of tile i goes where P of tile i - 2 was: its product, issued before, has read it
-        const uint64_t kd = smem_desc_sw128(smem_u32(ks + st * AT_TILE), 16, 1024);
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k)
-          umma_f16_ss(tmem + 64 * b, qd + (uint64_t)((((k >> 2) * 16384) + (k & 3) * 32) >> 4),
-                      kd + (uint64_t)((((k >> 2) * AT_BOX) + (k & 3) * 32) >> 4), IDESC_S, k > 0 ? 1u : 0u);
-        umma_commit(smem_u32(&kempty[st]));
-        umma_commit(smem_u32(&sfull[b]));
-        ++firsts;
-        if (i > 0) ok = second(i - 1);
-      }
-      if (ok) ok = second(x.nt - 1);
-      // every MMA issued here completes before the CTA tears down tensor memory
-      if (firsts > 0) mbar_wait(smem_u32(&sfull[(firsts - 1) & 1]), ((firsts - 1) >> 1) & 1, ws, nullptr);
-      if (issued > 0) mbar_wait(smem_u32(&pvdone[(issued - 1) & 1]), ((issued - 1) >> 1) & 1, ws, nullptr);
-    }
-  } else {
-    // ------------------------------------------------ softmax -------------
-    const int quarter = warp & 3, y = quarter * 32 + lane, t128 = tid - 64;
-    const int rep = y / ROWS;  // the copy (uniform in a warp)
-    const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-    const float scale2 = a.scale * 1.4426950408889634f, lazy = AT_LAZY / scale2;
-    const int row = r0 + y % ROWS;
-    const uint64_t mask = row < R ? at_mask(dm, a, x, row % dm.window) : 0;
-    float m = -INFINITY, z = 0.f;
-    bool ok = true;
-    for (int i = 0; i < x.nt; ++i) {
-      const int b = i & 1, st = i % AT_STAGES;
-      if (!mbar_wait(smem_u32(&sfull[b]), (i >> 1) & 1, ws, abort)) {
-        ok = false;
-        break;
-      }
-      tc_fence_after();
-      float v[NC];
-      if constexpr (NC == 64) {
-        tmem_ld32x2(tmem + 64 * b + lanes, tmem + 64 * b + 32 + lanes, (uint32_t*)v, (uint32_t*)(v + 32));
-      } else if constexpr (NC == 32) {
-        tmem_ld32(tmem + 64 * b + 32 * rep + lanes, v);
-      } else {
-        tmem_ld16(tmem + 64 * b + 16 * rep + lanes, v);
-      }
-      const bool drafted = i >= x.ncache;
-      const int nv = drafted ? x.nd : x.tok1 - x.tok0 - i * AT_TOK;  // rows of the tile that hold tokens
-      if (drafted) {
-        const uint64_t mine = mask >> (NC * rep);
-#pragma unroll
-        for (int e = 0; e < NC; ++e) v[e] = mine >> e & 1 ? v[e] : -INFINITY;
-      } else if (nv < AT_TOK) {
-#pragma unroll
-        for (int e = 0; e < NC; ++e) v[e] = NC * rep + e < nv ? v[e] : -INFINITY;
-      }
-      float mx[4] = {v[0], v[1], v[2], v[3]};
-#pragma unroll
-      for (int e = 4; e < NC; ++e) mx[e & 3] = fmaxf(mx[e & 3], v[e]);
-      const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-      const bool up = top > m + lazy;
-      if (__any_sync(0xffffffffu, up)) {
-        const float f = up ? (m == -INFINITY ? 0.f : ex2((m - top) * scale2)) : 1.f;
-        if (up) m = top;
-        z *= f;
-        if (i > 0) {
-          if (!mbar_wait(smem_u32(&pvdone[(i - 1) & 1]), ((i - 1) >> 1) & 1, ws, abort)) {
+      for (uint32_t k = 0; ok && take(k, x, false); ++k) {
+        if (x.nt == 0) continue;
+        nb = (min(R - x.r0, NB * 128) + 127) / 128;
+        // the rows are there, which the row warps put down when the item before no longer needed the space
+        if (!mbar_wait(smem_u32(&sh.rowsready), busy & 1, ws, abort)) break;
+        ++busy;
+        for (int i = 0; ok && i < x.nt; ++i, ++it, n += 2) {
+          const uint32_t b = it & 1, st = n % AT_RING;
+          if (!mbar_wait(smem_u32(&sh.full[st]), (n / AT_RING) & 1, ws, abort)) {
             ok = false;
             break;
           }
           tc_fence_after();
-#pragma unroll 1
-          for (int c = 0; c < D; c += 32) {
-            float w[32];
-            tmem_ld32(tmem + AT_O + c + lanes, w);
+          // S of tile it goes where P of tile it - 2 was: its product, issued before, has read it
+          const uint64_t kd = smem_desc_sw128(smem_u32(ring + st * AT_TILE), 16, 1024);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) w[e] *= f;
-            tmem_st_32x32b_x32(tmem + AT_O + c + lanes, *(const uint32_t(*)[32])w);
+          for (int j = 0; j < NB; ++j) {
+            if (j >= nb) break;
+#pragma unroll
+            for (int c = 0; c < D / 16; ++c)
+              umma_f16_ss(tmem + 128 * j + 64 * b, qd + (uint64_t)((j * 32768 + ((c >> 2) * 16384) + (c & 3) * 32) >> 4),
+                          kd + (uint64_t)((((c >> 2) * AT_BOX) + (c & 3) * 32) >> 4), IDESC_S, c > 0 ? 1u : 0u);
           }
-          tmem_wait_st();
+          umma_commit(smem_u32(&sh.empty[st]));
+          umma_commit(smem_u32(&sh.sfull[b]));
+          if (REP == 1 && i == x.nt - 1) umma_commit(smem_u32(&sh.rowsfree));  // the item's last use of its rows
+          if (i > 0) ok = second(it - 1, n - 1, i == 1);
         }
+        if (ok) ok = second(it - 1, n - 1, x.nt == 1);
       }
-      const float base = m == -INFINITY ? 0.f : m * scale2;
-      float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int e = 0; e < NC; ++e) {
-        v[e] = ex2(fmaf(v[e], scale2, -base));
-        sum[e & 3] += v[e];
+      // every MMA issued here completes before the CTA tears down tensor memory
+      if (it > 0) mbar_wait(smem_u32(&sh.sfull[(it - 1) & 1]), ((it - 1) >> 1) & 1, ws, nullptr);
+      if (issued > 0) mbar_wait(smem_u32(&sh.pvdone[(issued - 1) & 1]), ((issued - 1) >> 1) & 1, ws, nullptr);
+    }
+  } else if (warp >= AT_LOAD0) {
+    // ------------------ the rows, K-major with the 128-byte swizzle; a copy per group of lane quarters
+    const int e0 = (warp - AT_LOAD0) * 32 + lane;
+    uint32_t busy = 0;
+    AtUnit x;
+    for (uint32_t k = 0; take(k, x, true); ++k) {
+      if (x.nt == 0) continue;
+      const int nrow = min(R - x.r0, NB * ROWS);
+      const __nv_bfloat16* q = (const __nv_bfloat16*)a.q + x.s * dm.q_ss + x.l * dm.q_sl + (int64_t)x.g * dm.G * dm.q_sh;
+      auto row = [&](int r) {
+        const int h = at_head(dm, a, x.r0 + r), t = x.r0 + r - h * dm.window;
+        return q + h * dm.q_sh + t * dm.q_sp;
+      };
+      // into L2 while the item before is at work: two 128-byte lines per row
+      for (int e = e0; busy > 0 && e < 2 * nrow; e += 32 * AT_LOADERS)
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(row(e >> 1) + (e & 1) * 64));
+      // the item before's last tile has met its rows (with copies of them: and the space carried its sums out)
+      if (busy > 0 && !mbar_wait(smem_u32(&sh.rowsfree), (busy - 1) & 1, ws, abort)) break;
+      const int c = e0 & 15;
+#pragma unroll 8
+      for (int k2 = 0; k2 < 32; ++k2) {
+        const int y = (e0 >> 4) + k2 * 2 * AT_LOADERS, r = y % (NB * ROWS);
+        const bool on = r < nrow;
+        cp_async16(smem_u32(qs + (y >> 7) * 32768 + (c >> 3) * 16384 + sw128_off(y & 127, c & 7)),
+                   (const uint4*)row(on ? r : 0) + c, on);
       }
-      z += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-      uint32_t p[32];
-#pragma unroll
-      for (int c = 0; c < 32; ++c) {
-        const int cc = c % (NC / 2);
-        const uint32_t pk = pack_bf16x2(v[2 * cc], v[2 * cc + 1]);
-        p[c] = REP == 1 || c / (NC / 2) == rep ? pk : 0u;
+      cp_async_commit();
+      if (busy == 0) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sh.rowsasked));
       }
-      tmem_st_32x32b_x32(tmem + 64 * b + lanes, p);
-      if (drafted || nv < AT_TOK) {
-        if (!mbar_wait(smem_u32(&vfull[st]), (i / AT_STAGES) & 1, ws, abort)) {
+      cp_async_wait<0>();
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&sh.rowsready));
+      ++busy;
+    }
+  } else {
+    // ------------------------------------------------ softmax -------------
+    const int blk = (warp - 2) >> 2, quarter = warp & 3, y = quarter * 32 + lane, tsm = tid - 64;
+    constexpr int SM_THREADS = 128 * NB;
+    const uint32_t scol = tmem + 128 * blk, ocol = tmem + AT_O + 128 * blk;
+    uint8_t* stage = qs + 32768 * blk;
+    const int rep = y / ROWS;  // the copy (uniform in a warp)
+    const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+    const float scale2 = a.scale * 1.4426950408889634f, lazy = AT_LAZY / scale2;
+    uint32_t it = 0, n = 1;  // tiles, loads (of V)
+    bool ok = true;
+    AtUnit x;
+    for (uint32_t k = 0; ok; ++k) {
+      const bool more = take(k, x, true);
+      // (all warps decide together whether to go on: a wait may fail in one of them)
+      if (named_barrier_any(1, SM_THREADS, !more && *abort != 0) || !more) break;
+      const int b0 = x.r0 + 128 * blk, nrow = min(R - b0, ROWS);  // the block's first row, and rows
+      if (x.nt == 0) {  // nothing to see
+        for (int r = warp - 2 - 4 * blk; r < nrow; r += 4)
+          at_put<__nv_bfloat16>(dm, a, x, b0 + r, make_float4(0.f, 0.f, 0.f, 0.f), -INFINITY, 0.f, lane);
+        continue;
+      }
+      const int row = b0 + y % ROWS;
+      const uint64_t mask = row < R && x.nt > x.ncache ? at_mask(dm, a, x, row % dm.window) : 0;
+      float m = -INFINITY, z = 0.f;
+      for (int i = 0; i < x.nt; ++i, ++it, n += 2) {
+        const uint32_t b = it & 1;
+        if (!mbar_wait(smem_u32(&sh.sfull[b]), (it >> 1) & 1, ws, abort)) {
           ok = false;
           break;
         }
-        uint8_t* vt = vs + st * AT_TILE;
-        for (int e = t128 + (drafted ? 0 : nv * 16); e < AT_TOK * 16; e += 128) {
-          const int tok = e >> 4, c = e & 15;
-          uint4* at = (uint4*)(vt + (c >> 3) * AT_BOX + sw128_off(tok, c & 7));
-          if (tok >= nv) {
-            *at = make_uint4(0, 0, 0, 0);
-            continue;
-          }
-          uint4 w = *at;
-          uint32_t* ww = (uint32_t*)&w;
-          bool bad = false;
+        tc_fence_after();
+        const bool drafted = i >= x.ncache;
+        const int nv = drafted ? x.nd : x.tok1 - x.tok0 - i * AT_TOK;  // rows of the tile that hold tokens
+        if (nrow > 0) {  // (of two blocks the second may have no rows)
+        float v[NC];
+        if constexpr (NC == 64) {
+          tmem_ld32x2(scol + 64 * b + lanes, scol + 64 * b + 32 + lanes, (uint32_t*)v, (uint32_t*)(v + 32));
+        } else if constexpr (NC == 32) {
+          tmem_ld32(scol + 64 * b + 32 * rep + lanes, v);
+        } else {
+          tmem_ld16(scol + 64 * b + 16 * rep + lanes, v);
+        }
+        if (drafted) {
+          const uint64_t mine = mask >> (NC * rep);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            if ((ww[j] & 0x7f80u) == 0x7f80u) bad = true, ww[j] &= 0xffff0000u;
-            if ((ww[j] & 0x7f800000u) == 0x7f800000u) bad = true, ww[j] &= 0xffffu;
-          }
-          if (bad) {
-            *at = w;
-            atomicOr(&s_bad[tok >> 5], 1u << (tok & 31));
+          for (int e = 0; e < NC; ++e) v[e] = mine >> e & 1 ? v[e] : -INFINITY;
+        } else if (nv < AT_TOK) {
+#pragma unroll
+          for (int e = 0; e < NC; ++e) v[e] = NC * rep + e < nv ? v[e] : -INFINITY;
+        }
+        float mx[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+        for (int e = 4; e < NC; ++e) mx[e & 3] = fmaxf(mx[e & 3], v[e]);
+        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+        const bool up = top > m + lazy;
+        if (__any_sync(0xffffffffu, up)) {
+          const float f = up ? (m == -INFINITY ? 0.f : ex2((m - top) * scale2)) : 1.f;
+          if (up) m = top;
+          z *= f;
+          if (i > 0) {
+            if (!mbar_wait(smem_u32(&sh.pvdone[b ^ 1]), ((it - 1) >> 1) & 1, ws, abort)) {
+              ok = false;
+              break;
+            }
+            tc_fence_after();
+#pragma unroll 1
+            for (int c = 0; c < D; c += 32) {
+              float w[32];
+              tmem_ld32(ocol + c + lanes, w);
+#pragma unroll
+              for (int e = 0; e < 32; ++e) w[e] *= f;
+              tmem_st_32x32b_x32(ocol + c + lanes, *(const uint32_t(*)[32])w);
+            }
+            tmem_wait_st();
           }
         }
-        fence_proxy_async_smem();
+        const float base = m == -INFINITY ? 0.f : m * scale2;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < NC; ++e) {
+          v[e] = ex2(fmaf(v[e], scale2, -base));
+          sum[e & 3] += v[e];
+        }
+        z += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        uint32_t p[32];
+#pragma unroll
+        for (int c = 0; c < 32; ++c) {
+          const int cc = c % (NC / 2);
+          const uint32_t pk = pack_bf16x2(v[2 * cc], v[2 * cc + 1]);
+          p[c] = REP == 1 || c / (NC / 2) == rep ? pk : 0u;
+        }
+        tmem_st_32x32b_x32(scol + 64 * b + lanes, p);
+        }
+        if (drafted || nv < AT_TOK) {
+          if (!mbar_wait(smem_u32(&sh.full[n % AT_RING]), (n / AT_RING) & 1, ws, abort)) {
+            ok = false;
+            break;
+          }
+          uint8_t* vt = ring + n % AT_RING * AT_TILE;
+          for (int e = tsm + (drafted ? 0 : nv * 16); e < AT_TOK * 16; e += SM_THREADS) {
+            const int tok = e >> 4, c = e & 15;
+            uint4* at = (uint4*)(vt + (c >> 3) * AT_BOX + sw128_off(tok, c & 7));
+            if (tok >= nv) {
+              *at = make_uint4(0, 0, 0, 0);
+              continue;
+            }
+            uint4 w = *at;
+            uint32_t* ww = (uint32_t*)&w;
+            bool bad = false;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              if ((ww[j] & 0x7f80u) == 0x7f80u) bad = true, ww[j] &= 0xffff0000u;
+              if ((ww[j] & 0x7f800000u) == 0x7f800000u) bad = true, ww[j] &= 0xffffu;
+            }
+            if (bad) {
+              *at = w;
+              atomicOr(&sh.bad[tok >> 5], 1u << (tok & 31));
+            }
+          }
+          fence_proxy_async_smem();
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sh.pready[b]));
       }
-      tmem_wait_st();
+      if (ok) ok = mbar_wait(smem_u32(&sh.pvdone[(it - 1) & 1]), ((it - 1) >> 1) & 1, ws, abort);
+      // all warps meet here whether or not a wait failed, and leave together if one did
+      if (named_barrier_any(1, SM_THREADS, !ok)) break;
+      tc_fence_after();
+      const uint64_t bad = (uint64_t)sh.bad[1] << 32 | sh.bad[0];
+      if constexpr (REP == 1) {
+        // a lane has a whole row: 32 channels at a time, partial sums with the rows of a block next to each other
+        const int h = at_head(dm, a, row), t = row - h * dm.window;
+        const bool on = y < nrow && t < x.rows;
+        const float f = x.nsp > 1 ? 1.f : (z == 0.f ? 0.f : 1.f / z);
+        float4* part = nullptr;
+        __nv_bfloat16* o = nullptr;
+        if (on && x.nsp > 1) {
+          part = at_part(dm, a, x.u, x.split, row);
+          *(float2*)(a.mlpart + 2 * ((x.u * a.nsplit + x.split) * R + row)) = make_float2(m, z);
+        } else if (on) {
+          o = (__nv_bfloat16*)a.o + x.s * a.os[0] + x.l * a.os[1] + (int64_t)(x.g * dm.G + h) * a.os[2] + t * a.os[3];
+          if (a.lse != nullptr)
+            a.lse[x.s * a.ls[0] + x.l * a.ls[1] + (x.g * dm.G + h) * a.ls[2] + t] =
+                z == 0.f ? -INFINITY : m * a.scale + logf(z);
+        }
+        if (nrow > 0) {
+#pragma unroll 1
+          for (int c = 0; c < D; c += 32) {
+            float w[32];
+            tmem_ld32(ocol + c + lanes, w);
+            if (part != nullptr) {
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                part[(c / 4 + e) * a.prows] = make_float4(w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]);
+            } else if (o != nullptr) {
+#pragma unroll
+              for (int e = 0; e < 32; e += 8)
+                *(uint4*)(o + c + e) =
+                    make_uint4(pack_bf16x2(w[e] * f, w[e + 1] * f), pack_bf16x2(w[e + 2] * f, w[e + 3] * f),
+                               pack_bf16x2(w[e + 4] * f, w[e + 5] * f), pack_bf16x2(w[e + 6] * f, w[e + 7] * f));
+            }
+          }
+          if (bad != 0 && on) {  // added to what this lane has just written
+#pragma unroll 1
+            for (int c = 0; c < D; c += 4) {
+              float acc[4] = {0.f, 0.f, 0.f, 0.f};
+              at_bad(dm, a, x, bad, t, c, acc);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                if (acc[e] == 0.f) continue;
+                if (part != nullptr) ((float*)(part + c / 4 * a.prows))[e] += acc[e];
+                else o[c + e] = __float2bfloat16(__bfloat162float(o[c + e]) + acc[e]);
+              }
+            }
+          }
+        }
+      } else {
+        // A row's copies scaled to their common maximum (and by 1 / Z where there is one split) meet in the space
+        // of the query rows, which the item's last tile has met, half the channels at a time.
+        constexpr int RL = ROWS / 32;  // rows per lane: lane + 32 j
+        float mr[RL], zr[RL];
+        float2* ex = (float2*)stage;  // [128] (maximum, sum)
+        ex[y] = make_float2(m, z);
+        named_barrier_sync(1, SM_THREADS);
+        // (a copy whose logits are all NaN has the maximum -inf and a sum that is not 0)
+        const auto share = [&](float2 mz, float t) {
+          return mz.x == -INFINITY ? (mz.y == 0.f ? 0.f : 1.f) : ex2((mz.x - t) * scale2);
+        };
+        float4* part[RL];
+        __nv_bfloat16* o[RL];
+#pragma unroll
+        for (int j = 0; j < RL; ++j) {
+          mr[j] = -INFINITY, zr[j] = 0.f;
+#pragma unroll
+          for (int c = 0; c < REP; ++c) mr[j] = fmaxf(mr[j], ex[c * ROWS + 32 * j + lane].x);
+#pragma unroll
+          for (int c = 0; c < REP; ++c) zr[j] += ex[c * ROWS + 32 * j + lane].y * share(ex[c * ROWS + 32 * j + lane], mr[j]);
+          const int rr = lane + 32 * j, h = at_head(dm, a, rr), t = rr - h * dm.window;
+          part[j] = nullptr, o[j] = nullptr;
+          if (rr >= nrow || t >= x.rows) continue;
+          if (x.nsp > 1) {
+            part[j] = at_part(dm, a, x.u, x.split, rr);
+            if (warp == 2)
+              *(float2*)(a.mlpart + 2 * ((x.u * a.nsplit + x.split) * R + rr)) = make_float2(mr[j], zr[j]);
+          } else {
+            o[j] = (__nv_bfloat16*)a.o + x.s * a.os[0] + x.l * a.os[1] + (int64_t)(x.g * dm.G + h) * a.os[2] + t * a.os[3];
+            if (warp == 2 && a.lse != nullptr)
+              a.lse[x.s * a.ls[0] + x.l * a.ls[1] + (x.g * dm.G + h) * a.ls[2] + t] =
+                  zr[j] == 0.f ? -INFINITY : mr[j] * a.scale + logf(zr[j]);
+          }
+        }
+        float f = share(make_float2(m, z), mr[y % ROWS / 32]);
+        if (x.nsp == 1) f *= zr[y % ROWS / 32] == 0.f ? 0.f : 1.f / zr[y % ROWS / 32];
+        named_barrier_sync(1, SM_THREADS);
+        float4* out = (float4*)stage;  // [128][16], 16-byte pieces swizzled by the row
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {
+#pragma unroll
+          for (int c = 0; c < 64; c += 32) {
+            float w[32];
+            tmem_ld32(ocol + 64 * half + c + lanes, w);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              out[y * 16 + ((c / 4 + e) ^ (y & 7))] =
+                  make_float4(w[4 * e] * f, w[4 * e + 1] * f, w[4 * e + 2] * f, w[4 * e + 3] * f);
+          }
+          named_barrier_sync(1, SM_THREADS);
+          // a lane per row, a warp per four of the 16 pieces
+#pragma unroll
+          for (int j = 0; j < RL; ++j) {
+            const int r = lane + 32 * j;
+#pragma unroll
+            for (int k4 = 0; k4 < 4; ++k4) {
+              const int c = 4 * (warp - 2) + k4;
+              float acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+              for (int q = 0; q < REP; ++q) {
+                const float4 w = out[(q * ROWS + r) * 16 + (c ^ (r & 7))];
+                acc[0] += w.x, acc[1] += w.y, acc[2] += w.z, acc[3] += w.w;
+              }
+              if (bad != 0 && (part[j] != nullptr || o[j] != nullptr))
+                at_bad(dm, a, x, bad, r - at_head(dm, a, r) * dm.window, 64 * half + 4 * c, acc);
+              if (part[j] != nullptr)
+                part[j][(16 * half + c) * a.prows] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+              else if (o[j] != nullptr)
+                *(uint2*)(o[j] + 64 * half + 4 * c) = make_uint2(pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3]));
+            }
+          }
+          named_barrier_sync(1, SM_THREADS);
+        }
+      }
+      if (bad != 0) {
+        named_barrier_sync(1, SM_THREADS);  // (the same for all: the bits were set before the barriers above)
+        if (tsm == 0) sh.bad[0] = sh.bad[1] = 0;
+      }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&pready[b]));
-    }
-    if (ok) ok = mbar_wait(smem_u32(&pvdone[(x.nt - 1) & 1]), ((x.nt - 1) >> 1) & 1, ws, abort);
-    tc_fence_after();
-    s_m[y] = m;
-    s_z[y] = z;
-    // all four warps meet here whether or not a wait failed, and leave together if one did
-    if (!named_barrier_any(1, 128, !ok)) {
-      // a row's copies scaled to their common maximum, through the ring (its last reader
-      // was the last product) so that whole rows leave in one piece
-      float top = -INFINITY;
-#pragma unroll
-      for (int c = 0; c < REP; ++c) top = fmaxf(top, s_m[c * ROWS + y % ROWS]);
-      // (a copy whose logits are all NaN has the maximum -inf and a sum that is not 0)
-      const auto share = [&](float mc, float zc) {
-        return REP == 1 ? 1.f : (mc == -INFINITY ? (zc == 0.f ? 0.f : 1.f) : ex2((mc - top) * scale2));
-      };
-      const float f = share(m, z);
-      float4* out = (float4*)ks;  // [128][32], 16-byte pieces swizzled by the row
-#pragma unroll 1
-      for (int c = 0; c < D; c += 32) {
-        float w[32];
-        tmem_ld32(tmem + AT_O + c + lanes, w);
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          out[y * 32 + ((c / 4 + e) ^ (lane & 7))] =
-              make_float4(w[4 * e] * f, w[4 * e + 1] * f, w[4 * e + 2] * f, w[4 * e + 3] * f);
+      if (lane == 0) {
+        mbar_arrive(smem_u32(&sh.ofree));
+        if (REP > 1) mbar_arrive(smem_u32(&sh.rowsfree));
       }
-      named_barrier_sync(1, 128);
-      for (int r = warp - 2; r < nrow; r += 4) {
-        float mr = -INFINITY, zr = 0.f;
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int c = 0; c < REP; ++c) mr = fmaxf(mr, s_m[c * ROWS + r]);
-#pragma unroll
-        for (int c = 0; c < REP; ++c) {
-          const int yy = c * ROWS + r;
-          const float mc = s_m[yy];
-          top = mr;
-          zr += s_z[yy] * share(mc, s_z[yy]);
-          const float4 w = out[yy * 32 + (lane ^ (yy & 7))];
-          acc.x += w.x, acc.y += w.y, acc.z += w.z, acc.w += w.w;
+      if (REP == 4 && x.nsp > 1 && at_joins_inside(x.nsp, R)) {
+        __threadfence();
+        named_barrier_sync(1, SM_THREADS);
+        if (tsm == 0) {
+          sh.last = atomicAdd(a.counts + x.u, 1) == x.nsp - 1;
+          if (sh.last) a.counts[x.u] = 0;  // (zero between calls)
+          __threadfence();
         }
-        const uint64_t bad = (uint64_t)s_bad[1] << 32 | s_bad[0];
-        if (bad != 0) {  // drafted values that are not finite, for the rows that see them
-          uint64_t seen = bad & at_mask(dm, a, x, (r0 + r) % dm.window);
-          const __nv_bfloat16* vd = (const __nv_bfloat16*)a.vd + x.s * a.vds[0] + x.l * a.vds[1] + x.g * a.vds[2] + 4 * lane;
-          for (; seen != 0; seen &= seen - 1) {
-            const uint2 w = *(const uint2*)(vd + (__ffsll((long long)seen) - 1) * a.vds[3]);
-            const float e[4] = {bf16lo(w.x), bf16hi(w.x), bf16lo(w.y), bf16hi(w.y)};
-            if (!isfinite(e[0])) acc.x += e[0];
-            if (!isfinite(e[1])) acc.y += e[1];
-            if (!isfinite(e[2])) acc.z += e[2];
-            if (!isfinite(e[3])) acc.w += e[3];
-          }
-        }
-        at_put<__nv_bfloat16>(dm, a, x, r0 + r, acc, mr, zr, lane);
+        named_barrier_sync(1, SM_THREADS);
+        if (sh.last) at_join<__nv_bfloat16, 1, 8>(dm, a, x, 8 * (warp - 2), 0, nullptr, nullptr);
       }
     }
   }
@@ -466,7 +837,7 @@ __global__ void __launch_bounds__(AT_THREADS, 2)
   __syncthreads();
   if (warp == 1) {
     tc_fence_after();
-    tmem_dealloc(tmem, AT_COLS);
+    tmem_dealloc(tmem, C::COLS);
   }
 }
 
@@ -492,7 +863,7 @@ __global__ void __launch_bounds__(AF_THREADS, 1)
   pdl_wait();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rb = blockIdx.x % a.nrb, rest = blockIdx.x / a.nrb;
-  const AtUnit x = at_unit(dm, a, cu, rest / a.nsplit, rest % a.nsplit, AF_TOK);
+  const AtUnit x = at_unit(dm, a, cu, rest / a.nsplit, rest % a.nsplit, AF_TOK, a.chunk);
   if (x.split >= x.nsp) return;
   const int R = dm.G * dm.window, r0 = rb * RB, nrow = R - r0 < RB ? R - r0 : RB;
   if (x.nt == 0) {
@@ -645,52 +1016,46 @@ __global__ void __launch_bounds__(AF_THREADS, 1)
 }
 
 // --------------------------------------------------------- joined splits ----
-// A warp per row of a unit with several splits: their sums scaled to the largest
-// maximum, added in the splits' order.
-constexpr int AJ_THREADS = 128;
-template <typename T>
+// Joins the splits of units that have several: NR rows to W warps.
+constexpr int AJ_THREADS = 256, AJ_WARPS = AJ_THREADS / 32;
+template <typename T, int W, int NR>
 __global__ void __launch_bounds__(AJ_THREADS)
     attend_join_kernel(Dims dm, const __grid_constant__ AttendArgs a, const int32_t* __restrict__ cu) {
+  __shared__ float4 s_o[W > 1 ? AJ_WARPS * NR * 32 : 1];
+  __shared__ float s_z[AJ_WARPS][NR];
   pdl_wait();
-  const int R = dm.G * dm.window, lane = threadIdx.x & 31;
-  const int64_t w = (int64_t)blockIdx.x * (AJ_THREADS / 32) + (threadIdx.x >> 5);
-  if (w >= (int64_t)dm.L * dm.Hkv * dm.S * R) return;
-  const int r = (int)(w % R);
-  AtUnit x = at_unit(dm, a, cu, w / R, 0, AT_TOK);
-  if (x.nsp == 1 || r % dm.window >= x.rows) return;
-  const int64_t p0 = x.u * a.nsplit * R + r;
-  const float scale2 = a.scale * 1.4426950408889634f;
-  float m = -INFINITY;
-  for (int j = lane; j < x.nsp; j += 32) m = fmaxf(m, a.mlpart[2 * (p0 + (int64_t)j * R)]);
-#pragma unroll
-  for (int off = 16; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
-  float z = 0.f;
-  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int j = 0; j < x.nsp; ++j) {
-    const int64_t p = p0 + (int64_t)j * R;
-    const float2 ml = *(const float2*)(a.mlpart + 2 * p);
-    const float4 v = *(const float4*)(a.opart + p * D + 4 * lane);
-    const float f = ml.x == m ? 1.f : ex2((ml.x - m) * scale2);
-    const bool none = ml.x == -INFINITY && ml.y == 0.f;  // that split saw nothing
-    z += none ? 0.f : ml.y * f;
-    s.x += none ? 0.f : v.x * f;
-    s.y += none ? 0.f : v.y * f;
-    s.z += none ? 0.f : v.z * f;
-    s.w += none ? 0.f : v.w * f;
-  }
-  x.nsp = 1;  // straight to the output
-  at_put<T>(dm, a, x, r, s, m, z, lane);
+  const int R = dm.G * dm.window, groups = (R + NR - 1) / NR, warp = threadIdx.x >> 5;
+  const int w = blockIdx.x * (AJ_WARPS / W) + warp / W, units = dm.L * dm.Hkv * dm.S;
+  const bool real = w < units * groups;
+  const int u = real ? w / groups : 0;
+  const int chunk = sizeof(T) == 2 ? (int)a.status[AT_CHUNK] : a.chunk;
+  AtUnit x = at_unit(dm, a, cu, u, 0, AT_TOK, chunk);
+  const bool inside = sizeof(T) == 2 && at_joins_inside(x.nsp, R);  // that unit is done
+  at_join<T, W, NR>(dm, a, x, real && !inside ? (w - u * groups) * NR : R, warp % W,
+                    s_o + (W > 1 ? warp * NR * 32 : 0), s_z[warp]);
+}
+
+template <typename T, int W, int NR>
+static cudaError_t launch_join(const Dims& dm, const AttendArgs& a, const int32_t* cu, cudaStream_t st) {
+  const int64_t groups = (int64_t)dm.L * dm.Hkv * dm.S * ((dm.G * dm.window + NR - 1) / NR);
+  return launch_pdl(true, attend_join_kernel<T, W, NR>, dim3((unsigned)((groups * W + AJ_WARPS - 1) / AJ_WARPS)), AJ_THREADS,
+                    0, st, dm, a, cu);
+}
+template <typename T>
+static cudaError_t launch_join(const Dims& dm, const AttendArgs& a, const int32_t* cu, cudaStream_t st) {
+  return a.nsplit <= 16 ? launch_join<T, 1, 8>(dm, a, cu, st) : launch_join<T, 8, 4>(dm, a, cu, st);
 }
 
 // ------------------------------------------------------------- launchers ----
-template <int REP>
-static cudaError_t launch_bf16(const CUtensorMap* maps, const Dims& dm, const AttendArgs& a, const int32_t* cu,
-                               int grid, cudaStream_t st) {
-  static_assert(AT_SMEM + 2048 <= 116736, "two CTAs per SM");
-  JACAP_TRY(cudaFuncSetAttribute(attend_bf16_kernel<REP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)AT_SMEM));
-  return launch_pdl(true, attend_bf16_kernel<REP>, grid, AT_THREADS, AT_SMEM, st, maps[0], maps[1], maps[2], maps[3], dm,
-                    a, cu);
+template <int REP, int NB>
+static cudaError_t launch_bf16(const CUtensorMap* maps, const Dims& dm, const AttendArgs& args, const int32_t* cu,
+                               int64_t items, int sms, cudaStream_t st) {
+  auto kern = attend_bf16_kernel<REP, NB>;
+  JACAP_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)at_smem<NB>()));
+  AttendArgs a = args;
+  a.places = sms * (3 - NB);
+  return launch_pdl(true, kern, (int)(items < a.places ? items : a.places), AtCfg<NB>::THREADS, at_smem<NB>(), st, maps[0],
+                    maps[1], maps[2], maps[3], dm, a, cu);
 }
 template <int RB>
 static cudaError_t launch_f32(const Dims& dm, const AttendArgs& a, const int32_t* cu, int grid, cudaStream_t st) {
@@ -699,25 +1064,26 @@ static cudaError_t launch_f32(const Dims& dm, const AttendArgs& a, const int32_t
   return launch_pdl(true, attend_f32_kernel<RB>, grid, AF_THREADS, af_smem<RB>(), st, dm, a, cu);
 }
 
-int attend_row_block(int dtype, int rows) { return dtype == 1 ? 128 : (rows <= 8 ? 8 : 32); }
+int attend_row_block(int dtype, int rows) { return dtype == 1 ? (rows <= 128 ? 128 : 256) : (rows <= 8 ? 8 : 32); }
+
+int attend_part_rows(int rows) { return rows <= 32 ? 32 : (rows <= 64 ? 64 : 128); }
 
 cudaError_t launch_attend(const CUtensorMap* maps, const Dims& dm, int dtype, const AttendArgs& a, const int32_t* cu,
-                          cudaStream_t st) {
+                          int sms, cudaStream_t st) {
   const int R = dm.G * dm.window;
   const int64_t units = (int64_t)dm.L * dm.Hkv * dm.S, blocks = units * a.nsplit * a.nrb;
-  if (blocks > INT32_MAX || units * R / 4 + 1 > INT32_MAX) return cudaErrorInvalidValue;
+  if (blocks > INT32_MAX || units * R > INT32_MAX / 8) return cudaErrorInvalidValue;
   if (dtype == 1) {
-    if (R <= 32) JACAP_TRY(launch_bf16<4>(maps, dm, a, cu, (int)blocks, st));
-    else if (R <= 64) JACAP_TRY(launch_bf16<2>(maps, dm, a, cu, (int)blocks, st));
-    else JACAP_TRY(launch_bf16<1>(maps, dm, a, cu, (int)blocks, st));
+    if (R <= 32) JACAP_TRY((launch_bf16<4, 1>(maps, dm, a, cu, blocks, sms, st)));
+    else if (R <= 64) JACAP_TRY((launch_bf16<2, 1>(maps, dm, a, cu, blocks, sms, st)));
+    else if (R <= 128) JACAP_TRY((launch_bf16<1, 1>(maps, dm, a, cu, blocks, sms, st)));
+    else JACAP_TRY((launch_bf16<1, 2>(maps, dm, a, cu, blocks, sms, st)));
   } else {
     if (R <= 8) JACAP_TRY(launch_f32<8>(dm, a, cu, (int)blocks, st));
     else JACAP_TRY(launch_f32<32>(dm, a, cu, (int)blocks, st));
   }
-  if (a.nsplit == 1) return cudaSuccess;
-  const int grid = (int)((units * R + AJ_THREADS / 32 - 1) / (AJ_THREADS / 32));
-  return dtype == 1 ? launch_pdl(true, attend_join_kernel<__nv_bfloat16>, grid, AJ_THREADS, 0, st, dm, a, cu)
-                    : launch_pdl(true, attend_join_kernel<float>, grid, AJ_THREADS, 0, st, dm, a, cu);
+  if (a.nsplit == 1 || (dtype == 1 && at_joins_inside(a.nsplit, R))) return cudaSuccess;
+  return dtype == 1 ? launch_join<__nv_bfloat16>(dm, a, cu, st) : launch_join<float>(dm, a, cu, st);
 }
 
 }  // namespace jacap
