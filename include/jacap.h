@@ -555,8 +555,8 @@ jacap_status jacap_weigh(const jacap_layout* layout, const jacap_weighing* how, 
  * to the lower index), `budget` tokens in all (all n_s of them if there are no
  * more).
  *   weights      device float32 [num_layers][num_kv_heads][total_tokens], finite
- *                and not negative (else JACAP_ERR_NONFINITE in the status word and
- *                nothing is selected)
+ *                and not negative (else JACAP_ERR_NONFINITE in the status word, and
+ *                with pos nothing is selected, without it nothing of that unit)
  *   pos          NULL: first and last by row; or the tokens' tags (laid out as in
  *                jacap_compact_inplace): a token stays if its tag is below `sinks`
  *                or above the unit's largest tag less `recent`
@@ -564,6 +564,7 @@ jacap_status jacap_weigh(const jacap_layout* layout, const jacap_weighing* how, 
  *   weights_out  device float32 [num_layers][num_kv_heads][num_seqs][budget] or
  *                NULL: the kept tokens' weights (0 where idx is -1)
  *   keys         device float32, the shape of weights, not overlapping it: scratch
+ *                (NULL without pos)
  *   ws           device, 256-byte aligned, at least 64 bytes: the status word, zero
  *                at first (a workspace of jacap_weigh serves; one that holds an error
  *                selects nothing)
@@ -577,7 +578,9 @@ jacap_status jacap_select_weights(const jacap_layout* layout, const float* weigh
 /*
  * The same selection with the retained cache in place, as
  * jacap_select_compact_inplace leaves it: k, v, pos (unless NULL) and the weights
- * move together. Here the weights are laid out as pos is (for a dense K as above; K's
+ * move together; a weight that is negative or not finite ends the call
+ * (JACAP_ERR_NONFINITE in the status word, nothing moves). keys is needed here, dense
+ * [num_layers][num_kv_heads][total_tokens]. The weights are laid out as pos is (for a dense K as above; K's
  * layer and head strides must be multiples of its token stride); those of rows from
  * kept on are left as they were.
  */

@@ -377,7 +377,7 @@ class WeightEvictor:
         new = lambda shape, dtype: torch.empty(shape, dtype=dtype, device=self.device)  # noqa: E731
         self.weights = new((L, Hkv, N), torch.float32)
         self.lse = new((S, L, cache.num_q_heads, w), torch.float32)
-        self.keys = new((L, Hkv, N), torch.float32)
+        self.keys = None  # scratch of a selection by tags
         self.idx = new((L, Hkv, S, self.budget), torch.int32)
         self.kept = new((S,), torch.int32)
         self.k_out = new((L, Hkv, S, self.budget, d), cache.k.dtype)
@@ -426,9 +426,12 @@ class WeightEvictor:
             raise ValueError("tags need a dense cache")
 
         def select(st):
+            if pos is not None and self.keys is None:
+                self.keys = torch.empty_like(self.weights)
             _check(jacap_select_weights(self.lay, wp, pp, self.sinks, self.recent, self.budget, self.idx.data_ptr(),
                                         self.kept.data_ptr(), c.k.data_ptr(), c.v.data_ptr(), self.k_out.data_ptr(),
-                                        self.v_out.data_ptr(), self.weights_out.data_ptr(), self.keys.data_ptr(),
+                                        self.v_out.data_ptr(), self.weights_out.data_ptr(),
+                                        None if pos is None else self.keys.data_ptr(),
                                         self.ws.data_ptr(), self.ws.numel(), st), "jacap_select_weights")
 
         _enqueue(dev, stream, select)

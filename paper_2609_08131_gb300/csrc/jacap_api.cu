@@ -696,10 +696,11 @@ namespace {
 // Checks shared by the selections by attention weights.
 jacap_status check_weights(const jacap_layout* layout, const float* weights, const int32_t* pos, int32_t sinks,
                            int32_t recent, int32_t budget, const int32_t* idx, const int32_t* kept, const void* k,
-                           const void* v, const float* keys, void* ws, size_t ws_bytes, Ws* w, Dims* dm) {
+                           const void* v, const float* keys, bool keys_needed, void* ws, size_t ws_bytes, Ws* w, Dims* dm) {
   jacap_status st = check_layout(layout);
   if (st != JACAP_OK) return st;
-  if (weights == nullptr || idx == nullptr || kept == nullptr || k == nullptr || v == nullptr || keys == nullptr ||
+  if (weights == nullptr || idx == nullptr || kept == nullptr || k == nullptr || v == nullptr ||
+      (keys == nullptr && keys_needed) ||
       ws == nullptr || budget < 1 || sinks < 0 || recent < 0 || (int64_t)sinks + recent > budget || keys == weights)
     return JACAP_ERR_INVALID_ARG;
   if (((uintptr_t)weights & 3u) != 0 || ((uintptr_t)keys & 3u) != 0 || ((uintptr_t)idx & 3u) != 0 ||
@@ -722,20 +723,26 @@ jacap_status jacap_select_weights(const jacap_layout* layout, const float* weigh
                                   size_t ws_bytes, void* stream) {
   Ws w;
   Dims dm;
-  jacap_status st = check_weights(layout, weights, pos, sinks, recent, budget, idx, kept, k, v, keys, ws, ws_bytes, &w, &dm);
+  jacap_status st = check_weights(layout, weights, pos, sinks, recent, budget, idx, kept, k, v, keys, pos != nullptr, ws, ws_bytes,
+                                  &w, &dm);
   if (st != JACAP_OK) return st;
   if (k_out == nullptr || v_out == nullptr || !aligned16(k_out) || !aligned16(v_out) || ((uintptr_t)weights_out & 3u) != 0)
     return JACAP_ERR_INVALID_ARG;
   const cudaStream_t s = (cudaStream_t)stream;
   const TraceRange trace("jacap/select_weights");
   WeightRef wr = {const_cast<float*>(weights), (int64_t)dm.Hkv * dm.Ntot, dm.Ntot};
+  const int dt = layout->dtype == JACAP_BF16 ? 1 : 0;
+  if (pos == nullptr) {  // by row: in the selection itself
+    if (weights_out == nullptr) wr.p = nullptr;
+    return map_cuda(launch_select(dm, w, layout->cu_seqlens, weights, budget, idx, kept, layout->max_seqlen, s, dt, k, v,
+                                  k_out, v_out, nullptr, nullptr, nullptr, wr, weights_out, sinks, recent));
+  }
   if ((st = map_cuda(launch_protect(dm, w, layout->cu_seqlens, wr, pos, sinks, recent, keys, layout->max_seqlen, s))) !=
       JACAP_OK)
     return st;
   if (weights_out == nullptr) wr.p = nullptr;
-  return map_cuda(launch_select(dm, w, layout->cu_seqlens, keys, budget, idx, kept, layout->max_seqlen, s,
-                                layout->dtype == JACAP_BF16 ? 1 : 0, k, v, k_out, v_out, nullptr, nullptr, nullptr, wr,
-                                weights_out));
+  return map_cuda(launch_select(dm, w, layout->cu_seqlens, keys, budget, idx, kept, layout->max_seqlen, s, dt, k, v, k_out,
+                                v_out, nullptr, nullptr, nullptr, wr, weights_out));
 }
 
 jacap_status jacap_evict_weights(const jacap_layout* layout, float* weights, int32_t* pos, int32_t sinks, int32_t recent,
@@ -743,7 +750,8 @@ jacap_status jacap_evict_weights(const jacap_layout* layout, float* weights, int
                                  float* keys, void* ws, size_t ws_bytes, void* stream) {
   Ws w;
   Dims dm;
-  jacap_status st = check_weights(layout, weights, pos, sinks, recent, budget, idx, kept, k, v, keys, ws, ws_bytes, &w, &dm);
+  jacap_status st = check_weights(layout, weights, pos, sinks, recent, budget, idx, kept, k, v, keys, true, ws, ws_bytes,
+                                  &w, &dm);
   if (st != JACAP_OK) return st;
   if (preserve_order != 0 && preserve_order != 1) return JACAP_ERR_INVALID_ARG;
   if (dm.kv_sl % dm.kv_st != 0 || dm.kv_sh % dm.kv_st != 0) return JACAP_ERR_INVALID_ARG;

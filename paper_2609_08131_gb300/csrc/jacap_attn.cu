@@ -17,6 +17,11 @@ namespace {
 constexpr size_t ALIGN = 1024;
 inline size_t align_up(size_t x) { return (x + ALIGN - 1) & ~(ALIGN - 1); }
 
+// The tensor cores' float32 sums truncate: of the eight K-steps of a dot product of 128 channels the j-th
+// loses 2^-24 / (2 ln 2) of a sum of about j / 8 of the whole on average over a mantissa, together 9 2^-23 /
+// (8 ln 2) of it, by which logits are too small; the scale makes up for that.
+constexpr double TRUNCATION = 9.0 * 1.1920928955078125e-07 * 0.18033688011112042;
+
 // ------------------------------------------------------------- attention ----
 constexpr int AT_DRAFTS_MAX = 64;
 
@@ -65,7 +70,7 @@ jacap_status check_attend_layout(const jacap_layout* L) {
 
 // ----------------------------------------------------------------- weights ----
 struct WeighCarve {
-  size_t status, plan, chunks, counters, runs, sched, lse, stat, total;
+  size_t status, plan, chunks, counters, runs, sched, lse, stat, norm, total;
 };
 WeighCarve carve_weigh(const Dims& dm) {
   WeighCarve c;
@@ -79,6 +84,7 @@ WeighCarve carve_weigh(const Dims& dm) {
   c.sched = o; o = align_up(o + 32 + (2 * ((size_t)dm.S + 2) + dm.S + 1 + 1) * 4);
   c.lse = o; o = align_up(o + (size_t)dm.S * dm.L * dm.Hq * dm.window * 4);
   c.stat = o; o = align_up(o + planes * (size_t)dm.c_cap * 2 * rows * 8);
+  c.norm = o; o = align_up(o + planes * dm.S * rows * 8);
   c.total = o;
   return c;
 }
@@ -116,7 +122,7 @@ jacap_status jacap_rotate(const jacap_rope* rope, jacap_dtype dtype, int32_t num
                           const jacap_rope_tensor* q, const jacap_rope_tensor* k, void* stream) {
   if (rope == nullptr || positions == nullptr || position_strides == nullptr || (q == nullptr && k == nullptr))
     return JACAP_ERR_INVALID_ARG;
-  if ((dtype != JACAP_F32 && dtype != JACAP_BF16) || num_seqs < 0 || tokens < 0 || (inverse != 0 && inverse != 1))
+  if ((dtype != JACAP_F32 && dtype != JACAP_BF16) || num_seqs < 0 || tokens < 0 || (int64_t)num_seqs * tokens > INT32_MAX - 4 || (inverse != 0 && inverse != 1))
     return JACAP_ERR_INVALID_ARG;
   if (rope->head_dim != D) return JACAP_ERR_UNSUPPORTED;
   if (rope->rot_dim < 2 || rope->rot_dim > D || rope->rot_dim % 2 != 0 || rope->turns == nullptr ||
@@ -212,7 +218,7 @@ jacap_status jacap_attend(const jacap_layout* layout, const jacap_attention* att
     a.vds[i] = attn->k_draft != nullptr ? attn->draft_strides[4 + i] : 0;
   }
   for (int i = 0; i < 3; ++i) a.ls[i] = attn->lse_strides[i];
-  a.scale = attn->scale;
+  a.scale2 = (float)((double)attn->scale * 1.4426950408889634 * (bf ? 1.0 + TRUNCATION : 1.0));
   a.prows = attend_part_rows(dm.G * dm.window);
   a.tdiv = dm.window > 1 ? 0xffffffffu / (uint32_t)dm.window + 1u : 0u;
   a.chunk = p.chunk, a.nsplit = p.nsplit, a.nrb = p.nrb, a.max_seqlen = layout->max_seqlen;
@@ -276,8 +282,10 @@ jacap_status jacap_weigh(const jacap_layout* layout, const jacap_weighing* how, 
   a.given = how->lse_given;
   a.before = before;
   a.weights = weights;
-  a.scale = how->scale;
+  a.scale2 = (float)((double)how->scale * 1.4426950408889634 * (bf ? 1.0 + TRUNCATION : 1.0));
+  a.tdiv = dm.window > 1 ? 0xffffffffu / (uint32_t)dm.window + 1u : 0u;
   a.stat = (float2*)(b + c.stat);
+  a.norm = (float2*)(b + c.norm);
   const cudaStream_t s = (cudaStream_t)stream;
   const TraceRange trace("jacap/weigh");
   if ((st = map_cuda(launch_plan(dm, w, layout->cu_seqlens, s, how->lengths))) != JACAP_OK) return st;

@@ -113,12 +113,14 @@ cudaError_t launch_fused(const CUtensorMap& vmap, const Dims& dm, const Ws& ws, 
 // (dtype 1 = bf16, 0 = float32) are also copied into k_out and v_out, as
 // launch_compact does (and the kept tokens' weights wt into wt_out, unless null).
 // With kio: the holes of kio, vio (and pos, wt) are filled in place, as
-// launch_compact_inplace does without preserve_order.
+// launch_compact_inplace does without preserve_order. With sinks >= 0 (and k) the
+// scores are attention weights, and the first `sinks` and last `recent` tokens stay.
 cudaError_t launch_select(const Dims& dm, const Ws& ws, const int32_t* cu, const float* scores, int budget,
                           int32_t* idx, int32_t* kept, int max_seqlen, cudaStream_t st, int dtype = 1,
                           const void* k = nullptr, const void* v = nullptr, void* k_out = nullptr,
                           void* v_out = nullptr, void* kio = nullptr, void* vio = nullptr, int32_t* pos = nullptr,
-                          const WeightRef& wt = WeightRef{}, float* wt_out = nullptr);
+                          const WeightRef& wt = WeightRef{}, float* wt_out = nullptr, int sinks = -1,
+                          int recent = -1);
 // Selection keys from attention weights: +inf for the first `sinks` and the last
 // `recent` tokens of every unit.
 cudaError_t launch_protect(const Dims& dm, const Ws& ws, const int32_t* cu, const WeightRef& weights,
@@ -180,7 +182,7 @@ struct AttendArgs {
   const uint64_t* tree;       // [S][window] masks, or null: a chain
   int64_t os[4], kds[4], vds[4];  // strides of o and of the drafted K and V: request, layer, head, token
   int64_t ls[3];              // of lse: request, layer, head
-  float scale;
+  float scale2;               // scale log2 e, recentred for the tensor cores' truncation
   int chunk, nsplit, nrb, max_seqlen;  // tokens per split (bf16: at least), splits of the longest request, row blocks
   int places;                 // CTAs that the SMs hold at a time (bf16)
   int prows;                  // rows of a block of the splits' sums (attend_part_rows)
@@ -206,7 +208,9 @@ struct WeighArgs {
   int given;               // 1: lse is an input
   const float* before;     // earlier weights, or null
   float* weights;          // [L*Hkv][Ntot]
-  float scale;
+  float scale2;            // scale log2 e, recentred for the tensor cores' truncation
+  uint32_t tdiv;           // 2^32 / window, rounded up (window > 1)
+  float2* norm;            // [L*Hkv][S][row blocks][128] a row's (maximum, sum) over all its request's tokens
   float2* stat;            // [L*Hkv][c_cap][2][row blocks][128] (maximum, sum) of a run (float32: a chunk)
 };
 constexpr int WEIGH_ROWS_MAX = 512;  // query rows per KV head

@@ -169,7 +169,7 @@ __device__ __forceinline__ void at_put(const Dims& dm, const AttendArgs& a, cons
     *(float4*)o = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
   if (lane == 0 && a.lse != nullptr)
     a.lse[x.s * a.ls[0] + x.l * a.ls[1] + (x.g * dm.G + h) * a.ls[2] + t] =
-        z == 0.f ? -INFINITY : m * a.scale + logf(z);
+        z == 0.f ? -INFINITY : m * (a.scale2 * 0.6931471805599453f) + logf(z);
 }
 
 // Few rows in few splits (bf16) are joined by the CTA that finishes the unit's last split; the others by a
@@ -185,7 +185,7 @@ template <typename T, int W, int NR>
 __device__ __forceinline__ void at_join(const Dims& dm, const AttendArgs& a, const AtUnit& x, int r0, int part, float4* s_o,
                                         float* s_z) {
   const int R = dm.G * dm.window, lane = threadIdx.x & 31, rl = lane % NR;
-  const float scale2 = a.scale * 1.4426950408889634f;
+  const float scale2 = a.scale2;
   const bool on = r0 < R && x.nsp > 1;
   float m = -INFINITY, z = 0.f;  // of row r0 + rl
   float4 s[NR];
@@ -564,7 +564,7 @@ __global__ void __launch_bounds__(AtCfg<NB>::THREADS, 3 - NB)
     uint8_t* stage = qs + 32768 * blk;
     const int rep = y / ROWS;  // the copy (uniform in a warp)
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-    const float scale2 = a.scale * 1.4426950408889634f, lazy = AT_LAZY / scale2;
+    const float scale2 = a.scale2, lazy = AT_LAZY / scale2;
     uint32_t it = 0, n = 1;  // tiles, loads (of V)
     bool ok = true;
     AtUnit x;
@@ -702,7 +702,7 @@ __global__ void __launch_bounds__(AtCfg<NB>::THREADS, 3 - NB)
           o = (__nv_bfloat16*)a.o + x.s * a.os[0] + x.l * a.os[1] + (int64_t)(x.g * dm.G + h) * a.os[2] + t * a.os[3];
           if (a.lse != nullptr)
             a.lse[x.s * a.ls[0] + x.l * a.ls[1] + (x.g * dm.G + h) * a.ls[2] + t] =
-                z == 0.f ? -INFINITY : m * a.scale + logf(z);
+                z == 0.f ? -INFINITY : m * (a.scale2 * 0.6931471805599453f) + logf(z);
         }
         if (nrow > 0) {
 #pragma unroll 1
@@ -767,7 +767,7 @@ __global__ void __launch_bounds__(AtCfg<NB>::THREADS, 3 - NB)
             o[j] = (__nv_bfloat16*)a.o + x.s * a.os[0] + x.l * a.os[1] + (int64_t)(x.g * dm.G + h) * a.os[2] + t * a.os[3];
             if (warp == 2 && a.lse != nullptr)
               a.lse[x.s * a.ls[0] + x.l * a.ls[1] + (x.g * dm.G + h) * a.ls[2] + t] =
-                  zr[j] == 0.f ? -INFINITY : mr[j] * a.scale + logf(zr[j]);
+                  zr[j] == 0.f ? -INFINITY : mr[j] * (a.scale2 * 0.6931471805599453f) + logf(zr[j]);
           }
         }
         float f = share(make_float2(m, z), mr[y % ROWS / 32]);
@@ -903,7 +903,7 @@ __global__ void __launch_bounds__(AF_THREADS, 1)
     }
   }
   cp_async_commit();
-  const float scale2 = a.scale * 1.4426950408889634f, lazy = AT_LAZY / scale2;
+  const float scale2 = a.scale2, lazy = AT_LAZY / scale2;
   const int tok = lane >> 2, kq = lane & 3;
   float m[RB], z[RB];       // z: this lane's token's share
   float4 acc[RB];           // channels 4 lane .. + 3

@@ -16,6 +16,8 @@
 // token) and four rows each are in flight at a time. 16-byte loads where the rows'
 // addresses and strides allow them and no pair is split by a piece's end; otherwise a
 // thread takes a pair of single elements.
+#include <type_traits>
+
 #include "jacap_dev.cuh"
 #include "jacap_internal.h"
 
@@ -65,65 +67,77 @@ __global__ void __launch_bounds__(RP_THREADS) rope_kernel(const __grid_constant_
   pdl_wait();
   __shared__ float2 cs[RP_TB][D / 2];
   const int tid = threadIdx.x, half = a.rot / 2;
-  const int64_t tok0 = (int64_t)blockIdx.x * tb, ntok = (int64_t)a.seqs * a.tokens;
-  const int nt = (int)(ntok - tok0 < tb ? ntok - tok0 : tb);
-  for (int e = tid; e < nt * half; e += RP_THREADS) {
-    const int t = e / half, i = e - t * half;
-    const int64_t tok = tok0 + t;
-    const int64_t p = a.pos[tok / a.tokens * a.ps[0] + tok % a.tokens * a.ps[1]];
-    const uint64_t turn = (uint64_t)p * a.turns[i];
-    const uint32_t quarter = (uint32_t)((turn + (1ull << 61)) >> 62);  // 0 .. 3, 4 wraps to 0
-    const int64_t rest = (int64_t)(turn - ((uint64_t)quarter << 62));  // in [-2^61, 2^61)
-    float s, c;
-    sincospif((float)rest * 1.0842021724855044e-19f, &s, &c);  // 2^-63: rest in half turns
-    if (quarter & 1) {
-      const float x = c;
-      c = -s;
-      s = x;
-    }
-    if (quarter & 2) c = -c, s = -s;
-    cs[t][i] = make_float2(a.amplitude * c, a.inverse ? -a.amplitude * s : a.amplitude * s);
-  }
-  __syncthreads();
+  const int tok0 = blockIdx.x * tb, ntok = a.seqs * a.tokens;  // (fewer than 2^31)
+  const int nt = ntok - tok0 < tb ? ntok - tok0 : tb;
+  const int first_s = tok0 / a.tokens, first_j = tok0 - first_s * a.tokens;
   const int item = tid & ((1 << lgs) - 1), rpb = RP_THREADS >> lgs;
   const int heads = a.q.heads + a.k.heads;
   const int pairs = VEC ? (a.interleaved ? a.rot / V : half / V) : half;
   const int rest = VEC ? (D - a.rot) / V : D - a.rot;
-  int t = 0, h = tid >> lgs;
-  while (h >= heads) h -= heads, ++t;
-  while (t < nt) {
-    const T* src[RP_UNROLL];
-    T* dst[RP_UNROLL];
-    int tk[RP_UNROLL];
-    bool on[RP_UNROLL];
+  int t = 0, h = tid >> lgs, rs = first_s, rj = first_j;  // the row: token t of the block, its request and number
+  auto settle = [&]() {
+    while (h >= heads) {
+      h -= heads;
+      ++t;
+      if (++rj == a.tokens) rj = 0, ++rs;
+    }
+  };
+  settle();
+  const bool two = VEC && !a.interleaved && item < pairs;  // (a, b) are half a rotation apart
+  const int c0 = VEC ? (item < pairs ? item * V : a.rot + (item - pairs) * V)
+                     : (item < pairs ? (a.interleaved ? 2 * item : item) : a.rot + item - pairs);
+  const int c1 = VEC ? c0 + half : (a.interleaved ? c0 + 1 : c0 + half);
+  const bool second = VEC ? two : item < pairs;
+  using P = typename std::conditional<VEC, uint4, T>::type;  // a piece
+  P va[RP_UNROLL], vb[RP_UNROLL];
+  T* dst[RP_UNROLL];  // null: no row
+  int tk[RP_UNROLL];
+  auto load = [&]() {  // the next rows
 #pragma unroll
     for (int u = 0; u < RP_UNROLL; ++u) {
-      on[u] = t < nt;
-      tk[u] = on[u] ? t : 0;
-      const bool isq = h < a.q.heads;
-      const RopeTensor& x = isq ? a.q : a.k;
-      const int64_t tok = tok0 + tk[u], s = tok / a.tokens, j = tok - s * a.tokens;
-      const int hh = on[u] ? (isq ? h : h - a.q.heads) : 0;
-      src[u] = (const T*)x.x + s * x.xs[0] + j * x.xs[1] + hh * x.xs[2];
-      dst[u] = (T*)x.y + s * x.ys[0] + j * x.ys[1] + hh * x.ys[2];
-      on[u] = on[u] && (item < pairs || (item < pairs + rest && (const void*)src[u] != (const void*)dst[u]));
-      h += rpb;
-      while (h >= heads) h -= heads, ++t;
-    }
-    if constexpr (VEC) {
-      uint4 va[RP_UNROLL], vb[RP_UNROLL];
-      const bool two = !a.interleaved && item < pairs;  // (a, b) are half a rotation apart
-      const int c0 = item < pairs ? item * V : a.rot + (item - pairs) * V;
-#pragma unroll
-      for (int u = 0; u < RP_UNROLL; ++u) {
-        if (on[u]) {
-          va[u] = *(const uint4*)(src[u] + c0);
-          if (two) vb[u] = *(const uint4*)(src[u] + c0 + half);
+      dst[u] = nullptr;
+      tk[u] = t;
+      if (t < nt) {
+        const bool isq = h < a.q.heads;
+        const RopeTensor& x = isq ? a.q : a.k;
+        const int hh = isq ? h : h - a.q.heads;
+        const T* src = (const T*)x.x + rs * x.xs[0] + rj * x.xs[1] + hh * x.xs[2];
+        T* to = (T*)x.y + rs * x.ys[0] + rj * x.ys[1] + hh * x.ys[2];
+        if (item < pairs || (item < pairs + rest && (const void*)src != (const void*)to)) {
+          dst[u] = to;
+          va[u] = *(const P*)(src + c0);
+          if (second) vb[u] = *(const P*)(src + c1);
         }
       }
+      h += rpb;
+      settle();
+    }
+  };
+  load();  // under way while the angles are worked out
+  for (int e = tid; e < nt * half; e += RP_THREADS) {
+    const int t = e / half, i = e - t * half;
+    int s = first_s, j = first_j + t;
+    while (j >= a.tokens) j -= a.tokens, ++s;
+    const int64_t p = a.pos[s * a.ps[0] + j * a.ps[1]];
+    const uint64_t turn = (uint64_t)p * a.turns[i];
+    const uint32_t quarter = (uint32_t)((turn + (1ull << 61)) >> 62);  // 0 .. 3, 4 wraps to 0
+    const int64_t left = (int64_t)(turn - ((uint64_t)quarter << 62));  // in [-2^61, 2^61)
+    float sn, c;
+    sincospif((float)left * 1.0842021724855044e-19f, &sn, &c);  // 2^-63: left in half turns
+    if (quarter & 1) {
+      const float x = c;
+      c = -sn;
+      sn = x;
+    }
+    if (quarter & 2) c = -c, sn = -sn;
+    cs[t][i] = make_float2(a.amplitude * c, a.inverse ? -a.amplitude * sn : a.amplitude * sn);
+  }
+  __syncthreads();
+  for (bool more = true; more;) {
 #pragma unroll
-      for (int u = 0; u < RP_UNROLL; ++u) {
-        if (!on[u]) continue;
+    for (int u = 0; u < RP_UNROLL; ++u) {
+      if (dst[u] == nullptr) continue;
+      if constexpr (VEC) {
         if (item < pairs) {
           float x[V], y[V];
           rp_unpack<T>(va[u], x);
@@ -134,7 +148,7 @@ __global__ void __launch_bounds__(RP_THREADS) rope_kernel(const __grid_constant_
               const float2 r = rp_turn(x[i], y[i], cs[tk[u]][c0 + i]);
               x[i] = r.x, y[i] = r.y;
             }
-            *(uint4*)(dst[u] + c0 + half) = rp_pack<T>(y);
+            *(uint4*)(dst[u] + c1) = rp_pack<T>(y);
           } else {
 #pragma unroll
             for (int i = 0; i < V; i += 2) {
@@ -142,34 +156,19 @@ __global__ void __launch_bounds__(RP_THREADS) rope_kernel(const __grid_constant_
               x[i] = r.x, x[i + 1] = r.y;
             }
           }
-          *(uint4*)(dst[u] + c0) = rp_pack<T>(x);
-        } else {
-          *(uint4*)(dst[u] + c0) = va[u];
+          va[u] = rp_pack<T>(x);
         }
-      }
-    } else {
-      const int i0 = item < pairs ? (a.interleaved ? 2 * item : item) : a.rot + item - pairs;
-      const int i1 = a.interleaved ? i0 + 1 : i0 + half;
-      T xa[RP_UNROLL], xb[RP_UNROLL];
-#pragma unroll
-      for (int u = 0; u < RP_UNROLL; ++u) {
-        if (on[u]) {
-          xa[u] = src[u][i0];
-          if (item < pairs) xb[u] = src[u][i1];
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < RP_UNROLL; ++u) {
-        if (!on[u]) continue;
-        if (item < pairs) {
-          const float2 r = rp_turn(rp_load<T>(&xa[u]), rp_load<T>(&xb[u]), cs[tk[u]][item]);
-          rp_store(dst[u] + i0, r.x);
-          rp_store(dst[u] + i1, r.y);
-        } else {
-          dst[u][i0] = xa[u];
-        }
+        *(uint4*)(dst[u] + c0) = va[u];
+      } else if (item < pairs) {
+        const float2 r = rp_turn(rp_load<T>(&va[u]), rp_load<T>(&vb[u]), cs[tk[u]][item]);
+        rp_store(dst[u] + c0, r.x);
+        rp_store(dst[u] + c1, r.y);
+      } else {
+        dst[u][c0] = va[u];
       }
     }
+    more = t < nt;
+    if (more) load();
   }
 }
 
@@ -179,6 +178,7 @@ cudaError_t launch_rope(const RopeArgs& a, int dtype, bool vec, int sms, cudaStr
   int lgs = 0;
   while ((1 << lgs) < items) ++lgs;
   const int64_t ntok = (int64_t)a.seqs * a.tokens;
+  if (ntok > INT32_MAX - RP_TB) return cudaErrorInvalidValue;
   // a token per block until that fills the SMs with eight blocks each
   const int tb = ntok >= (int64_t)sms * 8 * RP_TB ? RP_TB : 1;
   const int64_t blocks = (ntok + tb - 1) / tb;

@@ -78,14 +78,21 @@ struct SeSmem {
 // sl * NT KPT + 32 KPT w + 32 j + lane (coalesced; all loads in flight at
 // once). KPT keys per lane (4 .. 32) is chosen from the longest request, so a
 // short cache does not carry empty register slots through every pass.
-template <int KPT, int NT>
+// PROT: only the keys of [lo, hi) take part (0 elsewhere); they are weights, and `bad`
+// collects whether one of them is negative or not finite.
+template <int KPT, int NT, bool PROT>
 __device__ __forceinline__ void load_slab(const uint32_t* key, int n, int sl, int warp, int lane,
-                                          uint32_t (&kr)[KPT]) {
+                                          uint32_t (&kr)[KPT], int lo, int hi, bool& bad) {
   const int base = sl * NT * KPT + warp * (32 * KPT) + lane;
 #pragma unroll
   for (int j = 0; j < KPT; ++j) {
     const int i = base + 32 * j;
     kr[j] = i < n ? __ldg(key + i) : 0u;
+    if constexpr (PROT) {
+      if (kr[j] == 0x80000000u) kr[j] = 0u;
+      bad |= kr[j] >= 0x7f800000u;
+      if (i < lo || i >= hi) kr[j] = 0u;
+    }
   }
 }
 
@@ -166,12 +173,14 @@ __device__ __forceinline__ void find_digit(SeSmem& sm, uint32_t need, int tid) {
   __syncthreads();
 }
 
-template <int KPT, typename E, int MODE, int NT>
+// PROT: the scores are attention weights, and the first `sinks` and the last `recent` tokens
+// are kept whatever theirs are: the others compete for the rest of the budget.
+template <int KPT, typename E, int MODE, int NT, bool PROT>
 __global__ void __launch_bounds__(NT, 1024 / NT)
     select_kernel(Dims dm, Ws ws, const int32_t* __restrict__ cu, const float* __restrict__ scores, int B,
                   int32_t* __restrict__ idx, int32_t* __restrict__ kept, const E* __restrict__ k,
                   const E* __restrict__ v, E* __restrict__ k_out, E* __restrict__ v_out, E* kio, E* vio,
-                  int32_t* pos, int parts, WeightRef wt, float* wt_out) {
+                  int32_t* pos, int parts, WeightRef wt, float* wt_out, int sinks, int recent) {
   constexpr bool GATHER = MODE == 1;
   pdl_wait();
   constexpr int SLAB = NT * KPT;  // warp w holds positions 32 KPT w .. + 32 KPT - 1 of a slab
@@ -184,7 +193,8 @@ __global__ void __launch_bounds__(NT, 1024 / NT)
   const int64_t end = cu[s + 1];
   if (tid == 0) {
     // (not a bit that another CTA of this launch may have set)
-    sm.skip = (*((volatile uint32_t*)ws.status) & ~(uint32_t)ST_SELECT) != 0u ? 1 : 0;
+    constexpr uint32_t mine = ST_SELECT | (PROT ? ST_NONFINITE : 0u);
+    sm.skip = (*((volatile uint32_t*)ws.status) & ~mine) != 0u ? 1 : 0;
     sm.max = 0;
   }
   for (int b = tid; b < SE_BINS; b += NT) sm.hist[b] = 0;
@@ -200,7 +210,16 @@ __global__ void __launch_bounds__(NT, 1024 / NT)
   const int n = valid ? (int)(end - start) : 0;
   if (!valid && tid == 0) flag(ws, ST_SELECT);  // malformed cu_seqlens: no reads
   if (plane == 0 && tid == 0) kept[s] = min(n, B);
+  const uint32_t* key = (const uint32_t*)(scores + (int64_t)plane * dm.Ntot + start);
+  bool bad = false;
   if (n <= B) {
+    if constexpr (PROT) {
+      for (int i = tid; i < n; i += NT) bad |= (key[i] & ~(key[i] == 0x80000000u ? 0x80000000u : 0u)) >= 0x7f800000u;
+      if (__syncthreads_or(bad)) {
+        if (tid == 0) flag(ws, ST_NONFINITE);
+        return;
+      }
+    }
     for (int r = tid; r < B; r += NT) out[r] = r < n ? r : -1;
     if constexpr (GATHER) {
       __syncthreads();
@@ -209,17 +228,21 @@ __global__ void __launch_bounds__(NT, 1024 / NT)
     }
     return;
   }
-  const uint32_t* key = (const uint32_t*)(scores + (int64_t)plane * dm.Ntot + start);
+  // the tokens that compete, and for how many places
+  const int lo = PROT ? sinks : 0, hi = PROT ? n - recent : n;
+  const uint32_t Bn = (uint32_t)(PROT ? B - (n - (hi - lo)) : B);
+  auto in = [&](int i) { return PROT ? i >= lo && i < hi : i < n; };
   const int nslab = (n + SLAB - 1) / SLAB;
   uint32_t kr[KPT];
   TRC_INC(4);
-  load_slab<KPT, NT>(key, n, 0, warp, lane, kr);  // one slab: register-resident for all steps
+  load_slab<KPT, NT, PROT>(key, n, 0, warp, lane, kr, lo, hi, bad);  // one slab: register-resident for all steps
   uint32_t m = 0;
 #pragma unroll
   for (int j = 0; j < KPT; ++j) m = max(m, kr[j]);
   if (nslab > 1) {  // of the other slabs, every 16th line
 #pragma unroll 8
-    for (int i = SLAB + warp * 512 + lane; i < n; i += NW * 512) m = max(m, __ldg(key + i));
+    for (int i = SLAB + warp * 512 + lane; i < n; i += NW * 512)
+      if (!PROT || in(i)) m = max(m, __ldg(key + i));
   }
   m = __reduce_max_sync(0xffffffffu, m);
   if (lane == 0) atomicMax(&sm.max, m);
@@ -232,118 +255,130 @@ __global__ void __launch_bounds__(NT, 1024 / NT)
   const int top = (int)((min(sm.max, 0xffffffffu - up) + up) >> 16) | 31;
 #pragma unroll 1
   for (int sl = 0; sl < nslab; ++sl) {
-    if (sl > 0) load_slab<KPT, NT>(key, n, sl, warp, lane, kr);
+    if (sl > 0) load_slab<KPT, NT, PROT>(key, n, sl, warp, lane, kr, lo, hi, bad);
     const int base = sl * SLAB + warp * (32 * KPT) + lane;
 #pragma unroll
     for (int j = 0; j < KPT; ++j) {
       const int d = max(top - (int)(kr[j] >> 16), -1) + 1;
-      if (base + 32 * j < n && d <= SE_FINE) atomicAdd(&sm.hist[d], 1u);
+      if (in(base + 32 * j) && d <= SE_FINE) atomicAdd(&sm.hist[d], 1u);
     }
   }
-  __syncthreads();
-  find_digit<NT>(sm, (uint32_t)B, tid);
-  // hist[digit(key)] over the keys (SE_BINS: not counted)
-  auto histogram = [&](auto digit) {
-    __syncthreads();  // everyone has read digit, need and count
-    for (int b = tid; b < SE_BINS; b += NT) sm.hist[b] = 0;
+  if constexpr (PROT) {
+    if (__syncthreads_or(bad)) {  // this unit is left as it is
+      if (tid == 0) flag(ws, ST_NONFINITE);
+      return;
+    }
+  } else {
     __syncthreads();
+  }
+  uint32_t T = 0xffffffffu;  // the key of the last token kept (none: above all)
+  if (!PROT || Bn > 0) {
+    find_digit<NT>(sm, Bn, tid);
+    // hist[digit(key)] over the keys (SE_BINS: not counted)
+    auto histogram = [&](auto digit) {
+      __syncthreads();  // everyone has read digit, need and count
+      for (int b = tid; b < SE_BINS; b += NT) sm.hist[b] = 0;
+      __syncthreads();
 #pragma unroll 1
-    for (int sl = 0; sl < nslab; ++sl) {
-      if (nslab > 1) load_slab<KPT, NT>(key, n, sl, warp, lane, kr);
-      const int base = sl * SLAB + warp * (32 * KPT) + lane;
+      for (int sl = 0; sl < nslab; ++sl) {
+        if (nslab > 1) load_slab<KPT, NT, PROT>(key, n, sl, warp, lane, kr, lo, hi, bad);
+        const int base = sl * SLAB + warp * (32 * KPT) + lane;
 #pragma unroll
-      for (int j = 0; j < KPT; ++j) {
-        const uint32_t d = digit(kr[j]);
-        if (base + 32 * j < n && d < SE_BINS) atomicAdd(&sm.hist[d], 1u);
-      }
-    }
-    __syncthreads();
-  };
-  // The sm.need-th of the sm.count keys with (key >> bits) == pre is the B-th.
-  uint32_t pre = (uint32_t)(top + 1 - (int)sm.digit);
-  int bits = 16;
-  if (sm.digit == 0 || sm.digit == SE_BINS) {
-    // above or below the fine bins: the keys there by their first 11 bits; 0, which
-    // many scores may be, has a bin of its own
-    const bool over = sm.digit == 0;
-    const uint32_t high = over ? 2047u : 2046u, left = over ? (uint32_t)B : sm.need;
-    histogram([&](uint32_t x) {
-      const int f = top - (int)(x >> 16);
-      return (over ? f < 0 : f >= SE_FINE) ? (x == 0u ? 2047u : high - (x >> 21)) : (uint32_t)SE_BINS;
-    });
-    find_digit<NT>(sm, left, tid);
-    bits = sm.digit == 2047u ? 0 : 21;
-    pre = sm.digit == 2047u ? 0u : high - sm.digit;
-  }
-#pragma unroll 1
-  while (sm.count > SE_CAND && bits > 0) {  // too many to rank: the next digit of those keys
-    const int w = min(bits, 11);
-    const uint32_t dmask = (1u << w) - 1u, left = sm.need;
-    histogram([&](uint32_t x) { return x >> bits == pre ? ~(x >> (bits - w)) & dmask : (uint32_t)SE_BINS; });
-    find_digit<NT>(sm, left, tid);
-    pre = (pre << w) | (~sm.digit & dmask);
-    bits -= w;
-  }
-  const int cand = (int)sm.count;
-  // The B-th key T; the first sm.need of the keys == T are kept.
-  uint32_t T = pre;  // (cand > SE_CAND: the whole key)
-  if (cand <= SE_CAND) {
-    __syncthreads();  // everyone has read the bin's count
-    if (tid == 0) sm.count = 0;
-    if (tid < 4 && cand + tid < SE_CAND) {  // ranked four at a time: the last ones count for nobody
-      sm.ckey[cand + tid] = 0u;
-      sm.cidx[cand + tid] = INT32_MAX;
-    }
-    __syncthreads();
-#pragma unroll 1
-    for (int sl = 0; sl < nslab; ++sl) {
-      if (nslab > 1) load_slab<KPT, NT>(key, n, sl, warp, lane, kr);
-      const int base = sl * SLAB + warp * (32 * KPT) + lane;
-#pragma unroll
-      for (int j = 0; j < KPT; ++j) {
-        if (base + 32 * j < n && kr[j] >> bits == pre) {
-          const uint32_t at = atomicAdd(&sm.count, 1u);
-          sm.ckey[at] = kr[j];
-          sm.cidx[at] = base + 32 * j;
+        for (int j = 0; j < KPT; ++j) {
+          const uint32_t d = digit(kr[j]);
+          if (in(base + 32 * j) && d < SE_BINS) atomicAdd(&sm.hist[d], 1u);
         }
       }
+      __syncthreads();
+    };
+    // The sm.need-th of the sm.count keys with (key >> bits) == pre is the B-th.
+    uint32_t pre = (uint32_t)(top + 1 - (int)sm.digit);
+    int bits = 16;
+    if (sm.digit == 0 || sm.digit == SE_BINS) {
+      // above or below the fine bins: the keys there by their first 11 bits; 0, which
+      // many scores may be, has a bin of its own
+      const bool over = sm.digit == 0;
+      const uint32_t high = over ? 2047u : 2046u, left = over ? Bn : sm.need;
+      histogram([&](uint32_t x) {
+        const int f = top - (int)(x >> 16);
+        return (over ? f < 0 : f >= SE_FINE) ? (x == 0u ? 2047u : high - (x >> 21)) : (uint32_t)SE_BINS;
+      });
+      find_digit<NT>(sm, left, tid);
+      bits = sm.digit == 2047u ? 0 : 21;
+      pre = sm.digit == 2047u ? 0u : high - sm.digit;
     }
-    const uint32_t need = sm.need;
-    __syncthreads();
-    for (int c = tid; c < cand; c += NT) {  // the token of rank need - 1 in the bin
-      const uint32_t x = sm.ckey[c];
-      const int32_t i = sm.cidx[c];
-      uint32_t more = 0, same = 0;  // keys above this one, equal ones before it
-      for (int e = 0; e < cand; e += 4) {
-        const uint4 y = *(const uint4*)&sm.ckey[e];
-        const int4 p = *(const int4*)&sm.cidx[e];
-        more += (y.x > x) + (y.y > x) + (y.z > x) + (y.w > x);
-        same += (y.x == x && p.x < i) + (y.y == x && p.y < i) + (y.z == x && p.z < i) + (y.w == x && p.w < i);
-      }
-      if (more + same == need - 1) {
-        sm.T = x;
-        sm.need = same + 1;
-      }
+#pragma unroll 1
+    while (sm.count > SE_CAND && bits > 0) {  // too many to rank: the next digit of those keys
+      const int w = min(bits, 11);
+      const uint32_t dmask = (1u << w) - 1u, left = sm.need;
+      histogram([&](uint32_t x) { return x >> bits == pre ? ~(x >> (bits - w)) & dmask : (uint32_t)SE_BINS; });
+      find_digit<NT>(sm, left, tid);
+      pre = (pre << w) | (~sm.digit & dmask);
+      bits -= w;
     }
-    __syncthreads();
-    T = sm.T;
+    const int cand = (int)sm.count;
+    // The B-th key T; the first sm.need of the keys == T are kept.
+    T = pre;  // (cand > SE_CAND: the whole key)
+    if (cand <= SE_CAND) {
+      __syncthreads();  // everyone has read the bin's count
+      if (tid == 0) sm.count = 0;
+      if (tid < 4 && cand + tid < SE_CAND) {  // ranked four at a time: the last ones count for nobody
+        sm.ckey[cand + tid] = 0u;
+        sm.cidx[cand + tid] = INT32_MAX;
+      }
+      __syncthreads();
+#pragma unroll 1
+      for (int sl = 0; sl < nslab; ++sl) {
+        if (nslab > 1) load_slab<KPT, NT, PROT>(key, n, sl, warp, lane, kr, lo, hi, bad);
+        const int base = sl * SLAB + warp * (32 * KPT) + lane;
+#pragma unroll
+        for (int j = 0; j < KPT; ++j) {
+          if (in(base + 32 * j) && kr[j] >> bits == pre) {
+            const uint32_t at = atomicAdd(&sm.count, 1u);
+            sm.ckey[at] = kr[j];
+            sm.cidx[at] = base + 32 * j;
+          }
+        }
+      }
+      const uint32_t need = sm.need;
+      __syncthreads();
+      for (int c = tid; c < cand; c += NT) {  // the token of rank need - 1 in the bin
+        const uint32_t x = sm.ckey[c];
+        const int32_t i = sm.cidx[c];
+        uint32_t more = 0, same = 0;  // keys above this one, equal ones before it
+        for (int e = 0; e < cand; e += 4) {
+          const uint4 y = *(const uint4*)&sm.ckey[e];
+          const int4 p = *(const int4*)&sm.cidx[e];
+          more += (y.x > x) + (y.y > x) + (y.z > x) + (y.w > x);
+          same += (y.x == x && p.x < i) + (y.y == x && p.y < i) + (y.z == x && p.z < i) + (y.w == x && p.w < i);
+        }
+        if (more + same == need - 1) {
+          sm.T = x;
+          sm.need = same + 1;
+        }
+      }
+      __syncthreads();
+      T = sm.T;
+    }
   }
   TRC_ADD(1, tr_r);
   TRC_T(tr_e);
   // ---- emission, slab by slab ----
-  const uint32_t nties = sm.need;
+  const uint32_t nties = PROT && Bn == 0 ? 0u : sm.need;
   uint32_t run = 0, eq_run = 0;  // keys > T and == T before this slab
 #pragma unroll 1
   for (int sl = 0; sl < nslab; ++sl) {
-    if (nslab > 1) load_slab<KPT, NT>(key, n, sl, warp, lane, kr);
+    if (nslab > 1) load_slab<KPT, NT, PROT>(key, n, sl, warp, lane, kr, lo, hi, bad);
     const int first = sl * SLAB + warp * (32 * KPT);
     // the tokens > T and == T of slot `lane` (keys past the request's end are 0 in kr:
     // not above T, and the last of any ties)
     uint32_t mine = 0, eq = 0;
 #pragma unroll
     for (int j = 0; j < KPT; ++j) {
-      const uint32_t b = __ballot_sync(0xffffffffu, kr[j] > T);
-      const uint32_t e = __ballot_sync(0xffffffffu, kr[j] == T);
+      const int i = first + 32 * j + lane;
+      const bool stays = PROT && i < n && !in(i);
+      const uint32_t b = __ballot_sync(0xffffffffu, kr[j] > T || stays);
+      const uint32_t e = __ballot_sync(0xffffffffu, kr[j] == T && (!PROT || in(i)));
       if (lane == j) {
         mine = b;
         eq = e;
@@ -478,37 +513,46 @@ template <int KPT, int NT>
 static cudaError_t launch_select_kpt(const Dims& dm, const Ws& ws, const int32_t* cu, const float* scores, int budget,
                                      int32_t* idx, int32_t* kept, int dtype, const void* k, const void* v,
                                      void* k_out, void* v_out, void* kio, void* vio, int32_t* pos, int grid, int parts,
-                                     const WeightRef& wt, float* wt_out, cudaStream_t st) {
+                                     const WeightRef& wt, float* wt_out, int sinks, int recent, cudaStream_t st) {
   using bf = __nv_bfloat16;
+  if (sinks >= 0) {  // attention weights, with tokens that stay
+    if (dtype == 1)
+      return launch_pdl(dm.pdl != 0, select_kernel<KPT, bf, 1, NT, true>, grid, NT, 0, st, dm, ws, cu, scores, budget,
+                        idx, kept, (const bf*)k, (const bf*)v, (bf*)k_out, (bf*)v_out, (bf*)nullptr, (bf*)nullptr,
+                        (int32_t*)nullptr, parts, wt, wt_out, sinks, recent);
+    return launch_pdl(dm.pdl != 0, select_kernel<KPT, float, 1, NT, true>, grid, NT, 0, st, dm, ws, cu, scores, budget,
+                      idx, kept, (const float*)k, (const float*)v, (float*)k_out, (float*)v_out, (float*)nullptr,
+                      (float*)nullptr, (int32_t*)nullptr, parts, wt, wt_out, sinks, recent);
+  }
   if (kio != nullptr) {  // hole filling in place
     if (dtype == 1)
-      return launch_pdl(dm.pdl != 0, select_kernel<KPT, bf, 2, NT>, grid, NT, 0, st, dm, ws, cu, scores, budget,
+      return launch_pdl(dm.pdl != 0, select_kernel<KPT, bf, 2, NT, false>, grid, NT, 0, st, dm, ws, cu, scores, budget,
                         idx, kept, (const bf*)nullptr, (const bf*)nullptr, (bf*)nullptr, (bf*)nullptr, (bf*)kio,
-                        (bf*)vio, pos, parts, wt, (float*)nullptr);
-    return launch_pdl(dm.pdl != 0, select_kernel<KPT, float, 2, NT>, grid, NT, 0, st, dm, ws, cu, scores, budget,
+                        (bf*)vio, pos, parts, wt, (float*)nullptr, 0, 0);
+    return launch_pdl(dm.pdl != 0, select_kernel<KPT, float, 2, NT, false>, grid, NT, 0, st, dm, ws, cu, scores, budget,
                       idx, kept, (const float*)nullptr, (const float*)nullptr, (float*)nullptr, (float*)nullptr,
-                      (float*)kio, (float*)vio, pos, parts, wt, (float*)nullptr);
+                      (float*)kio, (float*)vio, pos, parts, wt, (float*)nullptr, 0, 0);
   }
   if (k == nullptr)
-    return launch_pdl(dm.pdl != 0, select_kernel<KPT, bf, 0, NT>, grid, NT, 0, st, dm, ws, cu, scores, budget,
+    return launch_pdl(dm.pdl != 0, select_kernel<KPT, bf, 0, NT, false>, grid, NT, 0, st, dm, ws, cu, scores, budget,
                       idx, kept, (const bf*)nullptr, (const bf*)nullptr, (bf*)nullptr, (bf*)nullptr, (bf*)nullptr,
-                      (bf*)nullptr, (int32_t*)nullptr, parts, WeightRef{}, (float*)nullptr);
+                      (bf*)nullptr, (int32_t*)nullptr, parts, WeightRef{}, (float*)nullptr, 0, 0);
   if (dtype == 1)
-    return launch_pdl(dm.pdl != 0, select_kernel<KPT, bf, 1, NT>, grid, NT, 0, st, dm, ws, cu, scores, budget,
+    return launch_pdl(dm.pdl != 0, select_kernel<KPT, bf, 1, NT, false>, grid, NT, 0, st, dm, ws, cu, scores, budget,
                       idx, kept, (const bf*)k, (const bf*)v, (bf*)k_out, (bf*)v_out, (bf*)nullptr, (bf*)nullptr,
-                      (int32_t*)nullptr, parts, wt, wt_out);
-  return launch_pdl(dm.pdl != 0, select_kernel<KPT, float, 1, NT>, grid, NT, 0, st, dm, ws, cu, scores, budget,
+                      (int32_t*)nullptr, parts, wt, wt_out, 0, 0);
+  return launch_pdl(dm.pdl != 0, select_kernel<KPT, float, 1, NT, false>, grid, NT, 0, st, dm, ws, cu, scores, budget,
                     idx, kept, (const float*)k, (const float*)v, (float*)k_out, (float*)v_out, (float*)nullptr,
-                    (float*)nullptr, (int32_t*)nullptr, parts, wt, wt_out);
+                    (float*)nullptr, (int32_t*)nullptr, parts, wt, wt_out, 0, 0);
 }
 
 cudaError_t launch_select(const Dims& dm, const Ws& ws, const int32_t* cu, const float* scores, int budget,
                           int32_t* idx, int32_t* kept, int max_seqlen, cudaStream_t st, int dtype,
                           const void* k, const void* v, void* k_out, void* v_out, void* kio, void* vio,
-                          int32_t* pos, const WeightRef& wt, float* wt_out) {
+                          int32_t* pos, const WeightRef& wt, float* wt_out, int sinks, int recent) {
 #define JACAP_SELECT(KPT, NT)                                                                                   \
   JACAP_TRY((launch_select_kpt<KPT, NT>(dm, ws, cu, scores, budget, idx, kept, dtype, k, v, k_out, v_out, kio, vio, \
-                                        pos, grid, parts, wt, wt_out, st)))
+                                        pos, grid, parts, wt, wt_out, sinks, recent, st)))
   // More units than SMs: CTAs of 256 threads (four per SM) while they hold the
   // longest request in one slab, of 512 (two per SM) beyond that (256 units of 32768
   // tokens: 42 us, 46 with 1024 threads; of 131072: 119 and 120). Otherwise CTAs of

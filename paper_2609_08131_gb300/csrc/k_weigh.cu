@@ -26,9 +26,9 @@ namespace jacap {
 constexpr int WG_TILE_BYTES = TILE * D * 2;
 constexpr int WG_BOX = WG_TILE_BYTES / 2;
 constexpr int WG_IMG = 128 * D * 2;
-constexpr int WG_BUILD0 = 2, WG_READ0 = 4, WG_THREADS = 32 * 12;
+constexpr int WG_BUILD0 = 2, WG_READ0 = 4;
 constexpr float WG_LAZY = 8.f;  // log2 of how far a logit may pass the running maximum
-constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float wg_ex2(float x) {
   float y;
@@ -51,6 +51,10 @@ __device__ __forceinline__ WgReq wg_req(const Dims& dm, const WeighArgs& a, cons
   x.p0 = x.n - x.ql;
   return x;
 }
+// The head of row r (r / window, exact for r below 2^16).
+__device__ __forceinline__ int wg_head(const Dims& dm, const WeighArgs& a, int r) {
+  return dm.window == 1 ? r : (int)__umulhi((uint32_t)r, a.tdiv);
+}
 // Which query the j-th of request s is (-1: none).
 __device__ __forceinline__ int wg_query(const Dims& dm, const WeighArgs& a, const WgReq& x, int s, int j) {
   if (j >= x.ql) return -1;
@@ -58,36 +62,62 @@ __device__ __forceinline__ int wg_query(const Dims& dm, const WeighArgs& a, cons
   return q >= 0 && q < dm.window ? q : -1;
 }
 
-template <int NRB>
+// What a row's weights take: weight = f 2^(l scale2 - b), with b = M scale2 and f = 1 / Z for the row's maximum
+// and sum (b is the rounded product that the sum's terms used too, so that its rounding cancels), or, where lse is
+// given, b = lse log2 e and f = 1. No query, or nothing seen: b = inf and f = 0.
+__device__ __forceinline__ float2 wg_const(const Dims& dm, const WeighArgs& a, const Item& item, int l, int g, int h,
+                                           int qi, int r, int rows) {
+  const float2 none = make_float2(INFINITY, 0.f);
+  if (qi < 0) return none;
+  if (a.given) {
+    const float e = a.lse[(((int64_t)item.seq * dm.L + l) * dm.Hq + g * dm.G + h) * dm.window + qi];
+    return e == -INFINITY ? none : make_float2(e * LOG2E, 1.f);
+  }
+  const float2 mz = a.norm[((int64_t)item.plane * dm.S + item.seq) * rows + r];
+  return mz.y == 0.f ? none : make_float2(mz.x * a.scale2, 1.f / mz.y);
+}
+
+// Adds a (maximum, sum of exponentials from it) pair to (m, z). Nothing seen is (-inf, 0); NaN only, (-inf, NaN).
+__device__ __forceinline__ void wg_merge(float& m, float& z, float2 x, float scale2) {
+  if (x.x == -INFINITY && x.y == 0.f) return;
+  const float top = fmaxf(m, x.x);
+  z = (m == -INFINITY ? z : z * wg_ex2((m - top) * scale2)) + (x.x == -INFINITY ? x.y : x.y * wg_ex2((x.x - top) * scale2));
+  m = top;
+}
+
+template <int NRB, bool SUM>
 struct WgCfg {
+  // groups of four read warps, that take the tiles in turn. The weights of one row block have four (an
+  // accumulator each: with two, the latency of a group's chain through a tile bounds the pass, 114 us for
+  // 64 planes of 32768 tokens of which K takes 79).
+  static constexpr int GROUPS = SUM && NRB == 1 ? 4 : 2;
+  static constexpr int THREADS = 32 * (WG_READ0 + 4 * GROUPS);
   static constexpr int IMGS = NRB == 1 ? 2 : 1;  // images: the next run's is built ahead
   static constexpr int STAGES = NRB <= 2 ? 4 : (NRB == 3 ? 3 : 2);
   static constexpr int ROWS = NRB * 128;
-  static constexpr size_t SMEM = 1024 + (size_t)STAGES * WG_TILE_BYTES + (size_t)IMGS * NRB * WG_IMG + IMGS * ROWS * 8;
+  static constexpr size_t SMEM = 1024 + (size_t)STAGES * WG_TILE_BYTES + (size_t)IMGS * NRB * WG_IMG + IMGS * ROWS * 12;
 };
 
 template <int NRB, bool SUM>
-__global__ void __launch_bounds__(WG_THREADS, 1)
+__global__ void __launch_bounds__(WgCfg<NRB, SUM>::THREADS, 1)
     weigh_bf16_kernel(const __grid_constant__ CUtensorMap kmap, Dims dm, Ws ws, const __grid_constant__ WeighArgs a,
                       const int32_t* __restrict__ cu) {
-  using C = WgCfg<NRB>;
+  using C = WgCfg<NRB, SUM>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   uint8_t* tiles = smem;
   uint8_t* img = tiles + C::STAGES * WG_TILE_BYTES;            // [IMGS][NRB][128 rows]
-  float* cst = (float*)(img + C::IMGS * NRB * WG_IMG);         // [IMGS][ROWS] lse_r log2 e (+inf: no weight)
+  float2* cst = (float2*)(img + C::IMGS * NRB * WG_IMG);       // [IMGS][ROWS] (b, f): weight = f 2^(l scale2 - b)
   int* jrow = (int*)(cst + C::IMGS * C::ROWS);                 // [IMGS][ROWS] j of the row
   __shared__ uint64_t full[C::STAGES], empty[C::STAGES], accfull[4], accempty[4], imgready[2], imgfree[2];
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort, s_skip;
   __shared__ RunQueue s_queue;
-  pdl_wait();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int R = dm.G * dm.window;
   if (tid == 0) {
     s_abort = 0;
-    s_skip = status_failed(ws) ? 1 : 0;
-    run_queue_init(&s_queue, 1 + 2 + 8);  // MMA, build and read warps
+    run_queue_init(&s_queue, 1 + 2 + 4 * C::GROUPS);  // MMA, build and read warps
     for (int i = 0; i < C::STAGES; ++i) {
       mbar_init(smem_u32(&full[i]), 1);
       mbar_init(smem_u32(&empty[i]), 1);
@@ -98,21 +128,27 @@ __global__ void __launch_bounds__(WG_THREADS, 1)
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&imgready[i]), 2);
-      mbar_init(smem_u32(&imgfree[i]), 1 + (SUM ? 8 : 0));  // the MMAs, and the readers of the constants
+      mbar_init(smem_u32(&imgfree[i]), 1 + (SUM ? 4 * C::GROUPS : 0));  // the MMAs, and the readers of the constants
     }
     fence_mbar_init();
+    prefetch_tmap(&kmap);
   }
-  __syncthreads();
-  if (s_skip) return;
   if (warp == 1) {
     tmem_alloc(smem_u32(&s_tmem), 512);
     tmem_relinquish();
   }
+  pdl_wait();  // nothing before it touches global memory
+  if (tid == 0) s_skip = status_failed(ws) ? 1 : 0;
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = s_tmem;
   volatile int* abort = &s_abort;
+  if (s_skip) {
+    __syncthreads();
+    if (warp == 1) tmem_dealloc(tmem, 512);
+    return;
+  }
 
   if (warp == 0) {
     // ------------------------------------------------ TMA producer --------
@@ -204,19 +240,14 @@ __global__ void __launch_bounds__(WG_THREADS, 1)
       const __nv_bfloat16* q = (const __nv_bfloat16*)a.q + item.seq * dm.q_ss + l * dm.q_sl + (int64_t)g * dm.G * dm.q_sh;
       uint8_t* im = img + p * NRB * WG_IMG;
       for (int r0 = 32 * b; r0 < C::ROWS; r0 += 64) {  // 32 rows at a time, one per lane to look up
-        const int r = r0 + lane, h = r / dm.window, j = r - h * dm.window;
+        const int r = r0 + lane, h = wg_head(dm, a, r), j = r - h * dm.window;
         const int qi = r < R ? wg_query(dm, a, x, item.seq, j) : -1;
         const int64_t off = qi >= 0 ? h * dm.q_sh + qi * dm.q_sp : 0;
         if constexpr (SUM) {
-          float c = INFINITY;
-          if (qi >= 0) {
-            const float e = a.lse[(((int64_t)item.seq * dm.L + l) * dm.Hq + g * dm.G + h) * dm.window + qi];
-            c = e == -INFINITY ? INFINITY : e * LOG2E;
-          }
-          cst[p * C::ROWS + r] = c;
+          cst[p * C::ROWS + r] = wg_const(dm, a, item, l, g, h, qi, r, C::ROWS);
           jrow[p * C::ROWS + r] = j;
         }
-#pragma unroll 4
+#pragma unroll 8
         for (int k = 0; k < 16; ++k) {  // lanes 0-15 and 16-31: the 16-byte pieces of two rows
           const int rr = 2 * k + (lane >> 4), c = lane & 15;
           const int64_t o = __shfl_sync(0xffffffffu, off, rr);
@@ -236,7 +267,7 @@ __global__ void __launch_bounds__(WG_THREADS, 1)
     // ------------------------------------------------ readers -------------
     const int quarter = warp & 3, grp = (warp - WG_READ0) >> 2, y = quarter * 32 + lane;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-    const float scale2 = a.scale * LOG2E, lazy = WG_LAZY / scale2;
+    const float scale2 = a.scale2, lazy = WG_LAZY / scale2;
     uint32_t it = 0, nrun = 0;
     bool cont = false, bad = false;
     int c0 = 0;
@@ -252,7 +283,7 @@ __global__ void __launch_bounds__(WG_THREADS, 1)
 #pragma unroll
         for (int rb = 0; rb < NRB; ++rb) {
           m[rb] = -INFINITY, z[rb] = 0.f, zc[rb] = 0.f;
-          lim[rb] = x.p0 + (rb * 128 + y) % dm.window;
+          lim[rb] = x.p0 + (rb * 128 + y) - wg_head(dm, a, rb * 128 + y) * dm.window;
         }
         // (the constants are the builders' work: the tile's accumulators follow them)
         if (SUM && !mbar_wait(smem_u32(&imgready[p]), (nrun / C::IMGS) & 1, ws, abort)) goto done;
@@ -267,34 +298,31 @@ __global__ void __launch_bounds__(WG_THREADS, 1)
           const uint32_t e = it * NRB + rb;
           // which group: its accumulators are its own, so that no barrier's phase passes it by
           // (four row blocks use all accumulators for every tile: one group sums them all)
-          if ((SUM && NRB == 4 ? 0 : (int)((SUM ? it : e) & 1)) != grp) continue;
+          if ((SUM && NRB == 4 ? 0 : (int)((SUM ? it : e) % C::GROUPS)) != grp) continue;
           const int slot = e & 3;
           if (!mbar_wait(smem_u32(&accfull[slot]), (e >> 2) & 1, ws, abort)) goto done;
           tc_fence_after();
           const uint32_t acc = tmem + 128 * slot + lanes;
           if constexpr (SUM) {
             const int left = R - rb * 128, cols = left < 128 ? (left + 31) & ~31 : 128;
-            const float* cp = cst + p * C::ROWS + rb * 128;
+            const float2* cp = cst + p * C::ROWS + rb * 128;
             const int* jp = jrow + p * C::ROWS + rb * 128;
             float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
             for (int c = 0; c < cols; c += 32) {
               float v[32];
               tmem_ld32(acc + c, v);
-#pragma unroll
-              for (int q = 0; q < 32; q += 4) {
-                const float4 k4 = *(const float4*)(cp + c + q);
-                v[q] = wg_ex2(fmaf(v[q], scale2, -k4.x));
-                v[q + 1] = wg_ex2(fmaf(v[q + 1], scale2, -k4.y));
-                v[q + 2] = wg_ex2(fmaf(v[q + 2], scale2, -k4.z));
-                v[q + 3] = wg_ex2(fmaf(v[q + 3], scale2, -k4.w));
-              }
               if (late) {
                 const int need = rel + y - x.p0;  // queries j >= need see token rel + y
 #pragma unroll
-                for (int q = 0; q < 32; ++q) v[q] = jp[c + q] >= need ? v[q] : 0.f;
+                for (int q = 0; q < 32; ++q) v[q] = jp[c + q] >= need ? v[q] : -INFINITY;
               }
 #pragma unroll
-              for (int q = 0; q < 32; ++q) s[q & 3] += v[q];
+              for (int q = 0; q < 32; q += 2) {
+                const float4 k = *(const float4*)(cp + c + q);  // (no weight: f = 0)
+                s[q & 3] = fmaf(wg_ex2(fmaf(v[q], scale2, -k.x)), k.y, s[q & 3]);
+                s[(q + 1) & 3] = fmaf(wg_ex2(fmaf(v[q + 1], scale2, -k.z)), k.w, s[(q + 1) & 3]);
+              }
             }
             w += (s[0] + s[1]) + (s[2] + s[3]);
           } else {
@@ -333,7 +361,7 @@ __global__ void __launch_bounds__(WG_THREADS, 1)
           __syncwarp();
           if (lane == 0) mbar_arrive(smem_u32(&accempty[slot]));
         }
-        if (SUM && (NRB == 4 ? 0 : (int)(it & 1)) == grp && y < nv) {
+        if (SUM && (NRB == 4 ? 0 : (int)(it % C::GROUPS)) == grp && y < nv) {
           const int64_t at = (int64_t)item.plane * dm.Ntot + t + y;
           if (a.before != nullptr && rel + y < x.p0) w += a.before[at];
           bad |= !isfinite(w);
@@ -385,35 +413,28 @@ __global__ void __launch_bounds__(WM_THREADS)
     for (int i = part; i < count; i += 8) {
       const int c = by_chunk ? first + i : ws.runs[list * dm.c_cap + first + i].w;
       for (int g = 0; g < groups; ++g) {
-        const float2 x = a.stat[(((int64_t)plane * dm.c_cap + c) * groups + g) * rows + r];
-        if (x.x == -INFINITY && x.y == 0.f) continue;
-        const float top = fmaxf(m, x.x);
-        const float k = a.scale * LOG2E;
-        z = (m == -INFINITY ? z : z * exp2f((m - top) * k)) + (x.x == -INFINITY ? x.y : x.y * exp2f((x.x - top) * k));
-        m = top;
+        wg_merge(m, z, a.stat[(((int64_t)plane * dm.c_cap + c) * groups + g) * rows + r], a.scale2);
       }
     }
   sm[part][lane] = m;
   sz[part][lane] = z;
   __syncthreads();
   if (part != 0 || r >= R) return;
-  const float k = a.scale * LOG2E;
-  float top = -INFINITY, sum = 0.f;
-  for (int p = 0; p < 8; ++p) top = fmaxf(top, sm[p][lane]);
-  for (int p = 0; p < 8; ++p)
-    sum += sm[p][lane] == -INFINITY ? sz[p][lane] : sz[p][lane] * exp2f((sm[p][lane] - top) * k);
+  m = -INFINITY, z = 0.f;
+  for (int p = 0; p < 8; ++p) wg_merge(m, z, make_float2(sm[p][lane], sz[p][lane]), a.scale2);
+  a.norm[(int64_t)u * rows + r] = make_float2(m, z);
   const int h = r / dm.window, j = r - h * dm.window;
   const WgReq x = wg_req(dm, a, cu, s);
   const int q = wg_query(dm, a, x, s, j);
   if (q >= 0)
     a.lse[(((int64_t)s * dm.L + plane / dm.Hkv) * dm.Hq + plane % dm.Hkv * dm.G + h) * dm.window + q] =
-        sum == 0.f ? -INFINITY : top * a.scale + logf(sum);
+        z == 0.f ? -INFINITY : fmaf(m == -INFINITY ? 0.f : m, a.scale2 * LN2, logf(z));
 }
 
 // ------------------------------------------------------------- float32 ----
 // A block takes a chunk at a time, 64 rows of its unit at a time, in tiles of 64 tokens.
 constexpr int WF_THREADS = 256, WF_TOK = 64, WF_LD = D + 4, WF_ROWS = 64;
-constexpr size_t WF_SMEM = ((size_t)WF_ROWS * D + 2 * WF_TOK * WF_LD + 8 * WF_TOK + 2 * WF_ROWS) * 4;
+constexpr size_t WF_SMEM = ((size_t)WF_ROWS * D + 2 * WF_TOK * WF_LD + 8 * WF_TOK + 3 * WF_ROWS) * 4;
 
 template <bool SUM>
 __global__ void __launch_bounds__(WF_THREADS, 2)
@@ -422,13 +443,13 @@ __global__ void __launch_bounds__(WF_THREADS, 2)
   float* qs = sf;                        // [64][D]
   float* ks = qs + WF_ROWS * D;          // [2][64][LD]
   float* red = ks + 2 * WF_TOK * WF_LD;  // [8 warps][64]
-  float* cst = red + 8 * WF_TOK;         // [64]
+  float2* cst = (float2*)(red + 8 * WF_TOK);  // [64] (b, f)
   int* jrow = (int*)(cst + WF_ROWS);     // [64]
   pdl_wait();
   if (__syncthreads_or(status_failed(ws) ? 1 : 0)) return;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int R = dm.G * dm.window;
-  const float scale2 = a.scale * LOG2E, lazy = WG_LAZY / scale2;
+  const float scale2 = a.scale2, lazy = WG_LAZY / scale2;
   bool bad = false;
   Item item;
   for (ItemStream is(dm, ws, blockIdx.x, gridDim.x); is.next(item);) {
@@ -449,19 +470,12 @@ __global__ void __launch_bounds__(WF_THREADS, 2)
       __syncthreads();  // the rows and the tiles before are read
       fetch(item.t0, 0);
       for (int e = tid; e < WF_ROWS * 32; e += WF_THREADS) {
-        const int r = r0 + (e >> 5), c = (e & 31) * 4, h = r / dm.window, j = r - h * dm.window;
+        const int r = r0 + (e >> 5), c = (e & 31) * 4, h = wg_head(dm, a, r), j = r - h * dm.window;
         const int qi = r < R ? wg_query(dm, a, x, item.seq, j) : -1;
         cp_async16(smem_u32(qs + (e >> 5) * D + c), q + (qi >= 0 ? h * dm.q_sh + qi * dm.q_sp : 0) + c, qi >= 0);
         if (c == 0) {
           jrow[e >> 5] = j;
-          if constexpr (SUM) {
-            float k = INFINITY;
-            if (qi >= 0) {
-              const float v = a.lse[(((int64_t)item.seq * dm.L + l) * dm.Hq + g * dm.G + h) * dm.window + qi];
-              k = v == -INFINITY ? INFINITY : v * LOG2E;
-            }
-            cst[e >> 5] = k;
-          }
+          if constexpr (SUM) cst[e >> 5] = wg_const(dm, a, item, l, g, h, qi, r, rows);
         }
       }
       cp_async_commit();
@@ -498,8 +512,8 @@ __global__ void __launch_bounds__(WF_THREADS, 2)
             const int tok = lane + 32 * b;
             const bool see = t + tok < item.t1 && rel + tok <= x.p0 + j;
             if constexpr (SUM) {
-              const float p = wg_ex2(fmaf(s[i][b], scale2, -cst[8 * warp + i]));
-              w[b] += see ? p : 0.f;
+              const float2 k = cst[8 * warp + i];
+              if (see) w[b] = fmaf(wg_ex2(fmaf(s[i][b], scale2, -k.x)), k.y, w[b]);
             } else if (see) {
               const float v = s[i][b];
               if (v > m[i] + lazy) {
@@ -553,10 +567,10 @@ __global__ void __launch_bounds__(WF_THREADS, 2)
 template <int NRB, bool SUM>
 static cudaError_t launch_bf16(const CUtensorMap& kmap, const Dims& dm, const Ws& ws, const WeighArgs& a,
                                const int32_t* cu, int grid, cudaStream_t st) {
-  constexpr size_t smem = WgCfg<NRB>::SMEM;
+  constexpr size_t smem = WgCfg<NRB, SUM>::SMEM;
   static_assert(smem + 1024 <= 232448, "shared memory");  // 1024: the static variables
   JACAP_TRY(cudaFuncSetAttribute(weigh_bf16_kernel<NRB, SUM>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-  return launch_pdl(true, weigh_bf16_kernel<NRB, SUM>, grid, WG_THREADS, smem, st, kmap, dm, ws, a, cu);
+  return launch_pdl(true, weigh_bf16_kernel<NRB, SUM>, grid, WgCfg<NRB, SUM>::THREADS, smem, st, kmap, dm, ws, a, cu);
 }
 template <bool SUM>
 static cudaError_t launch_pass(const CUtensorMap& kmap, const Dims& dm, const Ws& ws, int dtype, const WeighArgs& a,
