@@ -317,9 +317,8 @@ def jacap_evict_host(layout, params, budget, group_layers, q_win_host, k_host, v
 
 
 def jacap_rotate(rope, dtype, num_seqs, tokens, positions, position_strides, inverse, q, k, stream) -> int:
-    """``q``, ``k``: ``jacap_rope_tensor`` or None; ``position_strides``: two element strides."""
-    return lib().jacap_rotate(ctypes.byref(rope), dtype, num_seqs, tokens, positions,
-                              (ctypes.c_int64 * 2)(*position_strides), int(inverse),
+    """``q``, ``k``: ``jacap_rope_tensor`` or None; ``position_strides``: two element strides (a ``c_int64`` array)."""
+    return lib().jacap_rotate(ctypes.byref(rope), dtype, num_seqs, tokens, positions, position_strides, int(inverse),
                               None if q is None else ctypes.byref(q), None if k is None else ctypes.byref(k), stream)
 
 

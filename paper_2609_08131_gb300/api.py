@@ -131,15 +131,15 @@ def _tensor(name, t, device, dtype, shape, contiguous=False):
     """Checks a tensor argument; its address. None passes, as None."""
     if t is None:
         return None
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device or t.shape != shape:
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.shape != shape or t.device != device:
         raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on {device}")
     if t.requires_grad and torch.is_grad_enabled():
         raise ValueError(f"{name} requires a gradient, which this call does not give")
-    if contiguous:
-        if not t.is_contiguous():
+    if not t.is_contiguous():
+        if contiguous:
             raise ValueError(f"{name} must be contiguous")
-    elif t.stride(-1) != 1:
-        raise ValueError(f"the last axis of {name} must be contiguous")
+        if t.stride(-1) != 1:
+            raise ValueError(f"the last axis of {name} must be contiguous")
     return t.data_ptr()
 
 
@@ -209,44 +209,66 @@ class Rope:
         self._c = jacap_rope()
         self._c.head_dim, self._c.rot_dim, self._c.interleaved = 128, self.rot_dim, int(self.interleaved)
         self._c.amplitude, self._c.turns = self.amplitude, self.turns.data_ptr()
+        self._calls = {}  # arguments of calls by the tensors' shapes and strides (not their addresses)
 
     def apply(self, q, k, positions, inverse: bool = False, inplace: bool = False, stream=None):
         """q, k: [..., heads, 128] (one of them may be None) with one or two leading axes,
         of any strides but the last axis' (float32 or bfloat16); positions: int32 of the
         leading axes' shape. Returns the turned (q, k): new tensors, or the same ones
         with ``inplace``. ``inverse`` turns back (and is the gradient)."""
+        key = (None if q is None else (q.dtype, q.shape, q.stride()), None if k is None else (k.dtype, k.shape, k.stride()),
+               positions.shape, positions.stride(), inplace)
+        call = self._calls.get(key)
+        if call is None:
+            call = self._arguments(q, k, positions, inplace)
+            if len(self._calls) >= 64:
+                self._calls.clear()
+            self._calls[key] = call
+        S, T, qa, ka, ps, dtype = call
+        dev = self.device
+        for t in (q, k, positions):
+            if t is not None and (t.device != dev or t.requires_grad and torch.is_grad_enabled()):
+                raise ValueError(f"the tensors must be on {dev} and require no gradient, which this call does not give")
+        if positions.dtype is not torch.int32:
+            raise ValueError("positions must be int32")
+
+        def turn(st):
+            qy = ky = None
+            if q is not None:
+                qy = q if inplace else torch.empty_like(q)
+                qa.x, qa.y = q.data_ptr(), qy.data_ptr()
+            if k is not None:
+                ky = k if inplace else torch.empty_like(k)
+                ka.x, ka.y = k.data_ptr(), ky.data_ptr()
+            if S and T:
+                _check(jacap_rotate(self._c, dtype, S, T, positions.data_ptr(), ps, inverse, qa, ka, st), "jacap_rotate")
+            return qy, ky
+
+        return _enqueue(dev, stream, turn)
+
+    def _arguments(self, q, k, positions, inplace):
+        """Checks shapes and strides; the call's arguments but for the addresses."""
         first = q if q is not None else k
         if first is None:
             raise ValueError("q or k must be given")
-        lead, dtype, dev = first.shape[:-2], first.dtype, self.device
+        lead, dtype = first.shape[:-2], first.dtype
         if len(lead) not in (1, 2) or dtype not in (torch.float32, torch.bfloat16):
             raise ValueError("q and k must be float32 or bfloat16 [tokens, heads, 128] or [requests, tokens, heads, 128]")
-        for name, t in (("q", q), ("k", k)):
-            if t is not None:
-                _tensor(name, t, dev, dtype, (*lead, t.shape[-2], 128))
-                if t.shape[-2] < 1:
-                    raise ValueError(f"{name} has no heads")
-        if (not isinstance(positions, torch.Tensor) or positions.dtype != torch.int32 or positions.device != dev
-                or positions.shape != lead):
-            raise ValueError(f"positions must be an int32 tensor of shape {tuple(lead)} on {dev}")
-        two = len(lead) == 2
+        if positions.shape != lead:
+            raise ValueError(f"positions must be of shape {tuple(lead)}")
+        two, args = len(lead) == 2, [None, None]
+        for i, (name, t) in enumerate((("q", q), ("k", k))):
+            if t is None:
+                continue
+            if t.dtype is not dtype or t.dim() != len(lead) + 2 or t.shape != (*lead, t.shape[-2], 128) or t.stride(-1) != 1:
+                raise ValueError(f"{name} must be {dtype} {(*lead, 'heads', 128)} with a contiguous last axis")
+            if t.shape[-2] < 1:
+                raise ValueError(f"{name} has no heads")
+            xs, ys = t.stride()[:-1], (t if inplace else torch.empty_like(t, device="meta")).stride()[:-1]
+            args[i] = jacap_rope_tensor(0, 0, t.shape[-2], xs if two else (0, *xs), ys if two else (0, *ys))
         S, T = lead if two else (1, lead[0])
-
-        def turn(st):
-            out, args = [None, None], [None, None]
-            for i, t in enumerate((q, k)):
-                if t is not None:
-                    y = out[i] = t if inplace else torch.empty_like(t)
-                    xs, ys = t.stride()[:-1], y.stride()[:-1]
-                    args[i] = jacap_rope_tensor(t.data_ptr(), y.data_ptr(), t.shape[-2], xs if two else (0, *xs),
-                                                ys if two else (0, *ys))
-            if S and T:
-                _check(jacap_rotate(self._c, JACAP_BF16 if dtype == torch.bfloat16 else JACAP_F32, S, T,
-                                    positions.data_ptr(), positions.stride() if two else (0, positions.stride(0)),
-                                    inverse, args[0], args[1], st), "jacap_rotate")
-            return out[0], out[1]
-
-        return _enqueue(dev, stream, turn)
+        ps = (ctypes.c_int64 * 2)(*(positions.stride() if two else (0, positions.stride(0))))
+        return S, T, args[0], args[1], ps, JACAP_BF16 if dtype == torch.bfloat16 else JACAP_F32
 
 
 def tree_masks(parents):

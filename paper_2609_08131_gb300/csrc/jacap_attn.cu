@@ -39,13 +39,14 @@ AttendPlan attend_plan(const jacap_layout* L) {
   p.nrb = (rows + block - 1) / block;
   const int64_t units = (int64_t)L->num_seqs * L->num_layers * L->num_kv_heads, ctas = units * p.nrb;
   const int64_t most = L->max_seqlen;
-  // float32: about three CTAs per SM where that leaves each 1024 tokens or more, at least one
+  // float32: about three CTAs for each place on an SM where that leaves 1024 tokens or more, about one
   // where it leaves 128. bf16: the least that a split may have (the kernel chooses from the live
   // lengths). A split's sums, written and read by the join, stay an eighth of its K and V.
   int64_t chunk = 256;
   if (!bf) {
-    chunk = most * ctas / (3 * 152);
-    if (chunk < 1024) chunk = std::min<int64_t>(1024, (most * ctas + 151) / 152);
+    const int64_t places = rows <= 8 ? 3 * 152 : 152;
+    chunk = most * ctas / (3 * places);
+    if (chunk < 1024) chunk = std::min<int64_t>(1024, (most * ctas + places - 1) / places);
     chunk = std::max<int64_t>(chunk, 128);
   }
   chunk = std::max<int64_t>(chunk, std::min(rows, block) * 16);

@@ -29,7 +29,7 @@
 // a drafted value that is not finite is zeroed too and added to the rows that see it.
 //
 // float32: CUDA cores, as the tensor cores would round the inputs. A warp takes 8 of a
-// tile's 64 tokens for all rows of the CTA (8 or 32), four lanes to a token's dot
+// tile's tokens for all rows of the CTA (8 or 32), four lanes to a token's dot
 // products, and keeps a maximum, sums and accumulators of its own, so that tiles need no
 // barrier but the one that says they have landed; the warps are joined at the end.
 #include "jacap_dev.cuh"
@@ -842,20 +842,26 @@ __global__ void __launch_bounds__(AtCfg<NB>::THREADS, 3 - NB)
 }
 
 // ------------------------------------------------------------- float32 ----
-constexpr int AF_THREADS = 256, AF_WARPS = 8, AF_TOK = 64, AF_LDK = D + 4;
-constexpr int AF_KF = AF_TOK * AF_LDK, AF_VF = AF_TOK * D;  // floats per stage
+// Up to 8 rows: K and V's arrival bounds it; four warps and tiles of 32 tokens, three CTAs per SM. More: the
+// multiply-adds; eight warps, 32 rows, one CTA.
 template <int RB>
-constexpr size_t af_smem() {
-  return (size_t)(RB * D + 2 * (AF_KF + AF_VF) + AF_WARPS * 8 * RB + 2 * AF_WARPS * RB) * 4;
-}
+struct AfCfg {
+  static constexpr int WARPS = RB == 8 ? 4 : 8, THREADS = 32 * WARPS, TOK = 8 * WARPS, LDK = D + 4;
+  static constexpr int KF = TOK * LDK, VF = TOK * D;  // floats per stage
+  static constexpr size_t SMEM = (size_t)(RB * D + 2 * (KF + VF) + WARPS * 8 * RB + 2 * WARPS * RB) * 4;
+  static constexpr int PER_SM = RB == 8 ? 3 : 1;
+};
 
 template <int RB>
-__global__ void __launch_bounds__(AF_THREADS, 1)
+__global__ void __launch_bounds__(AfCfg<RB>::THREADS, AfCfg<RB>::PER_SM)
     attend_f32_kernel(Dims dm, const __grid_constant__ AttendArgs a, const int32_t* __restrict__ cu) {
+  using C = AfCfg<RB>;
+  constexpr int AF_THREADS = C::THREADS, AF_WARPS = C::WARPS, AF_TOK = C::TOK, AF_LDK = C::LDK;
+  constexpr int AF_KF = C::KF, AF_VF = C::VF;
   extern __shared__ __align__(16) float sf[];
   float* qs = sf;                          // [RB][D]
-  float* ks = qs + RB * D;                 // [2][64][LDK]
-  float* vs = ks + 2 * AF_KF;              // [2][64][D]
+  float* ks = qs + RB * D;                 // [2][TOK][LDK]
+  float* vs = ks + 2 * AF_KF;              // [2][TOK][D]
   float* ps = vs + 2 * AF_VF;              // [warp][8 tokens][RB]
   float* sm = ps + AF_WARPS * 8 * RB;      // [warp][RB] maxima, then sums
   float* sz = sm + AF_WARPS * RB;
@@ -905,11 +911,14 @@ __global__ void __launch_bounds__(AF_THREADS, 1)
   cp_async_commit();
   const float scale2 = a.scale2, lazy = AT_LAZY / scale2;
   const int tok = lane >> 2, kq = lane & 3;
-  float m[RB], z[RB];       // z: this lane's token's share
-  float4 acc[RB];           // channels 4 lane .. + 3
+  // lane r: row r's maximum (all tokens of the warp) and sum; every lane: channels 4 lane .. + 3 of all rows
+  float m = -INFINITY, z = 0.f;
+  float4 acc[RB];
 #pragma unroll
-  for (int r = 0; r < RB; ++r) m[r] = -INFINITY, z[r] = 0.f, acc[r] = make_float4(0.f, 0.f, 0.f, 0.f);
-  float* pw = ps + warp * 8 * RB;
+  for (int r = 0; r < RB; ++r) acc[r] = make_float4(0.f, 0.f, 0.f, 0.f);
+  float* pw = ps + warp * 8 * RB;  // [8 tokens][RB]
+  const int myrow = lane % RB;
+  const uint64_t mask = x.nt > x.ncache && r0 + myrow < R ? at_mask(dm, a, x, r0 + myrow - at_head(dm, a, r0 + myrow) * dm.window) : 0;
   for (int i = 0; i < x.nt; ++i) {
     if (i + 1 < x.nt) fetch(i + 1);
     cp_async_commit();
@@ -932,37 +941,41 @@ __global__ void __launch_bounds__(AF_THREADS, 1)
           s[r] = fmaf(qq.x, kk.x, fmaf(qq.y, kk.y, fmaf(qq.z, kk.z, fmaf(qq.w, kk.w, s[r]))));
         }
       }
-      bool up = false;
+      // the logits to shared memory, four rows by each lane of a token, so that lane r has row r's eight
+      __syncwarp();  // the previous tile's weights are read
 #pragma unroll
       for (int r = 0; r < RB; ++r) {
         s[r] += __shfl_xor_sync(0xffffffffu, s[r], 1);
         s[r] += __shfl_xor_sync(0xffffffffu, s[r], 2);
-        bool see = tok < left;
-        if (drafted)
-          see = r < nrow && at_mask(dm, a, x, (r0 + r) % dm.window) >> (first + 8 * warp + tok & 63) & 1 && see;
-        if (!see) s[r] = -INFINITY;
-        up |= s[r] > m[r] + lazy;
+        if ((r & 3) == kq) pw[tok * RB + r] = s[r];
       }
-      if (__any_sync(0xffffffffu, up)) {
+      __syncwarp();
+      float l[8], top = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        l[j] = pw[j * RB + myrow];
+        if (j >= left || (drafted && !(mask >> (first + 8 * warp + j & 63) & 1))) l[j] = -INFINITY;
+        top = fmaxf(top, l[j]);
+      }
+      const bool up = top > m + lazy;
+      const uint32_t who = __ballot_sync(0xffffffffu, up);
+      if (who != 0) {
+        const float f = up ? (m == -INFINITY ? 0.f : ex2((m - top) * scale2)) : 1.f;
+        if (up) m = top;
+        z *= f;
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
-          float top = s[r];
-#pragma unroll
-          for (int off = 4; off <= 16; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-          if (top > m[r] + lazy) {  // the same on every lane
-            const float f = m[r] == -INFINITY ? 0.f : ex2((m[r] - top) * scale2);
-            m[r] = top;
-            z[r] *= f;
-            acc[r].x *= f, acc[r].y *= f, acc[r].z *= f, acc[r].w *= f;
-          }
+          if (!(who >> r & 1)) continue;
+          const float fr = __shfl_sync(0xffffffffu, f, r);
+          acc[r].x *= fr, acc[r].y *= fr, acc[r].z *= fr, acc[r].w *= fr;
         }
       }
-      __syncwarp();  // the previous tile's weights are read
+      const float base = m == -INFINITY ? 0.f : m * scale2;
 #pragma unroll
-      for (int r = 0; r < RB; ++r) {
-        const float p = ex2(fmaf(s[r], scale2, m[r] == -INFINITY ? 0.f : -m[r] * scale2));
-        z[r] += p;
-        if ((r & 3) == kq) pw[tok * RB + r] = p;
+      for (int j = 0; j < 8; ++j) {
+        l[j] = ex2(fmaf(l[j], scale2, -base));
+        z += l[j];
+        if (lane < RB) pw[j * RB + lane] = l[j];
       }
       __syncwarp();
       const float* vt = vs + (i & 1) * AF_VF + 8 * warp * D + 4 * lane;
@@ -990,14 +1003,9 @@ __global__ void __launch_bounds__(AF_THREADS, 1)
   cp_async_wait<0>();
   // the warps joined: accumulators through the tiles' space
   float4* out = (float4*)ks;  // [warp][RB][32]
+  if (lane < RB) sm[warp * RB + lane] = m, sz[warp * RB + lane] = z;
 #pragma unroll
-  for (int r = 0; r < RB; ++r) {
-    float zz = z[r];
-#pragma unroll
-    for (int off = 4; off <= 16; off <<= 1) zz += __shfl_xor_sync(0xffffffffu, zz, off);
-    if (lane == 0) sm[warp * RB + r] = m[r], sz[warp * RB + r] = zz;
-    out[(warp * RB + r) * 32 + lane] = acc[r];
-  }
+  for (int r = 0; r < RB; ++r) out[(warp * RB + r) * 32 + lane] = acc[r];
   __syncthreads();
   for (int r = warp; r < nrow; r += AF_WARPS) {
     float mr = -INFINITY, zr = 0.f;
@@ -1015,7 +1023,6 @@ __global__ void __launch_bounds__(AF_THREADS, 1)
   }
 }
 
-// --------------------------------------------------------- joined splits ----
 // Joins the splits of units that have several: NR rows to W warps.
 constexpr int AJ_THREADS = 256, AJ_WARPS = AJ_THREADS / 32;
 template <typename T, int W, int NR>
@@ -1059,9 +1066,10 @@ static cudaError_t launch_bf16(const CUtensorMap* maps, const Dims& dm, const At
 }
 template <int RB>
 static cudaError_t launch_f32(const Dims& dm, const AttendArgs& a, const int32_t* cu, int grid, cudaStream_t st) {
-  static_assert(af_smem<RB>() <= 232448 - 1024, "shared memory");
-  JACAP_TRY(cudaFuncSetAttribute(attend_f32_kernel<RB>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)af_smem<RB>()));
-  return launch_pdl(true, attend_f32_kernel<RB>, grid, AF_THREADS, af_smem<RB>(), st, dm, a, cu);
+  using C = AfCfg<RB>;
+  static_assert((C::SMEM + 1024) * C::PER_SM <= 233472, "shared memory");
+  JACAP_TRY(cudaFuncSetAttribute(attend_f32_kernel<RB>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM));
+  return launch_pdl(true, attend_f32_kernel<RB>, grid, C::THREADS, C::SMEM, st, dm, a, cu);
 }
 
 int attend_row_block(int dtype, int rows) { return dtype == 1 ? (rows <= 128 ? 128 : 256) : (rows <= 8 ? 8 : 32); }

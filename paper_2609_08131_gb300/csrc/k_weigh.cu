@@ -432,19 +432,21 @@ __global__ void __launch_bounds__(WM_THREADS)
 }
 
 // ------------------------------------------------------------- float32 ----
-// A block takes a chunk at a time, 64 rows of its unit at a time, in tiles of 64 tokens.
-constexpr int WF_THREADS = 256, WF_TOK = 64, WF_LD = D + 4, WF_ROWS = 64;
-constexpr size_t WF_SMEM = ((size_t)WF_ROWS * D + 2 * WF_TOK * WF_LD + 8 * WF_TOK + 3 * WF_ROWS) * 4;
+// A block takes a chunk at a time, 32 rows (four warps) or 64 of its unit at a time, in tiles of 64 tokens.
+constexpr int WF_TOK = 64, WF_LD = D + 4;
+template <int WARPS>
+constexpr size_t wf_smem() { return ((size_t)8 * WARPS * D + 2 * WF_TOK * WF_LD + WARPS * WF_TOK + 3 * 8 * WARPS) * 4; }
 
-template <bool SUM>
-__global__ void __launch_bounds__(WF_THREADS, 2)
+template <bool SUM, int WARPS>
+__global__ void __launch_bounds__(32 * WARPS, 2)
     weigh_f32_kernel(Dims dm, Ws ws, const __grid_constant__ WeighArgs a, const int32_t* __restrict__ cu, int rows) {
+  constexpr int WF_THREADS = 32 * WARPS, WF_ROWS = 8 * WARPS;
   extern __shared__ __align__(16) float sf[];
-  float* qs = sf;                        // [64][D]
+  float* qs = sf;                        // [ROWS][D]
   float* ks = qs + WF_ROWS * D;          // [2][64][LD]
-  float* red = ks + 2 * WF_TOK * WF_LD;  // [8 warps][64]
-  float2* cst = (float2*)(red + 8 * WF_TOK);  // [64] (b, f)
-  int* jrow = (int*)(cst + WF_ROWS);     // [64]
+  float* red = ks + 2 * WF_TOK * WF_LD;  // [warp][64]
+  float2* cst = (float2*)(red + WARPS * WF_TOK);  // [ROWS] (b, f)
+  int* jrow = (int*)(cst + WF_ROWS);     // [ROWS]
   pdl_wait();
   if (__syncthreads_or(status_failed(ws) ? 1 : 0)) return;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -536,7 +538,7 @@ __global__ void __launch_bounds__(WF_THREADS, 2)
         if (SUM && tid < WF_TOK && t + tid < item.t1) {
           float v = 0.f;
 #pragma unroll
-          for (int k = 0; k < 8; ++k) v += red[k * WF_TOK + tid];
+          for (int k = 0; k < WARPS; ++k) v += red[k * WF_TOK + tid];
           const int64_t at = (int64_t)item.plane * dm.Ntot + t + tid;
           if (r0 > 0) v += a.weights[at];  // the rows before, by this thread
           else if (a.before != nullptr && rel + tid < x.p0) v += a.before[at];
@@ -572,13 +574,19 @@ static cudaError_t launch_bf16(const CUtensorMap& kmap, const Dims& dm, const Ws
   JACAP_TRY(cudaFuncSetAttribute(weigh_bf16_kernel<NRB, SUM>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
   return launch_pdl(true, weigh_bf16_kernel<NRB, SUM>, grid, WgCfg<NRB, SUM>::THREADS, smem, st, kmap, dm, ws, a, cu);
 }
+template <bool SUM, int WARPS>
+static cudaError_t launch_f32(const Dims& dm, const Ws& ws, const WeighArgs& a, const int32_t* cu, int grid, int rows,
+                              cudaStream_t st) {
+  auto kern = weigh_f32_kernel<SUM, WARPS>;
+  JACAP_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)wf_smem<WARPS>()));
+  return launch_pdl(true, kern, grid, 32 * WARPS, wf_smem<WARPS>(), st, dm, ws, a, cu, rows);
+}
 template <bool SUM>
 static cudaError_t launch_pass(const CUtensorMap& kmap, const Dims& dm, const Ws& ws, int dtype, const WeighArgs& a,
                                const int32_t* cu, int grid, int nrb, cudaStream_t st) {
-  if (dtype != 1) {
-    JACAP_TRY(cudaFuncSetAttribute(weigh_f32_kernel<SUM>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)WF_SMEM));
-    return launch_pdl(true, weigh_f32_kernel<SUM>, 2 * grid, WF_THREADS, WF_SMEM, st, dm, ws, a, cu, 128 * nrb);
-  }
+  if (dtype != 1)
+    return dm.G * dm.window <= 32 ? launch_f32<SUM, 4>(dm, ws, a, cu, 2 * grid, 128 * nrb, st)
+                                  : launch_f32<SUM, 8>(dm, ws, a, cu, 2 * grid, 128 * nrb, st);
   switch (nrb) {
     case 1: return launch_bf16<1, SUM>(kmap, dm, ws, a, cu, grid, st);
     case 2: return launch_bf16<2, SUM>(kmap, dm, ws, a, cu, grid, st);
