@@ -58,6 +58,20 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
+// Two values at once: the same arithmetic in half the issue slots.
+__device__ __forceinline__ float2 fma2(float2 x, float2 y, float2 z) {
+  float2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(*(uint64_t*)&r)
+      : "l"(*(uint64_t*)&x), "l"(*(uint64_t*)&y), "l"(*(uint64_t*)&z));
+  return r;
+}
+__device__ __forceinline__ float2 add2(float2 x, float2 y) {
+  float2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(*(uint64_t*)&r) : "l"(*(uint64_t*)&x), "l"(*(uint64_t*)&y));
+  return r;
+}
+
 __device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, int c3, int c4,
                                             uint32_t bar) {
   asm volatile(
@@ -266,7 +280,8 @@ __device__ __forceinline__ void at_bad(const Dims& dm, const AttendArgs& a, cons
 // largest one's tokens, more than that the places' mean share and half an item at the end, and each
 // `extra` tokens' time to change over to.
 // Measured, 8 units of 131011 tokens: 38 splits of 3456 tokens 88 us, 114 of 1152 103 us; 128 units of about
-// 2100: two splits 33 us, four 40 us.
+// 2100: two splits 33 us, four 40 us. 128 units of 46 to 16383 tokens: 5 to 80 rows 97 us with `extra` 300,
+// 101 to 113 with 192; 320 rows 216 us with 700, 224 with 400.
 __device__ __forceinline__ int at_chunk(const Dims& dm, const AttendArgs& a, const int32_t* cu, int lane, float extra,
                                         int* longest_out) {
   const auto tokens_of = [&](int s) {
@@ -380,7 +395,7 @@ __global__ void __launch_bounds__(AtCfg<NB>::THREADS, 3 - NB)
     // ------------------------------------------------ TMA producer --------
     const uint32_t units = (uint32_t)dm.L * dm.Hkv * dm.S;
     int longest;
-    const int chunk = at_chunk(dm, a, cu, lane, NB == 1 ? 192.f : 400.f, &longest);
+    const int chunk = at_chunk(dm, a, cu, lane, NB == 1 ? 300.f : 700.f, &longest);
     if (lane == 0) {
       const uint32_t most = longest > chunk ? (longest - 1) / chunk + 1 : 1;
       const uint32_t total = units * a.nrb * most;  // (fewer than 2^31)
@@ -634,13 +649,16 @@ __global__ void __launch_bounds__(AtCfg<NB>::THREADS, 3 - NB)
           }
         }
         const float base = m == -INFINITY ? 0.f : m * scale2;
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        const float2 by = make_float2(scale2, scale2), less = make_float2(-base, -base);
+        float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-        for (int e = 0; e < NC; ++e) {
-          v[e] = ex2(fmaf(v[e], scale2, -base));
-          sum[e & 3] += v[e];
+        for (int e = 0; e < NC; e += 2) {
+          const float2 w = fma2(make_float2(v[e], v[e + 1]), by, less);
+          v[e] = ex2(w.x), v[e + 1] = ex2(w.y);
+          sum[e >> 1 & 1] = add2(sum[e >> 1 & 1], make_float2(v[e], v[e + 1]));
         }
-        z += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        sum[0] = add2(sum[0], sum[1]);
+        z += sum[0].x + sum[0].y;
         uint32_t p[32];
 #pragma unroll
         for (int c = 0; c < 32; ++c) {

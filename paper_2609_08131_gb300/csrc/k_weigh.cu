@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(WgCfg<NRB, SUM>::THREADS, 1)
   int* jrow = (int*)(cst + C::IMGS * C::ROWS);                 // [IMGS][ROWS] j of the row
   __shared__ uint64_t full[C::STAGES], empty[C::STAGES], accfull[4], accempty[4], imgready[2], imgfree[2];
   __shared__ uint32_t s_tmem;
-  __shared__ int s_abort, s_skip;
+  __shared__ int s_abort;
   __shared__ RunQueue s_queue;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int R = dm.G * dm.window;
@@ -137,18 +137,12 @@ __global__ void __launch_bounds__(WgCfg<NRB, SUM>::THREADS, 1)
     tmem_alloc(smem_u32(&s_tmem), 512);
     tmem_relinquish();
   }
-  pdl_wait();  // nothing before it touches global memory
-  if (tid == 0) s_skip = status_failed(ws) ? 1 : 0;
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  pdl_wait();  // nothing before it touches global memory (a plan that failed has no runs)
   const uint32_t tmem = s_tmem;
   volatile int* abort = &s_abort;
-  if (s_skip) {
-    __syncthreads();
-    if (warp == 1) tmem_dealloc(tmem, 512);
-    return;
-  }
 
   if (warp == 0) {
     // ------------------------------------------------ TMA producer --------
