@@ -459,7 +459,7 @@ jacap_status jacap_rotate(const jacap_rope* rope, jacap_dtype dtype, int32_t num
  * A row that sees nothing has o = 0 and lse = -inf. What a row does not see has
  * no effect on it, NaN and infinities included.
  *
- *   scale          > 0 (1 / sqrt(128) for plain attention)
+ *   scale          1e-30 to 1e30 (1 / sqrt(128) for plain attention)
  *   lengths        device int32 [num_seqs] (cached tokens of each request, the
  *                  first ones of its range, 0 up to min(n_s, max_seqlen)), or
  *                  NULL: all n_s. Read when the kernels run: a captured graph
@@ -515,7 +515,7 @@ jacap_status jacap_attend(const jacap_layout* layout, const jacap_attention* att
  *
  * The layout is that of the cache with Q_win as for jacap_score; num_q_heads /
  * num_kv_heads times window is at most 512 (else JACAP_ERR_UNSUPPORTED).
- *   scale      > 0
+ *   scale      1e-30 to 1e30
  *   lengths    device int32 [num_seqs] or NULL, as in jacap_attend (the device
  *              reports a length outside [0, n_s] and does nothing)
  *   q_lens     device int32 [num_seqs] or NULL: queries of each request, clamped

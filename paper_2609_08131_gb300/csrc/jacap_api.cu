@@ -711,8 +711,7 @@ jacap_status check_weights(const jacap_layout* layout, const float* weights, con
   if (((uintptr_t)ws & 255u) != 0 || ws_bytes < 64) return JACAP_ERR_WORKSPACE;
   memset(w, 0, sizeof(*w));
   w->status = (uint32_t*)ws;  // all that the selection needs
-  int sms = 0;
-  return check_device(&sms);
+  return JACAP_OK;
 }
 
 }  // namespace
@@ -728,6 +727,8 @@ jacap_status jacap_select_weights(const jacap_layout* layout, const float* weigh
   if (st != JACAP_OK) return st;
   if (k_out == nullptr || v_out == nullptr || !aligned16(k_out) || !aligned16(v_out) || ((uintptr_t)weights_out & 3u) != 0)
     return JACAP_ERR_INVALID_ARG;
+  int sms = 0;
+  if ((st = check_device(&sms)) != JACAP_OK) return st;
   const cudaStream_t s = (cudaStream_t)stream;
   const TraceRange trace("jacap/select_weights");
   WeightRef wr = {const_cast<float*>(weights), (int64_t)dm.Hkv * dm.Ntot, dm.Ntot};
@@ -755,6 +756,8 @@ jacap_status jacap_evict_weights(const jacap_layout* layout, float* weights, int
   if (st != JACAP_OK) return st;
   if (preserve_order != 0 && preserve_order != 1) return JACAP_ERR_INVALID_ARG;
   if (dm.kv_sl % dm.kv_st != 0 || dm.kv_sh % dm.kv_st != 0) return JACAP_ERR_INVALID_ARG;
+  int sms = 0;
+  if ((st = check_device(&sms)) != JACAP_OK) return st;
   const WeightRef wr = {weights, dm.kv_sl / dm.kv_st, dm.kv_sh / dm.kv_st};
   const int dt = layout->dtype == JACAP_BF16 ? 1 : 0;
   const cudaStream_t s = (cudaStream_t)stream;

@@ -111,6 +111,8 @@ jacap_status check_weigh_layout(const jacap_layout* L) {
   return (int64_t)(L->num_q_heads / L->num_kv_heads) * L->window > WEIGH_ROWS_MAX ? JACAP_ERR_UNSUPPORTED : JACAP_OK;
 }
 
+// far enough from the ends of float32 for the scale times log2 e and what is divided by it
+bool scale_ok(float s) { return s >= 1e-30f && s <= 1e30f; }
 bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
 bool aligned8(const void* p) { return ((uintptr_t)p & 7u) == 0; }
 
@@ -184,7 +186,7 @@ jacap_status jacap_attend(const jacap_layout* layout, const jacap_attention* att
   if (st != JACAP_OK) return st;
   if (attn == nullptr || q == nullptr || k == nullptr || v == nullptr || o == nullptr || ws == nullptr)
     return JACAP_ERR_INVALID_ARG;
-  if (!(attn->scale > 0.f) || !isfinite(attn->scale)) return JACAP_ERR_INVALID_ARG;
+  if (!scale_ok(attn->scale)) return JACAP_ERR_INVALID_ARG;
   if ((attn->k_draft == nullptr) != (attn->v_draft == nullptr) || (attn->tree != nullptr && attn->k_draft == nullptr))
     return JACAP_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o) || !aligned4(lse) || !aligned4(attn->lengths) ||
@@ -253,8 +255,7 @@ jacap_status jacap_weigh(const jacap_layout* layout, const jacap_weighing* how, 
   if (st != JACAP_OK) return st;
   if (how == nullptr || q_win == nullptr || k == nullptr || weights == nullptr || ws == nullptr)
     return JACAP_ERR_INVALID_ARG;
-  if (!(how->scale > 0.f) || !isfinite(how->scale) || (how->lse_given != 0 && how->lse_given != 1) ||
-      (how->lse_given == 1 && lse == nullptr))
+  if (!scale_ok(how->scale) || (how->lse_given != 0 && how->lse_given != 1) || (how->lse_given == 1 && lse == nullptr))
     return JACAP_ERR_INVALID_ARG;
   if (!aligned16(q_win) || !aligned16(k) || !aligned4(lse) || !aligned4(before) || !aligned4(weights) ||
       !aligned4(how->lengths) || !aligned4(how->q_lens) || !aligned4(how->q_rows))
