@@ -522,7 +522,8 @@ jacap_status jacap_attend(const jacap_layout* layout, const jacap_attention* att
  *              to [0, window]; w above
  *   q_rows     device int32 [num_seqs][window] or NULL: which of the window's
  *              queries is the j-th (the accepted path of a drafted tree); an entry
- *              outside [0, window) is no query
+ *              outside [0, window) is no query (of a query that is there twice, lse is
+ *              written as either row's)
  *   lse_given  1: lse is an input, as jacap_attend wrote it for these queries (K is
  *              then read once); 0: it is computed, and written unless NULL
  *   lse        device float32 [num_seqs][num_layers][num_q_heads][window], dense, indexed
