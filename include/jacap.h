@@ -568,7 +568,8 @@ jacap_status jacap_weigh(const jacap_layout* layout, const jacap_weighing* how, 
  *                (NULL without pos)
  *   ws           device, 256-byte aligned, at least 64 bytes: the status word, zero
  *                at first (a workspace of jacap_weigh serves; one that holds an error
- *                selects nothing)
+ *                selects nothing, except for JACAP_ERR_NONFINITE without pos: there
+ *                every unit's weights are looked at again)
  * The other arguments and results are those of jacap_select_compact.
  */
 jacap_status jacap_select_weights(const jacap_layout* layout, const float* weights, const int32_t* pos,

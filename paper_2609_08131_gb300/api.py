@@ -866,6 +866,8 @@ class DecodeEvictor:
                        .expand_as(self.pos))
         self.lengths = list(lengths)
         self.next_id = list(lengths)
+        self._attended = (0, set())
+        self._follow(stream)
         if self.rule == "weight":
             self._w.zero_()
             self._weigh(q_win, None, None, stream)
@@ -889,6 +891,7 @@ class DecodeEvictor:
                                 _ptr(self._pos), _ptr(self.stats), _ptr(self.counts), _stream(stream)), "jacap_append")
             self.lengths = [n + 1 for n in self.lengths]
             self.next_id = [n + 1 for n in self.next_id]
+            self._follow(stream)
             return [s for s in range(self.S) if self.lengths[s] >= self.cap]
         dev = self._k.device
         rows = torch.tensor(self.lengths, dtype=torch.long, device=dev)
@@ -900,6 +903,7 @@ class DecodeEvictor:
         self._pos[:, :, reqs, rows] = ids.view(1, 1, self.S).expand(self.L, self.Hkv, self.S)
         self.lengths = [n + 1 for n in self.lengths]
         self.next_id = [n + 1 for n in self.next_id]
+        self._follow(stream)
         self.merge_queries(q_new, stream)
         return [s for s in range(self.S) if self.lengths[s] >= self.cap]
 
@@ -988,6 +992,7 @@ class DecodeEvictor:
             tail[0].record(stream)
         for s in range(a, b):
             self.lengths[s] = self.budget
+        self._follow(stream)
         self.events += b - a
         self.passes += 1
 
@@ -1009,6 +1014,12 @@ class DecodeEvictor:
             t.copy_(host, non_blocking=True)
             self._ints[name] = ([list(v) if isinstance(v, (list, tuple)) else v for v in values], t)
         return t
+
+    def _follow(self, stream):
+        """The arrays on the device that captured calls read follow the slots' lengths and next ids."""
+        if self._ints and not torch.cuda.is_current_stream_capturing():
+            now = (("lengths", self.lengths), ("next ids", self.next_id))
+            _enqueue(self.device, stream, lambda _: [self._int32(k, x) for k, x in now if k in self._ints])
 
     def positions(self, tokens: int, depth=None):
         """int32 [S, tokens]: the ids that drafted tokens get if accepted; ``depth``: int32
@@ -1036,7 +1047,8 @@ class DecodeEvictor:
         (``tree_masks``; None: a chain; T = 1: the step's own token), draft_lens int32 [S] (rows
         behind are not written). Returns (o [S, Hq, T, 128], lse [S, Hq, T], a view of what the
         next call with as many tokens overwrites). Under the weight rule the normalisers are kept for ``step``,
-        ``append`` or ``accept``."""
+        ``append`` or ``accept`` (not those of a call without drafted tokens or with draft_lens, which are
+        computed again). A captured call follows the slots: its graph reads their lengths when it is replayed."""
         if not 0 <= layer < self.L:
             raise ValueError(f"layer must be 0 to {self.L - 1}")
         if not isinstance(q, torch.Tensor) or q.dim() != 4:
@@ -1075,7 +1087,10 @@ class DecodeEvictor:
                                 part.data_ptr(), ws.data_ptr(), ws.numel(), st), "jacap_attend")
             if self._attended[0] != T:
                 self._attended = (T, set())
-            self._attended[1].add(layer)
+            if k_draft is None or draft_lens is not None:  # not the normalisers of every token that may be entered
+                self._attended[1].discard(layer)
+            else:
+                self._attended[1].add(layer)
             return o, part
 
         return _enqueue(dev, stream, attend)
@@ -1083,7 +1098,7 @@ class DecodeEvictor:
     def accept(self, k_draft, v_draft, q_draft, path, stream=None):
         """Enter the accepted drafted tokens of a step: k_draft, v_draft [S, L, Hkv, T, 128],
         q_draft [S, L, Hq, T, 128] (turned, as ``attend`` took them), path[s]: which drafted
-        tokens of request s, in order (none: an empty list). As in ``step`` a request whose
+        tokens of request s, in order, each seen by those after it (none: an empty list). As in ``step`` a request whose
         slot becomes full is evicted, here in the middle of its path where that happens; returns the
         requests that were evicted."""
         if len(path) != self.S:
@@ -1127,6 +1142,7 @@ class DecodeEvictor:
         _enqueue(self.device, stream, append)
         self.lengths = [n + len(p) for n, p in zip(self.lengths, path)]
         self.next_id = [n + len(p) for n, p in zip(self.next_id, path)]
+        self._follow(stream)
         if self.rule == "weight":
             known = self._attended[0] == T and len(self._attended[1]) == L
             self._weigh(q, self._attention[T][2] if known else None, path, stream)

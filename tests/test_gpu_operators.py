@@ -735,6 +735,70 @@ def test_accepted_paths_keep_the_query_statistics():
         assert torch.equal(a, b)
 
 
+def test_normalisers_are_those_of_the_step_they_belong_to():
+    """Those that a call left for other tokens, another prompt or not for every token are not taken for the step's."""
+    S, L, Hq, Hkv, T = 2, 2, 4, 2, 3
+    g = gen(25)
+    k0, v0, k1, v1 = (randn(g, S, L, Hkv, 12, D, dtype=BF16) for _ in range(4))
+    qw = randn(g, S, L, Hq, 4, D, dtype=BF16)
+    k, v, q = (randn(g, S, L, n, T, D, dtype=BF16) for n in (Hkv, Hkv, Hq))
+
+    def enter(before):
+        ev = api.DecodeEvictor(S, L, Hq, Hkv, 30, 10, device=DEV, rule="weight")
+        before(ev)
+        ev.accept(k, v, q, [[0, 1, 2], [0, 1]])
+        ev.check()
+        return ev.weights.clone()
+
+    def attended(ev, **kw):
+        ev.start(k0, v0, qw, [12, 9])
+        for l in range(L):
+            ev.attend(l, q[:, l], **{n: x[:, l] if x.dim() == 5 else x for n, x in kw.items()})
+
+    want = enter(lambda ev: ev.start(k0, v0, qw, [12, 9]))
+    assert torch.equal(enter(attended), want)  # over the cached tokens only
+    short = torch.tensor([2, 1], dtype=torch.int32, device=DEV)
+    assert torch.equal(enter(lambda ev: attended(ev, k_draft=k, v_draft=v, draft_lens=short)), want)
+
+    def again(ev):  # another prompt in between
+        attended(ev, k_draft=k, v_draft=v)
+        ev.start(k1, v1, qw, [9, 12])
+
+    assert torch.equal(enter(again), enter(lambda ev: ev.start(k1, v1, qw, [9, 12])))
+
+
+@pytest.mark.parametrize("rule", ["jacap", "weight"])
+def test_a_captured_attention_follows_the_slots(rule):
+    S, Hq, Hkv, T = 2, 4, 2, 1
+    g = gen(26)
+    ev = api.DecodeEvictor(S, 1, Hq, Hkv, 20, 4, device=DEV, rule=rule)
+    rope = api.Rope(device=DEV)
+    k0, v0 = (randn(g, S, 1, Hkv, 23, D, dtype=BF16) for _ in range(2))
+    ev.start(k0, v0, randn(g, S, 1, Hq, 4, D, dtype=BF16), [23, 20])
+    q, k, v = (randn(g, S, n, T, D, dtype=BF16) for n in (Hq, Hkv, Hkv))
+
+    def layer():
+        tq, tk = ev.rotate(rope, q, k)
+        return (tq, tk, *ev.attend(0, tq, tk, v))
+
+    layer()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = layer()
+    for step in range(7):
+        for x in (q, k, v):
+            x.copy_(randn(g, *x.shape, dtype=BF16))
+        graph.replay()
+        got = [x.clone() for x in captured]
+        want = layer()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), step
+        ev.step(want[1][:, None, :, 0].contiguous(), v[:, None, :, 0].contiguous(),
+                want[0][:, None, :, 0].contiguous())
+    ev.check()
+    assert ev.events >= 3
+
+
 def test_loop_refusals_on_the_device_side():
     ev = api.DecodeEvictor(2, 1, 4, 2, 8, 2, device=DEV, rule="weight")
     g = gen(24)
