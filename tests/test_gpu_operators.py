@@ -243,6 +243,75 @@ def test_attend_against_64_bits(case, dtype):
     assert torch.equal(first[0], o) and torch.equal(first[1], lse)  # the order of every sum is fixed
 
 
+@pytest.mark.parametrize("L,Hq,Hkv,T,lens,dtype", [
+    (1, 4, 2, 1, (40000, 300, 9000), BF16), (2, 5, 1, 9, (17000, 3), BF16), (1, 5, 1, 20, (30000, 6000), BF16),
+    (1, 5, 1, 64, (26000, 40, 7000), BF16), (1, 8, 1, 32, (70000,), BF16), (1, 4, 2, 1, (20000, 300), F32),
+    (1, 5, 1, 9, (12000, 70), F32), (5, 16, 8, 3, (900, 100, 64, 400, 0, 1, 333, 640, 65), BF16),
+    (2, 8, 1, 20, tuple(range(20, 2000, 23)), BF16)])
+def test_attend_splits_joined_and_several_items_per_block(L, Hq, Hkv, T, lens, dtype):
+    """Requests in many splits, and more items than the GPU takes at once. A split's sum takes at most some hundred
+    additions one after the other (one per tile of 64 tokens), 2^-24 each: below a fifth of the logits' bound (their
+    size is above 10 here, the bound 8e-5)."""
+    S, g = len(lens), gen(300 + T)
+    cache = make_cache(g, S, L, Hq, Hkv, T, lens, dtype, spread=2.0)
+    kd, vd = (randn(g, S, L, Hkv, T, D, dtype=dtype) for _ in range(2))
+    tree = api.tree_masks(random_tree(T, S, T)).to(DEV)
+    att = api.CacheAttention(cache)
+    o, lse = att.run(k_draft=kd, v_draft=vd, tree=tree)
+    att.check()
+    check_attend(cache, o, lse, kd, vd, tree)
+    # shorter requests with the same workspace: other splits, and counters that the call before left at zero
+    lengths = [n // 3 for n in lens]
+    o, lse = att.run(k_draft=kd, v_draft=vd, tree=tree, lengths=torch.tensor(lengths, dtype=torch.int32, device=DEV))
+    att.check()
+    check_attend(cache, o, lse, kd, vd, tree, lengths)
+
+
+def test_caches_whose_offsets_pass_32_bits():
+    """Two heads of 8.5 million tokens: the second head's last rows are past 2^31 elements. All keys are zero but the
+    last 300 of a head, whose logits leave the others a share below 1e-2 of the least tolerance."""
+    N, T, n = 8_500_000, 2, 300
+    g = gen(31)
+    k = torch.zeros((1, 2, N, D), dtype=BF16, device=DEV)
+    v = torch.zeros_like(k)
+    k[:, :, -n:], v[:, :, -n:] = 20 * randn(g, 1, 2, n, D, dtype=BF16), randn(g, 1, 2, n, D, dtype=BF16)
+    q = randn(g, 1, 1, 4, T, D, dtype=BF16)
+    assert (q[0, 0].view(2, 4, D) @ k[0, :, -n:].transpose(1, 2)).amax(2).min() * SCALE > 36 and k.numel() > 2 ** 31
+    cache = api.Cache(q, k, v, torch.tensor([0, N], dtype=torch.int32, device=DEV), [N], 4)
+    att = api.CacheAttention(cache)
+    o, lse = att.run()
+    att.check()
+    seen = torch.ones(T, n, dtype=torch.bool, device=DEV)
+    for h in range(4):
+        wo, wl, to, tl = attend_plain(q[0, 0, h], k[0, h // 2, -n:], v[0, h // 2, -n:], seen, BF16)
+        others = N * math.exp(-36)  # of the sum of exponentials, at most
+        within(o[0, 0, h], wo, to + others * wo.abs(), "o")
+        within(lse[0, 0, h], wl, tl + others, "lse")
+    ev = api.WeightEvictor(cache, 64)
+    ev.run()
+    ev.check()
+    small = api.Cache(q, k[:, :, -n:].contiguous(), v[:, :, -n:].contiguous(),
+                      torch.tensor([0, n], dtype=torch.int32, device=DEV), [n], 4)
+    weights, tol, *_ = weigh_plain(small)
+    # (what is below float32's normal numbers, 2^-126, becomes zero: of four rows)
+    within(ev.weights[:, :, -n:], weights, tol + 2 * others * weights + 4 * 2.0 ** -126, "weights")
+    for h in range(2):
+        keep = select_plain(ev.weights[0, h, -n:], n, 64, 0, 0)
+        assert ev.idx[0, h, 0].tolist() == [N - n + i for i in keep]
+        for out, x in ((ev.k_out, k), (ev.v_out, v)):
+            assert torch.equal(out[0, h, 0], x[0, h, -n:][keep])
+    del k, v, cache, att, ev
+    x = torch.zeros((1_100_000, 16, D), dtype=BF16, device=DEV)
+    x[-3:] = randn(g, 3, 16, D, dtype=BF16)
+    assert x.numel() > 2 ** 31
+    at = torch.arange(x.shape[0], dtype=torch.int32, device=DEV)
+    y, _ = api.Rope(device=DEV).apply(x, None, at)
+    freq, amplitude = api.rope_frequencies(D, 10000.0)
+    want, tol = rope_plain(x[-3:], at[-3:], freq, amplitude, D, False, False)
+    within(y[-3:], want, tol, "rope")
+    assert not y[:-3].any()
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_attend_live_lengths_masks_and_rows_left_alone(dtype):
     S, L, Hq, Hkv, T, cap = 5, 2, 6, 2, 9, 200
@@ -577,6 +646,32 @@ def test_operators_on_another_stream_and_in_graphs():
             for s in range(2):
                 a0 = 900 * s
                 assert torch.equal(want[3][:, :, a0:a0 + n[s]], got[3][:, :, a0:a0 + n[s]])
+
+
+def test_two_calls_at_once():
+    """Two attentions and their weights on two streams, workspaces of their own: as one after the other."""
+    work = []
+    for i, (lens, T) in enumerate((((9000, 700, 3000), 3), ((20000,), 40))):
+        g = gen(40 + i)
+        cache = make_cache(g, len(lens), 2, 8, 2, T, lens, BF16)
+        kd, vd = (randn(g, len(lens), 2, 2, T, D, dtype=BF16) for _ in range(2))
+        att, ev = api.CacheAttention(cache), api.WeightEvictor(cache, 100, sinks=1, recent=3)
+
+        def call(att=att, ev=ev, kd=kd, vd=vd):
+            _, lse = att.run(k_draft=kd, v_draft=vd)
+            ev.run()
+            return [x.clone() for x in (att.o, lse, ev.weights, ev.lse, ev.idx, ev.v_out)]
+
+        work.append((call, call(), torch.cuda.Stream(device=DEV)))
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(5):
+        for call, _, stream in work:
+            with torch.cuda.stream(stream):
+                got.append(call())
+    torch.cuda.synchronize()
+    for i, out in enumerate(got):
+        assert all(torch.equal(a, b) for a, b in zip(out, work[i % 2][1]))
 
 
 # ------------------------------------------------------- the decoding loop ----
