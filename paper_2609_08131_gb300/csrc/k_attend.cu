@@ -8,30 +8,51 @@
 // row that sees nothing has o = 0 and lse = -inf.
 //
 // K and V are read once, in one pass with a running maximum and sum. A unit's tokens are
-// split over CTAs (`chunk` tokens each, the drafted ones with the last), which leave
-// unnormalised sums for a second launch to join where a request has several splits.
+// split into items (`chunk` tokens each, the drafted ones with the last), which leave
+// unnormalised sums to be joined where a request has several splits.
 //
-// bf16: R = G T rows are an M = 128 operand whatever R is: the memory's time for a tile
-// (64 tokens, 32 KB of K and V: ~700 SM cycles at the copy rate with two CTAs per SM)
-// covers its MMAs (N = 64 and N = 128: ~260 cycles) even where only a few rows are real,
-// and the softmax warps work on real rows only: with R <= 32 every tensor-memory lane
-// quarter holds a copy of the rows and takes a quarter of each tile's tokens (R <= 64: two
+// bf16: persistent CTAs to which items are dealt as they become free, so that the live
+// lengths need not be known to the host and a CTA's ring of tiles never runs dry between
+// two items (one CTA per item: 158 us instead of 92 for the long chain below). A CTA's
+// roles: a TMA producer, an MMA issuer, softmax warps with a row per lane, and warps that
+// fetch the next item's rows. R = G T rows are an M = 128 operand whatever R is: the
+// memory's time for a tile (64 tokens, 32 KB of K and V: ~700 SM cycles at the copy rate
+// with two CTAs per SM) covers its products even where only a few rows are real, and the
+// softmax warps work on real rows only: with R <= 32 every tensor-memory lane quarter
+// holds a copy of the rows and takes a quarter of each tile's tokens (R <= 64: two
 // copies, halves), each with a maximum and a sum of its own; the other tokens' weights are
-// zero in its lanes, and the copies are joined at the end. So a warp has 16 columns
-// per tile instead of 64, and no two warps ever wait for each other. More than 128 rows
-// take several CTAs, neighbours that share K and V through L2.
+// zero in its lanes, and the copies are joined at the item's end. So a warp has 16 columns
+// per tile instead of 64, and no two warps ever wait for each other. Up to 256 rows share a
+// CTA's tiles as two blocks of 128 (one CTA per SM); beyond that, items of the same tokens
+// follow each other and the second reads K and V from L2.
 // The weights p are rounded to bf16 for the second product (the sums Z are not): of an
 // output of many comparable terms that is an error of about the output's own rounding.
 // The maximum is only raised when a logit passes it by 2^8, which a rescaling of the
 // accumulators then follows: rare after the first tiles, and harmless to the sums (p <= 256).
+// The tensor cores truncate each of a logit's partial sums, which shrinks logits by some
+// 2^-23; the scale makes up for the mean of it.
 // Rows of V past the live tokens, and drafted rows past the request's, are zeroed in
 // shared memory before the product, as 0 times what an unwritten row holds may be NaN;
 // a drafted value that is not finite is zeroed too and added to the rows that see it.
+//
+// Measured (32 query heads on 8, 92 us = 5.8 TB/s of K and V for 8 drafted tokens over 131011
+// cached ones; 37 us = 3.7 TB/s for one token in 16 slots of 2100, of which ~8 us are the
+// launch and the first tiles' way; 9 us for one token over 37): bound by memory up to 128 rows.
+// 64 drafted tokens of 5 heads a group, 320 rows, over 110000 tokens in 16 requests: 216 us for
+// 138 GFLOP. There a tile of 256 rows takes ~1500 cycles: the products ~1280 (S reads its rows from
+// shared memory again for every 64 tokens, 48 cycles for each 128 x 64 x 16), and the softmax
+// ~1150 with two warps per scheduler, which overlap but for the waits between them. Tried and
+// left out: an MMA issuer per block (218 us), the barriers asked ahead of the issue (226 us),
+// shorter splits and the requests' last splits dealt last (217 to 222 us).
 //
 // float32: CUDA cores, as the tensor cores would round the inputs. A warp takes 8 of a
 // tile's tokens for all rows of the CTA (8 or 32), four lanes to a token's dot
 // products, and keeps a maximum, sums and accumulators of its own, so that tiles need no
 // barrier but the one that says they have landed; the warps are joined at the end.
+// 5 drafted tokens of 8 heads over 5473 tokens in two requests: 32 us (45 MB: 7 us at the copy
+// rate; the splits' start and end and the join are the rest); 64 rows a group or more are bound by
+// the reads of shared memory that feed the multiply-adds (256 rows over 8192 tokens: 574 us,
+// 553 for products and softmax by a library).
 #include "jacap_dev.cuh"
 #include "jacap_internal.h"
 

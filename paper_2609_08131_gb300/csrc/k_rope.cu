@@ -13,9 +13,13 @@
 //
 // A block takes TB tokens: their sines and cosines go to shared memory once, for all
 // heads (they cost ~60 instructions each), then GS threads take a row (a head of a
-// token) and four rows each are in flight at a time. 16-byte loads where the rows'
-// addresses and strides allow them and no pair is split by a piece's end; otherwise a
-// thread takes a pair of single elements.
+// token) and four rows each are in flight at a time, the first of them asked for before
+// the angles are worked out. 16-byte loads where the rows' addresses and strides allow them
+// and no pair is split by a piece's end; otherwise a thread takes a pair of single elements.
+//
+// Bound by memory, and for few tokens by the launch. Measured, 32 + 8 heads in bf16: 32768
+// tokens 125 us = 5.4 TB/s (1, 2, 3, 6 and 8 tokens per block: 193, 140, 124, 137, 134 us; five
+// rows in flight 143 us; streaming loads and stores 125 us); 4 tokens 2.9 us.
 #include <type_traits>
 
 #include "jacap_dev.cuh"

@@ -50,6 +50,12 @@
 // MODE 0 only selects. (The in-place compaction in ascending order moves
 // every kept row; it stays a launch of its own, whose small CTAs keep more
 // bytes in flight per SM than one selection CTA per unit could.)
+//
+// PROT: eviction by attention weights. The first `sinks` and the last `recent` tokens are
+// kept whatever their weights, the others compete for the rest. By row this is a range
+// of the keys, so that no launch has to write keys of its own first: one layer of 4099
+// tokens 27 -> 9 us, 1024 units of 16384 tokens (1638 kept) 384 -> 349 us = 5.2 TB/s of
+// weights read and rows copied. With tags protect_kernel writes the keys.
 #include <algorithm>
 
 #include "jacap_dev.cuh"
