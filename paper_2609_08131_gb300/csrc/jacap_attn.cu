@@ -32,6 +32,7 @@ struct AttendPlan {
   int chunk, nsplit, nrb;
   size_t status, counts, opart, mlpart, total;
 };
+constexpr int64_t F32_EXTRA = 128;
 AttendPlan attend_plan(const jacap_layout* L) {
   AttendPlan p;
   const int bf = L->dtype == JACAP_BF16 ? 1 : 0, rows = L->num_q_heads / L->num_kv_heads * L->window;
@@ -39,17 +40,20 @@ AttendPlan attend_plan(const jacap_layout* L) {
   p.nrb = (rows + block - 1) / block;
   const int64_t units = (int64_t)L->num_seqs * L->num_layers * L->num_kv_heads, ctas = units * p.nrb;
   const int64_t most = L->max_seqlen;
-  // float32: about three CTAs for each place on an SM where that leaves 1024 tokens or more, about one
-  // where it leaves 128. bf16: the least that a split may have (the kernel chooses from the live
-  // lengths). A split's sums, written and read by the join, stay an eighth of its K and V.
-  int64_t chunk = 256;
+  // bf16: the least that a split may have (the kernel chooses from the live lengths); a split's sums,
+  // written and read by the join, stay an eighth of its K and V. float32: of the numbers of splits that
+  // leave 128 tokens or more, the one whose rounds of CTAs (three, two or one on an SM) end first, with F32_EXTRA
+  // tokens' time for a CTA's start and end.
+  int64_t chunk = std::max<int64_t>(256, std::min(rows, block) * 16);
   if (!bf) {
-    const int64_t places = rows <= 8 ? 3 * 152 : 152;
-    chunk = most * ctas / (3 * places);
-    if (chunk < 1024) chunk = std::min<int64_t>(1024, (most * ctas + places - 1) / places);
-    chunk = std::max<int64_t>(chunk, 128);
+    const int64_t places = 152 * (block == 8 ? 3 : (block == 16 ? 2 : 1));
+    int64_t best = INT64_MAX;
+    for (int64_t k = 1; k <= 1024 && (k == 1 || (most + k - 1) / k >= 128); ++k) {
+      const int64_t c = ((most + k - 1) / k + 63) / 64 * 64, items = (most + c - 1) / c * ctas;
+      const int64_t time = (items + places - 1) / places * (c + F32_EXTRA);
+      if (time < best) best = time, chunk = c;
+    }
   }
-  chunk = std::max<int64_t>(chunk, std::min(rows, block) * 16);
   chunk = std::min<int64_t>((chunk + 63) / 64 * 64, (most + 63) / 64 * 64);
   p.chunk = (int)chunk;
   p.nsplit = (int)((most + chunk - 1) / chunk);

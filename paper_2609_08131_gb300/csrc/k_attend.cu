@@ -45,14 +45,15 @@
 // left out: an MMA issuer per block (218 us), the barriers asked ahead of the issue (226 us),
 // shorter splits and the requests' last splits dealt last (217 to 222 us).
 //
-// float32: CUDA cores, as the tensor cores would round the inputs. A warp takes 8 of a
-// tile's tokens for all rows of the CTA (8 or 32), four lanes to a token's dot
+// float32: CUDA cores, as the tensor cores would round the inputs. Up to 32 rows a warp takes
+// 8 of a tile's tokens for all rows of the CTA (8, 16 or 32), four lanes to a token's dot
 // products, and keeps a maximum, sums and accumulators of its own, so that tiles need no
-// barrier but the one that says they have landed; the warps are joined at the end.
-// 5 drafted tokens of 8 heads over 5473 tokens in two requests: 32 us (45 MB: 7 us at the copy
-// rate; the splits' start and end and the join are the rest); 64 rows a group or more are bound by
-// the reads of shared memory that feed the multiply-adds (256 rows over 8192 tokens: 574 us,
-// 553 for products and softmax by a library).
+// barrier but the one that says they have landed; the warps are joined at the end. More rows
+// are a product of tiles (attend_f32_rows_kernel). Measured, 8 KV heads: 5 rows over 5473 tokens
+// in two requests 32 us (45 MB: 7 us at the copy rate; the splits' start and end and the join are
+// the rest), over 32768 tokens 76 us (268 MB: 40 us); 4 requests of 4096 tokens with 12 rows 84 us,
+// 25 rows 154 us; 2 requests with 64 rows 94 us, 256 rows 337 us (8.6 GFLOP: 115 us at 75 TFLOP/s;
+// 574 us with 32 rows to a block, which read shared memory four times for as many multiply-adds).
 #include "jacap_dev.cuh"
 #include "jacap_internal.h"
 
@@ -881,14 +882,15 @@ __global__ void __launch_bounds__(AtCfg<NB>::THREADS, 3 - NB)
 }
 
 // ------------------------------------------------------------- float32 ----
-// Up to 8 rows: K and V's arrival bounds it; four warps and tiles of 32 tokens, three CTAs per SM. More: the
-// multiply-adds; eight warps, 32 rows, one CTA.
+// Up to 8 rows: K and V's arrival bounds it; four warps and tiles of 32 tokens, three CTAs per SM. More: the reads
+// of shared memory that feed the multiply-adds; up to 16 rows two such CTAs (12 rows: 84 us, with 32 rows to a block
+// 152), up to 32 eight warps, one CTA.
 template <int RB>
 struct AfCfg {
-  static constexpr int WARPS = RB == 8 ? 4 : 8, THREADS = 32 * WARPS, TOK = 8 * WARPS, LDK = D + 4;
+  static constexpr int WARPS = RB <= 16 ? 4 : 8, THREADS = 32 * WARPS, TOK = 8 * WARPS, LDK = D + 4;
   static constexpr int KF = TOK * LDK, VF = TOK * D;  // floats per stage
   static constexpr size_t SMEM = (size_t)(RB * D + 2 * (KF + VF) + WARPS * 8 * RB + 2 * WARPS * RB) * 4;
-  static constexpr int PER_SM = RB == 8 ? 3 : 1;
+  static constexpr int PER_SM = RB == 8 ? 3 : (RB == 16 ? 2 : 1);
 };
 
 template <int RB>
@@ -1062,6 +1064,169 @@ __global__ void __launch_bounds__(AfCfg<RB>::THREADS, AfCfg<RB>::PER_SM)
   }
 }
 
+// More than 32 rows (25 rows: 154 us above, 187 here): bound by the same reads. A block
+// takes 16 MR rows (MR 4 or 8): in both products a thread has the same MR rows, of 4 tokens (tx, tx + 16,
+// ...) and then of 8 channels (4 tx .. and 64 + 4 tx ..), so that a 16-byte read feeds 8 to 16 of them, a
+// row's maximum and sum stay with its 16 lanes, and its weights go from one product to the other within a
+// warp, 32 tokens at a time.
+template <int MR>
+struct AgCfg {
+  static constexpr int ROWS = 16 * MR, THREADS = 256, TOK = 64, LDK = D + 4, LDP = ROWS + 4, HALF = TOK / 2;
+  static constexpr int KF = TOK * LDK, VF = TOK * D;  // floats per stage
+  static constexpr size_t SMEM = (size_t)(ROWS * D + 2 * (KF + VF) + HALF * LDP) * 4;
+};
+
+template <int MR>
+__global__ void __launch_bounds__(AgCfg<MR>::THREADS, 1)
+    attend_f32_rows_kernel(Dims dm, const __grid_constant__ AttendArgs a, const int32_t* __restrict__ cu) {
+  using C = AgCfg<MR>;
+  constexpr int TOK = C::TOK, LDK = C::LDK, LDP = C::LDP;
+  extern __shared__ __align__(16) float sf[];
+  float* qs = sf;                  // [ROWS][D]
+  float* ks = qs + C::ROWS * D;    // [2][TOK][LDK]
+  float* vs = ks + 2 * C::KF;      // [2][TOK][D]
+  float* ps = vs + 2 * C::VF;      // [HALF tokens][LDP]
+  pdl_wait();
+  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+  const int rb = blockIdx.x % a.nrb, rest = blockIdx.x / a.nrb;
+  const AtUnit x = at_unit(dm, a, cu, rest / a.nsplit, rest % a.nsplit, TOK, a.chunk);
+  if (x.split >= x.nsp) return;
+  const int R = dm.G * dm.window, r0 = rb * C::ROWS, nrow = R - r0 < C::ROWS ? R - r0 : C::ROWS;
+  const int64_t plane = (int64_t)x.l * dm.kv_sl + (int64_t)x.g * dm.kv_sh;
+  const int64_t kd0 = x.s * a.kds[0] + x.l * a.kds[1] + x.g * a.kds[2];
+  const int64_t vd0 = x.s * a.vds[0] + x.l * a.vds[1] + x.g * a.vds[2];
+  auto fetch = [&](int i) {
+    float *kt = ks + (i & 1) * C::KF, *vt = vs + (i & 1) * C::VF;
+    const bool drafted = i >= x.ncache;
+    const int first = drafted ? 0 : x.tok0 + i * TOK;  // (the drafted tokens are one tile)
+    const int nv = (drafted ? x.nd : x.tok1) - first;
+    const float* kb = drafted ? (const float*)a.kd + kd0 : (const float*)a.k + plane + (x.t0 + first) * dm.kv_st;
+    const float* vb = drafted ? (const float*)a.vd + vd0 : (const float*)a.v + plane + (x.t0 + first) * dm.kv_st;
+    const int64_t kst = drafted ? a.kds[3] : dm.kv_st, vst = drafted ? a.vds[3] : dm.kv_st;
+#pragma unroll 4
+    for (int e = tid; e < TOK * 32; e += C::THREADS) {
+      const int tok = e >> 5, c = (e & 31) * 4;
+      const bool on = tok < nv;
+      cp_async16(smem_u32(kt + tok * LDK + c), kb + (on ? tok * kst : 0) + c, on);
+      cp_async16(smem_u32(vt + tok * D + c), vb + (on ? tok * vst : 0) + c, on);
+    }
+  };
+  if (x.nt > 0) fetch(0);
+  {
+    const float* q = (const float*)a.q + x.s * dm.q_ss + x.l * dm.q_sl + (int64_t)x.g * dm.G * dm.q_sh;
+    for (int e = tid; e < C::ROWS * 32; e += C::THREADS) {
+      const int r = e >> 5, c = (e & 31) * 4, h = at_head(dm, a, r0 + r), t = r0 + r - h * dm.window;
+      const bool on = r < nrow;
+      cp_async16(smem_u32(qs + r * D + c), q + (on ? h * dm.q_sh + t * dm.q_sp : 0) + c, on);
+    }
+  }
+  cp_async_commit();
+  const float scale2 = a.scale2, lazy = AT_LAZY / scale2;
+  float m[MR], z[MR];      // of row ty MR + i: the maximum, and the sum over this thread's tokens
+  float4 o[MR][2];
+#pragma unroll
+  for (int i = 0; i < MR; ++i) {
+    m[i] = -INFINITY, z[i] = 0.f;
+    o[i][0] = o[i][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  for (int i = 0; i < x.nt; ++i) {
+    if (i + 1 < x.nt) fetch(i + 1);
+    cp_async_commit();
+    cp_async_wait<1>();
+    __syncthreads();
+    const bool drafted = i >= x.ncache;
+    const int left = drafted ? x.nd : x.tok1 - x.tok0 - i * TOK;  // tokens of the tile
+    const float* kt = ks + (i & 1) * C::KF + tx * LDK;
+    const float* qt = qs + ty * MR * D;
+    float s[MR][4];
+#pragma unroll
+    for (int r = 0; r < MR; ++r) s[r][0] = s[r][1] = s[r][2] = s[r][3] = 0.f;
+#pragma unroll 1
+    for (int k = 0; k < D; k += 4) {
+      float4 kk[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) kk[j] = *(const float4*)(kt + 16 * j * LDK + k);
+#pragma unroll
+      for (int r = 0; r < MR; ++r) {
+        const float4 q = *(const float4*)(qt + r * D + k);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          s[r][j] = fmaf(q.x, kk[j].x, fmaf(q.y, kk[j].y, fmaf(q.z, kk[j].z, fmaf(q.w, kk[j].w, s[r][j]))));
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < MR; ++r) {
+      if (drafted) {
+        const int row = r0 + ty * MR + r, t = row - at_head(dm, a, row) * dm.window;
+        const uint64_t mask = row < R ? at_mask(dm, a, x, t) : 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (!(mask >> (tx + 16 * j) & 1)) s[r][j] = -INFINITY;
+      } else if (left < TOK) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (tx + 16 * j >= left) s[r][j] = -INFINITY;
+      }
+      float top = fmaxf(fmaxf(s[r][0], s[r][1]), fmaxf(s[r][2], s[r][3]));
+#pragma unroll
+      for (int off = 8; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+      if (top > m[r] + lazy) {
+        const float f = m[r] == -INFINITY ? 0.f : ex2((m[r] - top) * scale2);
+        m[r] = top;
+        z[r] *= f;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) o[r][c].x *= f, o[r][c].y *= f, o[r][c].z *= f, o[r][c].w *= f;
+      }
+      const float base = m[r] == -INFINITY ? 0.f : m[r] * scale2;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s[r][j] = ex2(fmaf(s[r][j], scale2, -base));
+      z[r] += (s[r][0] + s[r][1]) + (s[r][2] + s[r][3]);
+    }
+    // the weights of tokens tx + 16 j at [tx + 16 (j % 2)]: read by the lanes of the same rows alone
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      __syncwarp();  // the half before is read
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int r = 0; r < MR; r += 4)
+          *(float4*)(ps + (tx + 16 * j) * LDP + ty * MR + r) =
+              make_float4(s[r][2 * half + j], s[r + 1][2 * half + j], s[r + 2][2 * half + j], s[r + 3][2 * half + j]);
+      __syncwarp();
+      const float* vt = vs + (i & 1) * C::VF + half * C::HALF * D + 4 * tx;
+      const int n = left - half * C::HALF < C::HALF ? left - half * C::HALF : C::HALF;
+#pragma unroll 2
+      for (int j = 0; j < n; ++j) {
+        const float4 v0 = *(const float4*)(vt + j * D), v1 = *(const float4*)(vt + j * D + 64);
+#pragma unroll
+        for (int r = 0; r < MR; r += 4) {
+          const float4 p4 = *(const float4*)(ps + j * LDP + ty * MR + r);
+          const float p[4] = {p4.x, p4.y, p4.z, p4.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if (drafted && p[e] == 0.f) continue;  // a masked value may be anything
+            float4 &u = o[r + e][0], &w = o[r + e][1];
+            u.x = fmaf(p[e], v0.x, u.x), u.y = fmaf(p[e], v0.y, u.y), u.z = fmaf(p[e], v0.z, u.z), u.w = fmaf(p[e], v0.w, u.w);
+            w.x = fmaf(p[e], v1.x, w.x), w.y = fmaf(p[e], v1.y, w.y), w.z = fmaf(p[e], v1.z, w.z), w.w = fmaf(p[e], v1.w, w.w);
+          }
+        }
+      }
+    }
+    __syncthreads();  // the tile's stage is free
+  }
+  cp_async_wait<0>();
+#pragma unroll
+  for (int i = 0; i < MR; ++i) {
+#pragma unroll
+    for (int off = 8; off >= 1; off >>= 1) z[i] += __shfl_xor_sync(0xffffffffu, z[i], off);
+    const int r = r0 + ty * MR + i;
+    if (ty * MR + i < nrow) {
+      at_put<float>(dm, a, x, r, o[i][0], m[i], z[i], tx);
+      at_put<float>(dm, a, x, r, o[i][1], m[i], z[i], tx + 16);
+    }
+  }
+}
+
 // Joins the splits of units that have several: NR rows to W warps.
 constexpr int AJ_THREADS = 256, AJ_WARPS = AJ_THREADS / 32;
 template <typename T, int W, int NR>
@@ -1103,6 +1268,13 @@ static cudaError_t launch_bf16(const CUtensorMap* maps, const Dims& dm, const At
   return launch_pdl(true, kern, (int)(items < a.places ? items : a.places), AtCfg<NB>::THREADS, at_smem<NB>(), st, maps[0],
                     maps[1], maps[2], maps[3], dm, a, cu);
 }
+template <int MR>
+static cudaError_t launch_f32_rows(const Dims& dm, const AttendArgs& a, const int32_t* cu, int grid, cudaStream_t st) {
+  using C = AgCfg<MR>;
+  static_assert(C::SMEM <= 232448, "shared memory");
+  JACAP_TRY(cudaFuncSetAttribute(attend_f32_rows_kernel<MR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM));
+  return launch_pdl(true, attend_f32_rows_kernel<MR>, grid, C::THREADS, C::SMEM, st, dm, a, cu);
+}
 template <int RB>
 static cudaError_t launch_f32(const Dims& dm, const AttendArgs& a, const int32_t* cu, int grid, cudaStream_t st) {
   using C = AfCfg<RB>;
@@ -1111,7 +1283,12 @@ static cudaError_t launch_f32(const Dims& dm, const AttendArgs& a, const int32_t
   return launch_pdl(true, attend_f32_kernel<RB>, grid, C::THREADS, C::SMEM, st, dm, a, cu);
 }
 
-int attend_row_block(int dtype, int rows) { return dtype == 1 ? (rows <= 128 ? 128 : 256) : (rows <= 8 ? 8 : 32); }
+static int attend_f32_rows(int rows) {
+  for (int block = 8; block < 128; block *= 2)
+    if (rows <= block) return block;
+  return 128;
+}
+int attend_row_block(int dtype, int rows) { return dtype == 1 ? (rows <= 128 ? 128 : 256) : attend_f32_rows(rows); }
 
 int attend_part_rows(int rows) { return rows <= 32 ? 32 : (rows <= 64 ? 64 : 128); }
 
@@ -1127,7 +1304,10 @@ cudaError_t launch_attend(const CUtensorMap* maps, const Dims& dm, int dtype, co
     else JACAP_TRY((launch_bf16<1, 2>(maps, dm, a, cu, blocks, sms, st)));
   } else {
     if (R <= 8) JACAP_TRY(launch_f32<8>(dm, a, cu, (int)blocks, st));
-    else JACAP_TRY(launch_f32<32>(dm, a, cu, (int)blocks, st));
+    else if (R <= 16) JACAP_TRY(launch_f32<16>(dm, a, cu, (int)blocks, st));
+    else if (R <= 32) JACAP_TRY(launch_f32<32>(dm, a, cu, (int)blocks, st));
+    else if (R <= 64) JACAP_TRY(launch_f32_rows<4>(dm, a, cu, (int)blocks, st));
+    else JACAP_TRY(launch_f32_rows<8>(dm, a, cu, (int)blocks, st));
   }
   if (a.nsplit == 1 || (dtype == 1 && at_joins_inside(a.nsplit, R))) return cudaSuccess;
   return dtype == 1 ? launch_join<__nv_bfloat16>(dm, a, cu, st) : launch_join<float>(dm, a, cu, st);
