@@ -45,14 +45,14 @@
 // left out: an MMA issuer per block (218 us), the barriers asked ahead of the issue (226 us),
 // shorter splits and the requests' last splits dealt last (217 to 222 us).
 //
-// float32: CUDA cores, as the tensor cores would round the inputs. Up to 32 rows a warp takes
-// 8 of a tile's tokens for all rows of the CTA (8, 16 or 32), four lanes to a token's dot
+// float32: CUDA cores, as the tensor cores would round the inputs. Up to 16 rows a warp takes
+// 8 of a tile's tokens for all rows of the CTA (8 or 16), four lanes to a token's dot
 // products, and keeps a maximum, sums and accumulators of its own, so that tiles need no
 // barrier but the one that says they have landed; the warps are joined at the end. More rows
 // are a product of tiles (attend_f32_rows_kernel). Measured, 8 KV heads: 5 rows over 5473 tokens
 // in two requests 32 us (45 MB: 7 us at the copy rate; the splits' start and end and the join are
 // the rest), over 32768 tokens 76 us (268 MB: 40 us); 4 requests of 4096 tokens with 12 rows 84 us,
-// 25 rows 154 us; 2 requests with 64 rows 94 us, 256 rows 337 us (8.6 GFLOP: 115 us at 75 TFLOP/s;
+// 25 rows 157 us; 2 requests with 64 rows 94 us, 256 rows 337 us (8.6 GFLOP: 115 us at 75 TFLOP/s;
 // 574 us with 32 rows to a block, which read shared memory four times for as many multiply-adds).
 #include "jacap_dev.cuh"
 #include "jacap_internal.h"
@@ -884,13 +884,13 @@ __global__ void __launch_bounds__(AtCfg<NB>::THREADS, 3 - NB)
 // ------------------------------------------------------------- float32 ----
 // Up to 8 rows: K and V's arrival bounds it; four warps and tiles of 32 tokens, three CTAs per SM. More: the reads
 // of shared memory that feed the multiply-adds; up to 16 rows two such CTAs (12 rows: 84 us, with 32 rows to a block
-// 152), up to 32 eight warps, one CTA.
+// 152).
 template <int RB>
 struct AfCfg {
-  static constexpr int WARPS = RB <= 16 ? 4 : 8, THREADS = 32 * WARPS, TOK = 8 * WARPS, LDK = D + 4;
+  static constexpr int WARPS = 4, THREADS = 32 * WARPS, TOK = 8 * WARPS, LDK = D + 4;
   static constexpr int KF = TOK * LDK, VF = TOK * D;  // floats per stage
   static constexpr size_t SMEM = (size_t)(RB * D + 2 * (KF + VF) + WARPS * 8 * RB + 2 * WARPS * RB) * 4;
-  static constexpr int PER_SM = RB == 8 ? 3 : (RB == 16 ? 2 : 1);
+  static constexpr int PER_SM = RB == 8 ? 3 : 2;
 };
 
 template <int RB>
@@ -1064,7 +1064,7 @@ __global__ void __launch_bounds__(AfCfg<RB>::THREADS, AfCfg<RB>::PER_SM)
   }
 }
 
-// More than 32 rows (25 rows: 154 us above, 187 here): bound by the same reads. A block
+// More than 16 rows (25 rows: 157 us, 154 with 32 rows to a block of the kernel above): bound by the same reads. A block
 // takes 16 MR rows (MR 4 or 8): in both products a thread has the same MR rows, of 4 tokens (tx, tx + 16,
 // ...) and then of 8 channels (4 tx .. and 64 + 4 tx ..), so that a 16-byte read feeds 8 to 16 of them, a
 // row's maximum and sum stay with its 16 lanes, and its weights go from one product to the other within a
@@ -1283,11 +1283,7 @@ static cudaError_t launch_f32(const Dims& dm, const AttendArgs& a, const int32_t
   return launch_pdl(true, attend_f32_kernel<RB>, grid, C::THREADS, C::SMEM, st, dm, a, cu);
 }
 
-static int attend_f32_rows(int rows) {
-  for (int block = 8; block < 128; block *= 2)
-    if (rows <= block) return block;
-  return 128;
-}
+static int attend_f32_rows(int rows) { return rows <= 8 ? 8 : (rows <= 16 ? 16 : (rows <= 64 ? 64 : 128)); }
 int attend_row_block(int dtype, int rows) { return dtype == 1 ? (rows <= 128 ? 128 : 256) : attend_f32_rows(rows); }
 
 int attend_part_rows(int rows) { return rows <= 32 ? 32 : (rows <= 64 ? 64 : 128); }
@@ -1305,7 +1301,6 @@ cudaError_t launch_attend(const CUtensorMap* maps, const Dims& dm, int dtype, co
   } else {
     if (R <= 8) JACAP_TRY(launch_f32<8>(dm, a, cu, (int)blocks, st));
     else if (R <= 16) JACAP_TRY(launch_f32<16>(dm, a, cu, (int)blocks, st));
-    else if (R <= 32) JACAP_TRY(launch_f32<32>(dm, a, cu, (int)blocks, st));
     else if (R <= 64) JACAP_TRY(launch_f32_rows<4>(dm, a, cu, (int)blocks, st));
     else JACAP_TRY(launch_f32_rows<8>(dm, a, cu, (int)blocks, st));
   }
