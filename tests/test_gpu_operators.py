@@ -247,7 +247,8 @@ def test_attend_against_64_bits(case, dtype):
     (1, 4, 2, 1, (40000, 300, 9000), BF16), (2, 5, 1, 9, (17000, 3), BF16), (1, 5, 1, 20, (30000, 6000), BF16),
     (1, 5, 1, 64, (26000, 40, 7000), BF16), (1, 8, 1, 32, (70000,), BF16), (1, 4, 2, 1, (20000, 300), F32),
     (1, 5, 1, 9, (12000, 70), F32), (5, 16, 8, 3, (900, 100, 64, 400, 0, 1, 333, 640, 65), BF16),
-    (2, 8, 1, 20, tuple(range(20, 2000, 23)), BF16)])
+    (2, 8, 1, 20, tuple(range(20, 2000, 23)), BF16), (1, 4, 1, 4, (5000, 30), F32), (2, 5, 1, 20, (9000, 300), F32),
+    (1, 8, 1, 48, (3000,), F32)])
 def test_attend_splits_joined_and_several_items_per_block(L, Hq, Hkv, T, lens, dtype):
     """Requests in many splits, and more items than the GPU takes at once. A split's sum takes at most some hundred
     additions one after the other (one per tile of 64 tokens), 2^-24 each: below a fifth of the logits' bound (their
