@@ -52,7 +52,7 @@
 // are a product of tiles (attend_f32_rows_kernel). Measured, 8 KV heads: 5 rows over 5473 tokens
 // in two requests 32 us (45 MB: 7 us at the copy rate; the splits' start and end and the join are
 // the rest), over 32768 tokens 76 us (268 MB: 40 us); 4 requests of 4096 tokens with 12 rows 84 us,
-// 25 rows 157 us; 2 requests with 64 rows 94 us, 256 rows 337 us (8.6 GFLOP: 115 us at 75 TFLOP/s;
+// 25 rows 157 us; 2 requests with 64 rows 94 us, 256 rows 275 us (8.6 GFLOP: 115 us at 75 TFLOP/s;
 // 574 us with 32 rows to a block, which read shared memory four times for as many multiply-adds).
 #include "jacap_dev.cuh"
 #include "jacap_internal.h"
@@ -1064,23 +1064,24 @@ __global__ void __launch_bounds__(AfCfg<RB>::THREADS, AfCfg<RB>::PER_SM)
   }
 }
 
-// More than 16 rows (25 rows: 157 us, 154 with 32 rows to a block of the kernel above): bound by the same reads. A block
-// takes 16 MR rows (MR 4 or 8): in both products a thread has the same MR rows, of 4 tokens (tx, tx + 16,
-// ...) and then of 8 channels (4 tx .. and 64 + 4 tx ..), so that a 16-byte read feeds 8 to 16 of them, a
-// row's maximum and sum stay with its 16 lanes, and its weights go from one product to the other within a
-// warp, 32 tokens at a time.
-template <int MR>
+// More than 16 rows (25 rows: 157 us, 154 with 32 rows to a block of the kernel above): bound by the latency
+// between reads of shared memory and the multiply-adds that they feed. A block of NT threads takes NT / 4
+// rows (64 or 128): in both products a thread has the same four rows, of 4 tokens (tx, tx + 16, ...) and
+// then of 8 channels (4 tx .. and 64 + 4 tx ..), so that a 16-byte read feeds 8 to 11 of them, a row's
+// maximum and sum stay with its 16 lanes, and its weights go from one product to the other within a warp,
+// 32 tokens at a time. (256 rows: 275 us; with eight rows to a thread and half the threads 337 us.)
+template <int NT>
 struct AgCfg {
-  static constexpr int ROWS = 16 * MR, THREADS = 256, TOK = 64, LDK = D + 4, LDP = ROWS + 4, HALF = TOK / 2;
+  static constexpr int MR = 4, ROWS = NT / 16 * MR, THREADS = NT, TOK = 64, LDK = D + 4, LDP = ROWS + 4, HALF = TOK / 2;
   static constexpr int KF = TOK * LDK, VF = TOK * D;  // floats per stage
   static constexpr size_t SMEM = (size_t)(ROWS * D + 2 * (KF + VF) + HALF * LDP) * 4;
 };
 
-template <int MR>
-__global__ void __launch_bounds__(AgCfg<MR>::THREADS, 1)
+template <int NT>
+__global__ void __launch_bounds__(NT, 1)
     attend_f32_rows_kernel(Dims dm, const __grid_constant__ AttendArgs a, const int32_t* __restrict__ cu) {
-  using C = AgCfg<MR>;
-  constexpr int TOK = C::TOK, LDK = C::LDK, LDP = C::LDP;
+  using C = AgCfg<NT>;
+  constexpr int MR = C::MR, TOK = C::TOK, LDK = C::LDK, LDP = C::LDP;
   extern __shared__ __align__(16) float sf[];
   float* qs = sf;                  // [ROWS][D]
   float* ks = qs + C::ROWS * D;    // [2][TOK][LDK]
@@ -1141,7 +1142,7 @@ __global__ void __launch_bounds__(AgCfg<MR>::THREADS, 1)
     float s[MR][4];
 #pragma unroll
     for (int r = 0; r < MR; ++r) s[r][0] = s[r][1] = s[r][2] = s[r][3] = 0.f;
-#pragma unroll 1
+#pragma unroll(NT == 512 ? 2 : 1)
     for (int k = 0; k < D; k += 4) {
       float4 kk[4];
 #pragma unroll
@@ -1268,12 +1269,12 @@ static cudaError_t launch_bf16(const CUtensorMap* maps, const Dims& dm, const At
   return launch_pdl(true, kern, (int)(items < a.places ? items : a.places), AtCfg<NB>::THREADS, at_smem<NB>(), st, maps[0],
                     maps[1], maps[2], maps[3], dm, a, cu);
 }
-template <int MR>
+template <int NT>
 static cudaError_t launch_f32_rows(const Dims& dm, const AttendArgs& a, const int32_t* cu, int grid, cudaStream_t st) {
-  using C = AgCfg<MR>;
+  using C = AgCfg<NT>;
   static_assert(C::SMEM <= 232448, "shared memory");
-  JACAP_TRY(cudaFuncSetAttribute(attend_f32_rows_kernel<MR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM));
-  return launch_pdl(true, attend_f32_rows_kernel<MR>, grid, C::THREADS, C::SMEM, st, dm, a, cu);
+  JACAP_TRY(cudaFuncSetAttribute(attend_f32_rows_kernel<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM));
+  return launch_pdl(true, attend_f32_rows_kernel<NT>, grid, C::THREADS, C::SMEM, st, dm, a, cu);
 }
 template <int RB>
 static cudaError_t launch_f32(const Dims& dm, const AttendArgs& a, const int32_t* cu, int grid, cudaStream_t st) {
@@ -1301,8 +1302,8 @@ cudaError_t launch_attend(const CUtensorMap* maps, const Dims& dm, int dtype, co
   } else {
     if (R <= 8) JACAP_TRY(launch_f32<8>(dm, a, cu, (int)blocks, st));
     else if (R <= 16) JACAP_TRY(launch_f32<16>(dm, a, cu, (int)blocks, st));
-    else if (R <= 64) JACAP_TRY(launch_f32_rows<4>(dm, a, cu, (int)blocks, st));
-    else JACAP_TRY(launch_f32_rows<8>(dm, a, cu, (int)blocks, st));
+    else if (R <= 64) JACAP_TRY(launch_f32_rows<256>(dm, a, cu, (int)blocks, st));
+    else JACAP_TRY(launch_f32_rows<512>(dm, a, cu, (int)blocks, st));
   }
   if (a.nsplit == 1 || (dtype == 1 && at_joins_inside(a.nsplit, R))) return cudaSuccess;
   return dtype == 1 ? launch_join<__nv_bfloat16>(dm, a, cu, st) : launch_join<float>(dm, a, cu, st);
