@@ -26,14 +26,14 @@ def passed(status):
 
 
 # ------------------------------------------------------------------- rotate ----
-def rotate(rope=None, dtype=J.JACAP_BF16, S=2, T=3, pos=P, ps=(3, 1), inverse=0, q=True, k=True, **kw):
+def rotate(rope=None, dtype=J.JACAP_BF16, S=2, T=5, pos=P, ps=(5, 1), inverse=0, q=True, k=True, **kw):
     r = J.jacap_rope()
     r.head_dim, r.rot_dim, r.interleaved, r.amplitude, r.turns = 128, 128, 0, 1.0, 0x1000
     for n, v in (rope or {}).items():
         setattr(r, n, v)
-    t = {"x": 0x1000, "y": 0x2000, "heads": 8, "x_strides": (3 * 1024, 1024, 128), "y_strides": (3 * 1024, 1024, 128), **kw}
+    t = {"x": 0x1000, "y": 0x2000, "heads": 8, "x_strides": (5 * 1024, 1024, 128), "y_strides": (5 * 1024, 1024, 128), **kw}
     one = J.jacap_rope_tensor(t["x"], t["y"], t["heads"], t["x_strides"], t["y_strides"])
-    two = J.jacap_rope_tensor(0x3000, 0x4000, 2, (768, 256, 128), (768, 256, 128))
+    two = J.jacap_rope_tensor(0x3000, 0x4000, 2, (1280, 256, 128), (1280, 256, 128))
     return J.jacap_rotate(r, dtype, S, T, pos, None if ps is None else (ctypes.c_int64 * 2)(*ps), inverse,
                           one if q else None, two if k else None, None)
 
@@ -53,7 +53,7 @@ def test_rotate_takes(kw):
     ({"dtype": 7}, BAD), ({"S": -1}, BAD), ({"T": -1}, BAD), ({"S": 1 << 16, "T": 1 << 15}, BAD), ({"pos": None}, BAD),
     ({"pos": MIS2}, BAD), ({"ps": None}, BAD), ({"ps": (-1, 1)}, BAD), ({"inverse": 2}, BAD), ({"q": False, "k": False}, BAD),
     ({"x": 0}, BAD), ({"y": 0}, BAD), ({"x": 0x1001}, BAD), ({"x": 0x1002, "dtype": J.JACAP_F32}, BAD), ({"heads": 0}, BAD),
-    ({"x_strides": (3072 - 1024, -128, 128)}, BAD), ({"y_strides": (0, 1024, 128)}, BAD),
+    ({"x_strides": (5 * 1024, -128, 128)}, BAD), ({"y_strides": (0, 1024, 128)}, BAD),
     ({"y_strides": (4096, 1024, 64)}, BAD), ({"x": 0x2000, "x_strides": (8192, 1024, 128)}, BAD),
 ])
 def test_rotate_refuses(kw, expect):
