@@ -11,15 +11,16 @@
 // Runs of chunks are dealt to persistent CTAs as they become free (RunStream), from the
 // work plan of the eviction pass.
 //
-// Measured, 32 queries of 32 heads on 8: one layer of 4099 tokens 25.7 us (plan, statistics,
+// Measured, 32 queries of 32 heads on 8: one layer of 4099 tokens 24 us (plan, statistics,
 // their join and weights: four dependent launches of 5 to 7 us each bound it), 8 layers of
-// 32768 tokens 189 us: K twice is 1.07 GB, 5.7 TB/s. 28 layers of 8 slots of 2100 tokens, 4
-// queries of 28 heads on 4 with lse given: 83 us, 6.3 TB/s. 64 queries a head (256 rows) 233 us
+// 32768 tokens 188 us: K twice is 1.07 GB, 5.7 TB/s. 28 layers of 8 slots of 2100 tokens, 4
+// queries of 28 heads on 4 with lse given: 83 us, 6.3 TB/s. 64 queries a head (256 rows) 230 us
 // for 4 layers: the second row block doubles the products and exponentials. Bound by memory up
 // to 128 rows, by the exponentials beyond. Tried and left out: both passes in one launch so that
 // the second finds K in L2 (480 us and more: a batch of planes small enough for L2 has each CTA
 // wait for the others' statistics); the runs' join by the last run's own warp (n = 131072: 126
-// -> 210 us, one warp's chain over hundreds of runs; 8 layers 226 us).
+// -> 210 us, one warp's chain over hundreds of runs; 8 layers 226 us); two tiles at a time to each
+// reader, so that a read of a row's constants serves both (8 layers 184 us, the slots 88).
 //
 // A row's sum takes exp over thousands of tokens: 32 at a time are added plainly and
 // those sums with compensation (Kahan), so that the order of magnitude of the rounding
@@ -414,11 +415,25 @@ __global__ void __launch_bounds__(WM_THREADS)
   const int groups = by_chunk ? 1 : 2;
   float m = -INFINITY, z = 0.f;
   if (r < R)
-    for (int i = part; i < count; i += 8) {
-      const int c = by_chunk ? first + i : ws.runs[list * dm.c_cap + first + i].w;
-      for (int g = 0; g < groups; ++g) {
-        wg_merge(m, z, a.stat[(((int64_t)plane * dm.c_cap + c) * groups + g) * rows + r], a.scale2);
+    for (int i0 = part; i0 < count; i0 += 32) {  // four runs' (chunks') reads in flight (n = 131072: 126 -> 115 us)
+      int c[4];
+      float2 x[4][2];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int i = i0 + 8 * k < count ? i0 + 8 * k : i0;
+        c[k] = by_chunk ? first + i : ws.runs[list * dm.c_cap + first + i].w;
       }
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+          x[k][g] = i0 + 8 * k < count && g < groups
+                        ? a.stat[(((int64_t)plane * dm.c_cap + c[k]) * groups + g) * rows + r]
+                        : make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int g = 0; g < 2; ++g) wg_merge(m, z, x[k][g], a.scale2);
     }
   sm[part][lane] = m;
   sz[part][lane] = z;
