@@ -41,15 +41,16 @@ AttendPlan attend_plan(const jacap_layout* L) {
   const int64_t units = (int64_t)L->num_seqs * L->num_layers * L->num_kv_heads, ctas = units * p.nrb;
   const int64_t most = L->max_seqlen;
   // bf16: the least that a split may have (the kernel chooses from the live lengths); a split's sums,
-  // written and read by the join, stay an eighth of its K and V. float32: of the numbers of splits that
-  // leave 128 tokens or more, the one whose rounds of CTAs (three, two or one on an SM) end first, with F32_EXTRA
-  // tokens' time for a CTA's start and end.
+  // written and read by the join, stay an eighth of its K and V. float32: of the splits of 128 tokens or more
+  // that fill one to four rounds of CTAs (three, two or one on an SM), or none, those whose last round ends
+  // first, with F32_EXTRA tokens' time for a CTA's start and end (64 to 512 measured alike).
   int64_t chunk = std::max<int64_t>(256, std::min(rows, block) * 16);
   if (!bf) {
     const int64_t places = 152 * (block == 8 ? 3 : (block == 16 ? 2 : 1));
     int64_t best = INT64_MAX;
-    for (int64_t k = 1; k <= 1024 && (k == 1 || (most + k - 1) / k >= 128); ++k) {
-      const int64_t c = ((most + k - 1) / k + 63) / 64 * 64, items = (most + c - 1) / c * ctas;
+    for (int64_t rounds = 0; rounds <= 4; ++rounds) {
+      const int64_t k = std::max<int64_t>(1, rounds * places / ctas);
+      const int64_t c = std::max<int64_t>(128, ((most + k - 1) / k + 63) / 64 * 64), items = (most + c - 1) / c * ctas;
       const int64_t time = (items + places - 1) / places * (c + F32_EXTRA);
       if (time < best) best = time, chunk = c;
     }
