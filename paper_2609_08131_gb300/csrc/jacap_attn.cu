@@ -46,7 +46,7 @@ AttendPlan attend_plan(const jacap_layout* L) {
   // first, with F32_EXTRA tokens' time for a CTA's start and end (64 to 512 measured alike).
   int64_t chunk = std::max<int64_t>(256, std::min(rows, block) * 16);
   if (!bf) {
-    const int64_t places = 152 * (block == 8 ? 3 : (block == 16 ? 2 : 1));
+    const int64_t places = 152 * (block <= 8 ? 3 : (block == 16 ? 2 : 1));
     int64_t best = INT64_MAX;
     for (int64_t rounds = 0; rounds <= 4; ++rounds) {
       const int64_t k = std::max<int64_t>(1, rounds * places / ctas);

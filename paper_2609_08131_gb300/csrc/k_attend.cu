@@ -46,12 +46,12 @@
 // shorter splits and the requests' last splits dealt last (217 to 222 us).
 //
 // float32: CUDA cores, as the tensor cores would round the inputs. Up to 16 rows a warp takes
-// 8 of a tile's tokens for all rows of the CTA (8 or 16), four lanes to a token's dot
+// 8 of a tile's tokens for all rows of the CTA (4, 8 or 16), four lanes to a token's dot
 // products, and keeps a maximum, sums and accumulators of its own, so that tiles need no
 // barrier but the one that says they have landed; the warps are joined at the end. More rows
 // are a product of tiles (attend_f32_rows_kernel). Measured, 8 KV heads: 5 rows over 5473 tokens
 // in two requests 32 us (45 MB: 7 us at the copy rate; the splits' start and end and the join are
-// the rest), over 32768 tokens 76 us (268 MB: 40 us); 4 requests of 4096 tokens with 12 rows 84 us,
+// the rest), one row over 32768 tokens 57 us (268 MB: 40 us; with eight rows to a block 76 us); 4 requests of 4096 tokens with 12 rows 84 us,
 // 25 rows 157 us; 2 requests with 64 rows 94 us, 256 rows 275 us (8.6 GFLOP: 115 us at 75 TFLOP/s;
 // 574 us with 32 rows to a block, which read shared memory four times for as many multiply-adds).
 #include "jacap_dev.cuh"
@@ -882,7 +882,7 @@ __global__ void __launch_bounds__(AtCfg<NB>::THREADS, 3 - NB)
 }
 
 // ------------------------------------------------------------- float32 ----
-// Up to 8 rows: K and V's arrival bounds it; four warps and tiles of 32 tokens, three CTAs per SM. More: the reads
+// Up to 4 or 8 rows: K and V's arrival bounds it; four warps and tiles of 32 tokens, three CTAs per SM. More: the reads
 // of shared memory that feed the multiply-adds; up to 16 rows two such CTAs (12 rows: 84 us, with 32 rows to a block
 // 152).
 template <int RB>
@@ -890,7 +890,7 @@ struct AfCfg {
   static constexpr int WARPS = 4, THREADS = 32 * WARPS, TOK = 8 * WARPS, LDK = D + 4;
   static constexpr int KF = TOK * LDK, VF = TOK * D;  // floats per stage
   static constexpr size_t SMEM = (size_t)(RB * D + 2 * (KF + VF) + WARPS * 8 * RB + 2 * WARPS * RB) * 4;
-  static constexpr int PER_SM = RB == 8 ? 3 : 2;
+  static constexpr int PER_SM = RB <= 8 ? 3 : 2;
 };
 
 template <int RB>
@@ -973,7 +973,7 @@ __global__ void __launch_bounds__(AfCfg<RB>::THREADS, AfCfg<RB>::PER_SM)
       float s[RB];
 #pragma unroll
       for (int r = 0; r < RB; ++r) s[r] = 0.f;
-#pragma unroll 1
+#pragma unroll 2
       for (int k = 0; k < D; k += 16) {
         const float4 kk = *(const float4*)(kt + k);
 #pragma unroll
@@ -1021,7 +1021,7 @@ __global__ void __launch_bounds__(AfCfg<RB>::THREADS, AfCfg<RB>::PER_SM)
       __syncwarp();
       const float* vt = vs + (i & 1) * AF_VF + 8 * warp * D + 4 * lane;
       const int nt8 = left < 8 ? left : 8;
-#pragma unroll 1
+#pragma unroll 4
       for (int j = 0; j < nt8; ++j) {
         const float4 vv = *(const float4*)(vt + j * D);
 #pragma unroll
@@ -1284,7 +1284,7 @@ static cudaError_t launch_f32(const Dims& dm, const AttendArgs& a, const int32_t
   return launch_pdl(true, attend_f32_kernel<RB>, grid, C::THREADS, C::SMEM, st, dm, a, cu);
 }
 
-static int attend_f32_rows(int rows) { return rows <= 8 ? 8 : (rows <= 16 ? 16 : (rows <= 64 ? 64 : 128)); }
+static int attend_f32_rows(int rows) { return rows <= 4 ? 4 : rows <= 8 ? 8 : (rows <= 16 ? 16 : (rows <= 64 ? 64 : 128)); }
 int attend_row_block(int dtype, int rows) { return dtype == 1 ? (rows <= 128 ? 128 : 256) : attend_f32_rows(rows); }
 
 int attend_part_rows(int rows) { return rows <= 32 ? 32 : (rows <= 64 ? 64 : 128); }
@@ -1300,7 +1300,8 @@ cudaError_t launch_attend(const CUtensorMap* maps, const Dims& dm, int dtype, co
     else if (R <= 128) JACAP_TRY((launch_bf16<1, 1>(maps, dm, a, cu, blocks, sms, st)));
     else JACAP_TRY((launch_bf16<1, 2>(maps, dm, a, cu, blocks, sms, st)));
   } else {
-    if (R <= 8) JACAP_TRY(launch_f32<8>(dm, a, cu, (int)blocks, st));
+    if (R <= 4) JACAP_TRY(launch_f32<4>(dm, a, cu, (int)blocks, st));
+    else if (R <= 8) JACAP_TRY(launch_f32<8>(dm, a, cu, (int)blocks, st));
     else if (R <= 16) JACAP_TRY(launch_f32<16>(dm, a, cu, (int)blocks, st));
     else if (R <= 64) JACAP_TRY(launch_f32_rows<256>(dm, a, cu, (int)blocks, st));
     else JACAP_TRY(launch_f32_rows<512>(dm, a, cu, (int)blocks, st));
