@@ -29,8 +29,8 @@ constexpr int AT_DRAFTS_MAX = 64;
 // `nrb` row blocks. Depends on the layout alone (a GB300 has 152 SMs), so that the
 // workspace does.
 struct AttendPlan {
-  int chunk, nsplit, nrb;
-  size_t status, counts, opart, mlpart, total;
+  int chunk, nsplit, nrb, block, edge;
+  size_t status, counts, nsps, opart, mlpart, total;
 };
 constexpr int64_t F32_EXTRA = 128;
 AttendPlan attend_plan(const jacap_layout* L) {
@@ -40,8 +40,8 @@ AttendPlan attend_plan(const jacap_layout* L) {
   p.nrb = (rows + block - 1) / block;
   const int64_t units = (int64_t)L->num_seqs * L->num_layers * L->num_kv_heads, ctas = units * p.nrb;
   const int64_t most = L->max_seqlen;
-  // bf16: the least that a split may have (the kernel chooses from the live lengths); a split's sums,
-  // written and read by the join, stay an eighth of its K and V. float32: of the splits of 128 tokens or more
+  // bf16: the least that a CTA's share may have (the kernel shares out the live tokens); a split's sums,
+  // written and read by the join, stay an eighth of its K and V on the average. float32: of the splits of 128 tokens or more
   // that fill one to four rounds of CTAs (three, two or one on an SM), or none, those whose last round ends
   // first, with F32_EXTRA tokens' time for a CTA's start and end (64 to 512 measured alike).
   int64_t chunk = std::max<int64_t>(256, std::min(rows, block) * 16);
@@ -58,9 +58,13 @@ AttendPlan attend_plan(const jacap_layout* L) {
   chunk = std::min<int64_t>((chunk + 63) / 64 * 64, (most + 63) / 64 * 64);
   p.chunk = (int)chunk;
   p.nsplit = (int)((most + chunk - 1) / chunk);
+  p.block = block;
+  p.edge = std::max(4, std::min(rows, block) / 16);
+  if (bf) p.nsplit = (most + 63) / 64 + 1 < 2 * p.edge ? 1 : p.nsplit + 2;  // a share's borders are anywhere in a unit
   size_t o = 0;
   p.status = o; o += 64;
   p.counts = o; o = align_up(o + (p.nsplit > 1 ? (size_t)units * 4 : 0));
+  p.nsps = o; o = align_up(o + (bf ? (size_t)ctas * 4 : 0));
   const size_t parts = p.nsplit > 1 ? (size_t)units * p.nsplit : 0, prows = attend_part_rows(rows);
   p.opart = o; o = align_up(o + parts * ((rows + prows - 1) / prows * prows) * D * 4);
   p.mlpart = o; o = align_up(o + parts * rows * 8);
@@ -230,9 +234,11 @@ jacap_status jacap_attend(const jacap_layout* layout, const jacap_attention* att
   a.prows = attend_part_rows(dm.G * dm.window);
   a.tdiv = dm.window > 1 ? 0xffffffffu / (uint32_t)dm.window + 1u : 0u;
   a.chunk = p.chunk, a.nsplit = p.nsplit, a.nrb = p.nrb, a.max_seqlen = layout->max_seqlen;
+  a.block = p.block, a.least = p.chunk / 64, a.edge = p.edge;
   uint8_t* b = (uint8_t*)ws;
   a.status = (uint32_t*)(b + p.status);
   a.counts = (int32_t*)(b + p.counts);
+  a.nsps = (int32_t*)(b + p.nsps);
   a.opart = (float*)(b + p.opart);
   a.mlpart = (float*)(b + p.mlpart);
   CUtensorMap maps[4];

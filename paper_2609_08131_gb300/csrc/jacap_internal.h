@@ -183,13 +183,15 @@ struct AttendArgs {
   int64_t os[4], kds[4], vds[4];  // strides of o and of the drafted K and V: request, layer, head, token
   int64_t ls[3];              // of lse: request, layer, head
   float scale2;               // scale log2 e, recentred for the tensor cores' truncation
-  int chunk, nsplit, nrb, max_seqlen;  // tokens per split (bf16: at least), splits of the longest request, row blocks
-  int places;                 // CTAs that the SMs hold at a time (bf16)
+  int chunk, nsplit, nrb, max_seqlen;  // tokens per split (float32), splits of a request at most, row blocks
+  int block;                  // rows of a row block
+  int least, edge;            // bf16: least tiles of a CTA's share, and between a split's border and a unit's start or end
   int prows;                  // rows of a block of the splits' sums (attend_part_rows)
   uint32_t tdiv;              // 2^32 / window, rounded up (window > 1)
   float *opart, *mlpart;      // the splits' sums [units][nsplit][row blocks][32][prows][4], and their
                               // [units][nsplit][G window][2] (maximum, sum)
   int32_t* counts;            // [units] splits done, where the last one joins them (zero between calls)
+  int32_t* nsps;              // bf16: [units][row blocks] splits of this call
   uint32_t* status;
 };
 int attend_row_block(int dtype, int rows);  // rows of a CTA

@@ -112,6 +112,26 @@ struct AtUnit {
   int tok0, tok1, ncache, nt;  // this split's tokens, its tiles of cached tokens and in all (`tile` tokens each)
   int r0;                      // the CTA's first row
 };
+// A request's live cached tokens and queries, clamped to what there can be (`ok`: nothing had to be).
+struct AtLive {
+  int64_t start;
+  int n, rows;
+  bool ok;
+};
+__device__ __forceinline__ AtLive at_live(const Dims& dm, const AttendArgs& a, const int32_t* cu, int s) {
+  AtLive x;
+  const int64_t start = cu[s], end = cu[s + 1];
+  const int given = a.lengths != nullptr ? a.lengths[s] : 0;
+  const int want = a.draft_lens != nullptr ? a.draft_lens[s] : dm.window;
+  const bool ok = start >= 0 && end >= start && end <= dm.Ntot;
+  const int64_t room = ok ? (end - start < a.max_seqlen ? end - start : a.max_seqlen) : 0;
+  const int64_t live = a.lengths != nullptr ? (int64_t)given : end - start;
+  x.start = ok ? start : 0;
+  x.n = (int)(live < 0 ? 0 : (live < room ? live : room));
+  x.rows = want < 0 ? 0 : (want < dm.window ? want : dm.window);
+  x.ok = ok && live == x.n && want == x.rows;
+  return x;
+}
 __device__ __forceinline__ AtUnit at_unit(const Dims& dm, const AttendArgs& a, const int32_t* cu, uint32_t u, int split,
                                           int tile, int chunk) {  // (32-bit divisions: a 64-bit one takes ~300 cycles)
   AtUnit x;
@@ -121,16 +141,11 @@ __device__ __forceinline__ AtUnit at_unit(const Dims& dm, const AttendArgs& a, c
   x.s = (int)(u - plane * dm.S);
   x.l = (int)(plane / (uint32_t)dm.Hkv);
   x.g = (int)(plane - x.l * dm.Hkv);
-  const int64_t start = cu[x.s], end = cu[x.s + 1];
-  const int given = a.lengths != nullptr ? a.lengths[x.s] : 0;
-  const int want = a.draft_lens != nullptr ? a.draft_lens[x.s] : dm.window;
-  const bool ok = start >= 0 && end >= start && end <= dm.Ntot;
-  const int64_t room = ok ? (end - start < a.max_seqlen ? end - start : a.max_seqlen) : 0;
-  const int64_t live = a.lengths != nullptr ? (int64_t)given : end - start;
-  x.t0 = ok ? start : 0;
-  x.n = (int)(live < 0 ? 0 : (live < room ? live : room));
-  x.rows = want < 0 ? 0 : (want < dm.window ? want : dm.window);
-  if (!ok || live != x.n || want != x.rows) atomicOr(a.status, (uint32_t)ST_INVALID);
+  const AtLive live = at_live(dm, a, cu, x.s);
+  if (!live.ok) atomicOr(a.status, (uint32_t)ST_INVALID);
+  x.t0 = live.start;
+  x.n = live.n;
+  x.rows = live.rows;
   x.nd = a.kd != nullptr ? x.rows : 0;
   x.nsp = x.n > chunk ? (x.n - 1) / chunk + 1 : 1;
   x.tok0 = split * chunk;
@@ -159,12 +174,6 @@ template <int NB>
 constexpr size_t at_smem() { return 233472 / (3 - NB) - 1024; }
 static_assert(at_used<1>() <= at_smem<1>() && at_used<2>() <= at_smem<2>(), "shared memory");
 static_assert(128 * D * 2 >= 128 * 64 * 4, "the rows' space holds half the channels of the accumulators (copies)");
-// words beside the status word (zero between calls): items dealt beyond the first of each CTA,
-// CTAs that stopped claiming
-enum { AT_NEXT = 4, AT_DONE = 5 };
-// and the tokens per split that the call chose (for the joining kernel)
-enum { AT_CHUNK = 6 };
-
 // The head of a unit's row r (r / window, exact for r below 2^16).
 __device__ __forceinline__ int at_head(const Dims& dm, const AttendArgs& a, int r) {
   return dm.window == 1 ? r : (int)__umulhi((uint32_t)r, a.tdiv);
@@ -296,50 +305,20 @@ __device__ __forceinline__ void at_bad(const Dims& dm, const AttendArgs& a, cons
   }
 }
 
-// Tokens per split (a warp; every CTA finds the same from the live lengths): of 32 sizes around an
-// even share of a place (two CTAs on an SM, or one), at least a.chunk (the smallest that the workspace
-// has room for), the one that finishes first by a simple account: items that all run at once take the
-// largest one's tokens, more than that the places' mean share and half an item at the end, and each
-// `extra` tokens' time to change over to.
-// Measured, 8 units of 131011 tokens: 38 splits of 3456 tokens 88 us, 114 of 1152 103 us; 128 units of about
-// 2100: two splits 33 us, four 40 us. 128 units of 46 to 16383 tokens: 5 to 80 rows 97 us with `extra` 300,
-// 101 to 113 with 192; 320 rows 216 us with 700, 224 with 400.
-__device__ __forceinline__ int at_chunk(const Dims& dm, const AttendArgs& a, const int32_t* cu, int lane, float extra,
-                                        int* longest_out) {
-  const auto tokens_of = [&](int s) {
-    const int64_t room = (int64_t)cu[s + 1] - cu[s], live = a.lengths != nullptr ? (int64_t)a.lengths[s] : room;
-    return (int)max((int64_t)0, min(live, min(room, (int64_t)a.max_seqlen)));
-  };
-  const int mine = lane < dm.S ? tokens_of(lane) : 0;  // of the first 32 requests
-  int longest = mine;
-  float tokens = (float)mine;
-  for (int s = lane + 32; s < dm.S; s += 32) {
-    const int n = tokens_of(s);
-    longest = max(longest, n);
-    tokens += (float)n;
-  }
-  longest = __reduce_max_sync(0xffffffffu, longest);
-  *longest_out = longest;
-#pragma unroll
-  for (int off = 16; off >= 1; off >>= 1) tokens += __shfl_xor_sync(0xffffffffu, tokens, off);
-  if (longest <= a.chunk) return a.chunk;
-  const float same = (float)(dm.L * dm.Hkv * a.nrb), work = tokens * same, share = work / (float)a.places;
-  // (sizes from an eighth of the share to 27 times it)
-  int c = (int)fminf(share * exp2f(0.25f * (float)(lane - 12)), (float)longest) / AT_TOK * AT_TOK + AT_TOK;
-  c = max(c, a.chunk);
-  const float per = 1.f / (float)c;
-  float items = 0.f;
-  for (int s0 = 0; s0 < dm.S; s0 += 32) {
-    const int n32 = s0 == 0 ? mine : (s0 + lane < dm.S ? tokens_of(s0 + lane) : 0);
-    const int left = min(32, dm.S - s0);
-    for (int k = 0; k < left; ++k) items += fmaxf(1.f, ceilf((float)__shfl_sync(0xffffffffu, n32, k) * per));
-  }
-  items *= same;
-  const float most = (float)min(c, longest), places = (float)a.places;
-  const float time = items <= places ? most + extra : (work + items * extra) / places + 0.5f * most + extra;
-  const uint32_t best = __reduce_min_sync(0xffffffffu, (__float_as_uint(time) & ~31u) | (uint32_t)lane);
-  return __shfl_sync(0xffffffffu, c, (int)(best & 31u));
+// How the work is shared out (bf16): all tiles of all units lie on a line, plane by plane, row block by row block and
+// request by request, each with its cost (AT_START more tiles for a unit's start), and CTA k takes positions
+// [k per, (k + 1) per). A border that is fewer than `edge` tiles from a unit's start or end moves there, so that short
+// units stay whole and no split is a sliver. A unit whose first tile is at p0 then has its
+// first split in CTA floor((p0 + (edge - 1) cost) / per), and a further one in each CTA up to the one of position
+// p0 + (tiles - edge) cost. (Items dealt one by one as CTAs became free, of a size chosen by an account of their
+// number: 37 and 216 us where this takes 36.5 and 168, with one token in 16 slots and 16 trees; one
+// token over 16 requests of 46 to 16383 97 and 82.)
+template <int NB>
+__device__ __forceinline__ uint32_t at_cost(const Dims& dm, int rb) {  // of a tile; measured 0.86 and 0.63 us
+  return NB == 1 ? 1u : (dm.G * dm.window - rb * 256 > 128 ? 4u : 3u);
 }
+template <int NB>
+constexpr uint32_t AT_START = NB == 1 ? 3 : 4;
 
 template <int REP, int NB>
 __global__ void __launch_bounds__(AtCfg<NB>::THREADS, 3 - NB)
@@ -415,29 +394,86 @@ __global__ void __launch_bounds__(AtCfg<NB>::THREADS, 3 - NB)
 
   if (warp == 0) {
     // ------------------------------------------------ TMA producer --------
-    const uint32_t units = (uint32_t)dm.L * dm.Hkv * dm.S;
-    int longest;
-    const int chunk = at_chunk(dm, a, cu, lane, NB == 1 ? 300.f : 700.f, &longest);
+    const auto tiles_of = [&](int s) {  // as at_unit counts them, at least one
+      const AtLive x = at_live(dm, a, cu, s);
+      return (uint32_t)max(1, (x.n > 0 ? (x.n - 1) / AT_TOK + 1 : 0) + (a.kd != nullptr && x.rows > 0 ? 1 : 0));
+    };
+    const uint32_t planes = (uint32_t)dm.L * dm.Hkv;
+    uint32_t mine = 0, tp = 0, csum = 0;  // virtual tiles of request `lane`, of a plane, cost of a plane's tiles
+    for (int s0 = 0; s0 < dm.S; s0 += 32) {
+      const uint32_t v = s0 + lane < dm.S ? tiles_of(s0 + lane) + AT_START<NB> : 0u;
+      if (s0 == 0) mine = v;
+      tp += __reduce_add_sync(0xffffffffu, v);
+    }
+    for (int rb = 0; rb < a.nrb; ++rb) csum += at_cost<NB>(dm, rb);
+    const uint32_t total = planes * tp * csum;  // (fewer than 2^31: checked by the host)
+    const uint32_t per = max((total + gridDim.x - 1) / gridDim.x, (uint32_t)a.least * (NB == 1 ? 1u : 4u));
+    const uint32_t w0 = blockIdx.x * per, w1 = min(w0 + per, total);
+    // the unit at w0: plane, row block, request, and the position where it starts
+    uint32_t plane = w0 / (tp * csum), pos = plane * tp * csum;
+    int rb = 0, s = 0;
+    if (w0 < total) {
+      for (; w0 - pos >= tp * at_cost<NB>(dm, rb); ++rb) pos += tp * at_cost<NB>(dm, rb);
+      const uint32_t c = at_cost<NB>(dm, rb), v = (w0 - pos) / c;
+      uint32_t before = 0;
+      for (int s0 = 0; s0 < dm.S; s0 += 32) {
+        const uint32_t own = s0 == 0 ? mine : (s0 + lane < dm.S ? tiles_of(s0 + lane) + AT_START<NB> : 0u);
+        uint32_t sum = own;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const uint32_t x = __shfl_up_sync(0xffffffffu, sum, o);
+          if (lane >= o) sum += x;
+        }
+        const uint32_t past = __ballot_sync(0xffffffffu, before + sum > v);
+        if (past != 0) {
+          const int at = __ffs((int)past) - 1;
+          s = s0 + at;
+          before += __shfl_sync(0xffffffffu, sum - own, at);
+          break;
+        }
+        before += __shfl_sync(0xffffffffu, sum, 31);
+      }
+      pos += before * c;
+    }
     if (lane == 0) {
-      const uint32_t most = longest > chunk ? (longest - 1) / chunk + 1 : 1;
-      const uint32_t total = units * a.nrb * most;  // (fewer than 2^31)
-      if (blockIdx.x == 0) a.status[AT_CHUNK] = (uint32_t)chunk;
       uint32_t n = 0, published = 0;  // loads, items
       bool ok = true;
       AtUnit next;
-      uint32_t at = blockIdx.x;
-      // The next item that is not behind its request's last split, into `next` and the queue.
-      // Items are dealt as CTAs become free; row blocks of the same tokens follow each other.
+      // This CTA's next item, into `next` and the queue.
       auto publish = [&]() {
-        for (;; at = gridDim.x + atomicAdd(a.status + AT_NEXT, 1u)) {
-          if (at >= total) {
+        for (;;) {
+          if (pos >= w1) {
             next.nt = -1;
             break;
           }
-          const uint32_t rest = a.nrb == 1 ? at : at / (uint32_t)a.nrb, split = most == 1 ? 0u : rest / units;
-          next = at_unit(dm, a, cu, rest - split * units, (int)split, AT_TOK, chunk);
-          next.r0 = (int)(at - rest * a.nrb) * (128 * NB);
-          if (next.split < next.nsp) break;
+          next = at_unit(dm, a, cu, plane * dm.S + s, 0, AT_TOK, INT32_MAX);
+          next.r0 = rb * (128 * NB);
+          const uint32_t nt = max(next.nt, 1), c = at_cost<NB>(dm, rb), p0 = pos + AT_START<NB> * c, edge = a.edge;
+          const uint32_t first = (p0 + (min(edge, nt) - 1) * c) / per, last = nt >= edge ? (p0 + (nt - edge) * c) / per : 0;
+          const int at = rb + a.nrb * (int)next.u, split = (int)blockIdx.x - (int)first;
+          pos = p0 + nt * c;
+          if (++s == dm.S) {
+            s = 0;
+            if (++rb == a.nrb) rb = 0, ++plane;
+          }
+          next.nsp = last > first ? (int)(last - first) + 1 : 1;
+          if (next.nsp > a.nsplit) {  // (ranges of cu_seqlens that overlap)
+            atomicOr(a.status, (uint32_t)ST_INVALID);
+            next.nsp = a.nsplit;
+          }
+          if (split < 0 || split >= next.nsp) continue;
+          next.split = split;
+          if (split == 0) a.nsps[at] = next.nsp;
+          if (next.nt > 0) {
+            const int ta = split == 0 ? 0 : (int)((w0 - p0 + c - 1) / c);
+            const int tb = split == next.nsp - 1 ? (int)nt : (int)((w0 + per - p0 + c - 1) / c);
+            const int cached = next.ncache;
+            next.tok0 = ta * AT_TOK;
+            next.tok1 = min(next.n, tb * AT_TOK);
+            next.ncache = max(0, min(tb, cached) - ta);
+            next.nt = tb - ta;
+          }
+          break;
         }
         const int q = published % AT_QUEUE;
         if (published >= AT_QUEUE && !mbar_wait(smem_u32(&sh.qempty[q]), ((published / AT_QUEUE) & 1) ^ 1, ws, abort))
@@ -454,12 +490,8 @@ __global__ void __launch_bounds__(AtCfg<NB>::THREADS, 3 - NB)
         const AtUnit x = next;
         // the item after it, a few loads later: its rows are on their way long before they are needed
         const int when = 2 * x.nt < 4 ? 2 * x.nt : 4;
-        auto claim = [&]() {
-          at = gridDim.x + atomicAdd(a.status + AT_NEXT, 1u);
-          return publish();
-        };
         for (int i = 0; ok && i < 2 * x.nt; ++i, ++n) {  // K and V of each tile
-          if (i == when && !(ok = claim())) break;
+          if (i == when && !(ok = publish())) break;
           const int st = n % AT_RING;
           if (n >= AT_RING && !mbar_wait(smem_u32(&sh.empty[st]), ((n / AT_RING) & 1) ^ 1, ws, abort)) {
             ok = false;
@@ -478,17 +510,11 @@ __global__ void __launch_bounds__(AtCfg<NB>::THREADS, 3 - NB)
             tma_load_5d(dst + AT_BOX, map, 64, 0, x.g, x.l, x.s, bar);
           }
         }
-        if (ok && when == 2 * x.nt) ok = claim();
+        if (ok && when == 2 * x.nt) ok = publish();
       }
       // what is under way lands before the CTA leaves
       for (uint32_t k = n > AT_RING ? n - AT_RING : 0; k < n; ++k)
         mbar_wait(smem_u32(&sh.full[k % AT_RING]), (k / AT_RING) & 1, ws, nullptr);
-      // the last CTA to stop claiming leaves the counters as it found them
-      __threadfence();
-      if (atomicAdd(a.status + AT_DONE, 1u) == gridDim.x - 1) {
-        a.status[AT_NEXT] = 0u;
-        a.status[AT_DONE] = 0u;
-      }
     }
   } else if (warp == 1) {
     // ------------------------------------------------ MMA issuer ----------
@@ -1240,8 +1266,8 @@ __global__ void __launch_bounds__(AJ_THREADS)
   const int w = blockIdx.x * (AJ_WARPS / W) + warp / W, units = dm.L * dm.Hkv * dm.S;
   const bool real = w < units * groups;
   const int u = real ? w / groups : 0;
-  const int chunk = sizeof(T) == 2 ? (int)a.status[AT_CHUNK] : a.chunk;
-  AtUnit x = at_unit(dm, a, cu, u, 0, AT_TOK, chunk);
+  AtUnit x = at_unit(dm, a, cu, u, 0, AT_TOK, a.chunk);
+  if constexpr (sizeof(T) == 2) x.nsp = a.nsps[a.nrb * u + (w - u * groups) * NR / a.block];
   const bool inside = sizeof(T) == 2 && at_joins_inside(x.nsp, R);  // that unit is done
   at_join<T, W, NR>(dm, a, x, real && !inside ? (w - u * groups) * NR : R, warp % W,
                     s_o + (W > 1 ? warp * NR * 32 : 0), s_z[warp]);
@@ -1260,13 +1286,12 @@ static cudaError_t launch_join(const Dims& dm, const AttendArgs& a, const int32_
 
 // ------------------------------------------------------------- launchers ----
 template <int REP, int NB>
-static cudaError_t launch_bf16(const CUtensorMap* maps, const Dims& dm, const AttendArgs& args, const int32_t* cu,
+static cudaError_t launch_bf16(const CUtensorMap* maps, const Dims& dm, const AttendArgs& a, const int32_t* cu,
                                int64_t items, int sms, cudaStream_t st) {
   auto kern = attend_bf16_kernel<REP, NB>;
   JACAP_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)at_smem<NB>()));
-  AttendArgs a = args;
-  a.places = sms * (3 - NB);
-  return launch_pdl(true, kern, (int)(items < a.places ? items : a.places), AtCfg<NB>::THREADS, at_smem<NB>(), st, maps[0],
+  const int places = sms * (3 - NB);
+  return launch_pdl(true, kern, (int)(items < places ? items : places), AtCfg<NB>::THREADS, at_smem<NB>(), st, maps[0],
                     maps[1], maps[2], maps[3], dm, a, cu);
 }
 template <int NT>
@@ -1294,6 +1319,8 @@ cudaError_t launch_attend(const CUtensorMap* maps, const Dims& dm, int dtype, co
   const int R = dm.G * dm.window;
   const int64_t units = (int64_t)dm.L * dm.Hkv * dm.S, blocks = units * a.nsplit * a.nrb;
   if (blocks > INT32_MAX || units * R > INT32_MAX / 8) return cudaErrorInvalidValue;
+  // the positions on the line of tiles: at most 4 for each of a request's tiles, and of AT_START more
+  if ((dm.Ntot / AT_TOK + 8 * (int64_t)dm.S) * dm.L * dm.Hkv * a.nrb > INT32_MAX / 4) return cudaErrorInvalidValue;
   if (dtype == 1) {
     if (R <= 32) JACAP_TRY((launch_bf16<4, 1>(maps, dm, a, cu, blocks, sms, st)));
     else if (R <= 64) JACAP_TRY((launch_bf16<2, 1>(maps, dm, a, cu, blocks, sms, st)));
