@@ -8,12 +8,12 @@
 // row that sees nothing has o = 0 and lse = -inf.
 //
 // K and V are read once, in one pass with a running maximum and sum. A unit's tokens are
-// split into items (`chunk` tokens each, the drafted ones with the last), which leave
-// unnormalised sums to be joined where a request has several splits.
+// split into items (the drafted ones with the last), which leave unnormalised sums to be
+// joined where a request has several splits.
 //
-// bf16: persistent CTAs to which items are dealt as they become free, so that the live
-// lengths need not be known to the host and a CTA's ring of tiles never runs dry between
-// two items (one CTA per item: 158 us instead of 92 for the long chain below). A CTA's
+// bf16: persistent CTAs with even shares of the tiles, which each works out from the live
+// lengths, so that the host need not know them and a CTA's ring of tiles never runs dry
+// between two items (one CTA per item: 158 us instead of 92 for the long chain below). A CTA's
 // roles: a TMA producer, an MMA issuer, softmax warps with a row per lane, and warps that
 // fetch the next item's rows. R = G T rows are an M = 128 operand whatever R is: the
 // memory's time for a tile (64 tokens, 32 KB of K and V: ~700 SM cycles at the copy rate
@@ -23,8 +23,7 @@
 // copies, halves), each with a maximum and a sum of its own; the other tokens' weights are
 // zero in its lanes, and the copies are joined at the item's end. So a warp has 16 columns
 // per tile instead of 64, and no two warps ever wait for each other. Up to 256 rows share a
-// CTA's tiles as two blocks of 128 (one CTA per SM); beyond that, items of the same tokens
-// follow each other and the second reads K and V from L2.
+// CTA's tiles as two blocks of 128 (one CTA per SM); beyond that K and V are read again.
 // The weights p are rounded to bf16 for the second product (the sums Z are not): of an
 // output of many comparable terms that is an error of about the output's own rounding.
 // The maximum is only raised when a logit passes it by 2^8, which a rescaling of the
@@ -38,12 +37,12 @@
 // Measured (32 query heads on 8, 92 us = 5.8 TB/s of K and V for 8 drafted tokens over 131011
 // cached ones; 37 us = 3.7 TB/s for one token in 16 slots of 2100, of which ~8 us are the
 // launch and the first tiles' way; 9 us for one token over 37): bound by memory up to 128 rows.
-// 64 drafted tokens of 5 heads a group, 320 rows, over 110000 tokens in 16 requests: 216 us for
-// 138 GFLOP. There a tile of 256 rows takes ~1500 cycles: the products ~1280 (S reads its rows from
+// 64 drafted tokens of 5 heads a group, 320 rows, over 110000 tokens in 16 requests: 168 us for
+// 138 GFLOP and 842 MB (K and V twice, 5.4 TB/s). A tile of 256 rows takes ~1500 cycles: the products ~1280 (S reads its rows from
 // shared memory again for every 64 tokens, 48 cycles for each 128 x 64 x 16), and the softmax
 // ~1150 with two warps per scheduler, which overlap but for the waits between them. Tried and
-// left out: an MMA issuer per block (218 us), the barriers asked ahead of the issue (226 us),
-// shorter splits and the requests' last splits dealt last (217 to 222 us).
+// left out, of 216 us at the time: an MMA issuer per block (218), the barriers asked ahead of the
+// issue (226).
 //
 // float32: CUDA cores, as the tensor cores would round the inputs. Up to 16 rows a warp takes
 // 8 of a tile's tokens for all rows of the CTA (4, 8 or 16), four lanes to a token's dot
