@@ -398,14 +398,18 @@ __global__ void __launch_bounds__(AtCfg<NB>::THREADS, 3 - NB)
       return (uint32_t)max(1, (x.n > 0 ? (x.n - 1) / AT_TOK + 1 : 0) + (a.kd != nullptr && x.rows > 0 ? 1 : 0));
     };
     const uint32_t planes = (uint32_t)dm.L * dm.Hkv;
-    uint32_t mine = 0, tp = 0, csum = 0;  // virtual tiles of request `lane`, of a plane, cost of a plane's tiles
+    uint32_t mine = 0, csum = 0;  // virtual tiles of request `lane`, cost of a tile of a plane
+    uint64_t tiles = 0;           // virtual tiles of a plane
     for (int s0 = 0; s0 < dm.S; s0 += 32) {
       const uint32_t v = s0 + lane < dm.S ? tiles_of(s0 + lane) + AT_START<NB> : 0u;
       if (s0 == 0) mine = v;
-      tp += __reduce_add_sync(0xffffffffu, v);
+      tiles += __reduce_add_sync(0xffffffffu, v);
     }
     for (int rb = 0; rb < a.nrb; ++rb) csum += at_cost<NB>(dm, rb);
-    const uint32_t total = planes * tp * csum;  // (fewer than 2^31: checked by the host)
+    // below 2^31 (checked by the host), unless ranges of cu_seqlens overlap: nothing is done then
+    const bool fits = tiles * planes * csum <= (uint64_t)INT32_MAX;
+    if (!fits && lane == 0) atomicOr(a.status, (uint32_t)ST_INVALID);
+    const uint32_t tp = fits ? (uint32_t)tiles : 1u, total = fits ? planes * tp * csum : 0u;
     const uint32_t per = max((total + gridDim.x - 1) / gridDim.x, (uint32_t)a.least * (NB == 1 ? 1u : 4u));
     const uint32_t w0 = blockIdx.x * per, w1 = min(w0 + per, total);
     // the unit at w0: plane, row block, request, and the position where it starts
@@ -456,10 +460,6 @@ __global__ void __launch_bounds__(AtCfg<NB>::THREADS, 3 - NB)
             if (++rb == a.nrb) rb = 0, ++plane;
           }
           next.nsp = last > first ? (int)(last - first) + 1 : 1;
-          if (next.nsp > a.nsplit) {  // (ranges of cu_seqlens that overlap)
-            atomicOr(a.status, (uint32_t)ST_INVALID);
-            next.nsp = a.nsplit;
-          }
           if (split < 0 || split >= next.nsp) continue;
           next.split = split;
           if (split == 0) a.nsps[at] = next.nsp;

@@ -394,6 +394,25 @@ def test_attend_reports_lengths_out_of_range():
     att.check()  # the word was cleared
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("cu", [(0, 60, 50), (0, 50, 111), (-1, 50, 110)])
+def test_attend_reports_ranges_that_are_none(cu, dtype):
+    """A request whose range is not one of the cache's has no cached tokens, the other one its own."""
+    g = gen(12)
+    cache = make_cache(g, 2, 1, 4, 1, 3, (50, 60), dtype)
+    cache.cu_seqlens.copy_(torch.tensor(cu, dtype=torch.int32))
+    kd, vd = (randn(g, 2, 1, 1, 3, D, dtype=dtype) for _ in range(2))
+    att = api.CacheAttention(cache)
+    o, lse = att.run(k_draft=kd, v_draft=vd)
+    with pytest.raises(api.JacapError) as e:
+        att.check()
+    assert e.value.status == JACAP_ERR_INVALID_ARG
+    good = [0 <= cu[s] <= cu[s + 1] <= 110 for s in range(2)]
+    lengths = [cu[s + 1] - cu[s] if good[s] else 0 for s in range(2)]
+    cache.cu_seqlens.copy_(torch.tensor([max(0, c) for c in cu], dtype=torch.int32))
+    check_attend(cache, o, lse, kd, vd, lengths=lengths)
+
+
 # ------------------------------------------------------------------ weigh ----
 def weigh_plain(cache, lengths=None, q_lens=None, q_rows=None, lse=None, before=None):
     """weights and lse of every unit in 64 bits, with their bounds; NaN where nothing is written."""
