@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+import threading
 from dataclasses import dataclass
 
 import torch
@@ -210,7 +211,8 @@ class Rope:
         self._c.head_dim, self._c.rot_dim, self._c.interleaved = 128, self.rot_dim, int(self.interleaved)
         self._c.amplitude, self._c.turns = self.amplitude, self.turns.data_ptr()
         self._calls = {}  # arguments of calls by the tensors' shapes and strides (not their addresses)
-        self._last = self._call = None
+        self._last = None, None
+        self._lock = threading.Lock()
 
     def apply(self, q, k, positions, inverse: bool = False, inplace: bool = False, stream=None):
         """q, k: [..., heads, 128] (one of them may be None) with one or two leading axes,
@@ -219,34 +221,36 @@ class Rope:
         with ``inplace``. ``inverse`` turns back (and is the gradient)."""
         key = (None if q is None else (q.dtype, q.shape, q.stride()), None if k is None else (k.dtype, k.shape, k.stride()),
                positions.dtype, positions.shape, positions.stride(), inplace)
-        if key != self._last:  # (comparing with the call before is cheaper than a look-up)
+        last, call = self._last
+        if key != last:  # (comparing with the call before is cheaper than a look-up)
             call = self._calls.get(key)
             if call is None:
                 call = self._arguments(q, k, positions, inplace)
                 if len(self._calls) >= 64:
                     self._calls.clear()
                 self._calls[key] = call
-            self._last, self._call = key, call
+            self._last = key, call
         dev = self.device
         grad = torch.is_grad_enabled()
         if positions.device != dev or q is not None and (q.device != dev or grad and q.requires_grad) or \
                 k is not None and (k.device != dev or grad and k.requires_grad):
             raise ValueError(f"the tensors must be on {dev} and require no gradient, which this call does not give")
         if stream is None and dev.index == torch._C._cuda_getDevice():
-            return self._turn(q, k, positions, inverse, inplace, torch._C._cuda_getCurrentRawStream(dev.index))
-        return _enqueue(dev, stream, lambda st: self._turn(q, k, positions, inverse, inplace, st))
+            return self._turn(call, q, k, positions, inverse, inplace, torch._C._cuda_getCurrentRawStream(dev.index))
+        return _enqueue(dev, stream, lambda st: self._turn(call, q, k, positions, inverse, inplace, st))
 
-    def _turn(self, q, k, positions, inverse, inplace, stream):
-        S, T, qa, ka, ps, dtype = self._call
-        qy = ky = None
-        if q is not None:
-            qy = q if inplace else torch.empty_like(q)
-            qa.x, qa.y = q.data_ptr(), qy.data_ptr()
-        if k is not None:
-            ky = k if inplace else torch.empty_like(k)
-            ka.x, ka.y = k.data_ptr(), ky.data_ptr()
+    def _turn(self, call, q, k, positions, inverse, inplace, stream):
+        S, T, qa, ka, ps, dtype = call
+        qy = None if q is None else q if inplace else torch.empty_like(q)
+        ky = None if k is None else k if inplace else torch.empty_like(k)
         if S and T:
-            _check(jacap_rotate(self._c, dtype, S, T, positions.data_ptr(), ps, inverse, qa, ka, stream), "jacap_rotate")
+            with self._lock:  # the addresses are this call's until it returns (threads may share a Rope)
+                if q is not None:
+                    qa.x, qa.y = q.data_ptr(), qy.data_ptr()
+                if k is not None:
+                    ka.x, ka.y = k.data_ptr(), ky.data_ptr()
+                status = jacap_rotate(self._c, dtype, S, T, positions.data_ptr(), ps, inverse, qa, ka, stream)
+            _check(status, "jacap_rotate")
         return qy, ky
 
     def _arguments(self, q, k, positions, inplace):

@@ -124,6 +124,24 @@ def tol_of(before, positions, freq, amplitude):
     return rope_plain(before[..., 1:D + 1].transpose(1, 2), positions, freq, amplitude, 64, False, False)[1]
 
 
+def test_threads_share_a_rope():
+    from concurrent.futures import ThreadPoolExecutor
+    rope, g = api.Rope(device=DEV), gen(5)
+    data = [(randn(g, 64, 4, D, dtype=BF16), torch.randint(0, 9000, (64,), generator=g, device=DEV, dtype=torch.int32))
+            for _ in range(8)]
+    want = [rope.apply(x, None, at)[0] for x, at in data]
+    torch.cuda.synchronize()
+
+    def work(i):
+        with torch.cuda.stream(torch.cuda.Stream(device=DEV)):
+            got = [rope.apply(*data[i][:1], None, data[i][1])[0] for _ in range(200)]
+            torch.cuda.current_stream().synchronize()
+        return all(torch.equal(x, want[i]) for x in got)
+
+    with ThreadPoolExecutor(8) as pool:
+        assert all(pool.map(work, range(8)))
+
+
 def test_rope_turns_back_and_is_its_own_gradient():
     g, rope = gen(6), api.Rope(128, interleaved=True, device=DEV)
     x, y = randn(g, 50, 3, D), randn(g, 50, 3, D)
