@@ -460,7 +460,8 @@ __global__ void __launch_bounds__(PK_THREADS)
   const int64_t start = cu[s], end = cu[s + 1];
   if (start < 0 || end < start || end > dm.Ntot) return;  // the selection reports it
   const int64_t n = end - start, per = parts == 1 ? n : PK_PART;
-  const int64_t a = part * per, b = part + 1 < parts ? a + per : n;  // (n may pass max_seqlen)
+  // a request shorter than the longest ends in an earlier part (n may pass max_seqlen: the last part goes to its end)
+  const int64_t a = part * per, b = part + 1 < parts ? min(a + per, n) : n;
   const int l = plane / dm.Hkv, g = plane % dm.Hkv;
   const float* wt = weights.unit(l, g, start);
   float* key = keys + (int64_t)plane * dm.Ntot + start;
@@ -478,7 +479,7 @@ __global__ void __launch_bounds__(PK_THREADS)
   }
   bool bad = false;
 #pragma unroll 4
-  for (int64_t i = a + tid; i < b; i += PK_THREADS) {  // (no work where a > n)
+  for (int64_t i = a + tid; i < b; i += PK_THREADS) {  // (none where a >= n)
     const int64_t p = tag != nullptr ? (int64_t)tag[i] : i;
     const float w = wt[i];
     bad |= !(w >= 0.f && w < INFINITY);

@@ -635,6 +635,53 @@ def test_select_refuses_weights_that_are_none(bad):
     assert ev.idx[0, 0, 0].tolist() == select_plain(weights[0, 0], 100, 10, 0, 0)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("ordered", [0, 1])
+@pytest.mark.parametrize("lens", [(9000, 100, 5000), (100, 9000), (4096, 1, 4097, 8192), (40, 30), (8193, 4095, 50)])
+def test_evict_by_weights_without_tags(lens, ordered, dtype):
+    """In place and by row, over requests that end in different parts of the longest's tokens; what lies behind the
+    arrays stays."""
+    L, Hkv, budget, sinks, recent, guard = 2, 2, 48, 5, 9, 9216
+    g, S, N = gen(27), len(lens), sum(lens)
+    cache = make_cache(g, S, L, Hkv, Hkv, 1, lens, dtype)
+    k0, v0 = cache.k.clone(), cache.v.clone()
+    room = torch.full((L * Hkv * N + guard,), -77.0, device=DEV)  # (as a weight -77 is refused)
+    keys = torch.full((L * Hkv * N + guard,), -77.0, device=DEV)
+    weights = room[:L * Hkv * N].view(L, Hkv, N)
+    weights.copy_(torch.rand(weights.shape, generator=g, device=DEV))
+    weights[torch.rand(weights.shape, generator=g, device=DEV) < 0.3] = 0.25  # ties
+    w0 = weights.clone()
+    idx = torch.full((L, Hkv, S, budget), -7, dtype=torch.int32, device=DEV)
+    kept = torch.zeros(S, dtype=torch.int32, device=DEV)
+    ws = torch.zeros(64, dtype=torch.uint8, device=DEV)
+    at = lambda t: t.data_ptr()  # noqa: E731
+    stream = torch.cuda.current_stream().cuda_stream
+    status = api.jacap_evict_weights(cache.layout(), at(weights), None, sinks, recent, budget, at(idx), at(kept),
+                                     at(cache.k), at(cache.v), ordered, at(keys), at(ws), ws.numel(), stream)
+    assert status == 0 and api.jacap_device_status(at(ws), stream) == 0
+    assert (room[L * Hkv * N:] == -77.0).all() and (keys[L * Hkv * N:] == -77.0).all()
+    first = 0
+    for s, n in enumerate(lens):
+        for l in range(L):
+            for h in range(Hkv):
+                want = select_plain(w0[l, h, first:first + n], n, budget, sinks, recent)
+                assert idx[l, h, s].tolist() == want + [-1] * (budget - len(want))
+                rows = torch.tensor(want, device=DEV) + first
+                now = slice(first, first + len(want))
+                for got, src in ((cache.k, k0), (cache.v, v0), (weights, w0)):
+                    got, src = got[l, h, now].reshape(len(want), -1), src[l, h, rows].reshape(len(want), -1)
+                    if not ordered:  # the kept rows from past the budget fill the holes
+                        moved = sorted(r for r in want if r >= budget)
+                        place = [r for r in range(len(want)) if r not in set(want)] if n > budget else []
+                        order = {r: r for r in want if r < budget} | dict(zip(moved, place))
+                        src = src[torch.tensor(sorted(range(len(want)), key=lambda i: order[want[i]]), device=DEV)]
+                    assert torch.equal(got, src)
+                # rows that were not moved into, and those behind the kept ones
+                assert torch.equal(weights[l, h, first + len(want):first + n], w0[l, h, first + len(want):first + n])
+        assert kept[s] == min(n, budget)
+        first += n
+
+
 # --------------------------------------------------- streams, graphs, refusals ----
 def test_operators_on_another_stream_and_in_graphs():
     g, S, L, Hq, Hkv, T = gen(19), 2, 1, 8, 2, 3
