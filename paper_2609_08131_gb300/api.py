@@ -859,24 +859,43 @@ class DecodeEvictor:
     def start(self, k0, v0, q_win, lengths, stream=None):
         """Load the prefill caches (k0, v0: [S, L, Hkv, n, 128], request s using
         its first lengths[s] < cap rows) and start the statistics from the
-        prefill window queries q_win [S, L, Hq, w, 128]."""
+        prefill window queries q_win [S, L, Hq, w, 128]. All of it runs on ``stream``,
+        after what the current stream holds and before what it gets next."""
         if any(n < 0 or n >= self.cap for n in lengths):
             raise ValueError("a prefill cache must hold fewer than budget + interval tokens; evict it first")
         n = k0.shape[3]
-        self.k[:, :, :, :n].copy_(k0)
-        self.v[:, :, :, :n].copy_(v0)
-        ar = torch.arange(self.cap, dtype=torch.int32, device=self.pos.device)
-        self.pos.copy_(torch.where(ar < torch.tensor(lengths, device=ar.device)[:, None], ar, -1)[:, None, None, :]
-                       .expand_as(self.pos))
-        self.lengths = list(lengths)
-        self.next_id = list(lengths)
-        self._attended = (0, set())
-        self._follow(stream)
-        if self.rule == "weight":
-            self._w.zero_()
-            self._weigh(q_win, None, None, stream)
-            return
-        self._merge(q_win, reset=True, stream=stream)
+
+        def load(_):
+            self.k[:, :, :, :n].copy_(k0)
+            self.v[:, :, :, :n].copy_(v0)
+            ar = torch.arange(self.cap, dtype=torch.int32, device=self.pos.device)
+            self.pos.copy_(torch.where(ar < torch.tensor(lengths, device=ar.device)[:, None], ar, -1)[:, None, None, :]
+                           .expand_as(self.pos))
+            self.lengths = list(lengths)
+            self.next_id = list(lengths)
+            self._attended = (0, set())
+            self._follow(stream)
+            if self.rule == "weight":
+                self._w.zero_()
+                self._weigh(q_win, None, None, stream)
+            else:
+                self._merge(q_win, reset=True, stream=stream)
+
+        self._between(stream, load)
+
+    def _between(self, stream, call):
+        """call(handle) with its torch operations and kernels on `stream`, after what the current stream holds and
+        before what it gets next."""
+        if stream is None:
+            return _enqueue(self.device, None, call)
+        with torch.cuda.device(self.device):
+            current = torch.cuda.current_stream(self.device)
+        if stream != current:
+            stream.wait_stream(current)
+        out = _enqueue(self.device, stream, call)
+        if stream != current:
+            current.wait_stream(stream)
+        return out
 
     def append(self, k_new, v_new, q_new, stream=None):
         """One decode step for every request: k_new, v_new [S, L, Hkv, 128],

@@ -979,6 +979,29 @@ def test_a_captured_attention_follows_the_slots(rule):
     assert ev.events >= 3
 
 
+@pytest.mark.parametrize("rule", ["jacap", "weight"])
+def test_start_on_another_stream_than_the_current_one(rule):
+    """The slots and their statistics or weights as after a start on the current stream, which is busy here."""
+    S, L, Hq, Hkv, n = 3, 2, 4, 2, 900
+    g = gen(28)
+    k0, v0 = (randn(g, S, L, Hkv, n, D, dtype=BF16) for _ in range(2))
+    q, lens = randn(g, S, L, Hq, 16, D, dtype=BF16), [900, 411, 0]
+    want = api.DecodeEvictor(S, L, Hq, Hkv, 800, 128, device=DEV, rule=rule)
+    want.start(k0, v0, q, lens)
+    side = torch.cuda.Stream(device=DEV)
+    ev = api.DecodeEvictor(S, L, Hq, Hkv, 800, 128, device=DEV, rule=rule)
+    for again in range(2):
+        torch.cuda._sleep(20_000_000)  # some 10 ms
+        ev.start(k0.clone(), v0.clone(), q.clone(), lens, stream=side)
+        names = ("k", "v", "pos", "weights") if rule == "weight" else ("k", "v", "pos", "stats", "counts")
+        for x in names:  # (k and v: the prompt's rows; those behind are left as they were)
+            got, ref = getattr(ev, x), getattr(want, x)
+            assert torch.equal(got[:, :, :, :n], ref[:, :, :, :n]) if x in "kv" else torch.equal(got, ref), (again, x)
+        ev.check()
+        for x in names:
+            getattr(ev, x).fill_(3)
+
+
 def test_loop_refusals_on_the_device_side():
     ev = api.DecodeEvictor(2, 1, 4, 2, 8, 2, device=DEV, rule="weight")
     g = gen(24)
