@@ -813,8 +813,7 @@ class DecodeEvictor:
             raise JacapError(1, "jacap_workspace_size")
         nbytes = max(sizes) if rule == "jacap" else 1024
         self.ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
-        if rule == "weight":
-            self.ws.zero_()
+        self.ws[:64].zero_()  # the status word: nothing to report yet
         self._scores = torch.empty(L * Hkv * S * cap, dtype=torch.float32, device=dev)
         self._idx = torch.empty(L * Hkv * S * self.budget, dtype=torch.int32, device=dev)
         self._kept = torch.empty((S,), dtype=torch.int32, device=dev)

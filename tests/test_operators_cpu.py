@@ -281,6 +281,16 @@ def test_decode_evictor_refuses(kw):
         api.DecodeEvictor(1, 1, 2, 1, 8, 4, device="cpu", **kw)
 
 
+@pytest.mark.parametrize("rule", ["jacap", "weight"])
+def test_decode_evictor_starts_with_nothing_to_report(rule, monkeypatch):
+    """check() reads the status word, before the first pass writes one too."""
+    empty = torch.empty
+    monkeypatch.setattr(torch, "empty", lambda *a, **kw: empty(*a, **kw).fill_(7))
+    ev = api.DecodeEvictor(1, 1, 2, 1, 8, 4, device="cpu", rule=rule)
+    monkeypatch.undo()
+    assert (ev.ws[:64] == 0).all()
+
+
 def cpu_cache(S=1, L=1, Hq=2, Hkv=1, w=4, n=32):
     k = torch.zeros((L, Hkv, S * n, 128), dtype=torch.bfloat16)
     return api.Cache(torch.zeros((S, L, Hq, w, 128), dtype=torch.bfloat16), k, torch.zeros_like(k),
