@@ -713,6 +713,33 @@ def evict(cache: Cache, budget: int, params: jacap_params | None = None, check: 
     return ev
 
 
+class _SlotAttention:
+    """What ``DecodeEvictor.attend`` keeps for T tokens: its layer's layout and arguments, the workspace, and the
+    normalisers ``lse`` of all layers."""
+
+    def __init__(self, lay, nbytes):
+        self.lay, self.nbytes, self.args = lay, nbytes, jacap_attention()
+        self.ws = self.lse = None
+        self._zeroed, self._filled = False, set()
+
+    def ready(self, layer, shape, device):
+        """The layer's part of ``lse``, with the workspace zeroed, on the current stream. Captured calls zero for themselves
+        at every replay until an eager call has done so."""
+        if self.ws is None:
+            self.ws = torch.empty(self.nbytes, dtype=torch.uint8, device=device)
+            self.lse = torch.empty(shape, dtype=torch.float32, device=device)
+        part = self.lse[:, layer]
+        if not self._zeroed or layer not in self._filled:
+            if not self._zeroed:
+                self.ws.zero_()
+            if layer not in self._filled:
+                part.fill_(-math.inf)
+            if not torch.cuda.is_current_stream_capturing():
+                self._zeroed = True
+                self._filled.add(layer)
+        return part
+
+
 class DecodeEvictor:
     """Decoding-stage eviction (Sec. 3.4: statistics from the queries seen so
     far; the decoding experiments of Sec. 4): one cache slot of
@@ -793,7 +820,7 @@ class DecodeEvictor:
             self._w = torch.zeros((L, Hkv, S, cap), dtype=torch.float32, device=dev)
             self.weights = self._w.permute(2, 0, 1, 3)
         self._ints = {}        # small int32 arrays on the device and what they hold
-        self._attention = {}   # per number of drafted tokens: layout, workspace, normalisers
+        self._attention = {}   # per number of drafted tokens
         self._attended = (0, set())
         self._weigh_ws = {}
         self.lengths = [0] * S
@@ -1082,10 +1109,9 @@ class DecodeEvictor:
             nbytes = jacap_attend_workspace(lay)
             if nbytes == 0 or T == 0:
                 raise JacapError(2 if T > 64 else 1, "jacap_attend_workspace")
-            ws = torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
-            lse = torch.full((self.S, self.L, self.Hq, T), -math.inf, dtype=torch.float32, device=self.device)
-            self._attention[T] = (lay, ws, lse, jacap_attention())
-        lay, ws, lse, a = self._attention[T]
+            self._attention[T] = _SlotAttention(lay, nbytes)
+        at = self._attention[T]
+        lay, a = at.lay, at.args
         dev, S, Hq = self.device, self.S, self.Hq
         qp = _tensor("q", q, dev, self.dtype, (S, Hq, T, 128))
         if (k_draft is None) != (v_draft is None) or (tree is not None and k_draft is None):
@@ -1098,15 +1124,15 @@ class DecodeEvictor:
         if k_draft is not None:
             a.draft_strides[:] = _strides(k_draft.unsqueeze(1)) + _strides(v_draft.unsqueeze(1))
         _query_strides(lay, q.unsqueeze(1))
-        part = lse[:, layer]
-        a.lse_strides[:] = (lse.stride(0), lse.stride(1), lse.stride(2))
 
         def attend(st):
+            part = at.ready(layer, (S, self.L, Hq, T), dev)
+            a.lse_strides[:] = at.lse.stride()[:3]
             o = torch.empty((S, Hq, T, 128), dtype=self.dtype, device=dev)
             a.o_strides[:] = (o.stride(0), 0, o.stride(1), o.stride(2))
             a.lengths = self._int32("lengths", self.lengths).data_ptr()
             _check(jacap_attend(lay, a, qp, self._k[layer].data_ptr(), self._v[layer].data_ptr(), o.data_ptr(),
-                                part.data_ptr(), ws.data_ptr(), ws.numel(), st), "jacap_attend")
+                                part.data_ptr(), at.ws.data_ptr(), at.ws.numel(), st), "jacap_attend")
             if self._attended[0] != T:
                 self._attended = (T, set())
             if k_draft is None or draft_lens is not None:  # not the normalisers of every token that may be entered
@@ -1167,7 +1193,7 @@ class DecodeEvictor:
         self._follow(stream)
         if self.rule == "weight":
             known = self._attended[0] == T and len(self._attended[1]) == L
-            self._weigh(q, self._attention[T][2] if known else None, path, stream)
+            self._weigh(q, self._attention[T].lse if known else None, path, stream)
 
     def _weigh(self, q, lse, path, stream):
         """Add the weights of the queries q [S, L, Hq, w, 128] (of `path` of them; None: the window of a
@@ -1176,15 +1202,17 @@ class DecodeEvictor:
         if q.dtype != self.dtype or q.stride(-1) != 1 or tuple(q.shape) != (self.S, self.L, self.Hq, w, 128):
             raise ValueError("queries must be [S, L, Hq, w, 128] in the cache dtype")
         lay = self._layout(self.S, w, _strides(q))
-        if w not in self._weigh_ws:
-            nbytes = jacap_weigh_workspace(lay)
-            if nbytes == 0:
-                raise JacapError(2 if self.Hq // self.Hkv * w > 512 else 1, "jacap_weigh_workspace")
-            self._weigh_ws[w] = torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
-        ws, how = self._weigh_ws[w], jacap_weighing()
+        nbytes = jacap_weigh_workspace(lay)
+        if nbytes == 0:
+            raise JacapError(2 if self.Hq // self.Hkv * w > 512 else 1, "jacap_weigh_workspace")
+        how = jacap_weighing()
         how.scale, how.lse_given = self.scale, int(lse is not None)
 
         def weigh(st):
+            if w not in self._weigh_ws:  # (made on the stream that uses it)
+                self._weigh_ws[w] = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+                self._weigh_ws[w][:64].zero_()
+            ws = self._weigh_ws[w]
             how.lengths = self._int32("lengths", self.lengths).data_ptr()
             if path is not None and (w > 1 or any(not p for p in path)):
                 how.q_lens = self._int32("taken", [len(p) for p in path]).data_ptr()
@@ -1201,7 +1229,7 @@ class DecodeEvictor:
             _check(jacap_device_status(_ptr(self.ws), _stream(stream)), "device status")
         else:
             _check_and_clear(self.ws, self.device, stream)
-        for ws in [x[1] for x in self._attention.values()] + list(self._weigh_ws.values()):
+        for ws in [x.ws for x in self._attention.values() if x.ws is not None] + list(self._weigh_ws.values()):
             _check_and_clear(ws, self.device, stream)
 
 

@@ -52,14 +52,14 @@ class Order(TorchDispatchMode):
         super().__init__()
         self.main, self.side = Stream(self, "current", 1), Stream(self, "side", 2)
         self.current, self.capturing = self.main, False
-        self.accesses = []  # (what, stream's name, its number there, clock, reads, writes)
+        self.accesses = []  # (what, stream's name, its number there, clock, reads, writes, captured)
         self.held = {}      # address -> (end, storage's tensor): kept, so that no address comes back
 
     # ---- accesses
     def note(self, what, stream, reads, writes):
         number = stream.clock.get(stream.name, 0)
         stream.clock[stream.name] = number + 1
-        self.accesses.append((what, stream.name, number, dict(stream.clock), frozenset(reads), frozenset(writes)))
+        self.accesses.append((what, stream.name, number, dict(stream.clock), frozenset(reads), frozenset(writes), self.capturing))
 
     def storage(self, t):
         at = t.untyped_storage().data_ptr()
@@ -116,8 +116,8 @@ class Order(TorchDispatchMode):
     # ---- what is not ordered
     def races(self):
         out = []
-        for j, (what, stream, number, clock, reads, writes) in enumerate(self.accesses):
-            for other, on, earlier, _, r, w in self.accesses[:j]:
+        for j, (what, stream, _, clock, reads, writes, _) in enumerate(self.accesses):
+            for other, on, earlier, _, r, w, _ in self.accesses[:j]:
                 if on != stream and clock.get(on, 0) <= earlier and (w & (reads | writes) or writes & r):
                     out.append(f"{other} on the {on} stream, {what} on the {stream} one")
         return out

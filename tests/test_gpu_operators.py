@@ -979,6 +979,38 @@ def test_a_captured_attention_follows_the_slots(rule):
     assert ev.events >= 3
 
 
+@pytest.mark.parametrize("replays", [0, 1])
+def test_the_first_attention_may_be_captured(replays):
+    """Eager calls before or after the graph's first replay, and the replays, as without a graph. The slots are long
+    enough for splits that the kernel joins by counting them."""
+    S, L, Hq, Hkv, T, n = 4, 2, 8, 2, 3, 3000
+    g = gen(29)
+    k0, v0 = (randn(g, S, L, Hkv, n, D, dtype=BF16) for _ in range(2))
+    q0, lens = randn(g, S, L, Hq, 4, D, dtype=BF16), [3000, 2111, 7, 1500]
+    k, v, q = (randn(g, S, L, x, T, D, dtype=BF16) for x in (Hkv, Hkv, Hq))
+    want, ev = (api.DecodeEvictor(S, L, Hq, Hkv, n, 64, device=DEV, rule="weight") for _ in range(2))
+    for x in (want, ev):
+        x.start(k0, v0, q0, lens)
+
+    def attend(x):
+        return [t.clone() for l in range(L) for t in x.attend(l, q[:, l], k[:, l], v[:, l])]
+
+    ref = attend(want)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = attend(ev)
+    for _ in range(replays):
+        graph.replay()
+    assert all(torch.equal(a, b) for a, b in zip(attend(ev), ref))
+    for x in got:
+        x.fill_(7)
+    graph.replay()
+    assert all(torch.equal(a, b) for a, b in zip(got, ref))
+    assert all(torch.equal(a, b) for a, b in zip(attend(ev), ref))
+    ev.check()
+
+
 @pytest.mark.parametrize("rule", ["jacap", "weight"])
 def test_start_on_another_stream_than_the_current_one(rule):
     """The slots and their statistics or weights as after a start on the current stream, which is busy here."""

@@ -32,3 +32,35 @@ def test_start_on_another_stream(rule, monkeypatch):
         if rule == "weight":
             ev.weights.sum()
         assert order.races() == []
+
+
+@pytest.mark.parametrize("rule", ["jacap", "weight"])
+def test_first_calls_on_another_stream(rule, monkeypatch):
+    """What the first attention and the first accepted tokens make for themselves is made on their stream."""
+    with watch(monkeypatch) as order:
+        ev = slots(rule)
+        k0, q0, k, q = rows(S, L, HKV, 20), rows(S, L, HQ, 4), rows(S, L, HKV, 3), rows(S, L, HQ, 3)
+        ev.start(k0, k0.clone(), q0, [20, 17], stream=order.side)
+        for layer in range(L):
+            ev.attend(layer, q[:, layer], k[:, layer], k[:, layer], stream=order.side)
+        ev.accept(k, k, q, [[0, 1], [0]], stream=order.side)
+        assert [len(order.calls(c)) for c in ("jacap_attend", "jacap_append_path")] == [L, 1]
+        assert {a[1] for c in ("jacap_attend", "jacap_append_path", "jacap_weigh") for a in order.calls(c)} == {"side"}
+        assert order.races() == []
+
+
+def test_a_first_attention_that_is_captured_leaves_the_eager_ones_a_zeroed_workspace(monkeypatch):
+    with watch(monkeypatch) as order:
+        ev = slots("weight")
+        k0, q0, k, q = rows(S, L, HKV, 20), rows(S, L, HQ, 4), rows(S, L, HKV, 3), rows(S, L, HQ, 3)
+        ev.start(k0, k0.clone(), q0, [20, 17])
+        order.capturing = True
+        for layer in range(L):
+            ev.attend(layer, q[:, layer], k[:, layer], k[:, layer])
+        order.capturing = False
+        for layer in range(L):
+            ev.attend(layer, q[:, layer], k[:, layer], k[:, layer])
+        ws = order.buffer(ev._attention[3].ws.data_ptr())
+        calls = [(a[0], a[6]) for a in order.accesses if ws in a[5]]
+        # every captured call zeroes for itself (a graph may be replayed before any other runs), the first eager one for all
+        assert calls == [("zero_", True), ("jacap_attend", True)] * L + [("zero_", False)] + [("jacap_attend", False)] * L
