@@ -128,6 +128,24 @@ def _enqueue(device, stream, call):
             return call(stream.cuda_stream)
 
 
+def _made(device):
+    """An event behind what a constructor has enqueued, for the first call on another stream (None where there is no
+    device; a capture's beginning waits for the device)."""
+    if device.type != "cuda" or torch.cuda.is_current_stream_capturing():
+        return None
+    with torch.cuda.device(device):
+        event = torch.cuda.Event()
+        event.record()
+    return event
+
+
+def _wait_made(handle):
+    """The current stream after what the handle's constructor enqueued (its first eager call waits)."""
+    if handle._made is not None and not torch.cuda.is_current_stream_capturing():
+        handle._made.wait()
+        handle._made = None
+
+
 def _tensor(name, t, device, dtype, shape, contiguous=False):
     """Checks a tensor argument; its address. None passes, as None."""
     if t is None:
@@ -330,6 +348,7 @@ class CacheAttention:
         self._attn.o_strides[:] = self.o.stride()[:4]
         self._attn.lse_strides[:] = self.lse.stride()[:3]
         self._draft_at = self._q_at = None
+        self._made = _made(self.device)
 
     def run(self, q=None, k_draft=None, v_draft=None, tree=None, lengths=None, draft_lens=None, stream=None):
         """q: [S, L, Hq, T, 128] (the cache's q_win if None); k_draft, v_draft: [S, L, Hkv,
@@ -359,6 +378,7 @@ class CacheAttention:
             self._q_at = at
 
         def attend(st):
+            _wait_made(self)
             _check(jacap_attend(lay, a, qp, c.k.data_ptr(), c.v.data_ptr(), self.o.data_ptr(), self.lse.data_ptr(),
                                 self.ws.data_ptr(), self.ws.numel(), st), "jacap_attend")
             return self.o, self.lse
@@ -366,12 +386,13 @@ class CacheAttention:
         return _enqueue(dev, stream, attend)
 
     def check(self, stream=None):
-        _check_and_clear(self.ws, self.device, stream)
+        _check_and_clear(self, self.ws, self.device, stream)
 
 
-def _check_and_clear(ws, device, stream):
+def _check_and_clear(handle, ws, device, stream):
     """Raises what the status word holds, clearing it: a later call starts anew."""
     def read(st):
+        _wait_made(handle)
         status = jacap_device_status(ws.data_ptr(), st)
         if status != JACAP_OK:
             ws.zero_()
@@ -418,6 +439,7 @@ class WeightEvictor:
         self.k_out = new((L, Hkv, S, self.budget, d), cache.k.dtype)
         self.v_out = torch.empty_like(self.k_out)
         self.weights_out = new((L, Hkv, S, self.budget), torch.float32)
+        self._made = _made(self.device)
 
     def score(self, q=None, lse=None, before=None, lengths=None, q_lens=None, q_rows=None, stream=None):
         """The weights (``jacap_weigh``) into ``weights``; returns (weights, lse).
@@ -442,6 +464,7 @@ class WeightEvictor:
         lay = _query_strides(self.lay, q)
 
         def weigh(st):
+            _wait_made(self)
             _check(jacap_weigh(lay, h, qp, c.k.data_ptr(), lp, bp, self.weights.data_ptr(), self.ws.data_ptr(),
                                self.ws.numel(), st), "jacap_weigh")
             return self.weights, lse
@@ -461,6 +484,7 @@ class WeightEvictor:
             raise ValueError("tags need a dense cache")
 
         def select(st):
+            _wait_made(self)
             if pos is not None and self.keys is None:
                 self.keys = torch.empty_like(self.weights)
             _check(jacap_select_weights(self.lay, wp, pp, self.sinks, self.recent, self.budget, self.idx.data_ptr(),
@@ -476,7 +500,7 @@ class WeightEvictor:
         self.select_compact(stream=stream)
 
     def check(self, stream=None):
-        _check_and_clear(self.ws, self.device, stream)
+        _check_and_clear(self, self.ws, self.device, stream)
 
 
 class Evictor:
@@ -845,6 +869,15 @@ class DecodeEvictor:
         self._idx = torch.empty(L * Hkv * S * self.budget, dtype=torch.int32, device=dev)
         self._kept = torch.empty((S,), dtype=torch.int32, device=dev)
         self._views(1)
+        self._made = _made(self.device)
+
+    def _on(self, stream, call):
+        """call(handle of the stream) with the device and the stream current, after what the constructor enqueued."""
+        def after(st):
+            _wait_made(self)
+            return call(st)
+
+        return _enqueue(self.device, stream, after if self._made is not None else call)
 
     def _views(self, n):
         L, Hkv = self.L, self.Hkv
@@ -913,12 +946,12 @@ class DecodeEvictor:
         """call(handle) with its torch operations and kernels on `stream`, after what the current stream holds and
         before what it gets next."""
         if stream is None:
-            return _enqueue(self.device, None, call)
+            return self._on(None, call)
         with torch.cuda.device(self.device):
             current = torch.cuda.current_stream(self.device)
         if stream != current:
             stream.wait_stream(current)
-        out = _enqueue(self.device, stream, call)
+        out = self._on(stream, call)
         if stream != current:
             current.wait_stream(stream)
         return out
@@ -1068,7 +1101,7 @@ class DecodeEvictor:
         """The arrays on the device that captured calls read follow the slots' lengths and next ids."""
         if self._ints and not torch.cuda.is_current_stream_capturing():
             now = (("lengths", self.lengths), ("next ids", self.next_id))
-            _enqueue(self.device, stream, lambda _: [self._int32(k, x) for k, x in now if k in self._ints])
+            self._on(stream, lambda _: [self._int32(k, x) for k, x in now if k in self._ints])
 
     def positions(self, tokens: int, depth=None):
         """int32 [S, tokens]: the ids that drafted tokens get if accepted; ``depth``: int32
@@ -1088,7 +1121,7 @@ class DecodeEvictor:
             out = rope.apply(*(None if t is None else t.transpose(1, 2) for t in (q, k)), at)
             return tuple(None if t is None else t.transpose(1, 2) for t in out)
 
-        return _enqueue(self.device, stream, turn)
+        return self._on(stream, turn)
 
     def attend(self, layer: int, q, k_draft=None, v_draft=None, tree=None, draft_lens=None, stream=None):
         """Attention of one layer's drafted tokens over the slots and over themselves:
@@ -1141,7 +1174,7 @@ class DecodeEvictor:
                 self._attended[1].add(layer)
             return o, part
 
-        return _enqueue(dev, stream, attend)
+        return self._on(stream, attend)
 
     def accept(self, k_draft, v_draft, q_draft, path, stream=None):
         """Enter the accepted drafted tokens of a step: k_draft, v_draft [S, L, Hkv, T, 128],
@@ -1187,7 +1220,7 @@ class DecodeEvictor:
                                      self.lengths, self.next_id, _ptr(self._k), _ptr(self._v), _ptr(self._pos),
                                      _ptr(self.stats), _ptr(self.counts), st), "jacap_append_path")
 
-        _enqueue(self.device, stream, append)
+        self._on(stream, append)
         self.lengths = [n + len(p) for n, p in zip(self.lengths, path)]
         self.next_id = [n + len(p) for n, p in zip(self.next_id, path)]
         self._follow(stream)
@@ -1221,16 +1254,16 @@ class DecodeEvictor:
             _check(jacap_weigh(lay, how, _ptr(q), _ptr(self._k), _ptr(lse), None if path is None else wp, wp, _ptr(ws),
                                ws.numel(), st), "jacap_weigh")
 
-        _enqueue(self.device, stream, weigh)
+        self._on(stream, weigh)
 
     def check(self, stream=None):
         """Raises what the kernels reported so far."""
         if self.rule == "jacap":
             _check(jacap_device_status(_ptr(self.ws), _stream(stream)), "device status")
         else:
-            _check_and_clear(self.ws, self.device, stream)
+            _check_and_clear(self, self.ws, self.device, stream)
         for ws in [x.ws for x in self._attention.values() if x.ws is not None] + list(self._weigh_ws.values()):
-            _check_and_clear(ws, self.device, stream)
+            _check_and_clear(self, ws, self.device, stream)
 
 
 class HostEvictor:

@@ -47,6 +47,15 @@ class Stream:
         return self.cuda_stream
 
 
+class Event:
+    def __init__(self, stream):
+        self.stream = Stream(stream.order, stream.name, stream.cuda_stream)
+        self.stream.clock = dict(stream.clock)
+
+    def wait(self):
+        self.stream.order.current.wait_stream(self.stream)
+
+
 class Order(TorchDispatchMode):
     def __init__(self):
         super().__init__()
@@ -144,6 +153,7 @@ def watch(monkeypatch):
         m.setattr(torch.cuda, "is_current_stream_capturing", lambda: order.capturing)
         m.setattr(torch._C, "_cuda_getDevice", lambda: None, raising=False)
         m.setattr(torch._C, "_cuda_getCurrentRawStream", lambda d: order.current.cuda_stream, raising=False)
+        m.setattr(api, "_made", lambda device: Event(order.current), raising=False)
         for name in CALLS:
             m.setattr(api, name, order.library(name))
         with order:

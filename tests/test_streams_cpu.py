@@ -14,6 +14,11 @@ def rows(*shape):
     return torch.zeros((*shape, D), dtype=torch.bfloat16)
 
 
+def cache():
+    k = rows(L, HKV, S * 30)
+    return api.Cache(rows(S, L, HQ, 3), k, k.clone(), torch.arange(0, 61, 30, dtype=torch.int32), [30, 30], HQ)
+
+
 def slots(rule):
     return api.DecodeEvictor(S, L, HQ, HKV, 20, 4, device="cpu", rule=rule)
 
@@ -64,3 +69,28 @@ def test_a_first_attention_that_is_captured_leaves_the_eager_ones_a_zeroed_works
         calls = [(a[0], a[6]) for a in order.accesses if ws in a[5]]
         # every captured call zeroes for itself (a graph may be replayed before any other runs), the first eager one for all
         assert calls == [("zero_", True), ("jacap_attend", True)] * L + [("zero_", False)] + [("jacap_attend", False)] * L
+
+
+@pytest.mark.parametrize("call", ["attend", "score", "select"])
+def test_a_handle_s_first_call_on_another_stream(call, monkeypatch):
+    """What the constructor zeroed is zero when the first call's kernels run."""
+    with watch(monkeypatch) as order:
+        c, kd = cache(), rows(S, L, HKV, 3)
+        order.side.wait_stream(order.main)  # the caller's tensors are there
+        ev = api.CacheAttention(c) if call == "attend" else api.WeightEvictor(c, 8)
+        if call == "attend":
+            ev.run(k_draft=kd, v_draft=kd, stream=order.side)
+        else:
+            (ev.score if call == "score" else ev.select_compact)(stream=order.side)
+        assert order.races() == []
+
+
+@pytest.mark.parametrize("rule", ["jacap", "weight"])
+def test_slots_that_start_empty_on_another_stream(rule, monkeypatch):
+    with watch(monkeypatch) as order:
+        k, q = rows(S, L, HKV, 3), rows(S, L, HQ, 3)
+        order.side.wait_stream(order.main)
+        ev = slots(rule)
+        ev.attend(0, q[:, 0], k[:, 0], k[:, 0], stream=order.side)
+        ev.accept(k, k, q, [[0, 1], [0]], stream=order.side)
+        assert order.races() == []
