@@ -959,7 +959,9 @@ class DecodeEvictor:
     def append(self, k_new, v_new, q_new, stream=None):
         """One decode step for every request: k_new, v_new [S, L, Hkv, 128],
         q_new [S, L, Hq, 128]. Returns the requests whose cache is now full
-        (each must be evicted before its next append)."""
+        (each must be evicted before its next append). On another ``stream`` than the
+        current one indexed copies enter the tokens of the rule "jacap", after what the
+        current stream holds and before what it gets next."""
         full = [s for s in range(self.S) if self.lengths[s] >= self.cap]
         if full:
             raise RuntimeError(f"request {full[0]} is full; evict it first")
@@ -975,18 +977,22 @@ class DecodeEvictor:
             self.next_id = [n + 1 for n in self.next_id]
             self._follow(stream)
             return [s for s in range(self.S) if self.lengths[s] >= self.cap]
-        dev = self._k.device
-        rows = torch.tensor(self.lengths, dtype=torch.long, device=dev)
-        reqs = torch.arange(self.S, device=dev)
-        # one indexed copy per tensor for all requests (each writes its next free row)
-        self._k[:, :, reqs, rows] = k_new.permute(1, 2, 0, 3).to(self.dtype)
-        self._v[:, :, reqs, rows] = v_new.permute(1, 2, 0, 3).to(self.dtype)
-        ids = torch.tensor(self.next_id, dtype=torch.int32, device=dev)
-        self._pos[:, :, reqs, rows] = ids.view(1, 1, self.S).expand(self.L, self.Hkv, self.S)
-        self.lengths = [n + 1 for n in self.lengths]
-        self.next_id = [n + 1 for n in self.next_id]
-        self._follow(stream)
-        self.merge_queries(q_new, stream)
+
+        def copy(_):
+            dev = self._k.device
+            rows = torch.tensor(self.lengths, dtype=torch.long, device=dev)
+            reqs = torch.arange(self.S, device=dev)
+            # one indexed copy per tensor for all requests (each writes its next free row)
+            self._k[:, :, reqs, rows] = k_new.permute(1, 2, 0, 3).to(self.dtype)
+            self._v[:, :, reqs, rows] = v_new.permute(1, 2, 0, 3).to(self.dtype)
+            ids = torch.tensor(self.next_id, dtype=torch.int32, device=dev)
+            self._pos[:, :, reqs, rows] = ids.view(1, 1, self.S).expand(self.L, self.Hkv, self.S)
+            self.lengths = [n + 1 for n in self.lengths]
+            self.next_id = [n + 1 for n in self.next_id]
+            self._follow(stream)
+            self.merge_queries(q_new, stream)
+
+        self._between(stream, copy)
         return [s for s in range(self.S) if self.lengths[s] >= self.cap]
 
     def _one_launch(self, k_new, v_new, q_new, stream) -> bool:

@@ -94,3 +94,20 @@ def test_slots_that_start_empty_on_another_stream(rule, monkeypatch):
         ev.attend(0, q[:, 0], k[:, 0], k[:, 0], stream=order.side)
         ev.accept(k, k, q, [[0, 1], [0]], stream=order.side)
         assert order.races() == []
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rule", ["jacap", "weight"])
+def test_steps_on_another_stream(rule, dtype, monkeypatch):
+    """Tokens entered one by one (also those that indexed copies enter) and attended to; what the current stream does
+    with the slots afterwards comes after."""
+    with watch(monkeypatch) as order:
+        ev = slots(rule)
+        k0, q0, q1 = rows(S, L, HKV, 20), rows(S, L, HQ, 4), rows(S, L, HQ, 1)
+        k, q = rows(S, L, HKV).to(dtype if rule == "jacap" else torch.bfloat16), rows(S, L, HQ)
+        ev.start(k0, k0.clone(), q0, [20, 17], stream=order.side)
+        for _ in range(3):
+            ev.append(k, k, q, stream=order.side)
+            for layer in range(L):
+                ev.attend(layer, q1[:, layer], stream=order.side)
+        assert order.races() == []
