@@ -912,8 +912,8 @@ class DecodeEvictor:
         if q.dtype != self.dtype or q.stride(-1) != 1 or tuple(q.shape[:3]) != (self.S, self.L, self.Hq):
             raise ValueError("queries must be [S, L, Hq, m, 128] in the cache dtype")
         lay = self._layout(self.S, q.shape[3], (q.stride(0), q.stride(1), q.stride(2), q.stride(3)))
-        _check(jacap_stats_update(lay, _ptr(q), 1 if reset else 0, _ptr(self.stats), _ptr(self.counts),
-                                  _stream(stream)), "jacap_stats_update")
+        self._on(stream, lambda st: _check(jacap_stats_update(lay, _ptr(q), 1 if reset else 0, _ptr(self.stats),
+                                                              _ptr(self.counts), st), "jacap_stats_update"))
 
     def start(self, k0, v0, q_win, lengths, stream=None):
         """Load the prefill caches (k0, v0: [S, L, Hkv, n, 128], request s using
@@ -970,9 +970,10 @@ class DecodeEvictor:
             self._attended = (0, set())  # the next step's normalisers are others
             return [s for s in range(self.S) if self.lengths[s] >= self.cap]
         if self._one_launch(k_new, v_new, q_new, stream):
-            _check(jacap_append(self.step_layout, _ptr(k_new), _ptr(v_new), k_new.stride()[:3] + v_new.stride()[:3],
-                                _ptr(q_new), self.lengths, self.next_id, _ptr(self._k), _ptr(self._v),
-                                _ptr(self._pos), _ptr(self.stats), _ptr(self.counts), _stream(stream)), "jacap_append")
+            self._on(stream, lambda st: _check(
+                jacap_append(self.step_layout, _ptr(k_new), _ptr(v_new), k_new.stride()[:3] + v_new.stride()[:3],
+                             _ptr(q_new), self.lengths, self.next_id, _ptr(self._k), _ptr(self._v), _ptr(self._pos),
+                             _ptr(self.stats), _ptr(self.counts), st), "jacap_append"))
             self.lengths = [n + 1 for n in self.lengths]
             self.next_id = [n + 1 for n in self.next_id]
             self._follow(stream)
@@ -1013,8 +1014,8 @@ class DecodeEvictor:
     def merge_queries(self, q_new, stream=None):
         """Merge one decode step's queries [S, L, Hq, 128] into the running statistics."""
         if q_new.is_contiguous() and q_new.dtype == self.dtype and tuple(q_new.shape) == (self.S, self.L, self.Hq, 128):
-            _check(jacap_stats_update(self.step_layout, _ptr(q_new), 0, _ptr(self.stats), _ptr(self.counts),
-                                      _stream(stream)), "jacap_stats_update")
+            self._on(stream, lambda st: _check(jacap_stats_update(self.step_layout, _ptr(q_new), 0, _ptr(self.stats),
+                                                                  _ptr(self.counts), st), "jacap_stats_update"))
         else:
             self._merge(q_new.unsqueeze(3), reset=False, stream=stream)
 
@@ -1052,32 +1053,32 @@ class DecodeEvictor:
         if any(self.lengths[s] != self.cap for s in range(a, b)):
             raise RuntimeError("only full slots are evicted")
         n = b - a
-        lay, st = self._group_layout(n), _stream(stream)
+        lay = self._group_layout(n)
         handles = [e.cuda_event for e in events] if events is not None else []
-        if self.rule == "weight":
-            if events is not None:
-                raise ValueError("there are no scoring kernels to time: the weights are kept up step by step")
-            self._views(n)
-            _check(jacap_evict_weights(lay, _ptr(self._w[0, 0, a]), _ptr(self._pos[0, 0, a]), self.sinks, self.recent,
-                                       self.budget, _ptr(self.idx), _ptr(self.kept), _ptr(self._k[0, 0, a]),
-                                       _ptr(self._v[0, 0, a]), self.preserve_order, _ptr(self.scores), _ptr(self.ws),
-                                       self.ws.numel(), st), "jacap_evict_weights")
-            self._evicted(a, b, stream, tail)
-            return
-        stats = ctypes.c_void_p(self.stats[a].data_ptr())
-        counts = ctypes.c_void_p(self.counts[a].data_ptr())
         k, v, pos = _ptr(self._k[0, 0, a]), _ptr(self._v[0, 0, a]), _ptr(self._pos[0, 0, a])
+        if self.rule == "weight" and events is not None:
+            raise ValueError("there are no scoring kernels to time: the weights are kept up step by step")
         self._views(n)
-        _check(jacap_score_stats(lay, self.params, stats, counts, k, v, _ptr(self.scores), _ptr(self.ws),
-                                 self.ws.numel(), st, handles), "jacap_score_stats")
-        _check(jacap_select_compact_inplace(lay, _ptr(self.scores), self.budget, _ptr(self.idx), _ptr(self.kept), k,
-                                            v, pos, self.preserve_order, _ptr(self.ws), self.ws.numel(), st),
-               "jacap_select_compact_inplace")
+
+        def evict(st):
+            if self.rule == "weight":
+                _check(jacap_evict_weights(lay, _ptr(self._w[0, 0, a]), pos, self.sinks, self.recent, self.budget,
+                                           _ptr(self.idx), _ptr(self.kept), k, v, self.preserve_order,
+                                           _ptr(self.scores), _ptr(self.ws), self.ws.numel(), st), "jacap_evict_weights")
+                return
+            _check(jacap_score_stats(lay, self.params, _ptr(self.stats[a]), _ptr(self.counts[a]), k, v,
+                                     _ptr(self.scores), _ptr(self.ws), self.ws.numel(), st, handles),
+                   "jacap_score_stats")
+            _check(jacap_select_compact_inplace(lay, _ptr(self.scores), self.budget, _ptr(self.idx), _ptr(self.kept), k,
+                                                v, pos, self.preserve_order, _ptr(self.ws), self.ws.numel(), st),
+                   "jacap_select_compact_inplace")
+
+        self._on(stream, evict)
         self._evicted(a, b, stream, tail)
 
     def _evicted(self, a, b, stream, tail):
         if tail is not None:
-            tail[0].record(stream)
+            self._on(stream, lambda _: tail[0].record())
         for s in range(a, b):
             self.lengths[s] = self.budget
         self._follow(stream)
@@ -1265,7 +1266,7 @@ class DecodeEvictor:
     def check(self, stream=None):
         """Raises what the kernels reported so far."""
         if self.rule == "jacap":
-            _check(jacap_device_status(_ptr(self.ws), _stream(stream)), "device status")
+            self._on(stream, lambda st: _check(jacap_device_status(_ptr(self.ws), st), "device status"))
         else:
             _check_and_clear(self, self.ws, self.device, stream)
         for ws in [x.ws for x in self._attention.values() if x.ws is not None] + list(self._weigh_ws.values()):

@@ -61,6 +61,7 @@ class Order(TorchDispatchMode):
         super().__init__()
         self.main, self.side = Stream(self, "current", 1), Stream(self, "side", 2)
         self.current, self.capturing = self.main, False
+        self.other, self.device = Stream(self, "other device's", 3), None  # (None: the tensors')
         self.accesses = []  # (what, stream's name, its number there, clock, reads, writes, captured)
         self.held = {}      # address -> (end, storage's tensor): kept, so that no address comes back
 
@@ -97,10 +98,10 @@ class Order(TorchDispatchMode):
     def library(self, name):
         place, written = CALLS[name]
 
-        def pointers(x):
+        def pointers(x, written=False):
             if isinstance(x, ctypes.Structure):
                 for field, kind in x._fields_:
-                    if kind is ctypes.c_void_p:
+                    if kind is ctypes.c_void_p and not (written and field == "x"):
                         yield getattr(x, field) or 0
             elif isinstance(x, ctypes.c_void_p):
                 yield x.value or 0
@@ -108,15 +109,15 @@ class Order(TorchDispatchMode):
                 yield x
 
         def call(*args):
+            assert self.device is None, f"{name} with another device current"
             handle = args[place].value if isinstance(args[place], ctypes.c_void_p) else args[place]
             stream = self.main if handle == self.main.cuda_stream else self.side
             assert handle == stream.cuda_stream, name
             reads, writes = set(), set()
             for i, x in enumerate(args):
-                found = {self.buffer(p) for p in pointers(x) if p > 1 << 16} - {None}
-                reads |= found
+                reads |= {self.buffer(p) for p in pointers(x) if p > 1 << 16} - {None}
                 if i in written:
-                    writes |= found
+                    writes |= {self.buffer(p) for p in pointers(x, True) if p > 1 << 16} - {None}
             self.note(name, stream, reads, writes)
             return api.JACAP_OK
 
@@ -145,13 +146,20 @@ def watch(monkeypatch):
         yield
         order.current = before
 
+    @contextlib.contextmanager
+    def device(d):
+        before, order.device = order.device, None
+        yield
+        order.device = before
+
     with monkeypatch.context() as m:
-        m.setattr(torch.cuda, "current_stream", lambda *a: order.current)
-        m.setattr(torch.cuda, "current_device", lambda: None)
-        m.setattr(torch.cuda, "device", lambda d: contextlib.nullcontext())
+        m.setattr(torch.cuda, "current_stream",
+                  lambda d=None: order.current if order.device is None or d is not None else order.other)
+        m.setattr(torch.cuda, "current_device", lambda: order.device)
+        m.setattr(torch.cuda, "device", device)
         m.setattr(torch.cuda, "stream", on)
         m.setattr(torch.cuda, "is_current_stream_capturing", lambda: order.capturing)
-        m.setattr(torch._C, "_cuda_getDevice", lambda: None, raising=False)
+        m.setattr(torch._C, "_cuda_getDevice", lambda: order.device, raising=False)
         m.setattr(torch._C, "_cuda_getCurrentRawStream", lambda d: order.current.cuda_stream, raising=False)
         m.setattr(api, "_made", lambda device: Event(order.current), raising=False)
         for name in CALLS:

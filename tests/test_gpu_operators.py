@@ -1034,6 +1034,41 @@ def test_start_on_another_stream_than_the_current_one(rule):
             getattr(ev, x).fill_(3)
 
 
+@pytest.mark.parametrize("rule", ["jacap", "weight"])
+def test_the_loop_on_another_stream_than_the_current_one(rule):
+    """Every call of the loop with stream=, evictions among them, with the current stream busy: as on the current one."""
+    S, L, Hq, Hkv, T = 3, 2, 8, 2, 3
+    g = gen(30)
+    rope = api.Rope(device=DEV)
+    k0, v0 = (randn(g, S, L, Hkv, 600, D, dtype=BF16) for _ in range(2))
+    q0, lens = randn(g, S, L, Hq, 16, D, dtype=BF16), [600, 597, 411]
+    steps = [[randn(g, S, L, n, T, D, dtype=BF16) for n in (Hkv, Hkv, Hq)] for _ in range(6)]
+    one = [[x[:, :, :, 0].contiguous() for x in step] for step in steps]
+    side = torch.cuda.Stream(device=DEV)
+    torch.cuda.synchronize()
+
+    def loop(stream):
+        ev = api.DecodeEvictor(S, L, Hq, Hkv, 590, 16, device=DEV, rule=rule)
+        out = []
+        if stream is not None:
+            torch.cuda._sleep(20_000_000)  # some 10 ms
+        ev.start(k0, v0, q0, lens, stream=stream)
+        for (k, v, q), token in zip(steps, one):
+            if stream is not None:
+                torch.cuda._sleep(2_000_000)
+            turned = [ev.rotate(rope, q[:, l], k[:, l], stream=stream) for l in range(L)]
+            out += [t for l, (tq, tk) in enumerate(turned) for t in ev.attend(l, tq, tk, v[:, l], stream=stream)[:1]]
+            out += ev.accept(k, v, q, [[0, 1, 2], [0], []], stream=stream)
+            out += ev.step(*token, stream=stream)
+        ev.check(stream)
+        torch.cuda.synchronize()
+        assert ev.events >= 3
+        return out + [ev.k, ev.v, ev.pos] + ([ev.weights] if rule == "weight" else [ev.stats, ev.counts])
+
+    for a, b in zip(loop(side), loop(None)):
+        assert torch.equal(a, b) if isinstance(a, torch.Tensor) else a == b
+
+
 def test_loop_refusals_on_the_device_side():
     ev = api.DecodeEvictor(2, 1, 4, 2, 8, 2, device=DEV, rule="weight")
     g = gen(24)

@@ -111,3 +111,28 @@ def test_steps_on_another_stream(rule, dtype, monkeypatch):
             for layer in range(L):
                 ev.attend(layer, q1[:, layer], stream=order.side)
         assert order.races() == []
+
+
+@pytest.mark.parametrize("rule", ["jacap", "weight"])
+@pytest.mark.parametrize("side", [False, True])
+def test_slots_on_another_device_than_the_current_one(rule, side, monkeypatch):
+    """Every call of the loop, evictions among them, is made with the slots' device current and goes to one of its
+    streams; on another stream nothing is left unordered."""
+    with watch(monkeypatch) as order:
+        ev = slots(rule)
+        k0, q0, k, q = rows(S, L, HKV, 22), rows(S, L, HQ, 4), rows(S, L, HKV, 3), rows(S, L, HQ, 3)
+        one = [x.contiguous() for x in (k[:, :, :, 0], k[:, :, :, 1], q[:, :, :, 0])]
+        order.device = 5
+        stream = order.side if side else None
+        ev.start(k0, k0.clone(), q0, [22, 20], stream=stream)
+        rope = api.Rope(device="cpu")
+        order.side.wait_stream(order.main)
+        for _ in range(2):
+            ev.rotate(rope, q[:, 0], k[:, 0], stream=stream)
+            for layer in range(L):
+                ev.attend(layer, q[:, layer], k[:, layer], k[:, layer], stream=stream)
+            ev.accept(k, k, q, [[0, 1], [0]], stream=stream)
+            ev.step(*one, stream=stream)
+        if rule == "jacap":
+            ev.merge_queries(q[:, :, :, 2], stream=stream)
+        assert ev.events >= 2 and order.races() == []
