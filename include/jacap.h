@@ -480,8 +480,10 @@ jacap_status jacap_rotate(const jacap_rope* rope, jacap_dtype dtype, int32_t num
  *                  array over all layers)
  *   ws             device, 256-byte aligned, jacap_attend_workspace() bytes (0 for
  *                  a layout that is refused), zeroed once before its first call: it
- *                  starts with the status word and holds counters that every call
- *                  leaves at zero. A length outside its range is clamped and reported
+ *                  starts with the status word and with counters that every call
+ *                  leaves at zero, at the same place for every layout (calls of several
+ *                  layouts may use one after the other, not at the same time). A length
+ *                  outside its range is clamped and reported
  *                  in the word (JACAP_ERR_INVALID_ARG), which stays set until the
  *                  workspace is zeroed again.
  * o must not overlap an input. Sums are float32; with bf16 caches the softmax

@@ -63,7 +63,8 @@ AttendPlan attend_plan(const jacap_layout* L) {
   if (bf) p.nsplit = (most + 63) / 64 + 1 < 2 * p.edge ? 1 : p.nsplit + 2;  // a share's borders are anywhere in a unit
   size_t o = 0;
   p.status = o; o += 64;
-  p.counts = o; o = align_up(o + (p.nsplit > 1 ? (size_t)units * 4 : 0));
+  // (whatever the layout, so that calls of several layouts may use a workspace one after the other)
+  p.counts = o; o = align_up(o + (size_t)ATTEND_CTAS * 4);
   p.nsps = o; o = align_up(o + (bf ? (size_t)ctas * 4 : 0));
   const size_t parts = p.nsplit > 1 ? (size_t)units * p.nsplit : 0, prows = attend_part_rows(rows);
   p.opart = o; o = align_up(o + parts * ((rows + prows - 1) / prows * prows) * D * 4);

@@ -190,10 +190,12 @@ struct AttendArgs {
   uint32_t tdiv;              // 2^32 / window, rounded up (window > 1)
   float *opart, *mlpart;      // the splits' sums [units][nsplit][row blocks][32][prows][4], and their
                               // [units][nsplit][G window][2] (maximum, sum)
-  int32_t* counts;            // [units] splits done, where the last one joins them (zero between calls)
+  int32_t* counts;            // [ATTEND_CTAS] splits done of the unit whose first split is the CTA's, where the last one
+                              // joins them (zero between calls, and at one place in every layout's workspace)
   int32_t* nsps;              // bf16: [units][row blocks] splits of this call
   uint32_t* status;
 };
+constexpr int ATTEND_CTAS = 320;  // CTAs that share out a bf16 call's tiles, at most (two to each of 160 SMs; a GB300 has 152)
 int attend_row_block(int dtype, int rows);  // rows of a CTA
 int attend_part_rows(int rows);
 // maps: K, V, drafted K, drafted V (bf16)

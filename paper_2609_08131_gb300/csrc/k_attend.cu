@@ -108,6 +108,7 @@ struct AtUnit {
   int s, l, g, split;
   int64_t u, t0;
   int n, rows, nd, nsp;
+  int first;                   // bf16: the CTA that has the unit's first split
   int tok0, tok1, ncache, nt;  // this split's tokens, its tiles of cached tokens and in all (`tile` tokens each)
   int r0;                      // the CTA's first row
 };
@@ -462,6 +463,7 @@ __global__ void __launch_bounds__(AtCfg<NB>::THREADS, 3 - NB)
           next.nsp = last > first ? (int)(last - first) + 1 : 1;
           if (split < 0 || split >= next.nsp) continue;
           next.split = split;
+          next.first = (int)first;
           if (split == 0) a.nsps[at] = next.nsp;
           if (next.nt > 0) {
             const int ta = split == 0 ? 0 : (int)((w0 - p0 + c - 1) / c);
@@ -889,8 +891,9 @@ __global__ void __launch_bounds__(AtCfg<NB>::THREADS, 3 - NB)
         __threadfence();
         named_barrier_sync(1, SM_THREADS);
         if (tsm == 0) {
-          sh.last = atomicAdd(a.counts + x.u, 1) == x.nsp - 1;
-          if (sh.last) a.counts[x.u] = 0;  // (zero between calls)
+          // (a CTA has the first split of one unit of several at most: the one that its end divides)
+          sh.last = atomicAdd(a.counts + x.first, 1) == x.nsp - 1;
+          if (sh.last) a.counts[x.first] = 0;  // (zero between calls)
           __threadfence();
         }
         named_barrier_sync(1, SM_THREADS);
@@ -1289,7 +1292,7 @@ static cudaError_t launch_bf16(const CUtensorMap* maps, const Dims& dm, const At
                                int64_t items, int sms, cudaStream_t st) {
   auto kern = attend_bf16_kernel<REP, NB>;
   JACAP_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)at_smem<NB>()));
-  const int places = sms * (3 - NB);
+  const int places = sms * (3 - NB) < ATTEND_CTAS ? sms * (3 - NB) : ATTEND_CTAS;
   return launch_pdl(true, kern, (int)(items < places ? items : places), AtCfg<NB>::THREADS, at_smem<NB>(), st, maps[0],
                     maps[1], maps[2], maps[3], dm, a, cu);
 }

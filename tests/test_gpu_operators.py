@@ -733,6 +733,31 @@ def test_operators_on_another_stream_and_in_graphs():
                 assert torch.equal(want[3][:, :, a0:a0 + n[s]], got[3][:, :, a0:a0 + n[s]])
 
 
+def test_attentions_of_several_layouts_share_a_workspace():
+    """Zeroed once, used by one layout after the other: many units in splits that the kernel joins by counting them,
+    calls of one split, of more rows, of many splits, float32."""
+    calls = []
+    for i, (S, L, Hq, Hkv, T, n, dtype) in enumerate((
+            (4, 4, 64, 16, 1, 600, BF16), (1, 2, 8, 8, 64, 450, BF16), (2, 1, 16, 2, 64, 1900, BF16), (3, 1, 4, 4, 2, 700, F32),
+            (16, 1, 8, 1, 1, 40, BF16), (1, 1, 8, 2, 3, 30000, BF16), (1, 8, 32, 32, 1, 5000, BF16), (2, 1, 8, 1, 40, 3000, F32))):
+        g = gen(60 + i)
+        cache = make_cache(g, S, L, Hq, Hkv, T, (n,) * S, dtype)
+        kd, vd = (randn(g, S, L, Hkv, T, D, dtype=dtype) for _ in range(2))
+        att = api.CacheAttention(cache)
+        want = [x.clone() for x in att.run(k_draft=kd, v_draft=vd)]
+        calls.append((att, kd, vd, want))
+    shared = torch.zeros(max(c[0].ws.numel() for c in calls), dtype=torch.uint8, device=DEV)
+    for c in calls:
+        c[0].ws = shared
+    for order in (range(8), (0, 1, 0, 2, 0, 3, 6, 4, 6, 5, 0, 7, 6, 3, 5, 1, 5)):
+        for i in order:
+            att, kd, vd, want = calls[i]
+            att.o.fill_(7)
+            att.lse.fill_(7)
+            assert all(torch.equal(a, b) for a, b in zip(att.run(k_draft=kd, v_draft=vd), want)), i
+            att.check()
+
+
 def test_two_calls_at_once():
     """Two attentions and their weights on two streams, workspaces of their own: as one after the other."""
     work = []
