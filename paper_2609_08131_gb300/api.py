@@ -1175,7 +1175,8 @@ class DecodeEvictor:
                                 part.data_ptr(), at.ws.data_ptr(), at.ws.numel(), st), "jacap_attend")
             if self._attended[0] != T:
                 self._attended = (T, set())
-            if k_draft is None or draft_lens is not None:  # not the normalisers of every token that may be entered
+            # not the normalisers of every token that may be entered, or not there before a replay
+            if k_draft is None or draft_lens is not None or torch.cuda.is_current_stream_capturing():
                 self._attended[1].discard(layer)
             else:
                 self._attended[1].add(layer)

@@ -62,14 +62,14 @@ class Order(TorchDispatchMode):
         self.main, self.side = Stream(self, "current", 1), Stream(self, "side", 2)
         self.current, self.capturing = self.main, False
         self.other, self.device = Stream(self, "other device's", 3), None  # (None: the tensors')
-        self.accesses = []  # (what, stream's name, its number there, clock, reads, writes, captured)
+        self.accesses = []  # (what, stream's name, its number there, clock, reads, writes, captured, arguments)
         self.held = {}      # address -> (end, storage's tensor): kept, so that no address comes back
 
     # ---- accesses
-    def note(self, what, stream, reads, writes):
+    def note(self, what, stream, reads, writes, args=()):
         number = stream.clock.get(stream.name, 0)
         stream.clock[stream.name] = number + 1
-        self.accesses.append((what, stream.name, number, dict(stream.clock), frozenset(reads), frozenset(writes), self.capturing))
+        self.accesses.append((what, stream.name, number, dict(stream.clock), frozenset(reads), frozenset(writes), self.capturing, args))
 
     def storage(self, t):
         at = t.untyped_storage().data_ptr()
@@ -118,7 +118,7 @@ class Order(TorchDispatchMode):
                 reads |= {self.buffer(p) for p in pointers(x) if p > 1 << 16} - {None}
                 if i in written:
                     writes |= {self.buffer(p) for p in pointers(x, True) if p > 1 << 16} - {None}
-            self.note(name, stream, reads, writes)
+            self.note(name, stream, reads, writes, args)
             return api.JACAP_OK
 
         return call
@@ -126,8 +126,8 @@ class Order(TorchDispatchMode):
     # ---- what is not ordered
     def races(self):
         out = []
-        for j, (what, stream, _, clock, reads, writes, _) in enumerate(self.accesses):
-            for other, on, earlier, _, r, w, _ in self.accesses[:j]:
+        for j, (what, stream, _, clock, reads, writes, _, _) in enumerate(self.accesses):
+            for other, on, earlier, _, r, w, _, _ in self.accesses[:j]:
                 if on != stream and clock.get(on, 0) <= earlier and (w & (reads | writes) or writes & r):
                     out.append(f"{other} on the {on} stream, {what} on the {stream} one")
         return out

@@ -972,6 +972,26 @@ def test_normalisers_are_those_of_the_step_they_belong_to():
     assert torch.equal(enter(again), enter(lambda ev: ev.start(k1, v1, qw, [9, 12])))
 
 
+def test_a_capture_alone_leaves_no_normalisers():
+    """A captured attention that has not been replayed: the entered tokens' normalisers are computed."""
+    S, L, Hq, Hkv, T = 2, 2, 4, 2, 3
+    g = gen(31)
+    k0, v0, k, v = (randn(g, S, L, Hkv, n, D, dtype=BF16) for n in (12, 12, T, T))
+    qw, q = randn(g, S, L, Hq, 4, D, dtype=BF16), randn(g, S, L, Hq, T, D, dtype=BF16)
+    evs = [api.DecodeEvictor(S, L, Hq, Hkv, 30, 10, device=DEV, rule="weight") for _ in range(2)]
+    for ev in evs:
+        ev.start(k0, v0, qw, [12, 9])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for l in range(L):
+            evs[1].attend(l, q[:, l], k[:, l], v[:, l])
+    for ev in evs:
+        ev.accept(k, v, q, [[0, 1, 2], [0, 1]])
+        ev.check()
+    assert torch.equal(evs[0].weights, evs[1].weights)
+
+
 @pytest.mark.parametrize("rule", ["jacap", "weight"])
 def test_a_captured_attention_follows_the_slots(rule):
     S, Hq, Hkv, T = 2, 4, 2, 1

@@ -136,3 +136,36 @@ def test_slots_on_another_device_than_the_current_one(rule, side, monkeypatch):
         if rule == "jacap":
             ev.merge_queries(q[:, :, :, 2], stream=stream)
         assert ev.events >= 2 and order.races() == []
+
+
+@pytest.mark.parametrize("enter", ["accept", "step"])
+def test_captured_attentions_leave_no_normalisers_before_a_replay(enter, monkeypatch):
+    """Tokens entered after a capture alone: their normalisers are computed."""
+    with watch(monkeypatch) as order:
+        ev, T = slots("weight"), 3 if enter == "accept" else 1
+        k0, q0, k, q = rows(S, L, HKV, 17), rows(S, L, HQ, 4), rows(S, L, HKV, T), rows(S, L, HQ, T)
+        ev.start(k0, k0.clone(), q0, [17, 17])
+
+        def enters():
+            if enter == "accept":
+                ev.accept(k, k, q, [[0, 1], [0]])
+            else:
+                ev.step(k[:, :, :, 0], k[:, :, :, 0], q[:, :, :, 0])
+            return order.calls("jacap_weigh")[-1][7][1].lse_given
+
+        def attends():
+            for layer in range(L):
+                ev.attend(layer, q[:, layer], k[:, layer], k[:, layer])
+
+        attends()
+        assert enters() == 1
+        assert enters() == 0  # (those were the step's before)
+        order.capturing = True
+        attends()
+        order.capturing = False
+        assert enters() == 0
+        attends()
+        order.capturing = True  # captured again after an eager step: its normalisers may be overwritten by a replay
+        attends()
+        order.capturing = False
+        assert enters() == 0
