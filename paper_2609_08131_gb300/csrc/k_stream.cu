@@ -118,8 +118,8 @@ __global__ void __launch_bounds__(256) plan_kernel(Dims dm, Ws ws, const int32_t
   const int64_t planes = (int64_t)dm.L * dm.Hkv;
   for (int b = threadIdx.x; b <= dm.gram_parts; b += blockDim.x) {
     int64_t item = planes * ctot;
-    const int64_t at = (int64_t)b * planes * s_ttot / dm.gram_parts;  // tiles before the share
-    if (b < dm.gram_parts && s_ttot > 0) {
+    if (b < dm.gram_parts && s_ttot > 0) {  // (a pass without a Gram has no parts)
+      const int64_t at = (int64_t)b * planes * s_ttot / dm.gram_parts;  // tiles before the share
       const int64_t plane = at / s_ttot;
       const int x = (int)(at % s_ttot), s = request_of(ws.tpre, x), ct = dm.chunk / TILE;
       const int j = min((x - ws.tpre[s] + ct / 2) / ct, cpre[s + 1] - cpre[s]);
