@@ -452,7 +452,8 @@ jacap_status jacap_rotate(const jacap_rope* rope, jacap_dtype dtype, int32_t num
  * a chain, or a tree whose tokens see their ancestors.
  *
  * The layout is that of the cache; `window` (T, at most 64, else
- * JACAP_ERR_UNSUPPORTED) is the number of queries per request and head, and the
+ * JACAP_ERR_UNSUPPORTED, as are more than 2^28 rows of queries in all, or 2^29 tiles of
+ * 64 tokens over all layers and KV heads) is the number of queries per request and head, and the
  * q strides are those of q. Row (s, l, h, t) sees the first lengths[s] tokens of
  * its request and the drafted tokens j of its mask:
  *   logit = scale q . k,  o = sum softmax(logit) v,  lse = ln sum exp(logit).

@@ -707,6 +707,8 @@ jacap_status check_weights(const jacap_layout* layout, const float* weights, con
       ((uintptr_t)kept & 3u) != 0 || ((uintptr_t)pos & 3u) != 0 || !aligned16(k) || !aligned16(v))
     return JACAP_ERR_INVALID_ARG;
   if (!pos_layout_ok(layout, pos)) return JACAP_ERR_INVALID_ARG;
+  if (layout_units(layout) * (keys_needed ? protect_parts(layout->max_seqlen, pos) : 1) > INT32_MAX)
+    return JACAP_ERR_UNSUPPORTED;
   make_dims(layout, nullptr, *dm);
   if (((uintptr_t)ws & 255u) != 0 || ws_bytes < 64) return JACAP_ERR_WORKSPACE;
   memset(w, 0, sizeof(*w));

@@ -76,7 +76,14 @@ AttendPlan attend_plan(const jacap_layout* L) {
 jacap_status check_attend_layout(const jacap_layout* L) {
   const jacap_status st = check_layout(L);
   if (st != JACAP_OK) return st;
-  return L->window > AT_DRAFTS_MAX ? JACAP_ERR_UNSUPPORTED : JACAP_OK;
+  const int64_t planes = (int64_t)L->num_layers * L->num_kv_heads, units = layout_units(L);
+  const int64_t rows = (int64_t)L->num_q_heads / L->num_kv_heads * L->window;
+  if (L->window > AT_DRAFTS_MAX || units * rows > INT32_MAX / 8) return JACAP_ERR_UNSUPPORTED;
+  const AttendPlan p = attend_plan(L);
+  if (units * p.nsplit * p.nrb > INT32_MAX) return JACAP_ERR_UNSUPPORTED;
+  // the positions on the line of tiles (k_attend.cu): at most 4 for each of a request's tiles, and of AT_START more
+  if (L->total_tokens / 64 + 8 * (int64_t)L->num_seqs > INT32_MAX / 4 / (planes * p.nrb)) return JACAP_ERR_UNSUPPORTED;
+  return JACAP_OK;
 }
 
 // ----------------------------------------------------------------- weights ----
@@ -118,7 +125,11 @@ Ws make_weigh_ws(void* base, const WeighCarve& c, const Dims& dm) {
 jacap_status check_weigh_layout(const jacap_layout* L) {
   const jacap_status st = check_layout(L);
   if (st != JACAP_OK) return st;
-  return (int64_t)(L->num_q_heads / L->num_kv_heads) * L->window > WEIGH_ROWS_MAX ? JACAP_ERR_UNSUPPORTED : JACAP_OK;
+  const int64_t rows = (int64_t)L->num_q_heads / L->num_kv_heads * L->window;
+  if (rows > WEIGH_ROWS_MAX || layout_units(L) * ((rows + 31) / 32) > INT32_MAX) return JACAP_ERR_UNSUPPORTED;
+  Dims dm;
+  make_dims(L, nullptr, dm);
+  return plan_items(L, dm) > INT32_MAX ? JACAP_ERR_UNSUPPORTED : JACAP_OK;
 }
 
 // far enough from the ends of float32 for the scale times log2 e and what is divided by it
@@ -283,7 +294,6 @@ jacap_status jacap_weigh(const jacap_layout* layout, const jacap_weighing* how, 
   memset(&kmap, 0, sizeof(kmap));
   if (bf && !encode_kv_map(&kmap, layout, k)) return JACAP_ERR_CUDA;
   const int64_t items = plan_items(layout, dm);
-  if (items >= ((int64_t)1 << 31)) return JACAP_ERR_UNSUPPORTED;
   plan_runs(dm, items, sms);
   dm.gram_parts = 0;
   const Ws w = make_weigh_ws(ws, c, dm);

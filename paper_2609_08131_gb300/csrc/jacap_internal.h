@@ -24,6 +24,12 @@ bool encode_draft_map(CUtensorMap* map, const jacap_layout* L, const void* base,
 int64_t plan_items(const jacap_layout* L, const Dims& dm);
 void plan_runs(Dims& dm, int64_t items, int sms);
 int plan_grid(int64_t items, int sms);
+// Units (layer, KV head, request) of a layout, 2^31 where there are more.
+inline int64_t layout_units(const jacap_layout* L) {
+  const int64_t top = (int64_t)1 << 31, planes = (int64_t)L->num_layers * L->num_kv_heads;
+  const int64_t units = (planes < top ? planes : top) * L->num_seqs;
+  return units < top ? units : top;
+}
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 inline jacap_status map_cuda(cudaError_t e) { return e == cudaSuccess ? JACAP_OK : JACAP_ERR_CUDA; }
 
@@ -121,6 +127,8 @@ cudaError_t launch_select(const Dims& dm, const Ws& ws, const int32_t* cu, const
                           void* v_out = nullptr, void* kio = nullptr, void* vio = nullptr, int32_t* pos = nullptr,
                           const WeightRef& wt = WeightRef{}, float* wt_out = nullptr, int sinks = -1,
                           int recent = -1);
+// Blocks of launch_protect per unit.
+int protect_parts(int max_seqlen, const int32_t* pos);
 // Selection keys from attention weights: +inf for the first `sinks` and the last
 // `recent` tokens of every unit.
 cudaError_t launch_protect(const Dims& dm, const Ws& ws, const int32_t* cu, const WeightRef& weights,

@@ -1320,9 +1320,6 @@ cudaError_t launch_attend(const CUtensorMap* maps, const Dims& dm, int dtype, co
                           int sms, cudaStream_t st) {
   const int R = dm.G * dm.window;
   const int64_t units = (int64_t)dm.L * dm.Hkv * dm.S, blocks = units * a.nsplit * a.nrb;
-  if (blocks > INT32_MAX || units * R > INT32_MAX / 8) return cudaErrorInvalidValue;
-  // the positions on the line of tiles: at most 4 for each of a request's tiles, and of AT_START more
-  if ((dm.Ntot / AT_TOK + 8 * (int64_t)dm.S) * dm.L * dm.Hkv * a.nrb > INT32_MAX / 4) return cudaErrorInvalidValue;
   if (dtype == 1) {
     if (R <= 32) JACAP_TRY((launch_bf16<4, 1>(maps, dm, a, cu, blocks, sms, st)));
     else if (R <= 64) JACAP_TRY((launch_bf16<2, 1>(maps, dm, a, cu, blocks, sms, st)));

@@ -588,13 +588,13 @@ cudaError_t launch_select(const Dims& dm, const Ws& ws, const int32_t* cu, const
   return cudaGetLastError();
 }
 
+int protect_parts(int max_seqlen, const int32_t* pos) { return pos != nullptr ? 1 : (max_seqlen - 1) / PK_PART + 1; }
+
 cudaError_t launch_protect(const Dims& dm, const Ws& ws, const int32_t* cu, const WeightRef& weights,
                            const int32_t* pos, int sinks, int recent, float* keys, int max_seqlen, cudaStream_t st) {
-  const int parts = pos != nullptr ? 1 : (max_seqlen - 1) / PK_PART + 1;
-  const int64_t blocks = (int64_t)dm.L * dm.Hkv * dm.S * parts;
-  if (blocks > INT32_MAX) return cudaErrorInvalidValue;
-  return launch_pdl(dm.pdl != 0, protect_kernel, dim3((unsigned)blocks), PK_THREADS, 0, st, dm, ws, cu, weights, pos,
-                    sinks, recent, keys, parts);
+  const int parts = protect_parts(max_seqlen, pos);
+  return launch_pdl(dm.pdl != 0, protect_kernel, dim3((unsigned)(dm.L * dm.Hkv * dm.S * parts)), PK_THREADS, 0, st, dm, ws,
+                    cu, weights, pos, sinks, recent, keys, parts);
 }
 
 cudaError_t launch_compact(const Dims& dm, int dtype, const int32_t* cu, const void* k, const void* v,

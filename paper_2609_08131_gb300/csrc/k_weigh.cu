@@ -619,7 +619,6 @@ cudaError_t launch_weigh(const CUtensorMap& kmap, const Dims& dm, const Ws& ws, 
                          const int32_t* cu, int grid, cudaStream_t st) {
   const int R = dm.G * dm.window, nrb = (R + 127) / 128;
   const int64_t blocks = (int64_t)dm.L * dm.Hkv * dm.S * ((R + 31) / 32);
-  if (blocks > INT32_MAX) return cudaErrorInvalidValue;
   if (!a.given) {
     JACAP_TRY(launch_pass<false>(kmap, dm, ws, dtype, a, cu, grid, nrb, st));
     JACAP_TRY(launch_pdl(true, weigh_lse_kernel, (int)blocks, WM_THREADS, 0, st, dm, ws, a, cu, 128 * nrb,

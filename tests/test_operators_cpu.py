@@ -193,6 +193,37 @@ def test_select_and_evict_take():
     passed(evict(lay={"kv_stride_token": 256}))  # a head's 500 x 128 elements are 250 of these strides
 
 
+# ------------------------------------------------------ more than a launch takes ----
+MANY = {"num_layers": 1 << 10, "num_q_heads": 1 << 10, "num_kv_heads": 1 << 10}
+HUGE = {"num_layers": (1 << 31) - 1, "num_q_heads": (1 << 31) - 1, "num_kv_heads": (1 << 31) - 1}
+
+
+@pytest.mark.parametrize("lay", [
+    {**MANY, "num_seqs": 1 << 11}, {**HUGE, "num_seqs": (1 << 31) - 1}, {**HUGE, "num_seqs": 2},
+    {"total_tokens": 1 << 30, "max_seqlen": 1 << 30, "num_layers": 32, "num_q_heads": 8, "num_kv_heads": 8},
+    {**MANY, "num_seqs": 1 << 8, "window": 64}, {**MANY, "num_seqs": 1 << 8, "dtype": J.JACAP_F32}])
+def test_attend_refuses_sizes_past_a_launch_s(lay):
+    assert J.jacap_attend_workspace(good_layout(**lay)) == 0
+    refused(attend(lay=lay), NO)
+
+
+@pytest.mark.parametrize("lay", [
+    {**MANY, "num_seqs": 1 << 11}, {**HUGE, "num_seqs": (1 << 31) - 1},
+    {**MANY, "num_seqs": 1 << 8, "num_q_heads": 1 << 13, "window": 64},
+    {**MANY, "total_tokens": 1 << 30, "max_seqlen": 1 << 30}])
+def test_weigh_refuses_sizes_past_a_launch_s(lay):
+    assert J.jacap_weigh_workspace(good_layout(**lay)) == 0
+    refused(weigh(lay=lay), NO)
+
+
+@pytest.mark.parametrize("lay", [{**MANY, "num_seqs": 1 << 11}, {**HUGE, "num_seqs": (1 << 31) - 1}])
+def test_selections_refuse_more_units_than_a_launch_s(lay):
+    refused(select(lay=lay), NO)
+    refused(evict(lay=lay), NO)
+    # the keys of long requests come from several blocks each
+    refused(evict(lay={**MANY, "num_seqs": 1 << 8, "total_tokens": 1 << 20, "max_seqlen": 1 << 18}), NO)
+
+
 # -------------------------------------------------------------- append_path ----
 def append(lay=None, path=((0, 1), (2, 3)), depth=2, taken=(2, 1), lengths=(3, 0), ids=(3, 0), strides=None, k_new=P, v_new=P,
            q_new=P, k=P, v=P, pos=P, stats=P, counts=P):
