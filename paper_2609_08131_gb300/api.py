@@ -745,6 +745,7 @@ class _SlotAttention:
         self.lay, self.nbytes, self.args = lay, nbytes, jacap_attention()
         self.ws = self.lse = None
         self._zeroed, self._filled = False, set()
+        self.complete = set()  # layers whose last call, captured or not, was one that leaves every token's normalisers
 
     def ready(self, layer, shape, device):
         """The layer's part of ``lse``, with the workspace zeroed, on the current stream. Captured calls zero for themselves
@@ -956,17 +957,18 @@ class DecodeEvictor:
             current.wait_stream(stream)
         return out
 
-    def append(self, k_new, v_new, q_new, stream=None):
+    def append(self, k_new, v_new, q_new, stream=None, attended=None):
         """One decode step for every request: k_new, v_new [S, L, Hkv, 128],
         q_new [S, L, Hq, 128]. Returns the requests whose cache is now full
         (each must be evicted before its next append). On another ``stream`` than the
         current one indexed copies enter the tokens of the rule "jacap", after what the
-        current stream holds and before what it gets next."""
+        current stream holds and before what it gets next. ``attended``: as in ``accept``."""
         full = [s for s in range(self.S) if self.lengths[s] >= self.cap]
         if full:
             raise RuntimeError(f"request {full[0]} is full; evict it first")
         if self.rule == "weight":
-            self._take(k_new.unsqueeze(3), v_new.unsqueeze(3), q_new.unsqueeze(3), [[0]] * self.S, stream)
+            known = self._normalisers(1, attended)
+            self._take(k_new.unsqueeze(3), v_new.unsqueeze(3), q_new.unsqueeze(3), [[0]] * self.S, stream, known)
             self._attended = (0, set())  # the next step's normalisers are others
             return [s for s in range(self.S) if self.lengths[s] >= self.cap]
         if self._one_launch(k_new, v_new, q_new, stream):
@@ -1085,9 +1087,9 @@ class DecodeEvictor:
         self.events += b - a
         self.passes += 1
 
-    def step(self, k_new, v_new, q_new, stream=None):
+    def step(self, k_new, v_new, q_new, stream=None, attended=None):
         """append() then evict every request that became full (neighbours together)."""
-        full = self.append(k_new, v_new, q_new, stream)
+        full = self.append(k_new, v_new, q_new, stream, attended)
         self.evict_many(full, stream)
         return full
 
@@ -1137,7 +1139,8 @@ class DecodeEvictor:
         behind are not written). Returns (o [S, Hq, T, 128], lse [S, Hq, T], a view of what the
         next call with as many tokens overwrites). Under the weight rule the normalisers are kept for ``step``,
         ``append`` or ``accept`` (not those of a call without drafted tokens or with draft_lens, which are
-        computed again). A captured call follows the slots: its graph reads their lengths when it is replayed."""
+        computed again). A captured call follows the slots: its graph reads their lengths when it is replayed; say
+        ``attended=True`` when its tokens are entered."""
         if not 0 <= layer < self.L:
             raise ValueError(f"layer must be 0 to {self.L - 1}")
         if not isinstance(q, torch.Tensor) or q.dim() != 4:
@@ -1175,21 +1178,27 @@ class DecodeEvictor:
                                 part.data_ptr(), at.ws.data_ptr(), at.ws.numel(), st), "jacap_attend")
             if self._attended[0] != T:
                 self._attended = (T, set())
-            # not the normalisers of every token that may be entered, or not there before a replay
-            if k_draft is None or draft_lens is not None or torch.cuda.is_current_stream_capturing():
-                self._attended[1].discard(layer)
-            else:
-                self._attended[1].add(layer)
+            # the normalisers of every token that may be entered, if a call by itself leaves them
+            whole = k_draft is not None and draft_lens is None
+            (at.complete.add if whole else at.complete.discard)(layer)
+            whole = whole and not torch.cuda.is_current_stream_capturing()  # (else a replay does)
+            (self._attended[1].add if whole else self._attended[1].discard)(layer)
             return o, part
 
         return self._on(stream, attend)
 
-    def accept(self, k_draft, v_draft, q_draft, path, stream=None):
+    def accept(self, k_draft, v_draft, q_draft, path, stream=None, attended=None):
         """Enter the accepted drafted tokens of a step: k_draft, v_draft [S, L, Hkv, T, 128],
         q_draft [S, L, Hq, T, 128] (turned, as ``attend`` took them), path[s]: which drafted
         tokens of request s, in order, each seen by those after it (none: an empty list). As in ``step`` a request whose
         slot becomes full is evicted, here in the middle of its path where that happens; returns the
-        requests that were evicted."""
+        requests that were evicted.
+
+        ``attended`` (the weight rule): whether the last ``attend`` of T tokens of every layer was that of these
+        tokens, so that its normalisers serve for their weights; else they are computed, with another pass over the
+        keys. None: as far as this object saw the calls. True: also the replays of captured ones, which it does not
+        see (every layer's last call of T tokens, captured or not, must have been one with drafted tokens and without
+        draft_lens). False: computed."""
         if len(path) != self.S:
             raise ValueError("one path per request")
         T = k_draft.shape[3]
@@ -1198,11 +1207,12 @@ class DecodeEvictor:
             raise ValueError(f"a path holds at most {T} tokens, 0 to {T - 1}")
         if any(n >= self.cap for n in self.lengths):
             raise RuntimeError("a request is full; evict it first")
+        known = self._normalisers(T, attended)
         gone = set()
         while True:
             now = [p[:self.cap - n] for p, n in zip(left, self.lengths)]
             left = [p[len(x):] for p, x in zip(left, now)]
-            self._take(k_draft, v_draft, q_draft, now, stream)
+            self._take(k_draft, v_draft, q_draft, now, stream, known)
             full = [s for s in range(self.S) if self.lengths[s] >= self.cap]
             self.evict_many(full, stream)
             gone.update(full)
@@ -1210,8 +1220,20 @@ class DecodeEvictor:
                 self._attended = (0, set())  # the next step's normalisers are others
                 return sorted(gone)
 
-    def _take(self, k, v, q, path, stream):
-        """The drafted tokens `path` into the slots, and their queries into the statistics or weights."""
+    def _normalisers(self, T, attended):
+        """What the last attentions of T tokens left, where they are those of the tokens that are entered now."""
+        if self.rule != "weight":
+            return None
+        at = self._attention.get(T)
+        if attended and (at is None or len(at.complete) != self.L):
+            raise ValueError(f"not every layer's last attention of {T} tokens left the normalisers of all of them")
+        if attended is None:
+            attended = self._attended[0] == T and len(self._attended[1]) == self.L
+        return at.lse if attended else None
+
+    def _take(self, k, v, q, path, stream, lse):
+        """The drafted tokens `path` into the slots, and their queries into the statistics or weights (with the
+        normalisers lse, or computed if None)."""
         S, L, Hq, Hkv, T = self.S, self.L, self.Hq, self.Hkv, k.shape[3]
         for name, t, heads in (("k", k, Hkv), ("v", v, Hkv), ("q", q, Hq)):
             _tensor(name, t, self.device, self.dtype, (S, L, heads, T, 128))
@@ -1233,8 +1255,7 @@ class DecodeEvictor:
         self.next_id = [n + len(p) for n, p in zip(self.next_id, path)]
         self._follow(stream)
         if self.rule == "weight":
-            known = self._attended[0] == T and len(self._attended[1]) == L
-            self._weigh(q, self._attention[T].lse if known else None, path, stream)
+            self._weigh(q, lse, path, stream)
 
     def _weigh(self, q, lse, path, stream):
         """Add the weights of the queries q [S, L, Hq, w, 128] (of `path` of them; None: the window of a

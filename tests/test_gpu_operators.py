@@ -1024,6 +1024,49 @@ def test_a_captured_attention_follows_the_slots(rule):
     assert ev.events >= 3
 
 
+@pytest.mark.parametrize("T", [1, 4])
+def test_a_captured_loop_by_weights(T, monkeypatch):
+    """Rotary positions and attention of all layers as a graph, its normalisers taken for the entered tokens: slots and
+    weights as an eager loop leaves them, through evictions, with one pass over the keys in each weighing."""
+    S, L, Hq, Hkv = 2, 3, 8, 2
+    g = gen(32 + T)
+    k0, v0 = (randn(g, S, L, Hkv, 150, D, dtype=BF16) for _ in range(2))
+    q0, rope = randn(g, S, L, Hq, 8, D, dtype=BF16), api.Rope(device=DEV)
+    k, v, q = (randn(g, S, L, n, T, D, dtype=BF16) for n in (Hkv, Hkv, Hq))
+    evs = [api.DecodeEvictor(S, L, Hq, Hkv, 148, 6, device=DEV, rule="weight", sinks=2, recent=8) for _ in range(2)]
+    for ev in evs:
+        ev.start(k0, v0, q0, [150, 131])
+    given, weigh = [], api.jacap_weigh
+    monkeypatch.setattr(api, "jacap_weigh", lambda lay, how, *a: (given.append(how.lse_given), weigh(lay, how, *a))[1])
+
+    def layers(ev):
+        turned, out = [ev.rotate(rope, q[:, l], k[:, l]) for l in range(L)], []
+        for l, (tq, tk) in enumerate(turned):
+            out.append(ev.attend(l, tq, tk, v[:, l])[0])
+        return torch.stack([x[0] for x in turned], 1), torch.stack([x[1] for x in turned], 1), torch.stack(out)
+
+    layers(evs[1])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = layers(evs[1])
+    for step in range(8):
+        for x in (q, k, v):
+            x.copy_(randn(g, *x.shape, dtype=BF16))
+        tq, tk, o = layers(evs[0])
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(captured, (tq, tk, o))), step
+        for ev, attended in zip(evs, (None, True)):
+            if T == 1:
+                ev.step(tk[:, :, :, 0], v[:, :, :, 0], tq[:, :, :, 0], attended=attended)
+            else:
+                ev.accept(tk, v, tq, [[0, 1, 2][:step % 4], [0, 1]], attended=attended)
+            ev.check()
+    assert evs[0].events >= 1 and evs[0].lengths == evs[1].lengths and set(given) == {1}
+    for x in ("k", "v", "pos", "weights"):
+        assert torch.equal(getattr(evs[0], x), getattr(evs[1], x)), x
+
+
 @pytest.mark.parametrize("replays", [0, 1])
 def test_the_first_attention_may_be_captured(replays):
     """Eager calls before or after the graph's first replay, and the replays, as without a graph. The slots are long

@@ -169,3 +169,43 @@ def test_captured_attentions_leave_no_normalisers_before_a_replay(enter, monkeyp
         attends()
         order.capturing = False
         assert enters() == 0
+
+
+def test_the_caller_says_that_a_replay_left_the_normalisers(monkeypatch):
+    with watch(monkeypatch) as order:
+        ev, T = slots("weight"), 3
+        k0, q0, k, q = rows(S, L, HKV, 8), rows(S, L, HQ, 4), rows(S, L, HKV, T), rows(S, L, HQ, T)
+        ev.start(k0, k0.clone(), q0, [8, 8])
+        one = k[:, :, :, 0], k[:, :, :, 0], q[:, :, :, 0]
+
+        def given():
+            return order.calls("jacap_weigh")[-1][7][1].lse_given
+
+        def attends(layers, **kw):
+            for layer in layers:
+                ev.attend(layer, q[:, layer], k[:, layer], k[:, layer], **kw)
+
+        for refused in (lambda: ev.accept(k, k, q, [[0], [0]], attended=True), lambda: ev.step(*one, attended=True)):
+            with pytest.raises(ValueError):
+                refused()
+        order.capturing = True
+        attends(range(L - 1))
+        order.capturing = False
+        with pytest.raises(ValueError):  # a layer is missing
+            ev.accept(k, k, q, [[0], [0]], attended=True)
+        assert ev.lengths == [8, 8] and ev.next_id == [8, 8]
+        order.capturing = True
+        attends(range(L))
+        order.capturing = False
+        for attended, want in ((True, 1), (None, 0), (False, 0), (True, 1)):
+            ev.accept(k, k, q, [[0], [0, 1]], attended=attended)
+            assert given() == want
+        attends(range(L))
+        ev.accept(k, k, q, [[0], []], attended=False)
+        assert given() == 0
+        attends([1], draft_lens=torch.ones(S, dtype=torch.int32))
+        with pytest.raises(ValueError):  # not every token's
+            ev.accept(k, k, q, [[0], []], attended=True)
+        with pytest.raises(ValueError):  # of other tokens
+            ev.step(*one, attended=True)
+        assert order.races() == []
