@@ -29,7 +29,7 @@ constexpr int AT_DRAFTS_MAX = 64;
 // `nrb` row blocks. Depends on the layout alone (a GB300 has 152 SMs), so that the
 // workspace does.
 struct AttendPlan {
-  int chunk, nsplit, nrb, block, edge;
+  int chunk, nsplit, nrb, block, edge, slots, srows;
   size_t status, counts, nsps, opart, mlpart, total;
 };
 constexpr int64_t F32_EXTRA = 128;
@@ -66,9 +66,14 @@ AttendPlan attend_plan(const jacap_layout* L) {
   // (whatever the layout, so that calls of several layouts may use a workspace one after the other)
   p.counts = o; o = align_up(o + (size_t)ATTEND_CTAS * 4);
   p.nsps = o; o = align_up(o + (bf ? (size_t)ctas * 4 : 0));
-  const size_t parts = p.nsplit > 1 ? (size_t)units * p.nsplit : 0, prows = attend_part_rows(rows);
-  p.opart = o; o = align_up(o + parts * ((rows + prows - 1) / prows * prows) * D * 4);
-  p.mlpart = o; o = align_up(o + parts * rows * 8);
+  // bf16: two slots for each border between CTAs, whatever the units' number: the split before and the one after
+  const int64_t most_ctas = ATTEND_CTAS * 128 / block;
+  const int64_t slots = bf ? 2 * (std::min<int64_t>(ctas * p.nsplit, most_ctas) - 1) : units * p.nsplit;
+  const size_t parts = p.nsplit > 1 ? (size_t)slots : 0, prows = attend_part_rows(rows);
+  p.slots = bf ? (int)slots : 0;
+  p.srows = bf ? std::min(rows, block) : rows;
+  p.opart = o; o = align_up(o + parts * ((p.srows + prows - 1) / prows * prows) * D * 4);
+  p.mlpart = o; o = align_up(o + parts * p.srows * 8);
   p.total = o;
   return p;
 }
@@ -243,7 +248,7 @@ jacap_status jacap_attend(const jacap_layout* layout, const jacap_attention* att
   }
   for (int i = 0; i < 3; ++i) a.ls[i] = attn->lse_strides[i];
   a.scale2 = (float)((double)attn->scale * 1.4426950408889634 * (bf ? 1.0 + TRUNCATION : 1.0));
-  a.prows = attend_part_rows(dm.G * dm.window);
+  a.slots = p.slots, a.srows = p.srows, a.prows = attend_part_rows(dm.G * dm.window);
   a.tdiv = dm.window > 1 ? 0xffffffffu / (uint32_t)dm.window + 1u : 0u;
   a.chunk = p.chunk, a.nsplit = p.nsplit, a.nrb = p.nrb, a.max_seqlen = layout->max_seqlen;
   a.block = p.block, a.least = p.chunk / 64, a.edge = p.edge;

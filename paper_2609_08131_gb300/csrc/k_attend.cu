@@ -110,7 +110,7 @@ struct AtUnit {
   int n, rows, nd, nsp;
   int first;                   // bf16: the CTA that has the unit's first split
   int tok0, tok1, ncache, nt;  // this split's tokens, its tiles of cached tokens and in all (`tile` tokens each)
-  int r0;                      // the CTA's first row
+  int r0;                      // bf16: the CTA's first row (float32: 0)
 };
 // A request's live cached tokens and queries, clamped to what there can be (`ok`: nothing had to be).
 struct AtLive {
@@ -137,6 +137,7 @@ __device__ __forceinline__ AtUnit at_unit(const Dims& dm, const AttendArgs& a, c
   AtUnit x;
   x.u = u;
   x.split = split;
+  x.first = x.r0 = 0;
   const uint32_t plane = u / (uint32_t)dm.S;
   x.s = (int)(u - plane * dm.S);
   x.l = (int)(plane / (uint32_t)dm.Hkv);
@@ -179,11 +180,22 @@ __device__ __forceinline__ int at_head(const Dims& dm, const AttendArgs& a, int 
   return dm.window == 1 ? r : (int)__umulhi((uint32_t)r, a.tdiv);
 }
 
-// A split's unnormalised sums of row r: channels 4 c .. + 3 at [c prows] (the rows of a block lie
+// Where a split's sums lie. bf16: a border between two CTAs divides one unit (and row block) at most, so the first split
+// of a unit of several has slot 2 k, of the CTA k that has it, and each further one 2 k - 1. float32: by unit and split.
+template <typename T>
+__device__ __forceinline__ int64_t at_slot(const AttendArgs& a, const AtUnit& x, int split) {
+  if constexpr (sizeof(T) == 2) return 2 * (x.first + split) - (split > 0 ? 1 : 0);
+  return x.u * a.nsplit + split;
+}
+// A slot's unnormalised sums of row r: channels 4 c .. + 3 at [c prows] (the rows of a block lie
 // next to each other, as a warp's lanes have them).
-__device__ __forceinline__ float4* at_part(const Dims& dm, const AttendArgs& a, int64_t u, int split, int r) {
-  const int rows = a.prows, blocks = (dm.G * dm.window - 1) / rows + 1, b = r / rows;
-  return (float4*)a.opart + ((u * a.nsplit + split) * blocks + b) * (32 * rows) + (r - b * rows);
+__device__ __forceinline__ float4* at_part(const AttendArgs& a, const AtUnit& x, int64_t slot, int r) {
+  const int rows = a.prows, blocks = (a.srows - 1) / rows + 1, b = (r - x.r0) / rows;
+  return (float4*)a.opart + (slot * blocks + b) * (32 * rows) + (r - x.r0 - b * rows);
+}
+// A slot's (maximum, sum) of row r.
+__device__ __forceinline__ float2* at_ml(const AttendArgs& a, const AtUnit& x, int64_t slot, int r) {
+  return (float2*)a.mlpart + slot * a.srows + (r - x.r0);
 }
 
 // Drafted tokens that drafted token t of request s sees (bit j: token j).
@@ -201,9 +213,9 @@ __device__ __forceinline__ void at_put(const Dims& dm, const AttendArgs& a, cons
   const int h = at_head(dm, a, r), t = r - h * dm.window;
   if (t >= x.rows) return;
   if (x.nsp > 1) {
-    const int64_t p = (x.u * a.nsplit + x.split) * ((int64_t)dm.G * dm.window) + r;
-    at_part(dm, a, x.u, x.split, r)[lane * a.prows] = acc;
-    if (lane == 0) *(float2*)(a.mlpart + 2 * p) = make_float2(m, z);
+    const int64_t slot = at_slot<T>(a, x, x.split);
+    at_part(a, x, slot, r)[lane * a.prows] = acc;
+    if (lane == 0) *at_ml(a, x, slot, r) = make_float2(m, z);
     return;
   }
   const float inv = z == 0.f ? 0.f : 1.f / z;
@@ -238,18 +250,19 @@ __device__ __forceinline__ void at_join(const Dims& dm, const AttendArgs& a, con
   for (int i = 0; i < NR; ++i) s[i] = make_float4(0.f, 0.f, 0.f, 0.f);
   if (on) {
     const int r = r0 + rl < R ? r0 + rl : R - 1;
-    const float2* ml = (const float2*)a.mlpart + x.u * a.nsplit * R + r;
-    const float4* o = at_part(dm, a, x.u, 0, r0) + lane * a.prows;
-    const int64_t step = at_part(dm, a, x.u, 1, r0) - at_part(dm, a, x.u, 0, r0);
-    for (int j = lane / NR; j < x.nsp; j += 32 / NR) m = fmaxf(m, ml[(int64_t)j * R].x);
+    const float2* ml = at_ml(a, x, 0, r);
+    const float4* o = at_part(a, x, 0, r0) + lane * a.prows;
+    const int64_t step = at_part(a, x, 1, r0) - at_part(a, x, 0, r0);
+    for (int j = lane / NR; j < x.nsp; j += 32 / NR) m = fmaxf(m, ml[at_slot<T>(a, x, j) * a.srows].x);
 #pragma unroll
     for (int off = NR; off < 32; off <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
 #pragma unroll (NR == 8 ? 2 : 4)
     for (int j = part; j < x.nsp; j += W) {
-      const float2 w = ml[(int64_t)j * R];
+      const int64_t slot = at_slot<T>(a, x, j);
+      const float2 w = ml[slot * a.srows];
       float4 v[NR];
 #pragma unroll
-      for (int i = 0; i < NR; ++i) v[i] = o[j * step + i];  // (rows behind the last lie in the block too)
+      for (int i = 0; i < NR; ++i) v[i] = o[slot * step + i];  // (rows behind the last lie in the block too)
       // (a split that saw nothing has the maximum -inf and the sum 0, one of NaN only -inf and NaN)
       const float f = w.x == m ? 1.f : ex2((w.x - m) * scale2);
       const bool none = w.x == -INFINITY && w.y == 0.f;
@@ -464,7 +477,7 @@ __global__ void __launch_bounds__(AtCfg<NB>::THREADS, 3 - NB)
           if (split < 0 || split >= next.nsp) continue;
           next.split = split;
           next.first = (int)first;
-          if (split == 0) a.nsps[at] = next.nsp;
+          if (split == 0) a.nsps[at] = next.nsp << 16 | (int)first;
           if (next.nt > 0) {
             const int ta = split == 0 ? 0 : (int)((w0 - p0 + c - 1) / c);
             const int tb = split == next.nsp - 1 ? (int)nt : (int)((w0 + per - p0 + c - 1) / c);
@@ -763,8 +776,9 @@ __global__ void __launch_bounds__(AtCfg<NB>::THREADS, 3 - NB)
         float4* part = nullptr;
         __nv_bfloat16* o = nullptr;
         if (on && x.nsp > 1) {
-          part = at_part(dm, a, x.u, x.split, row);
-          *(float2*)(a.mlpart + 2 * ((x.u * a.nsplit + x.split) * R + row)) = make_float2(m, z);
+          const int64_t slot = at_slot<__nv_bfloat16>(a, x, x.split);
+          part = at_part(a, x, slot, row);
+          *at_ml(a, x, slot, row) = make_float2(m, z);
         } else if (on) {
           o = (__nv_bfloat16*)a.o + x.s * a.os[0] + x.l * a.os[1] + (int64_t)(x.g * dm.G + h) * a.os[2] + t * a.os[3];
           if (a.lse != nullptr)
@@ -827,9 +841,9 @@ __global__ void __launch_bounds__(AtCfg<NB>::THREADS, 3 - NB)
           part[j] = nullptr, o[j] = nullptr;
           if (rr >= nrow || t >= x.rows) continue;
           if (x.nsp > 1) {
-            part[j] = at_part(dm, a, x.u, x.split, rr);
-            if (warp == 2)
-              *(float2*)(a.mlpart + 2 * ((x.u * a.nsplit + x.split) * R + rr)) = make_float2(mr[j], zr[j]);
+            const int64_t slot = at_slot<__nv_bfloat16>(a, x, x.split);
+            part[j] = at_part(a, x, slot, rr);
+            if (warp == 2) *at_ml(a, x, slot, rr) = make_float2(mr[j], zr[j]);
           } else {
             o[j] = (__nv_bfloat16*)a.o + x.s * a.os[0] + x.l * a.os[1] + (int64_t)(x.g * dm.G + h) * a.os[2] + t * a.os[3];
             if (warp == 2 && a.lse != nullptr)
@@ -1269,7 +1283,14 @@ __global__ void __launch_bounds__(AJ_THREADS)
   const bool real = w < units * groups;
   const int u = real ? w / groups : 0;
   AtUnit x = at_unit(dm, a, cu, u, 0, AT_TOK, a.chunk);
-  if constexpr (sizeof(T) == 2) x.nsp = a.nsps[a.nrb * u + (w - u * groups) * NR / a.block];
+  if constexpr (sizeof(T) == 2) {
+    const int rb = (w - u * groups) * NR / a.block, shares = a.nsps[a.nrb * u + rb];
+    x.nsp = shares >> 16;
+    x.first = shares & 0xffff;
+    x.r0 = rb * a.block;
+    // (a call that failed may not have written them)
+    if (x.nsp < 0 || x.nsp > a.nsplit || at_slot<T>(a, x, x.nsp) > a.slots + 1) x.nsp = 0;
+  }
   const bool inside = sizeof(T) == 2 && at_joins_inside(x.nsp, R);  // that unit is done
   at_join<T, W, NR>(dm, a, x, real && !inside ? (w - u * groups) * NR : R, warp % W,
                     s_o + (W > 1 ? warp * NR * 32 : 0), s_z[warp]);
@@ -1292,7 +1313,7 @@ static cudaError_t launch_bf16(const CUtensorMap* maps, const Dims& dm, const At
                                int64_t items, int sms, cudaStream_t st) {
   auto kern = attend_bf16_kernel<REP, NB>;
   JACAP_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)at_smem<NB>()));
-  const int places = sms * (3 - NB) < ATTEND_CTAS ? sms * (3 - NB) : ATTEND_CTAS;
+  const int places = sms * (3 - NB) < ATTEND_CTAS / NB ? sms * (3 - NB) : ATTEND_CTAS / NB;
   return launch_pdl(true, kern, (int)(items < places ? items : places), AtCfg<NB>::THREADS, at_smem<NB>(), st, maps[0],
                     maps[1], maps[2], maps[3], dm, a, cu);
 }

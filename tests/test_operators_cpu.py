@@ -120,6 +120,15 @@ def test_attend_workspace_follows_the_splits():
         assert size(131072, window) < 2 * 2 * 2 * 131072 * 256 / 4 + (1 << 16)
 
 
+@pytest.mark.parametrize("window", [1, 8, 20, 64])
+def test_attend_workspace_of_many_units(window):
+    """bf16: what the borders between CTAs leave, however many units and tokens there are."""
+    lay = good_layout(num_seqs=64, num_layers=28, num_q_heads=64, num_kv_heads=8, max_seqlen=131072, total_tokens=64 * 131072,
+                      window=window)
+    units = 64 * 28 * 8
+    assert 0 < J.jacap_attend_workspace(lay) < 2 * 320 * 128 * (512 + 8) + 8 * units + (1 << 14)
+
+
 # -------------------------------------------------------------------- weigh ----
 def weigh(lay=None, how=None, q=P, k=P, lse=P, before=P, weights=P, ws=P, less=0):
     layout = good_layout(**(lay or {}))
