@@ -539,7 +539,8 @@ jacap_status jacap_attend(const jacap_layout* layout, const jacap_attention* att
  *              as they were
  *   ws         device, 256-byte aligned, jacap_weigh_workspace() bytes (0 for a
  *              layout that is refused); the call resets its status word. A weight
- *              that is not finite is reported there (JACAP_ERR_NONFINITE).
+ *              that is not finite (a token's whose K is not, and that a query sees) is reported
+ *              there (JACAP_ERR_NONFINITE).
  */
 typedef struct {
   float scale;

@@ -25,7 +25,8 @@
 // A row's sum takes exp over thousands of tokens: 32 at a time are added plainly and
 // those sums with compensation (Kahan), so that the order of magnitude of the rounding
 // does not grow with the run. Queries that a request does not have, and rows that see
-// nothing (lse = -inf), give no weight: their constant is +inf.
+// nothing (lse = -inf), give no weight: their constant is +inf, and they see no token (a token
+// whose K is not finite and that no row sees has no weight either; one that a row sees, NaN).
 //
 // float32: CUDA cores; a warp takes 8 rows and two tokens per lane, so that 16-byte reads
 // of K and (one address per warp) of Q feed 64 multiply-adds.
@@ -39,6 +40,7 @@ constexpr int WG_BOX = WG_TILE_BYTES / 2;
 constexpr int WG_IMG = 128 * D * 2;
 constexpr int WG_BUILD0 = 2, WG_READ0 = 4;
 constexpr float WG_LAZY = 8.f;  // log2 of how far a logit may pass the running maximum
+constexpr int WG_NONE = -(1 << 30);  // j of a row that gives no weight: it sees no token
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float wg_ex2(float x) {
@@ -249,8 +251,9 @@ __global__ void __launch_bounds__(WgCfg<NRB, SUM>::THREADS, 1)
         const int qi = r < R ? wg_query(dm, a, x, item.seq, j) : -1;
         const int64_t off = qi >= 0 ? h * dm.q_sh + qi * dm.q_sp : 0;
         if constexpr (SUM) {
-          cst[p * C::ROWS + r] = wg_const(dm, a, item, l, g, h, qi, r, C::ROWS);
-          jrow[p * C::ROWS + r] = j;
+          const float2 k = wg_const(dm, a, item, l, g, h, qi, r, C::ROWS);
+          cst[p * C::ROWS + r] = k;
+          jrow[p * C::ROWS + r] = k.y != 0.f ? j : WG_NONE;
         }
 #pragma unroll 8
         for (int k = 0; k < 16; ++k) {  // lanes 0-15 and 16-31: the 16-byte pieces of two rows
@@ -274,7 +277,7 @@ __global__ void __launch_bounds__(WgCfg<NRB, SUM>::THREADS, 1)
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     const float scale2 = a.scale2, lazy = WG_LAZY / scale2;
     uint32_t it = 0, nrun = 0;
-    bool cont = false, bad = false;
+    bool cont = false, bad = false, live = false;
     int c0 = 0;
     WgReq x = {};
     float m[NRB], z[NRB], zc[NRB];  // statistics: running maximum, sum and its compensation
@@ -292,6 +295,12 @@ __global__ void __launch_bounds__(WgCfg<NRB, SUM>::THREADS, 1)
         }
         // (the constants are the builders' work: the tile's accumulators follow them)
         if (SUM && !mbar_wait(smem_u32(&imgready[p]), (nrun / C::IMGS) & 1, ws, abort)) goto done;
+        if constexpr (SUM) {
+          live = false;
+#pragma unroll
+          for (int r = 0; r < C::ROWS; r += 32) live |= jrow[p * C::ROWS + r + lane] != WG_NONE;
+          live = __any_sync(0xffffffffu, live);
+        }
       }
       for (int64_t t = item.t0; t < item.t1; t += TILE, ++it) {
         const int rel = (int)(t - x.start);  // the tile's first token
@@ -368,6 +377,7 @@ __global__ void __launch_bounds__(WgCfg<NRB, SUM>::THREADS, 1)
         }
         if (SUM && (NRB == 4 ? 0 : (int)(it % C::GROUPS)) == grp && y < nv) {
           const int64_t at = (int64_t)item.plane * dm.Ntot + t + y;
+          if (!live) w = 0.f;  // (no row: what K holds is nobody's, NaN included)
           if (a.before != nullptr && rel + y < x.p0) w += a.before[at];
           bad |= !isfinite(w);
           a.weights[at] = w;
@@ -496,7 +506,11 @@ __global__ void __launch_bounds__(32 * WARPS, 2)
         cp_async16(smem_u32(qs + (e >> 5) * D + c), q + (qi >= 0 ? h * dm.q_sh + qi * dm.q_sp : 0) + c, qi >= 0);
         if (c == 0) {
           jrow[e >> 5] = j;
-          if constexpr (SUM) cst[e >> 5] = wg_const(dm, a, item, l, g, h, qi, r, rows);
+          if constexpr (SUM) {
+            const float2 k = wg_const(dm, a, item, l, g, h, qi, r, rows);
+            cst[e >> 5] = k;
+            if (k.y == 0.f) jrow[e >> 5] = WG_NONE;
+          }
         }
       }
       cp_async_commit();

@@ -564,6 +564,31 @@ def test_weigh_reports_what_is_not_finite_and_bad_lengths():
         assert e.value.status == JACAP_ERR_INVALID_ARG
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("given", [False, True])
+@pytest.mark.parametrize("Hq,w", [(3, 3), (8, 40)])
+def test_weigh_keys_that_no_query_sees(Hq, w, given, dtype):
+    """NaN and infinities in K where no query of the request looks: earlier weights stay, nothing is reported."""
+    cap, lengths = 500, [300, 500, 130, 200]
+    q_lens, rows = [0, 3, 2, 3], [[0, 1, 2], [-1, 7 + w, -1], [0, 1, 2], [1, -1, -1]]
+    g = gen(33)
+    cache = make_cache(g, 4, 1, Hq, 1, w, (cap,) * 4, dtype)
+    for s, (first, last) in enumerate(((10, 300), (0, 500), (130, 500), (198, 200))):  # request 2: behind its length
+        cache.k[:, :, s * cap + first:s * cap + last, ::2] = math.nan
+        cache.k[:, :, s * cap + first:s * cap + last, 1::4] = math.inf
+    rows = torch.tensor([r + [-1] * (w - 3) for r in rows], dtype=torch.int32)
+    dev = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    ev = api.WeightEvictor(cache, 1)
+    before = torch.rand(ev.weights.shape, generator=g, device=DEV)
+    args = dict(lengths=dev(lengths), q_lens=dev(q_lens), q_rows=rows.to(DEV), before=before)
+    got, lse = ev.score(**args)
+    if given:
+        got, _ = ev.score(lse=lse.clone(), **args)
+    ev.check()
+    plain = api.Cache(cache.q_win, cache.k.nan_to_num(0.0, 0.0, 0.0), cache.v, cache.cu_seqlens, cache.seqlens, Hq)
+    check_weigh(plain, got, None, weigh_plain(plain, lengths, q_lens, rows, lse=lse if given else None, before=before))
+
+
 # ------------------------------------------------------------------ evict ----
 def select_plain(weights, n, budget, sinks, recent, tags=None):
     tag = torch.arange(n) if tags is None else tags.cpu().long()
