@@ -162,6 +162,15 @@ def _tensor(name, t, device, dtype, shape, contiguous=False):
     return t.data_ptr()
 
 
+def _on_one_device(cache):
+    """The cache's tensors are on one device and its ranges int32 there: the kernels read all of them."""
+    if cache.v.device != cache.k.device or cache.q_win.device != cache.k.device:
+        raise ValueError(f"q_win, k and v must be on one device, not {cache.q_win.device}, {cache.k.device} and "
+                         f"{cache.v.device}")
+    _tensor("cu_seqlens", cache.cu_seqlens, cache.k.device, torch.int32, (len(cache.seqlens) + 1,), True)
+    return cache
+
+
 def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling=None):
     """(frequencies, amplitude): the rot_dim / 2 angles per position in 64 bits,
     base^(-2 i / rot_dim), changed for long contexts by ``scaling``:
@@ -330,7 +339,7 @@ class CacheAttention:
     ``o`` [S, L, Hq, T, 128] and ``lse`` [S, L, Hq, T] (float32), which each run overwrites."""
 
     def __init__(self, cache: Cache, scale: float | None = None):
-        self.cache = cache
+        self.cache = _on_one_device(cache)
         self.device, self.dtype = cache.k.device, cache.k.dtype
         q = cache.q_win
         if q.dim() != 5 or q.shape != (len(cache.seqlens), cache.k.shape[0], cache.num_q_heads, q.shape[3], 128):
@@ -412,7 +421,7 @@ class WeightEvictor:
     ``v_out`` as ``Evictor``'s, and ``weights_out`` [L, Hkv, S, budget]."""
 
     def __init__(self, cache: Cache, budget: int, sinks: int = 0, recent: int = 0, scale: float | None = None):
-        self.cache, self.budget = cache, int(budget)
+        self.cache, self.budget = _on_one_device(cache), int(budget)
         self.sinks, self.recent = int(sinks), int(recent)
         if self.budget < 1 or self.sinks < 0 or self.recent < 0 or self.sinks + self.recent > self.budget:
             raise ValueError("the budget must be positive and hold the sinks and the recent tokens")
@@ -908,10 +917,14 @@ class DecodeEvictor:
             self._layouts[n] = self._layout(n, window=1, q_strides=(128, 128, 128, 128))
         return self._layouts[n]
 
+    def _queries(self, q):
+        if (q.dtype != self.dtype or q.device != self.device or q.dim() != 5 or q.stride(-1) != 1
+                or tuple(q.shape) != (self.S, self.L, self.Hq, q.shape[3], 128)):
+            raise ValueError("queries must be [S, L, Hq, m, 128] in the cache dtype, on its device")
+
     def _merge(self, q, reset: bool, stream=None):
         """q: [S, L, Hq, m, 128] queries (the slot dtype, channel contiguous)."""
-        if q.dtype != self.dtype or q.stride(-1) != 1 or tuple(q.shape[:3]) != (self.S, self.L, self.Hq):
-            raise ValueError("queries must be [S, L, Hq, m, 128] in the cache dtype")
+        self._queries(q)
         lay = self._layout(self.S, q.shape[3], (q.stride(0), q.stride(1), q.stride(2), q.stride(3)))
         self._on(stream, lambda st: _check(jacap_stats_update(lay, _ptr(q), 1 if reset else 0, _ptr(self.stats),
                                                               _ptr(self.counts), st), "jacap_stats_update"))
@@ -923,6 +936,7 @@ class DecodeEvictor:
         after what the current stream holds and before what it gets next."""
         if any(n < 0 or n >= self.cap for n in lengths):
             raise ValueError("a prefill cache must hold fewer than budget + interval tokens; evict it first")
+        (self._weighing if self.rule == "weight" else self._queries)(q_win)  # refused before the slots change
         n = k0.shape[3]
 
         def load(_):
@@ -1015,7 +1029,8 @@ class DecodeEvictor:
 
     def merge_queries(self, q_new, stream=None):
         """Merge one decode step's queries [S, L, Hq, 128] into the running statistics."""
-        if q_new.is_contiguous() and q_new.dtype == self.dtype and tuple(q_new.shape) == (self.S, self.L, self.Hq, 128):
+        if (q_new.is_contiguous() and (q_new.dtype, q_new.device) == (self.dtype, self.device)
+                and tuple(q_new.shape) == (self.S, self.L, self.Hq, 128)):
             self._on(stream, lambda st: _check(jacap_stats_update(self.step_layout, _ptr(q_new), 0, _ptr(self.stats),
                                                                   _ptr(self.counts), st), "jacap_stats_update"))
         else:
@@ -1257,16 +1272,20 @@ class DecodeEvictor:
         if self.rule == "weight":
             self._weigh(q, lse, path, stream)
 
+    def _weighing(self, q):
+        """The layout of a weighing by the queries q and the bytes of its workspace; refuses what has none."""
+        self._queries(q)
+        lay = self._layout(self.S, q.shape[3], _strides(q))
+        nbytes = jacap_weigh_workspace(lay)
+        if nbytes == 0:
+            raise JacapError(2 if self.Hq // self.Hkv * q.shape[3] > 512 else 1, "jacap_weigh_workspace")
+        return lay, nbytes
+
     def _weigh(self, q, lse, path, stream):
         """Add the weights of the queries q [S, L, Hq, w, 128] (of `path` of them; None: the window of a
         prompt) to the slots' tokens; lse: their normalisers, or None."""
         w = q.shape[3]
-        if q.dtype != self.dtype or q.stride(-1) != 1 or tuple(q.shape) != (self.S, self.L, self.Hq, w, 128):
-            raise ValueError("queries must be [S, L, Hq, w, 128] in the cache dtype")
-        lay = self._layout(self.S, w, _strides(q))
-        nbytes = jacap_weigh_workspace(lay)
-        if nbytes == 0:
-            raise JacapError(2 if self.Hq // self.Hkv * w > 512 else 1, "jacap_weigh_workspace")
+        lay, nbytes = self._weighing(q)
         how = jacap_weighing()
         how.scale, how.lse_given = self.scale, int(lse is not None)
 

@@ -376,6 +376,40 @@ def test_arguments_are_checked_before_anything_runs():
         ev.select_compact(pos=torch.zeros((1, 1, 32)))
 
 
+@pytest.mark.parametrize("change", [
+    {"cu_seqlens": torch.tensor([0, 32])}, {"cu_seqlens": torch.tensor([0, 16, 32], dtype=torch.int32)},
+    {"cu_seqlens": torch.tensor([0, 0, 32, 0], dtype=torch.int32)[::2]}, {"cu_seqlens": [0, 32]},
+    {"cu_seqlens": torch.tensor([0, 32], dtype=torch.int32, device="meta")},
+    {"v": torch.zeros((1, 1, 32, 128), dtype=torch.bfloat16, device="meta")},
+    {"q_win": torch.zeros((1, 1, 2, 4, 128), dtype=torch.bfloat16, device="meta")}])
+def test_a_cache_is_on_one_device(change):
+    cache = cpu_cache()
+    for name, t in change.items():
+        setattr(cache, name, t)
+    with pytest.raises(ValueError):
+        api.CacheAttention(cache)
+    with pytest.raises(ValueError):
+        api.WeightEvictor(cache, 8)
+
+
+@pytest.mark.parametrize("rule", ["jacap", "weight"])
+def test_queries_are_refused_before_the_slots_change(rule):
+    ev = api.DecodeEvictor(1, 1, 2, 1, 8, 4, device="cpu", rule=rule)
+    k0 = torch.ones((1, 1, 1, 5, 128), dtype=torch.bfloat16)
+    good = torch.zeros((1, 1, 2, 4, 128), dtype=torch.bfloat16)
+    bad = [good.float(), good[..., :64], good[:, :, :1], good.to("meta"), good.transpose(3, 4).contiguous().transpose(3, 4)]
+    for q in bad:
+        with pytest.raises(ValueError):
+            ev.start(k0, k0, q, [5])
+        if rule == "jacap":
+            with pytest.raises(ValueError):
+                ev.merge_queries(q[:, :, :, 0])
+    if rule == "weight":
+        with pytest.raises(api.JacapError):
+            ev.start(k0, k0, torch.zeros((1, 1, 2, 257, 128), dtype=torch.bfloat16), [5])
+    assert ev.lengths == [0] and not ev.k.any()
+
+
 @pytest.mark.parametrize("w,Hq", [(65, 2), (64, 64)])
 def test_windows_past_the_limits_are_refused(w, Hq):
     cache = cpu_cache(w=w, Hq=Hq, Hkv=Hq // 2 if Hq < 64 else 4, n=80)
