@@ -456,7 +456,8 @@ class WeightEvictor:
         ``CacheAttention`` returned them for these queries (computed into ``lse`` if None);
         before: earlier weights to add to (``weights`` itself works); lengths, q_lens: int32
         [S] live tokens and queries of each request; q_rows: int32 [S, w] which query is
-        the j-th."""
+        the j-th. All of a prompt's queries: w at a time, from the first ones, with
+        lengths the tokens up to the last of them and before=weights from the second call on."""
         c, h, dev = self.cache, self._how, self.device
         if q is None:
             q = c.q_win

@@ -565,6 +565,37 @@ def test_weigh_reports_what_is_not_finite_and_bad_lengths():
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+def test_weights_of_all_of_a_prompt_s_queries(dtype):
+    """Window by window from the first token on, each on top of the ones before: the causal softmax weights of every
+    query, summed. Bounds as in weigh_plain, and a rounding for each window's addition."""
+    S, Hq, Hkv, w, lens = 2, 6, 2, 32, (310, 75)
+    g = gen(34)
+    cache = make_cache(g, S, 1, Hq, Hkv, w, lens, dtype, spread=2.0)
+    q = torch.zeros((S, 1, Hq, 320, D), dtype=dtype, device=DEV)
+    q[:] = (2.0 * randn(g, *q.shape)).to(dtype)
+    ev = api.WeightEvictor(cache, 1)
+    dev = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    for c in range(10):
+        q_lens = [min(max(n - w * c, 0), w) for n in lens]
+        ev.score(q[:, :, :, w * c:w * (c + 1)], lengths=dev([min(n, w * (c + 1)) for n in lens]), q_lens=dev(q_lens),
+                 before=ev.weights if c else None)
+        ev.check()
+    first = 0
+    for s, n in enumerate(lens):
+        for h in range(Hkv):
+            k, sums, tol = cache.k[0, h, first:first + n].double(), 0.0, 0.0
+            for hq in range(3 * h, 3 * h + 3):
+                x = q[s, 0, hq, :n].double() @ k.t() * SCALE
+                size = (q[s, 0, hq, :n].abs().double() @ k.abs().t()).amax(1, keepdim=True) * SCALE
+                x = x.masked_fill(~torch.ones(n, n, dtype=torch.bool, device=DEV).tril(), -math.inf)
+                p = torch.softmax(x, 1)
+                sums = sums + p.sum(0)
+                tol = tol + (p * (2 * (136 * 2.0 ** -24 * size + 2.0 ** -20) + 2.0 ** -22 * x.clamp(min=-1e4).abs())).sum(0)
+            within(ev.weights[0, h, first:first + n], sums, tol + sums * (2.0 ** -22 + 10 * 2.0 ** -24), "weights")
+        first += n
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("given", [False, True])
 @pytest.mark.parametrize("Hq,w", [(3, 3), (8, 40)])
 def test_weigh_keys_that_no_query_sees(Hq, w, given, dtype):
