@@ -23,8 +23,8 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libjacap.so")
 
 SOURCES = ["jacap_api.cu", "k_stream.cu", "k_kpass.cu", "k_gram.cu", "k_factor.cu", "k_score.cu", "k_select.cu",
-           "jacap_static.cu", "k_kfull.cu", "k_decode.cu", "jacap_host.cu", "k_fused.cu", "jacap_attn.cu", "k_attend.cu",
-           "k_weigh.cu", "k_rope.cu"]
+           "jacap_static.cu", "k_kfull.cu", "k_decode.cu", "jacap_host.cu", "k_fused.cu", "jacap_attn.cu",
+           "k_attend.cu", "k_weigh.cu", "k_rope.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 CFLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr",
           "-I" + INCLUDE, "-I" + CSRC]

@@ -246,8 +246,9 @@ class Rope:
         of any strides but the last axis' (float32 or bfloat16); positions: int32 of the
         leading axes' shape. Returns the turned (q, k): new tensors, or the same ones
         with ``inplace``. ``inverse`` turns back (and is the gradient)."""
-        key = (None if q is None else (q.dtype, q.shape, q.stride()), None if k is None else (k.dtype, k.shape, k.stride()),
-               positions.dtype, positions.shape, positions.stride(), inplace)
+        key = (None if q is None else (q.dtype, q.shape, q.stride()),
+               None if k is None else (k.dtype, k.shape, k.stride()), positions.dtype, positions.shape,
+               positions.stride(), inplace)
         last, call = self._last
         if key != last:  # (comparing with the call before is cheaper than a look-up)
             call = self._calls.get(key)
@@ -287,14 +288,16 @@ class Rope:
             raise ValueError("q or k must be given")
         lead, dtype = first.shape[:-2], first.dtype
         if len(lead) not in (1, 2) or dtype not in (torch.float32, torch.bfloat16):
-            raise ValueError("q and k must be float32 or bfloat16 [tokens, heads, 128] or [requests, tokens, heads, 128]")
+            raise ValueError("q and k must be float32 or bfloat16 [tokens, heads, 128] or [requests, tokens, heads, "
+                             "128]")
         if positions.dtype is not torch.int32 or positions.shape != lead:
             raise ValueError(f"positions must be int32 of shape {tuple(lead)}")
         two, args = len(lead) == 2, [None, None]
         for i, (name, t) in enumerate((("q", q), ("k", k))):
             if t is None:
                 continue
-            if t.dtype is not dtype or t.dim() != len(lead) + 2 or t.shape != (*lead, t.shape[-2], 128) or t.stride(-1) != 1:
+            if (t.dtype is not dtype or t.dim() != len(lead) + 2 or t.shape != (*lead, t.shape[-2], 128)
+                    or t.stride(-1) != 1):
                 raise ValueError(f"{name} must be {dtype} {(*lead, 'heads', 128)} with a contiguous last axis")
             if t.shape[-2] < 1:
                 raise ValueError(f"{name} has no heads")
@@ -758,8 +761,8 @@ class _SlotAttention:
         self.complete = set()  # layers whose last call, captured or not, was one that leaves every token's normalisers
 
     def ready(self, layer, shape, device):
-        """The layer's part of ``lse``, with the workspace zeroed, on the current stream. Captured calls zero for themselves
-        at every replay until an eager call has done so."""
+        """The layer's part of ``lse``, with the workspace zeroed, on the current stream. Captured calls zero for
+        themselves at every replay until an eager call has done so."""
         if self.ws is None:
             self.ws = torch.empty(self.nbytes, dtype=torch.uint8, device=device)
             self.lse = torch.empty(shape, dtype=torch.float32, device=device)
@@ -1082,7 +1085,8 @@ class DecodeEvictor:
             if self.rule == "weight":
                 _check(jacap_evict_weights(lay, _ptr(self._w[0, 0, a]), pos, self.sinks, self.recent, self.budget,
                                            _ptr(self.idx), _ptr(self.kept), k, v, self.preserve_order,
-                                           _ptr(self.scores), _ptr(self.ws), self.ws.numel(), st), "jacap_evict_weights")
+                                           _ptr(self.scores), _ptr(self.ws), self.ws.numel(), st),
+                       "jacap_evict_weights")
                 return
             _check(jacap_score_stats(lay, self.params, _ptr(self.stats[a]), _ptr(self.counts[a]), k, v,
                                      _ptr(self.scores), _ptr(self.ws), self.ws.numel(), st, handles),

@@ -685,8 +685,8 @@ jacap_status jacap_append_path(const jacap_layout* layout, const void* k_new, co
   a.k = k, a.v = v, a.pos = pos, a.stats = stats, a.counts = counts;
   const TraceRange trace("jacap/append_path");
   for (int j = 0; j < most; ++j)
-    if ((st = map_cuda(launch_append(dm, layout->dtype == JACAP_BF16 ? 1 : 0, a, lengths, ids, (cudaStream_t)stream, path,
-                                     depth, taken, j))) != JACAP_OK)
+    if ((st = map_cuda(launch_append(dm, layout->dtype == JACAP_BF16 ? 1 : 0, a, lengths, ids, (cudaStream_t)stream,
+                                     path, depth, taken, j))) != JACAP_OK)
       return st;
   return JACAP_OK;
 }
@@ -696,7 +696,8 @@ namespace {
 // Checks shared by the selections by attention weights.
 jacap_status check_weights(const jacap_layout* layout, const float* weights, const int32_t* pos, int32_t sinks,
                            int32_t recent, int32_t budget, const int32_t* idx, const int32_t* kept, const void* k,
-                           const void* v, const float* keys, bool keys_needed, void* ws, size_t ws_bytes, Ws* w, Dims* dm) {
+                           const void* v, const float* keys, bool keys_needed, void* ws, size_t ws_bytes, Ws* w,
+                           Dims* dm) {
   jacap_status st = check_layout(layout);
   if (st != JACAP_OK) return st;
   if (weights == nullptr || idx == nullptr || kept == nullptr || k == nullptr || v == nullptr ||
@@ -724,10 +725,11 @@ jacap_status jacap_select_weights(const jacap_layout* layout, const float* weigh
                                   size_t ws_bytes, void* stream) {
   Ws w;
   Dims dm;
-  jacap_status st = check_weights(layout, weights, pos, sinks, recent, budget, idx, kept, k, v, keys, pos != nullptr, ws, ws_bytes,
-                                  &w, &dm);
+  jacap_status st = check_weights(layout, weights, pos, sinks, recent, budget, idx, kept, k, v, keys, pos != nullptr,
+                                  ws, ws_bytes, &w, &dm);
   if (st != JACAP_OK) return st;
-  if (k_out == nullptr || v_out == nullptr || !aligned16(k_out) || !aligned16(v_out) || ((uintptr_t)weights_out & 3u) != 0)
+  if (k_out == nullptr || v_out == nullptr || !aligned16(k_out) || !aligned16(v_out) ||
+      ((uintptr_t)weights_out & 3u) != 0)
     return JACAP_ERR_INVALID_ARG;
   int sms = 0;
   if ((st = check_device(&sms)) != JACAP_OK) return st;
@@ -737,24 +739,24 @@ jacap_status jacap_select_weights(const jacap_layout* layout, const float* weigh
   const int dt = layout->dtype == JACAP_BF16 ? 1 : 0;
   if (pos == nullptr) {  // by row: in the selection itself
     if (weights_out == nullptr) wr.p = nullptr;
-    return map_cuda(launch_select(dm, w, layout->cu_seqlens, weights, budget, idx, kept, layout->max_seqlen, s, dt, k, v,
-                                  k_out, v_out, nullptr, nullptr, nullptr, wr, weights_out, sinks, recent));
+    return map_cuda(launch_select(dm, w, layout->cu_seqlens, weights, budget, idx, kept, layout->max_seqlen, s, dt, k,
+                                  v, k_out, v_out, nullptr, nullptr, nullptr, wr, weights_out, sinks, recent));
   }
   if ((st = map_cuda(launch_protect(dm, w, layout->cu_seqlens, wr, pos, sinks, recent, keys, layout->max_seqlen, s))) !=
       JACAP_OK)
     return st;
   if (weights_out == nullptr) wr.p = nullptr;
-  return map_cuda(launch_select(dm, w, layout->cu_seqlens, keys, budget, idx, kept, layout->max_seqlen, s, dt, k, v, k_out,
-                                v_out, nullptr, nullptr, nullptr, wr, weights_out));
+  return map_cuda(launch_select(dm, w, layout->cu_seqlens, keys, budget, idx, kept, layout->max_seqlen, s, dt, k, v,
+                                k_out, v_out, nullptr, nullptr, nullptr, wr, weights_out));
 }
 
-jacap_status jacap_evict_weights(const jacap_layout* layout, float* weights, int32_t* pos, int32_t sinks, int32_t recent,
-                                 int32_t budget, int32_t* idx, int32_t* kept, void* k, void* v, int32_t preserve_order,
+jacap_status jacap_evict_weights(const jacap_layout* layout, float* weights, int32_t* pos, int32_t sinks,
+                                 int32_t recent, int32_t budget, int32_t* idx, int32_t* kept, void* k, void* v, int32_t preserve_order,
                                  float* keys, void* ws, size_t ws_bytes, void* stream) {
   Ws w;
   Dims dm;
-  jacap_status st = check_weights(layout, weights, pos, sinks, recent, budget, idx, kept, k, v, keys, true, ws, ws_bytes,
-                                  &w, &dm);
+  jacap_status st = check_weights(layout, weights, pos, sinks, recent, budget, idx, kept, k, v, keys, true, ws,
+                                  ws_bytes, &w, &dm);
   if (st != JACAP_OK) return st;
   if (preserve_order != 0 && preserve_order != 1) return JACAP_ERR_INVALID_ARG;
   if (dm.kv_sl % dm.kv_st != 0 || dm.kv_sh % dm.kv_st != 0) return JACAP_ERR_INVALID_ARG;
@@ -768,9 +770,10 @@ jacap_status jacap_evict_weights(const jacap_layout* layout, float* weights, int
       JACAP_OK)
     return st;
   if (!preserve_order)
-    return map_cuda(launch_select(dm, w, layout->cu_seqlens, keys, budget, idx, kept, layout->max_seqlen, s, dt, nullptr,
-                                  nullptr, nullptr, nullptr, k, v, pos, wr));
-  if ((st = map_cuda(launch_select(dm, w, layout->cu_seqlens, keys, budget, idx, kept, layout->max_seqlen, s))) != JACAP_OK)
+    return map_cuda(launch_select(dm, w, layout->cu_seqlens, keys, budget, idx, kept, layout->max_seqlen, s, dt,
+                                  nullptr, nullptr, nullptr, nullptr, k, v, pos, wr));
+  if ((st = map_cuda(launch_select(dm, w, layout->cu_seqlens, keys, budget, idx, kept, layout->max_seqlen, s))) !=
+      JACAP_OK)
     return st;
   return map_cuda(launch_compact_inplace(dm, w, dt, layout->cu_seqlens, k, v, pos, idx, budget, 1, s, wr));
 }

@@ -41,9 +41,9 @@ AttendPlan attend_plan(const jacap_layout* L) {
   const int64_t units = (int64_t)L->num_seqs * L->num_layers * L->num_kv_heads, ctas = units * p.nrb;
   const int64_t most = L->max_seqlen;
   // bf16: the least that a CTA's share may have (the kernel shares out the live tokens); a split's sums,
-  // written and read by the join, stay an eighth of its K and V on the average. float32: of the splits of 128 tokens or more
-  // that fill one to four rounds of CTAs (three, two or one on an SM), or none, those whose last round ends
-  // first, with F32_EXTRA tokens' time for a CTA's start and end (64 to 512 measured alike).
+  // written and read by the join, stay an eighth of its K and V on the average. float32: of the splits of 128
+  // tokens or more that fill one to four rounds of CTAs (three, two or one on an SM), or none, those whose last
+  // round ends first, with F32_EXTRA tokens' time for a CTA's start and end (64 to 512 measured alike).
   int64_t chunk = std::max<int64_t>(256, std::min(rows, block) * 16);
   if (!bf) {
     const int64_t places = 152 * (block <= 8 ? 3 : (block == 16 ? 2 : 1));
@@ -151,7 +151,8 @@ jacap_status jacap_rotate(const jacap_rope* rope, jacap_dtype dtype, int32_t num
                           const jacap_rope_tensor* q, const jacap_rope_tensor* k, void* stream) {
   if (rope == nullptr || positions == nullptr || position_strides == nullptr || (q == nullptr && k == nullptr))
     return JACAP_ERR_INVALID_ARG;
-  if ((dtype != JACAP_F32 && dtype != JACAP_BF16) || num_seqs < 0 || tokens < 0 || (int64_t)num_seqs * tokens > INT32_MAX - 4 || (inverse != 0 && inverse != 1))
+  if ((dtype != JACAP_F32 && dtype != JACAP_BF16) || num_seqs < 0 || tokens < 0 ||
+      (int64_t)num_seqs * tokens > INT32_MAX - 4 || (inverse != 0 && inverse != 1))
     return JACAP_ERR_INVALID_ARG;
   if (rope->head_dim != D) return JACAP_ERR_UNSUPPORTED;
   if (rope->rot_dim < 2 || rope->rot_dim > D || rope->rot_dim % 2 != 0 || rope->turns == nullptr ||
@@ -173,7 +174,8 @@ jacap_status jacap_rotate(const jacap_rope* rope, jacap_dtype dtype, int32_t num
     const int64_t count[3] = {num_seqs, tokens, t.heads};
     for (int d = 0; d < 3; ++d) {
       // rows of the result do not overlap; in place the two are laid out alike
-      if (t.x_strides[d] < 0 || t.y_strides[d] < 0 || (count[d] > 1 && t.y_strides[d] < D)) return JACAP_ERR_INVALID_ARG;
+      if (t.x_strides[d] < 0 || t.y_strides[d] < 0 || (count[d] > 1 && t.y_strides[d] < D))
+        return JACAP_ERR_INVALID_ARG;
       if (t.x == t.y && count[d] > 1 && t.x_strides[d] != t.y_strides[d]) return JACAP_ERR_INVALID_ARG;
       if (count[d] > 1) vec = vec && t.x_strides[d] % V == 0 && t.y_strides[d] % V == 0;
       out[i]->xs[d] = t.x_strides[d];

@@ -108,6 +108,19 @@ enum { TR_GRAM0 = 0, TR_GRAM1, TR_FAC0, TR_FAC1, TR_SC_IMG, TR_SC1, TR_SC_MMA, T
 enum { TR_K_GRAM = 0, TR_K_SCORE = 1, TR_K_KPASS = 2, TR_K_FACTOR = 3, TR_K_SELECT = 4, TR_KERNELS = 5, TR_CTAS = 1024,
        TR_CTA_SLOTS = 16 };
 
+// 2^x, off by some 2^-22 relative; 0 below 2^-126.
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// The head of row r of a group's heads with `window` queries each: r / window, exact for r below 2^16 and
+// tdiv = 2^32 / window, rounded up.
+__device__ __forceinline__ int row_head(int window, uint32_t tdiv, int r) {
+  return window == 1 ? r : (int)__umulhi((uint32_t)r, tdiv);
+}
+
 // One float per token beside a cache: that of token t of plane (l, g) at l sl + g sh + t.
 struct WeightRef {
   float* p;  // or null

@@ -193,18 +193,20 @@ struct AttendArgs {
   float scale2;               // scale log2 e, recentred for the tensor cores' truncation
   int chunk, nsplit, nrb, max_seqlen;  // tokens per split (float32), splits of a request at most, row blocks
   int block;                  // rows of a row block
-  int least, edge;            // bf16: least tiles of a CTA's share, and between a split's border and a unit's start or end
+  int least, edge;            // bf16: least tiles of a CTA's share, and between a split's border and a unit's start
+                              // or end
   int slots;                  // bf16: of splits' sums
   int srows, prows;           // rows of a split's sums, and of a block of them (attend_part_rows)
   uint32_t tdiv;              // 2^32 / window, rounded up (window > 1)
   float *opart, *mlpart;      // the splits' sums [slots][blocks of srows][32][prows][4], and their
                               // [slots][srows][2] (maximum, sum); slot of a split: at_slot (k_attend.cu)
-  int32_t* counts;            // [ATTEND_CTAS] splits done of the unit whose first split is the CTA's, where the last one
-                              // joins them (zero between calls, and at one place in every layout's workspace)
+  int32_t* counts;            // [ATTEND_CTAS] splits done of the unit whose first split is the CTA's, where the last
+                              // one joins them (zero between calls, and at one place in every layout's workspace)
   int32_t* nsps;              // bf16: [units][row blocks] this call's splits (<< 16) and the CTA of the first
   uint32_t* status;
 };
-constexpr int ATTEND_CTAS = 320;  // CTAs that share out a bf16 call's tiles, at most (two to each of 160 SMs; a GB300 has 152)
+// CTAs that share out a bf16 call's tiles, at most (two to each of 160 SMs; a GB300 has 152)
+constexpr int ATTEND_CTAS = 320;
 int attend_row_block(int dtype, int rows);  // rows of a CTA
 int attend_part_rows(int rows);
 // maps: K, V, drafted K, drafted V (bf16)

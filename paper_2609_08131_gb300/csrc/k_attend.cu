@@ -38,8 +38,8 @@
 // cached ones; 37 us = 3.7 TB/s for one token in 16 slots of 2100, of which ~8 us are the
 // launch and the first tiles' way; 9 us for one token over 37): bound by memory up to 128 rows.
 // 64 drafted tokens of 5 heads a group, 320 rows, over 110000 tokens in 16 requests: 168 us for
-// 138 GFLOP and 842 MB (K and V twice, 5.4 TB/s). A tile of 256 rows takes ~1500 cycles: the products ~1280 (S reads its rows from
-// shared memory again for every 64 tokens, 48 cycles for each 128 x 64 x 16), and the softmax
+// 138 GFLOP and 842 MB (K and V twice, 5.4 TB/s). A tile of 256 rows takes ~1500 cycles: the products ~1280
+// (S reads its rows from shared memory again for every 64 tokens, 48 cycles for each 128 x 64 x 16), and the softmax
 // ~1150 with two warps per scheduler, which overlap but for the waits between them. Tried and
 // left out, of 216 us at the time: an MMA issuer per block (218), the barriers asked ahead of the
 // issue (226).
@@ -50,9 +50,9 @@
 // barrier but the one that says they have landed; the warps are joined at the end. More rows
 // are a product of tiles (attend_f32_rows_kernel). Measured, 8 KV heads: 5 rows over 5473 tokens
 // in two requests 32 us (45 MB: 7 us at the copy rate; the splits' start and end and the join are
-// the rest), one row over 32768 tokens 57 us (268 MB: 40 us; with eight rows to a block 76 us); 4 requests of 4096 tokens with 12 rows 84 us,
-// 25 rows 157 us; 2 requests with 64 rows 94 us, 256 rows 275 us (8.6 GFLOP: 115 us at 75 TFLOP/s;
-// 574 us with 32 rows to a block, which read shared memory four times for as many multiply-adds).
+// the rest), one row over 32768 tokens 57 us (268 MB: 40 us; with eight rows to a block 76 us); 4 requests of
+// 4096 tokens with 12 rows 84 us, 25 rows 157 us; 2 requests with 64 rows 94 us, 256 rows 275 us (8.6 GFLOP: 115 us
+// at 75 TFLOP/s; 574 us with 32 rows to a block, which read shared memory four times for as many multiply-adds).
 #include "jacap_dev.cuh"
 #include "jacap_internal.h"
 
@@ -73,12 +73,6 @@ struct AtCfg {
 };
 constexpr float AT_LAZY = 8.f;         // log2 of how far a logit may pass the maximum
 
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
 // Two values at once: the same arithmetic in half the issue slots.
 __device__ __forceinline__ float2 fma2(float2 x, float2 y, float2 z) {
   float2 r;
@@ -93,8 +87,8 @@ __device__ __forceinline__ float2 add2(float2 x, float2 y) {
   return r;
 }
 
-__device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, int c3, int c4,
-                                            uint32_t bar) {
+__device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, int c3,
+                                            int c4, uint32_t bar) {
   asm volatile(
       "cp.async.bulk.tensor.5d.shared::cta.global.tile.mbarrier::complete_tx::bytes"
       " [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst),
@@ -162,7 +156,8 @@ __device__ __forceinline__ AtUnit at_unit(const Dims& dm, const AttendArgs& a, c
 template <int NB>
 struct AtSmem {
   uint64_t full[AtCfg<NB>::RING], empty[AtCfg<NB>::RING], sfull[2], pready[2];
-  uint64_t pvdone[2];  // by a tile's parity: a wait for tile i knows that tile i - 2's product is done (S of tile i follows it)
+  uint64_t pvdone[2];  // by a tile's parity: a wait for tile i knows that tile i - 2's product is done (S of tile i
+                       // follows it)
   uint64_t qfull[AT_QUEUE], qempty[AT_QUEUE];
   uint64_t rowsready, rowsfree, rowsasked, ofree;
   AtUnit queue[AT_QUEUE];
@@ -175,13 +170,10 @@ template <int NB>
 constexpr size_t at_smem() { return 233472 / (3 - NB) - 1024; }
 static_assert(at_used<1>() <= at_smem<1>() && at_used<2>() <= at_smem<2>(), "shared memory");
 static_assert(128 * D * 2 >= 128 * 64 * 4, "the rows' space holds half the channels of the accumulators (copies)");
-// The head of a unit's row r (r / window, exact for r below 2^16).
-__device__ __forceinline__ int at_head(const Dims& dm, const AttendArgs& a, int r) {
-  return dm.window == 1 ? r : (int)__umulhi((uint32_t)r, a.tdiv);
-}
 
-// Where a split's sums lie. bf16: a border between two CTAs divides one unit (and row block) at most, so the first split
-// of a unit of several has slot 2 k, of the CTA k that has it, and each further one 2 k - 1. float32: by unit and split.
+// Where a split's sums lie. bf16: a border between two CTAs divides one unit (and row block) at most, so the first
+// split of a unit of several has slot 2 k, of the CTA k that has it, and each further one 2 k - 1. float32: by unit
+// and split.
 template <typename T>
 __device__ __forceinline__ int64_t at_slot(const AttendArgs& a, const AtUnit& x, int split) {
   if constexpr (sizeof(T) == 2) return 2 * (x.first + split) - (split > 0 ? 1 : 0);
@@ -210,7 +202,7 @@ __device__ __forceinline__ uint64_t at_mask(const Dims& dm, const AttendArgs& a,
 template <typename T>
 __device__ __forceinline__ void at_put(const Dims& dm, const AttendArgs& a, const AtUnit& x, int r, float4 acc, float m,
                                        float z, int lane) {
-  const int h = at_head(dm, a, r), t = r - h * dm.window;
+  const int h = row_head(dm.window, a.tdiv, r), t = r - h * dm.window;
   if (t >= x.rows) return;
   if (x.nsp > 1) {
     const int64_t slot = at_slot<T>(a, x, x.split);
@@ -239,8 +231,8 @@ __host__ __device__ __forceinline__ bool at_joins_inside(int nsp, int R) { retur
 // other; with a barrier of the whole block, which all its warps reach); one warp needs none. A lane
 // has channels 4 lane .. + 3 of all the rows.
 template <typename T, int W, int NR>
-__device__ __forceinline__ void at_join(const Dims& dm, const AttendArgs& a, const AtUnit& x, int r0, int part, float4* s_o,
-                                        float* s_z) {
+__device__ __forceinline__ void at_join(const Dims& dm, const AttendArgs& a, const AtUnit& x, int r0, int part,
+                                        float4* s_o, float* s_z) {
   const int R = dm.G * dm.window, lane = threadIdx.x & 31, rl = lane % NR;
   const float scale2 = a.scale2;
   const bool on = r0 < R && x.nsp > 1;
@@ -341,7 +333,8 @@ __global__ void __launch_bounds__(AtCfg<NB>::THREADS, 3 - NB)
   using C = AtCfg<NB>;
   static_assert(NB == 1 || REP == 1, "copies are for few rows");
   constexpr int AT_RING = C::RING, AT_LOAD0 = C::LOAD0, AT_LOADERS = C::LOADERS;
-  constexpr uint32_t AT_O = 128 * NB;  // columns [0, AT_O): S of block j at 128 j + 64 (tile % 2); O of block j at AT_O + 128 j
+  // columns [0, AT_O): S of block j at 128 j + 64 (tile % 2); O of block j at AT_O + 128 j
+  constexpr uint32_t AT_O = 128 * NB;
   constexpr int ROWS = 128 / REP;      // rows per copy (and block)
   constexpr int NC = AT_TOK / REP;     // columns per softmax warp
   extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -466,7 +459,8 @@ __global__ void __launch_bounds__(AtCfg<NB>::THREADS, 3 - NB)
           next = at_unit(dm, a, cu, plane * dm.S + s, 0, AT_TOK, INT32_MAX);
           next.r0 = rb * (128 * NB);
           const uint32_t nt = max(next.nt, 1), c = at_cost<NB>(dm, rb), p0 = pos + AT_START<NB> * c, edge = a.edge;
-          const uint32_t first = (p0 + (min(edge, nt) - 1) * c) / per, last = nt >= edge ? (p0 + (nt - edge) * c) / per : 0;
+          const uint32_t first = (p0 + (min(edge, nt) - 1) * c) / per;
+          const uint32_t last = nt >= edge ? (p0 + (nt - edge) * c) / per : 0;
           const int at = rb + a.nrb * (int)next.u, split = (int)blockIdx.x - (int)first;
           pos = p0 + nt * c;
           if (++s == dm.S) {
@@ -554,8 +548,8 @@ __global__ void __launch_bounds__(AtCfg<NB>::THREADS, 3 - NB)
           if (j >= nb) break;
 #pragma unroll
           for (int k = 0; k < AT_TOK / 16; ++k)
-            umma_f16_ts(tmem + AT_O + 128 * j, tmem + 128 * j + 64 * b + 8 * k, vd + (uint64_t)((k * 2048) >> 4), IDESC_O,
-                        !first || k > 0 ? 1u : 0u);
+            umma_f16_ts(tmem + AT_O + 128 * j, tmem + 128 * j + 64 * b + 8 * k, vd + (uint64_t)((k * 2048) >> 4),
+                        IDESC_O, !first || k > 0 ? 1u : 0u);
         }
         umma_commit(smem_u32(&sh.empty[st]));
         umma_commit(smem_u32(&sh.pvdone[b]));
@@ -582,7 +576,8 @@ __global__ void __launch_bounds__(AtCfg<NB>::THREADS, 3 - NB)
             if (j >= nb) break;
 #pragma unroll
             for (int c = 0; c < D / 16; ++c)
-              umma_f16_ss(tmem + 128 * j + 64 * b, qd + (uint64_t)((j * 32768 + ((c >> 2) * 16384) + (c & 3) * 32) >> 4),
+              umma_f16_ss(tmem + 128 * j + 64 * b,
+                          qd + (uint64_t)((j * 32768 + ((c >> 2) * 16384) + (c & 3) * 32) >> 4),
                           kd + (uint64_t)((((c >> 2) * AT_BOX) + (c & 3) * 32) >> 4), IDESC_S, c > 0 ? 1u : 0u);
           }
           umma_commit(smem_u32(&sh.empty[st]));
@@ -604,9 +599,10 @@ __global__ void __launch_bounds__(AtCfg<NB>::THREADS, 3 - NB)
     for (uint32_t k = 0; take(k, x, true); ++k) {
       if (x.nt == 0) continue;
       const int nrow = min(R - x.r0, NB * ROWS);
-      const __nv_bfloat16* q = (const __nv_bfloat16*)a.q + x.s * dm.q_ss + x.l * dm.q_sl + (int64_t)x.g * dm.G * dm.q_sh;
+      const __nv_bfloat16* q =
+          (const __nv_bfloat16*)a.q + x.s * dm.q_ss + x.l * dm.q_sl + (int64_t)x.g * dm.G * dm.q_sh;
       auto row = [&](int r) {
-        const int h = at_head(dm, a, x.r0 + r), t = x.r0 + r - h * dm.window;
+        const int h = row_head(dm.window, a.tdiv, x.r0 + r), t = x.r0 + r - h * dm.window;
         return q + h * dm.q_sh + t * dm.q_sp;
       };
       // into L2 while the item before is at work: two 128-byte lines per row
@@ -770,7 +766,7 @@ __global__ void __launch_bounds__(AtCfg<NB>::THREADS, 3 - NB)
       const uint64_t bad = (uint64_t)sh.bad[1] << 32 | sh.bad[0];
       if constexpr (REP == 1) {
         // a lane has a whole row: 32 channels at a time, partial sums with the rows of a block next to each other
-        const int h = at_head(dm, a, row), t = row - h * dm.window;
+        const int h = row_head(dm.window, a.tdiv, row), t = row - h * dm.window;
         const bool on = y < nrow && t < x.rows;
         const float f = x.nsp > 1 ? 1.f : (z == 0.f ? 0.f : 1.f / z);
         float4* part = nullptr;
@@ -836,8 +832,9 @@ __global__ void __launch_bounds__(AtCfg<NB>::THREADS, 3 - NB)
 #pragma unroll
           for (int c = 0; c < REP; ++c) mr[j] = fmaxf(mr[j], ex[c * ROWS + 32 * j + lane].x);
 #pragma unroll
-          for (int c = 0; c < REP; ++c) zr[j] += ex[c * ROWS + 32 * j + lane].y * share(ex[c * ROWS + 32 * j + lane], mr[j]);
-          const int rr = lane + 32 * j, h = at_head(dm, a, rr), t = rr - h * dm.window;
+          for (int c = 0; c < REP; ++c)
+            zr[j] += ex[c * ROWS + 32 * j + lane].y * share(ex[c * ROWS + 32 * j + lane], mr[j]);
+          const int rr = lane + 32 * j, h = row_head(dm.window, a.tdiv, rr), t = rr - h * dm.window;
           part[j] = nullptr, o[j] = nullptr;
           if (rr >= nrow || t >= x.rows) continue;
           if (x.nsp > 1) {
@@ -845,7 +842,8 @@ __global__ void __launch_bounds__(AtCfg<NB>::THREADS, 3 - NB)
             part[j] = at_part(a, x, slot, rr);
             if (warp == 2) *at_ml(a, x, slot, rr) = make_float2(mr[j], zr[j]);
           } else {
-            o[j] = (__nv_bfloat16*)a.o + x.s * a.os[0] + x.l * a.os[1] + (int64_t)(x.g * dm.G + h) * a.os[2] + t * a.os[3];
+            o[j] = (__nv_bfloat16*)a.o + x.s * a.os[0] + x.l * a.os[1] + (int64_t)(x.g * dm.G + h) * a.os[2] +
+                   t * a.os[3];
             if (warp == 2 && a.lse != nullptr)
               a.lse[x.s * a.ls[0] + x.l * a.ls[1] + (x.g * dm.G + h) * a.ls[2] + t] =
                   zr[j] == 0.f ? -INFINITY : mr[j] * (a.scale2 * 0.6931471805599453f) + logf(zr[j]);
@@ -881,11 +879,12 @@ __global__ void __launch_bounds__(AtCfg<NB>::THREADS, 3 - NB)
                 acc[0] += w.x, acc[1] += w.y, acc[2] += w.z, acc[3] += w.w;
               }
               if (bad != 0 && (part[j] != nullptr || o[j] != nullptr))
-                at_bad(dm, a, x, bad, r - at_head(dm, a, r) * dm.window, 64 * half + 4 * c, acc);
+                at_bad(dm, a, x, bad, r - row_head(dm.window, a.tdiv, r) * dm.window, 64 * half + 4 * c, acc);
               if (part[j] != nullptr)
                 part[j][(16 * half + c) * a.prows] = make_float4(acc[0], acc[1], acc[2], acc[3]);
               else if (o[j] != nullptr)
-                *(uint2*)(o[j] + 64 * half + 4 * c) = make_uint2(pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3]));
+                *(uint2*)(o[j] + 64 * half + 4 * c) =
+                    make_uint2(pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3]));
             }
           }
           named_barrier_sync(1, SM_THREADS);
@@ -1001,7 +1000,8 @@ __global__ void __launch_bounds__(AfCfg<RB>::THREADS, AfCfg<RB>::PER_SM)
   for (int r = 0; r < RB; ++r) acc[r] = make_float4(0.f, 0.f, 0.f, 0.f);
   float* pw = ps + warp * 8 * RB;  // [8 tokens][RB]
   const int myrow = lane % RB;
-  const uint64_t mask = x.nt > x.ncache && r0 + myrow < R ? at_mask(dm, a, x, r0 + myrow - at_head(dm, a, r0 + myrow) * dm.window) : 0;
+  const int myt = r0 + myrow - row_head(dm.window, a.tdiv, r0 + myrow) * dm.window;
+  const uint64_t mask = x.nt > x.ncache && r0 + myrow < R ? at_mask(dm, a, x, myt) : 0;
   for (int i = 0; i < x.nt; ++i) {
     if (i + 1 < x.nt) fetch(i + 1);
     cp_async_commit();
@@ -1158,7 +1158,7 @@ __global__ void __launch_bounds__(NT, 1)
   {
     const float* q = (const float*)a.q + x.s * dm.q_ss + x.l * dm.q_sl + (int64_t)x.g * dm.G * dm.q_sh;
     for (int e = tid; e < C::ROWS * 32; e += C::THREADS) {
-      const int r = e >> 5, c = (e & 31) * 4, h = at_head(dm, a, r0 + r), t = r0 + r - h * dm.window;
+      const int r = e >> 5, c = (e & 31) * 4, h = row_head(dm.window, a.tdiv, r0 + r), t = r0 + r - h * dm.window;
       const bool on = r < nrow;
       cp_async16(smem_u32(qs + r * D + c), q + (on ? h * dm.q_sh + t * dm.q_sp : 0) + c, on);
     }
@@ -1200,7 +1200,7 @@ __global__ void __launch_bounds__(NT, 1)
 #pragma unroll
     for (int r = 0; r < MR; ++r) {
       if (drafted) {
-        const int row = r0 + ty * MR + r, t = row - at_head(dm, a, row) * dm.window;
+        const int row = r0 + ty * MR + r, t = row - row_head(dm.window, a.tdiv, row) * dm.window;
         const uint64_t mask = row < R ? at_mask(dm, a, x, t) : 0;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -1249,8 +1249,10 @@ __global__ void __launch_bounds__(NT, 1)
           for (int e = 0; e < 4; ++e) {
             if (drafted && p[e] == 0.f) continue;  // a masked value may be anything
             float4 &u = o[r + e][0], &w = o[r + e][1];
-            u.x = fmaf(p[e], v0.x, u.x), u.y = fmaf(p[e], v0.y, u.y), u.z = fmaf(p[e], v0.z, u.z), u.w = fmaf(p[e], v0.w, u.w);
-            w.x = fmaf(p[e], v1.x, w.x), w.y = fmaf(p[e], v1.y, w.y), w.z = fmaf(p[e], v1.z, w.z), w.w = fmaf(p[e], v1.w, w.w);
+            u.x = fmaf(p[e], v0.x, u.x), u.y = fmaf(p[e], v0.y, u.y);
+            u.z = fmaf(p[e], v0.z, u.z), u.w = fmaf(p[e], v0.w, u.w);
+            w.x = fmaf(p[e], v1.x, w.x), w.y = fmaf(p[e], v1.y, w.y);
+            w.z = fmaf(p[e], v1.z, w.z), w.w = fmaf(p[e], v1.w, w.w);
           }
         }
       }
@@ -1299,8 +1301,8 @@ __global__ void __launch_bounds__(AJ_THREADS)
 template <typename T, int W, int NR>
 static cudaError_t launch_join(const Dims& dm, const AttendArgs& a, const int32_t* cu, cudaStream_t st) {
   const int64_t groups = (int64_t)dm.L * dm.Hkv * dm.S * ((dm.G * dm.window + NR - 1) / NR);
-  return launch_pdl(true, attend_join_kernel<T, W, NR>, dim3((unsigned)((groups * W + AJ_WARPS - 1) / AJ_WARPS)), AJ_THREADS,
-                    0, st, dm, a, cu);
+  const dim3 grid((unsigned)((groups * W + AJ_WARPS - 1) / AJ_WARPS));
+  return launch_pdl(true, attend_join_kernel<T, W, NR>, grid, AJ_THREADS, 0, st, dm, a, cu);
 }
 template <typename T>
 static cudaError_t launch_join(const Dims& dm, const AttendArgs& a, const int32_t* cu, cudaStream_t st) {
@@ -1321,8 +1323,9 @@ template <int NT>
 static cudaError_t launch_f32_rows(const Dims& dm, const AttendArgs& a, const int32_t* cu, int grid, cudaStream_t st) {
   using C = AgCfg<NT>;
   static_assert(C::SMEM <= 232448, "shared memory");
-  JACAP_TRY(cudaFuncSetAttribute(attend_f32_rows_kernel<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM));
-  return launch_pdl(true, attend_f32_rows_kernel<NT>, grid, C::THREADS, C::SMEM, st, dm, a, cu);
+  auto kern = attend_f32_rows_kernel<NT>;
+  JACAP_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM));
+  return launch_pdl(true, kern, grid, C::THREADS, C::SMEM, st, dm, a, cu);
 }
 template <int RB>
 static cudaError_t launch_f32(const Dims& dm, const AttendArgs& a, const int32_t* cu, int grid, cudaStream_t st) {
@@ -1332,7 +1335,9 @@ static cudaError_t launch_f32(const Dims& dm, const AttendArgs& a, const int32_t
   return launch_pdl(true, attend_f32_kernel<RB>, grid, C::THREADS, C::SMEM, st, dm, a, cu);
 }
 
-static int attend_f32_rows(int rows) { return rows <= 4 ? 4 : rows <= 8 ? 8 : (rows <= 16 ? 16 : (rows <= 64 ? 64 : 128)); }
+static int attend_f32_rows(int rows) {
+  return rows <= 4 ? 4 : rows <= 8 ? 8 : (rows <= 16 ? 16 : (rows <= 64 ? 64 : 128));
+}
 int attend_row_block(int dtype, int rows) { return dtype == 1 ? (rows <= 128 ? 128 : 256) : attend_f32_rows(rows); }
 
 int attend_part_rows(int rows) { return rows <= 32 ? 32 : (rows <= 64 ? 64 : 128); }

@@ -452,7 +452,8 @@ __global__ void __launch_bounds__(NT, 1024 / NT)
 constexpr int PK_THREADS = 256, PK_PART = 4096;
 
 __global__ void __launch_bounds__(PK_THREADS)
-    protect_kernel(Dims dm, Ws ws, const int32_t* __restrict__ cu, WeightRef weights, const int32_t* __restrict__ pos, int sinks, int recent, float* __restrict__ keys, int parts) {
+    protect_kernel(Dims dm, Ws ws, const int32_t* __restrict__ cu, WeightRef weights, const int32_t* __restrict__ pos,
+                   int sinks, int recent, float* __restrict__ keys, int parts) {
   pdl_wait();
   __shared__ int32_t s_max[PK_THREADS / 32];
   const int tid = threadIdx.x, u = blockIdx.x / parts, part = blockIdx.x % parts;
@@ -593,8 +594,9 @@ int protect_parts(int max_seqlen, const int32_t* pos) { return pos != nullptr ? 
 cudaError_t launch_protect(const Dims& dm, const Ws& ws, const int32_t* cu, const WeightRef& weights,
                            const int32_t* pos, int sinks, int recent, float* keys, int max_seqlen, cudaStream_t st) {
   const int parts = protect_parts(max_seqlen, pos);
-  return launch_pdl(dm.pdl != 0, protect_kernel, dim3((unsigned)(dm.L * dm.Hkv * dm.S * parts)), PK_THREADS, 0, st, dm, ws,
-                    cu, weights, pos, sinks, recent, keys, parts);
+  const dim3 grid((unsigned)(dm.L * dm.Hkv * dm.S * parts));
+  return launch_pdl(dm.pdl != 0, protect_kernel, grid, PK_THREADS, 0, st, dm, ws, cu, weights, pos, sinks, recent, keys,
+                    parts);
 }
 
 cudaError_t launch_compact(const Dims& dm, int dtype, const int32_t* cu, const void* k, const void* v,

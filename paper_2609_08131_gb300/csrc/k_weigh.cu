@@ -43,12 +43,6 @@ constexpr float WG_LAZY = 8.f;  // log2 of how far a logit may pass the running 
 constexpr int WG_NONE = -(1 << 30);  // j of a row that gives no weight: it sees no token
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
-__device__ __forceinline__ float wg_ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
 // Query rows of a request: `ql` queries, the first of them at position `p0` (it may be
 // negative) of `n` live tokens that start at `start`.
 struct WgReq {
@@ -63,10 +57,6 @@ __device__ __forceinline__ WgReq wg_req(const Dims& dm, const WeighArgs& a, cons
   x.ql = ql < 0 ? 0 : (ql < dm.window ? ql : dm.window);
   x.p0 = x.n - x.ql;
   return x;
-}
-// The head of row r (r / window, exact for r below 2^16).
-__device__ __forceinline__ int wg_head(const Dims& dm, const WeighArgs& a, int r) {
-  return dm.window == 1 ? r : (int)__umulhi((uint32_t)r, a.tdiv);
 }
 // Which query the j-th of request s is (-1: none).
 __device__ __forceinline__ int wg_query(const Dims& dm, const WeighArgs& a, const WgReq& x, int s, int j) {
@@ -94,7 +84,7 @@ __device__ __forceinline__ float2 wg_const(const Dims& dm, const WeighArgs& a, c
 __device__ __forceinline__ void wg_merge(float& m, float& z, float2 x, float scale2) {
   if (x.x == -INFINITY && x.y == 0.f) return;
   const float top = fmaxf(m, x.x);
-  z = (m == -INFINITY ? z : z * wg_ex2((m - top) * scale2)) + (x.x == -INFINITY ? x.y : x.y * wg_ex2((x.x - top) * scale2));
+  z = (m == -INFINITY ? z : z * ex2((m - top) * scale2)) + (x.x == -INFINITY ? x.y : x.y * ex2((x.x - top) * scale2));
   m = top;
 }
 
@@ -244,10 +234,11 @@ __global__ void __launch_bounds__(WgCfg<NRB, SUM>::THREADS, 1)
       const int p = nrun % C::IMGS, l = item.plane / dm.Hkv, g = item.plane % dm.Hkv, b = warp - WG_BUILD0;
       const WgReq x = wg_req(dm, a, cu, item.seq);
       if (nrun >= (uint32_t)C::IMGS && !mbar_wait(smem_u32(&imgfree[p]), ((nrun / C::IMGS) & 1) ^ 1, ws, abort)) break;
-      const __nv_bfloat16* q = (const __nv_bfloat16*)a.q + item.seq * dm.q_ss + l * dm.q_sl + (int64_t)g * dm.G * dm.q_sh;
+      const __nv_bfloat16* q =
+          (const __nv_bfloat16*)a.q + item.seq * dm.q_ss + l * dm.q_sl + (int64_t)g * dm.G * dm.q_sh;
       uint8_t* im = img + p * NRB * WG_IMG;
       for (int r0 = 32 * b; r0 < C::ROWS; r0 += 64) {  // 32 rows at a time, one per lane to look up
-        const int r = r0 + lane, h = wg_head(dm, a, r), j = r - h * dm.window;
+        const int r = r0 + lane, h = row_head(dm.window, a.tdiv, r), j = r - h * dm.window;
         const int qi = r < R ? wg_query(dm, a, x, item.seq, j) : -1;
         const int64_t off = qi >= 0 ? h * dm.q_sh + qi * dm.q_sp : 0;
         if constexpr (SUM) {
@@ -291,7 +282,7 @@ __global__ void __launch_bounds__(WgCfg<NRB, SUM>::THREADS, 1)
 #pragma unroll
         for (int rb = 0; rb < NRB; ++rb) {
           m[rb] = -INFINITY, z[rb] = 0.f, zc[rb] = 0.f;
-          lim[rb] = x.p0 + (rb * 128 + y) - wg_head(dm, a, rb * 128 + y) * dm.window;
+          lim[rb] = x.p0 + (rb * 128 + y) - row_head(dm.window, a.tdiv, rb * 128 + y) * dm.window;
         }
         // (the constants are the builders' work: the tile's accumulators follow them)
         if (SUM && !mbar_wait(smem_u32(&imgready[p]), (nrun / C::IMGS) & 1, ws, abort)) goto done;
@@ -334,8 +325,8 @@ __global__ void __launch_bounds__(WgCfg<NRB, SUM>::THREADS, 1)
 #pragma unroll
               for (int q = 0; q < 32; q += 2) {
                 const float4 k = *(const float4*)(cp + c + q);  // (no weight: f = 0)
-                s[q & 3] = fmaf(wg_ex2(fmaf(v[q], scale2, -k.x)), k.y, s[q & 3]);
-                s[(q + 1) & 3] = fmaf(wg_ex2(fmaf(v[q + 1], scale2, -k.z)), k.w, s[(q + 1) & 3]);
+                s[q & 3] = fmaf(ex2(fmaf(v[q], scale2, -k.x)), k.y, s[q & 3]);
+                s[(q + 1) & 3] = fmaf(ex2(fmaf(v[q + 1], scale2, -k.z)), k.w, s[(q + 1) & 3]);
               }
             }
             w += (s[0] + s[1]) + (s[2] + s[3]);
@@ -357,14 +348,14 @@ __global__ void __launch_bounds__(WgCfg<NRB, SUM>::THREADS, 1)
               const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
               const bool up = top > mm + lazy;
               if (__any_sync(0xffffffffu, up)) {
-                const float f = up ? (mm == -INFINITY ? 0.f : wg_ex2((mm - top) * scale2)) : 1.f;
+                const float f = up ? (mm == -INFINITY ? 0.f : ex2((mm - top) * scale2)) : 1.f;
                 zz *= f, cc *= f;
                 mm = up ? top : mm;
               }
               const float base = mm == -INFINITY ? 0.f : mm * scale2;
               float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-              for (int q = 0; q < 32; ++q) s[q & 3] += wg_ex2(fmaf(v[q], scale2, -base));
+              for (int q = 0; q < 32; ++q) s[q & 3] += ex2(fmaf(v[q], scale2, -base));
               const float add = ((s[0] + s[1]) + (s[2] + s[3])) - cc, sum = zz + add;
               cc = (sum - zz) - add;
               zz = sum;
@@ -501,7 +492,7 @@ __global__ void __launch_bounds__(32 * WARPS, 2)
       __syncthreads();  // the rows and the tiles before are read
       fetch(item.t0, 0);
       for (int e = tid; e < WF_ROWS * 32; e += WF_THREADS) {
-        const int r = r0 + (e >> 5), c = (e & 31) * 4, h = wg_head(dm, a, r), j = r - h * dm.window;
+        const int r = r0 + (e >> 5), c = (e & 31) * 4, h = row_head(dm.window, a.tdiv, r), j = r - h * dm.window;
         const int qi = r < R ? wg_query(dm, a, x, item.seq, j) : -1;
         cp_async16(smem_u32(qs + (e >> 5) * D + c), q + (qi >= 0 ? h * dm.q_sh + qi * dm.q_sp : 0) + c, qi >= 0);
         if (c == 0) {
@@ -548,15 +539,15 @@ __global__ void __launch_bounds__(32 * WARPS, 2)
             const bool see = t + tok < item.t1 && rel + tok <= x.p0 + j;
             if constexpr (SUM) {
               const float2 k = cst[8 * warp + i];
-              if (see) w[b] = fmaf(wg_ex2(fmaf(s[i][b], scale2, -k.x)), k.y, w[b]);
+              if (see) w[b] = fmaf(ex2(fmaf(s[i][b], scale2, -k.x)), k.y, w[b]);
             } else if (see) {
               const float v = s[i][b];
               if (v > m[i] + lazy) {
-                const float f = m[i] == -INFINITY ? 0.f : wg_ex2((m[i] - v) * scale2);
+                const float f = m[i] == -INFINITY ? 0.f : ex2((m[i] - v) * scale2);
                 z[i] *= f, zc[i] *= f;
                 m[i] = v;
               }
-              const float add = wg_ex2(fmaf(v, scale2, m[i] == -INFINITY ? 0.f : -m[i] * scale2)) - zc[i];
+              const float add = ex2(fmaf(v, scale2, m[i] == -INFINITY ? 0.f : -m[i] * scale2)) - zc[i];
               const float sum = z[i] + add;
               zc[i] = (sum - z[i]) - add;
               z[i] = sum;
@@ -587,11 +578,12 @@ __global__ void __launch_bounds__(32 * WARPS, 2)
           float top = mm;
 #pragma unroll
           for (int off = 16; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-          zz = mm == -INFINITY ? zz : zz * wg_ex2((mm - top) * scale2);
+          zz = mm == -INFINITY ? zz : zz * ex2((mm - top) * scale2);
 #pragma unroll
           for (int off = 16; off >= 1; off >>= 1) zz += __shfl_xor_sync(0xffffffffu, zz, off);
           const int r = r0 + 8 * warp + i;
-          if (lane == 0 && r < R) a.stat[((int64_t)item.plane * dm.c_cap + item.cidx) * rows + r] = make_float2(top, zz);
+          if (lane == 0 && r < R)
+            a.stat[((int64_t)item.plane * dm.c_cap + item.cidx) * rows + r] = make_float2(top, zz);
         }
       }
     }

@@ -2,8 +2,8 @@
 
 ``watch(monkeypatch)`` replaces torch's streams by ones that only keep clocks, and the library's calls by ones that only
 note the buffers they take. Every torch operation and every library call then is an access on the stream that is current
-(or whose handle the call got), with the storages that it reads and writes, and ``races()`` lists the pairs of accesses of
-one storage, at least one of them a write, of which neither is ordered before the other. Tensors are small ones on
+(or whose handle the call got), with the storages that it reads and writes, and ``races()`` lists the pairs of accesses
+of one storage, at least one of them a write, of which neither is ordered before the other. Tensors are small ones on
 the CPU.
 """
 
@@ -69,7 +69,8 @@ class Order(TorchDispatchMode):
     def note(self, what, stream, reads, writes, args=()):
         number = stream.clock.get(stream.name, 0)
         stream.clock[stream.name] = number + 1
-        self.accesses.append((what, stream.name, number, dict(stream.clock), frozenset(reads), frozenset(writes), self.capturing, args))
+        self.accesses.append((what, stream.name, number, dict(stream.clock), frozenset(reads), frozenset(writes),
+                              self.capturing, args))
 
     def storage(self, t):
         at = t.untyped_storage().data_ptr()
