@@ -458,7 +458,8 @@ jacap_status jacap_rotate(const jacap_rope* rope, jacap_dtype dtype, int32_t num
  * its request and the drafted tokens j of its mask:
  *   logit = scale q . k,  o = sum softmax(logit) v,  lse = ln sum exp(logit).
  * A row that sees nothing has o = 0 and lse = -inf. What a row does not see has
- * no effect on it, NaN and infinities included.
+ * no effect on it, NaN and infinities included. (An infinite value in a cached V that a row
+ * sees may come out as NaN.)
  *
  *   scale          1e-30 to 1e30 (1 / sqrt(128) for plain attention)
  *   lengths        device int32 [num_seqs] (cached tokens of each request, the

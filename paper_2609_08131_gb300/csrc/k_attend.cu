@@ -37,8 +37,8 @@
 // Measured (32 query heads on 8, 92 us = 5.8 TB/s of K and V for 8 drafted tokens over 131011
 // cached ones; 37 us = 3.7 TB/s for one token in 16 slots of 2100, of which ~8 us are the
 // launch and the first tiles' way; 9 us for one token over 37): bound by memory up to 128 rows.
-// 64 drafted tokens of 5 heads a group, 320 rows, over 110000 tokens in 16 requests: 168 us for
-// 138 GFLOP and 842 MB (K and V twice, 5.4 TB/s). A tile of 256 rows takes ~1500 cycles: the products ~1280
+// 64 drafted tokens of 5 heads a group, 320 rows, over 110000 tokens in 16 requests: 173 us, 157 of them this
+// kernel, for 138 GFLOP and 842 MB (K and V twice, 5.4 TB/s). A tile of 256 rows takes ~1500 cycles: the products ~1280
 // (S reads its rows from shared memory again for every 64 tokens, 48 cycles for each 128 x 64 x 16), and the softmax
 // ~1150 with two warps per scheduler, which overlap but for the waits between them. Tried and
 // left out, of 216 us at the time: an MMA issuer per block (218), the barriers asked ahead of the
@@ -316,7 +316,7 @@ __device__ __forceinline__ void at_bad(const Dims& dm, const AttendArgs& a, cons
 // units stay whole and no split is a sliver. A unit whose first tile is at p0 then has its
 // first split in CTA floor((p0 + (edge - 1) cost) / per), and a further one in each CTA up to the one of position
 // p0 + (tiles - edge) cost. (Items dealt one by one as CTAs became free, of a size chosen by an account of their
-// number: 37 and 216 us where this takes 36.5 and 168, with one token in 16 slots and 16 trees; one
+// number: 37 and 216 us where this takes 36 and 173, with one token in 16 slots and 16 trees; one
 // token over 16 requests of 46 to 16383 97 and 82.)
 template <int NB>
 __device__ __forceinline__ uint32_t at_cost(const Dims& dm, int rb) {  // of a tile; measured 0.86 and 0.63 us

@@ -54,8 +54,9 @@
 // PROT: eviction by attention weights. The first `sinks` and the last `recent` tokens are
 // kept whatever their weights, the others compete for the rest. By row this is a range
 // of the keys, so that no launch has to write keys of its own first: one layer of 4099
-// tokens 27 -> 9 us, 1024 units of 16384 tokens (1638 kept) 384 -> 349 us = 5.2 TB/s of
-// weights read and rows copied. With tags protect_kernel writes the keys.
+// tokens 13.6 -> 9.0 us in a graph (27 -> 16 in a stream, with the host's call), 1024 units
+// of 16384 tokens (1638 kept) 384 -> 349 us = 5.2 TB/s of weights read and rows copied. With
+// tags protect_kernel writes the keys (16 and 427 us there).
 #include <algorithm>
 
 #include "jacap_dev.cuh"
