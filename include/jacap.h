@@ -481,13 +481,12 @@ jacap_status jacap_rotate(const jacap_rope* rope, jacap_dtype dtype, int32_t num
  *                  + h [2] + t (elements; a layer's call can write its part of an
  *                  array over all layers)
  *   ws             device, 256-byte aligned, jacap_attend_workspace() bytes (0 for
- *                  a layout that is refused), zeroed once before its first call: it
- *                  starts with the status word and with counters that every call
- *                  leaves at zero, at the same place for every layout (calls of several
+ *                  a layout that is refused), its first JACAP_ATTEND_ZERO_BYTES zeroed
+ *                  once before its first call: the status word, and counters that every
+ *                  call leaves at zero, at the same place for every layout (calls of several
  *                  layouts may use one after the other, not at the same time). A length
- *                  outside its range is clamped and reported
- *                  in the word (JACAP_ERR_INVALID_ARG), which stays set until the
- *                  workspace is zeroed again.
+ *                  outside its range is clamped and reported in the word
+ *                  (JACAP_ERR_INVALID_ARG), which stays set until it is zeroed again.
  * o must not overlap an input. Sums are float32; with bf16 caches the softmax
  * weights are rounded to bf16 for their product with V.
  */
@@ -502,6 +501,7 @@ typedef struct {
   int64_t o_strides[4];
   int64_t lse_strides[3];
 } jacap_attention;
+#define JACAP_ATTEND_ZERO_BYTES ((size_t)2048)
 size_t jacap_attend_workspace(const jacap_layout* layout);
 jacap_status jacap_attend(const jacap_layout* layout, const jacap_attention* attn, const void* q,
                           const void* k, const void* v, void* o, float* lse,

@@ -280,6 +280,7 @@ def jacap_compact_inplace(layout, k, v, pos, idx, budget, preserve_order, ws, ws
 
 
 JACAP_STATIC_SCRATCH_BYTES = 64 << 20
+JACAP_ATTEND_ZERO_BYTES = 2048
 
 
 def jacap_score_static(layout, params, q_win, k, v, scores, stream):

@@ -14,6 +14,7 @@ from dataclasses import dataclass
 import torch
 
 from . import (
+    JACAP_ATTEND_ZERO_BYTES,
     JACAP_BF16,
     JACAP_F32,
     JACAP_OK,
@@ -769,7 +770,7 @@ class _SlotAttention:
         part = self.lse[:, layer]
         if not self._zeroed or layer not in self._filled:
             if not self._zeroed:
-                self.ws.zero_()
+                self.ws[:JACAP_ATTEND_ZERO_BYTES].zero_()
             if layer not in self._filled:
                 part.fill_(-math.inf)
             if not torch.cuda.is_current_stream_capturing():

@@ -65,6 +65,7 @@ AttendPlan attend_plan(const jacap_layout* L) {
   p.status = o; o += 64;
   // (whatever the layout, so that calls of several layouts may use a workspace one after the other)
   p.counts = o; o = align_up(o + (size_t)ATTEND_CTAS * 4);
+  static_assert(64 + (size_t)ATTEND_CTAS * 4 <= JACAP_ATTEND_ZERO_BYTES, "what starts at zero");
   p.nsps = o; o = align_up(o + (bf ? (size_t)ctas * 4 : 0));
   // bf16: two slots for each border between CTAs, whatever the units' number: the split before and the one after
   const int64_t most_ctas = ATTEND_CTAS * 128 / block;

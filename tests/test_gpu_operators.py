@@ -17,7 +17,7 @@ import pytest
 import torch
 
 import paper_2609_08131_gb300.api as api
-from paper_2609_08131_gb300 import JACAP_ERR_INVALID_ARG, JACAP_ERR_NONFINITE
+from paper_2609_08131_gb300 import JACAP_ATTEND_ZERO_BYTES, JACAP_ERR_INVALID_ARG, JACAP_ERR_NONFINITE
 
 pytestmark = pytest.mark.gpu
 
@@ -790,7 +790,7 @@ def test_operators_on_another_stream_and_in_graphs():
 
 
 def test_attentions_of_several_layouts_share_a_workspace():
-    """Zeroed once, used by one layout after the other: many units in splits that the kernel joins by counting them,
+    """Its start zeroed once, used by one layout after the other: many units in splits that the kernel joins by counting them,
     calls of one split, of more rows, of many splits, float32."""
     calls = []
     for i, (S, L, Hq, Hkv, T, n, dtype) in enumerate((
@@ -802,7 +802,8 @@ def test_attentions_of_several_layouts_share_a_workspace():
         att = api.CacheAttention(cache)
         want = [x.clone() for x in att.run(k_draft=kd, v_draft=vd)]
         calls.append((att, kd, vd, want))
-    shared = torch.zeros(max(c[0].ws.numel() for c in calls), dtype=torch.uint8, device=DEV)
+    shared = torch.full((max(c[0].ws.numel() for c in calls),), 255, dtype=torch.uint8, device=DEV)
+    shared[:JACAP_ATTEND_ZERO_BYTES].zero_()
     for c in calls:
         c[0].ws = shared
     for order in (range(8), (0, 1, 0, 2, 0, 3, 6, 4, 6, 5, 0, 7, 6, 3, 5, 1, 5)):
