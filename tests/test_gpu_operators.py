@@ -1214,6 +1214,37 @@ def test_the_loop_on_another_stream_than_the_current_one(rule):
         assert torch.equal(a, b) if isinstance(a, torch.Tensor) else a == b
 
 
+def test_steps_enqueued_ahead_of_the_device():
+    """Lengths and paths that change many times while the device is busy: each step's own, as when it is waited for."""
+    S, L, Hq, Hkv, T = 4, 1, 8, 2, 4
+    g = gen(35)
+    k0, v0 = (randn(g, S, L, Hkv, 100, D, dtype=BF16) for _ in range(2))
+    q0 = randn(g, S, L, Hq, 8, D, dtype=BF16)
+    k, v, q = (randn(g, S, L, n, T, D, dtype=BF16) for n in (Hkv, Hkv, Hq))
+    r = torch.Generator().manual_seed(3)
+    paths = [[sorted(torch.randperm(T, generator=r)[:int(torch.randint(0, T + 1, (1,), generator=r))].tolist())
+              for _ in range(S)] for _ in range(60)]
+
+    def loop(wait):
+        ev = api.DecodeEvictor(S, L, Hq, Hkv, 110, 9, device=DEV, rule="weight", sinks=2, recent=4)
+        ev.start(k0, v0, q0, [100, 97, 60, 1])
+        torch.cuda.synchronize()
+        out = []
+        if not wait:
+            torch.cuda._sleep(100_000_000)  # some 50 ms
+        for path in paths:
+            out.append(ev.attend(0, q[:, 0], k[:, 0], v[:, 0])[0])
+            ev.accept(k, v, q, path, attended=False)
+            if wait:
+                torch.cuda.synchronize()
+        ev.check()
+        return out + [ev.k, ev.v, ev.pos, ev.weights], ev.lengths, ev.events
+
+    (ahead, *end), (want, *other) = loop(False), loop(True)
+    assert end == other and end[1] >= 8
+    assert all(torch.equal(a, b) for a, b in zip(ahead, want))
+
+
 def test_loop_refusals_on_the_device_side():
     ev = api.DecodeEvictor(2, 1, 4, 2, 8, 2, device=DEV, rule="weight")
     g = gen(24)
