@@ -698,8 +698,8 @@ jacap_status jacap_bytes_append(const jacap_byte_cache* cache, jacap_dtype dtype
  * attn->lengths is needed here (0 to slot_tokens); the other members, o and lse are
  * those of jacap_attend. The cache's scales are finite and not negative, powers of two or not, with zero bytes
  * where V's is 0. The bytes' values take part exactly; the softmax weights are rounded to eight significant bits for
- * their product with V (those of less than 2^-2 of the largest of 128 neighbouring tokens, V's
- * scale included, to 2^-10 of that).
+ * their product with V (those of less than 2^-6 of the largest of 128 neighbouring tokens, V's
+ * scale included, to 2^-14 of that or, where it is more, 2^-58 of the row's largest).
  */
 jacap_status jacap_bytes_attend(const jacap_byte_cache* cache, const jacap_attention* attn, int32_t tokens,
                                 const void* q, const int64_t* q_strides, void* o, float* lse, void* ws,

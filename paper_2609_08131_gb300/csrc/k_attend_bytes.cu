@@ -5,11 +5,13 @@
 // b being token i's block; drafted tokens as in k_attend.cu.
 //
 // The tensor cores multiply the cache's bytes as they lie in memory, so that nothing is converted per token:
-// what meets them is split into two e4m3 parts instead. A bf16 value has eight significant bits and e4m3 four, so
-// that x = hi + lo exactly (from 2^-10 of the largest one on; below that to 2^-18 of it), and
+// what meets them is split into two parts of 8 bits instead, hi = e4m3(x) and lo = e5m2(x - hi). A bf16 value has
+// eight significant bits: e4m3 keeps four, what is left is at most half of their last step and three bits of it remain,
+// as many as e5m2 has, so that x = hi + lo exactly (from e4m3's lowest normal value, 2^-6, on; below that to 2^-14), and
 //   q . k8 = hi . k8 + lo . k8
-// are two products into one accumulator. The softmax weights are split alike, after a rounding to
-// eight bits, as they would be for a product in bf16.
+// are two products into one accumulator. The softmax weights are split alike, which rounds them to
+// eight bits, as they would be for a product in bf16. (e5m2, not e4m3 again, because of its lowest step, 2^-16: with e4m3
+// weights below 2^-10 would be lost, and with them the output of rows whose largest weight meets a value near zero.)
 //
 // S is computed transposed, S^T = K8 Q^T: tokens are the 128 lanes of tensor memory and rows its columns (16, 32 or 64
 // per CTA, padded), so that one query row costs a small product, not one of 128 rows. A softmax warp
@@ -20,7 +22,9 @@
 // A weight is w = exp2(l log2 e + log2 vs_b - ref_r), which takes in V's scale, and fits e4m3 (448) as ref_r follows the
 // rows' maxima: a tile whose largest weight would pass 2^8.75, or not reach 2^0.25, moves ref_r so that it is
 // 2^4.5, and the accumulators are rescaled. (Downwards too, so that weights that are small beside one seen before, but not
-// beside their neighbours, keep their bits; 2^-40 below the largest one seen it stops.) Z takes w / vs_b.
+// beside their neighbours, keep their bits; 2^-40 below the largest one seen it stops.) Where one of a tile's four
+// quarters has none above 2^-6 of the largest (a prompt's first token may have nearly all of the weight, and a value
+// near zero), the largest is put to 2^8.5 instead, so that the others keep eight bits down to 2^-14.5 of it. Z takes w / vs_b.
 //
 // CTAs and splits are those of k_attend.cu: persistent CTAs with even shares of all tiles (128 tokens: 16 KB of K, 16 of
 // V); a split's sums are joined by the CTA that finishes its unit's last one. More than 64 rows: K and V
@@ -52,6 +56,7 @@ struct AbCfg {
   static constexpr uint32_t COLS = N == 16 ? 128 : (N == 32 ? 256 : 512);  // S N AB_SBUF, O N AB_TURNS
 };
 constexpr float AB_HIGH = 8.75f, AB_LOW = 0.25f, AB_TOP = 4.5f, AB_DEEP = 40.f;  // log2 of the weights' bounds, see above
+constexpr float AB_WIDE = 6.f, AB_WIDE_LOW = 7.f, AB_WIDE_TOP = 8.5f;            // where a tile's quarters are that far apart
 constexpr float AB_UNIT = -8.f;  // log2 of V's unit in the sums: about the scale of a block of ordinary values
 
 template <int N>
@@ -78,12 +83,12 @@ template <int N>
 constexpr size_t ab_smem() { return 233472 / AbCfg<N>::PER_SM - 1024; }
 static_assert(ab_used<16>() <= ab_smem<16>() && ab_used<32>() <= ab_smem<32>() && ab_used<64>() <= ab_smem<64>(), "shared memory");
 
-// Instruction descriptor of kind::f8f6f4: e4m3 A and B, f32 D (the fields of kind::f16's).
-__host__ __device__ constexpr uint32_t idesc_e4m3_f32(int M, int N, int a_mn, int b_mn) {
-  return (1u << 4) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(N >> 3) << 17) |
+// Instruction descriptor of kind::f8f6f4: A of e4m3, B of e4m3 or e5m2, f32 D (the fields of kind::f16's).
+__host__ __device__ constexpr uint32_t idesc_e4m3_f32(int M, int N, int a_mn, int b_mn, bool b_e5m2) {
+  return (1u << 4) | (b_e5m2 ? 1u << 10 : 0u) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(N >> 3) << 17) |
          ((uint32_t)(M >> 4) << 24);
 }
-// D[tmem] (+)= A[smem] B[smem], e4m3, K = 32.
+// D[tmem] (+)= A[smem] B[smem], 8 bits, K = 32.
 __device__ __forceinline__ void umma_f8_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
                                            uint32_t accumulate) {
   asm volatile(
@@ -98,14 +103,15 @@ __device__ __forceinline__ float warp_max(float x) {  // (without NaN)
   asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
   return r;
 }
-// Four values as e4m3 parts, hi and lo = e4m3(x - hi), packed (a's in the low bytes).
-__device__ __forceinline__ void split_e4m3(float a, float b, float c, float d, uint32_t& hi, uint32_t& lo) {
+// Four values' parts, hi = e4m3(x) and lo = e5m2(x - hi), packed (a's in the low bytes). The difference is taken in 16 bits
+// (eleven significant ones, exact from there on), two at a time.
+__device__ __forceinline__ void split_f8(float a, float b, float c, float d, uint32_t& hi, uint32_t& lo) {
   asm("{\n\t.reg .b16 h0, h1, l0, l1;\n\t.reg .b32 v0, v1, x0, x1;\n\t"
       "cvt.rn.satfinite.e4m3x2.f32 h0, %3, %2;\n\tcvt.rn.satfinite.e4m3x2.f32 h1, %5, %4;\n\t"
       "cvt.rn.f16x2.e4m3x2 v0, h0;\n\tcvt.rn.f16x2.e4m3x2 v1, h1;\n\t"
       "cvt.rn.f16x2.f32 x0, %3, %2;\n\tcvt.rn.f16x2.f32 x1, %5, %4;\n\t"
       "sub.rn.f16x2 x0, x0, v0;\n\tsub.rn.f16x2 x1, x1, v1;\n\t"
-      "cvt.rn.satfinite.e4m3x2.f16x2 l0, x0;\n\tcvt.rn.satfinite.e4m3x2.f16x2 l1, x1;\n\t"
+      "cvt.rn.satfinite.e5m2x2.f16x2 l0, x0;\n\tcvt.rn.satfinite.e5m2x2.f16x2 l1, x1;\n\t"
       "mov.b32 %0, {h0, h1};\n\tmov.b32 %1, {l0, l1};\n\t}"
       : "=r"(hi), "=r"(lo)
       : "f"(a), "f"(b), "f"(c), "f"(d));
@@ -430,7 +436,8 @@ __global__ void __launch_bounds__(AbCfg<N>::THREADS, AbCfg<N>::PER_SM)
     // is. Both parts of the weights in one product of twice the columns, and of the rows with 32, gained nothing: an issue
     // that ends sooner waits longer for the weights.)
     const bool leader = elect_one();
-    constexpr uint32_t IDESC_S = idesc_e4m3_f32(128, N, 0, 0), IDESC_O = idesc_e4m3_f32(128, N, 1, 1);
+    constexpr uint32_t IDESC_S[2] = {idesc_e4m3_f32(128, N, 0, 0, false), idesc_e4m3_f32(128, N, 0, 0, true)};  // hi, lo
+    constexpr uint32_t IDESC_O[2] = {idesc_e4m3_f32(128, N, 1, 1, false), idesc_e4m3_f32(128, N, 1, 1, true)};
     constexpr uint32_t IDESC_SD = idesc_bf16_f32(128, N, 0, 0), IDESC_OD = idesc_bf16_f32(128, N, 1, 0);
     const uint64_t qd = smem_desc_sw128(smem_u32(q8), 16, 1024), qbd = smem_desc_sw128(smem_u32(qb), 16, 1024);
     const uint64_t pd = weight_desc<N>(smem_u32(ps)), pbd = smem_desc_sw128(smem_u32(ps), 16, 1024);
@@ -472,7 +479,7 @@ __global__ void __launch_bounds__(AbCfg<N>::THREADS, AbCfg<N>::PER_SM)
 #pragma unroll
               for (int c = 0; c < 8; ++c)  // the rows' hi parts, then their lo parts
                 umma_f8_ss(d, kd + (uint64_t)((c & 3) * 32 >> 4), qd + (uint64_t)((c >> 2) * PART + (c & 3) * 32 >> 4),
-                           IDESC_S, c > 0 ? 1u : 0u);
+                           IDESC_S[c >> 2], c > 0 ? 1u : 0u);
             }
           }
           used();
@@ -503,7 +510,7 @@ __global__ void __launch_bounds__(AbCfg<N>::THREADS, AbCfg<N>::PER_SM)
 #pragma unroll
               for (int c = 0; c < 8; ++c)  // the weights' hi parts, then their lo parts: 32 tokens each
                 umma_f8_ss(o, vd + (uint64_t)((c & 3) * 4096 >> 4),
-                           pd + (uint64_t)(w + (c >> 2) * N + (c & 3) * 64 * N >> 4), IDESC_O, c > 0 ? 1u : more);
+                           pd + (uint64_t)(w + (c >> 2) * N + (c & 3) * 64 * N >> 4), IDESC_O[c >> 2], c > 0 ? 1u : more);
             }
           }
           used();
@@ -591,7 +598,7 @@ __global__ void __launch_bounds__(AbCfg<N>::THREADS, AbCfg<N>::PER_SM)
           float y[4] = {bf16lo(u[2 * j]) * by, bf16hi(u[2 * j]) * by, bf16lo(u[2 * j + 1]) * by, bf16hi(u[2 * j + 1]) * by};
 #pragma unroll
           for (int k2 = 0; k2 < 4; ++k2) y[k2] = fabsf(y[k2]) < INFINITY ? y[k2] : NAN;
-          split_e4m3(y[0], y[1], y[2], y[3], hi[j], lo[j]);
+          split_f8(y[0], y[1], y[2], y[3], hi[j], lo[j]);
         }
         const uint32_t at = r * 128 + ((((uint32_t)c >> 1) ^ (r & 7)) << 4) + (c & 1) * 8;
         sts_u32s(smem_u32(q8) + at, hi);
@@ -704,9 +711,10 @@ __global__ void __launch_bounds__(AbCfg<N>::THREADS, AbCfg<N>::PER_SM)
           named_barrier_sync(3 + gi, 128);
           const float4 top4 = lds_f32x4(tops);
           const float top = fmaxf(fmaxf(top4.x, top4.y), fmaxf(top4.z, top4.w));
+          const bool wide = top > fminf(fminf(top4.x, top4.y), fminf(top4.z, top4.w)) + AB_WIDE;
           float f = 1.f;
-          if (top > ref + AB_HIGH || top < ref + AB_LOW) {
-            const float to = fmaxf(top - AB_TOP, deep);
+          if (top > ref + AB_HIGH || top < ref + (wide ? AB_WIDE_LOW : AB_LOW)) {
+            const float to = fmaxf(top - (wide ? AB_WIDE_TOP : AB_TOP), deep);
             if (top > -INFINITY && to != ref) {
               f = ref == -INFINITY ? 0.f : ex2(ref - to);
               ref = to;
@@ -773,7 +781,7 @@ __global__ void __launch_bounds__(AbCfg<N>::THREADS, AbCfg<N>::PER_SM)
               uint32_t hi[CH / 4], lo[CH / 4];
 #pragma unroll
               for (int e = 0; e < CH / 4; ++e)
-                split_e4m3(v[2 * e].x, v[2 * e].y, v[2 * e + 1].x, v[2 * e + 1].y, hi[e], lo[e]);
+                split_f8(v[2 * e].x, v[2 * e].y, v[2 * e + 1].x, v[2 * e + 1].y, hi[e], lo[e]);
               sts_u32s(line + (swizzle ^ (c0 & ~15)) + (c0 & 15), hi);
               sts_u32s(line + (swizzle ^ (N | (c0 & ~15))) + (c0 & 15), lo);
             } else if (tok < 64) {
