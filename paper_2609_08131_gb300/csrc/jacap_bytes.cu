@@ -218,7 +218,8 @@ jacap_status jacap_bytes_attend(const jacap_byte_cache* cache, const jacap_atten
   a.mlpart = (float*)(b + c.mlpart);
   ByteScales sc;
   sc.ks = cache->k_scales, sc.vs = cache->v_scales;
-  for (int i = 0; i < 3; ++i) sc.strides[i] = cache->scale_strides[i];
+  sc.k = (const uint8_t*)cache->k, sc.v = (const uint8_t*)cache->v;
+  for (int i = 0; i < 3; ++i) sc.strides[i] = cache->scale_strides[i], sc.row_strides[i] = cache->strides[i];
   sc.scale2 = (float)((double)attn->scale * 1.4426950408889634);
   CUtensorMap maps[4];
   memset(maps, 0, sizeof(maps));

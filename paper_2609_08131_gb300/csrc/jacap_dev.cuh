@@ -976,6 +976,13 @@ __device__ __forceinline__ uint32_t sw128_off(uint32_t row, uint32_t chunk16) {
 
 __device__ __forceinline__ float bf16lo(uint32_t x) { return __uint_as_float(x << 16); }
 __device__ __forceinline__ float bf16hi(uint32_t x) { return __uint_as_float(x & 0xFFFF0000u); }
+// Two e4m3 bytes' values, exact.
+__device__ __forceinline__ float2 e4m3_values(uint32_t two) {
+  uint32_t h;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)two));
+  return make_float2(__half2float(__ushort_as_half((unsigned short)(h & 0xffff))),
+                     __half2float(__ushort_as_half((unsigned short)(h >> 16))));
+}
 
 // Round two floats to bf16 (nearest even) and pack (a in the low half).
 __device__ __forceinline__ uint32_t pack_bf16x2(float a, float b) {

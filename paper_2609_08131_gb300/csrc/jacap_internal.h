@@ -234,11 +234,13 @@ cudaError_t launch_bytes_append(const ByteArgs& a, int dtype, cudaStream_t st);
 // Which drafted tokens are accepted (k_verify.cu).
 cudaError_t launch_verify(const jacap_verification& a, uint32_t* status, cudaStream_t st);
 
-// Attention over a cache held in 8 bits (k_attend_bytes.cu): its blocks' scales. The AttendArgs' scale2 is 1 (partial
+// Attention over a cache held in 8 bits (k_attend_bytes.cu): its blocks' scales, and its bytes. The AttendArgs' scale2 is 1 (partial
 // maxima are log2 of weights), its lengths are given, and a request's tokens are a slot of max_seqlen.
 struct ByteScales {
   const float *ks, *vs;
   int64_t strides[3];  // layer, head, slot
+  const uint8_t *k, *v;
+  int64_t row_strides[3];
   float scale2;        // scale log2 e
 };
 int attend_bytes_block(int rows);  // rows of a CTA

@@ -26,6 +26,11 @@
 // quarters has none above 2^-6 of the largest (a prompt's first token may have nearly all of the weight, and a value
 // near zero), the largest is put to 2^8.5 instead, so that the others keep eight bits down to 2^-14.5 of it. Z takes w / vs_b.
 //
+// That holds while V's scales are of ordinary size. Beside a block of 2^120 (of a value that is infinite) or 2^-126 the
+// other blocks' weights, or its own part of Z, would leave float32's range, and eight bits long before. So a block whose
+// scale is outside 2^-32 .. 2^16 (values all below 1e-7, or one above 2.9e7) counts in Z with the scale of an ordinary one,
+// and its part of the output is not left to the tensor cores but added at the item's end, one by one (add_far).
+//
 // CTAs and splits are those of k_attend.cu: persistent CTAs with even shares of all tiles (128 tokens: 16 KB of K, 16 of
 // V); a split's sums are joined by the CTA that finishes its unit's last one. More than 64 rows: K and V
 // are read again for each 64. (Turning the tiles to bf16 in shared memory for products of 128 rows and more takes 151 us
@@ -73,7 +78,9 @@ struct AbSmem {
   float sum[2][4][N], ref[2][N], inv[2][N];        // by team
   float qmax[C::LOADERS], qfac[AB_QUEUE];
   uint32_t tmem, bad[2];
-  int abort, last;
+  float2 norm[N];                          // a row's reference, and what exp2(logit - reference) is multiplied with
+  float far[C::GROUPS][4][64];             // add_far's weights
+  int abort, last, any_far;
 };
 template <int N>
 constexpr size_t ab_used() {
@@ -162,6 +169,11 @@ __device__ __forceinline__ void tmem_ld_cols(uint32_t at, float (&v)[8]) {
                : "r"(at)
                : "memory");
 }
+__device__ __forceinline__ void tmem_st_cols(uint32_t at, const float (&v)[4]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "f"(v[0]), "f"(v[1]), "f"(v[2]),
+               "f"(v[3])
+               : "memory");
+}
 __device__ __forceinline__ void tmem_st_cols(uint32_t at, const float (&v)[8]) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(at), "f"(v[0]),
                "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
@@ -208,6 +220,9 @@ __device__ __forceinline__ float log2_scale(float x) {
   const uint32_t b = __float_as_uint(x), m = b & 0x7fffffu;
   return (float)((int)(b >> 23) - 127) + (m == 0 ? 0.f : __log2f(__uint_as_float(m | 0x3f800000u)));
 }
+
+// Whether a block's values go past the tensor cores (see above).
+__device__ __forceinline__ bool is_far(float vs) { return vs > 0.f && (vs < 0x1p-32f || vs > 0x1p16f); }
 
 // Drafted values that are not finite (of the tokens `seen`, zeroed in the product), one channel, added up.
 __device__ __noinline__ float bad_values(const __nv_bfloat16* vd, int64_t stride, uint64_t seen) {
@@ -292,6 +307,98 @@ __device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, uint32_t
   }
 }
 
+// What such blocks of the item add to rows c0 .. c0 + 3 (of `nrow`), one channel (that of the thread) each. All of the
+// group's 128 threads: two rows' logits of a token each, then the sums over the block's tokens. An infinite value is added
+// as it is, whatever its weight.
+__device__ __forceinline__ float4 far_values(const Dims& dm, const AttendArgs& a, const ByteScales& sc, const AtUnit& x,
+                                          int c0, int nrow, const float2* norm, float (*w)[64], int bar, int tok) {
+  const int64_t scales = x.l * sc.strides[0] + x.g * sc.strides[1] + x.s * sc.strides[2];
+  const int64_t slot = x.l * sc.row_strides[0] + x.g * sc.row_strides[1] + x.s * sc.row_strides[2];
+  float y[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+  for (int b = x.tok0 / 64; b * 64 < x.tok1; ++b) {
+    const float vs = __ldg(sc.vs + scales + b);
+    if (!is_far(vs)) continue;
+    const float scale = sc.scale2 * __ldg(sc.ks + scales + b);
+    const int live = min(64, x.tok1 - b * 64), j = tok & 63;
+    const int64_t at = slot + (int64_t)b * 64 * D;
+#pragma unroll 1
+    for (int e = (tok >> 6) * 2; e < (tok >> 6) * 2 + 2; ++e) {
+      const int row = x.r0 + c0 + e, h = row_head(dm.window, a.tdiv, row), t = row - h * dm.window;
+      float p = 0.f;
+      if (j < live && c0 + e < nrow && t < x.rows) {
+        const uint4* k = (const uint4*)(sc.k + at + j * D);
+        const uint4* q = (const uint4*)((const __nv_bfloat16*)a.q + x.s * dm.q_ss + x.l * dm.q_sl +
+                                        (int64_t)(x.g * dm.G + h) * dm.q_sh + t * dm.q_sp);
+        float dot = 0.f;
+#pragma unroll 1
+        for (int c = 0; c < D / 16; ++c) {
+          const uint4 kw = __ldg(k + c), q0 = __ldg(q + 2 * c), q1 = __ldg(q + 2 * c + 1);
+          const uint32_t kk[4] = {kw.x, kw.y, kw.z, kw.w}, qq[8] = {q0.x, q0.y, q0.z, q0.w, q1.x, q1.y, q1.z, q1.w};
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float2 two = e4m3_values(kk[i >> 1] >> (16 * (i & 1)) & 0xffffu);
+            dot = fmaf(bf16hi(qq[i]), two.y, fmaf(bf16lo(qq[i]), two.x, dot));
+          }
+        }
+        p = ex2(fmaf(dot, scale, -norm[c0 + e].x)) * norm[c0 + e].y;
+      }
+      w[e][j] = p;
+    }
+    named_barrier_sync(bar, 128);
+#pragma unroll 4
+    for (int i = 0; i < live; ++i) {
+      const float v = vs * e4m3_values(__ldg(sc.v + at + i * D + tok)).x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] += isinf(v) ? v : w[e][i] * v;
+    }
+    named_barrier_sync(bar, 128);
+  }
+  return make_float4(y[0], y[1], y[2], y[3]);
+}
+
+// Such a block's rows of V's tile (place n of the ring) are zeros to the tensor cores: a warp's 32. False: the wait failed.
+template <int N>
+__device__ __noinline__ bool drop_far(AbSmem<N>& sh, uint8_t* ring, uint32_t n, int quarter, int lane, uint32_t* status) {
+  constexpr int RING = AbCfg<N>::RING;
+  if (lane == 0) sh.any_far = 1;
+  const bool ok = wait_for(smem_u32(&sh.full[n % RING]), (n / RING) & 1, status, &sh.abort);
+#pragma unroll 1
+  for (int e = lane; e < 32 * 8; e += 32)
+    ((uint4*)(ring + n % RING * AB_TILE))[quarter * 32 * 8 + e] = make_uint4(0, 0, 0, 0);
+  return ok;
+}
+
+// An item with such blocks, whose first tile was team `one`'s: what both teams have of a row, normalised, and the far
+// values come to be that team's sums, with a factor of 1, and the other's have one of 0. All threads of the softmax groups.
+template <int N>
+__device__ __noinline__ void add_far(const Dims& dm, const AttendArgs& a, const ByteScales& sc, AbSmem<N>& sh, uint32_t k,
+                                     int one) {
+  const int warp = threadIdx.x >> 5, gi = (warp - 2) >> 2, tok = (warp & 3) * 32 + (threadIdx.x & 31);
+  const AtUnit& x = sh.queue[k % AB_QUEUE];
+  const int nrow = min(dm.G * dm.window - x.r0, N);
+  const uint32_t o0 = sh.tmem + AB_SBUF * N + ((uint32_t)((warp & 3) * 32) << 16);
+#pragma unroll 1
+  for (int c0 = 4 * gi; c0 < nrow; c0 += 4 * AbCfg<N>::GROUPS) {
+    const float4 far = far_values(dm, a, sc, x, c0, nrow, sh.norm, sh.far[gi], 3 + gi, tok);
+    float v[4], w[4] = {0.f, 0.f, 0.f, 0.f};
+    tmem_ld_cols(o0 + N * one + c0, v);
+    if (x.nt > 1) tmem_ld_cols(o0 + N * (one ^ 1) + c0, w);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[e] = fmaf(w[e], sh.inv[one ^ 1][c0 + e], v[e] * sh.inv[one][c0 + e]);
+      v[e] += e == 0 ? far.x : (e == 1 ? far.y : (e == 2 ? far.z : far.w));
+      w[e] = 0.f;
+    }
+    tmem_st_cols(o0 + N * one + c0, v);
+    if (x.nt > 1) tmem_st_cols(o0 + N * (one ^ 1) + c0, w);
+    named_barrier_sync(3 + gi, 128);  // the factors are read
+    if (tok < 4) sh.inv[one][c0 + tok] = 1.f, sh.inv[one ^ 1][c0 + tok] = 0.f;
+  }
+  tmem_wait_st();
+  named_barrier_sync(3 + gi, 128);
+}
+
 struct AbCost {
   static constexpr uint32_t UNIT = 1;
   __device__ __forceinline__ uint32_t operator()(int) const { return 1u; }
@@ -329,7 +436,7 @@ __global__ void __launch_bounds__(AbCfg<N>::THREADS, AbCfg<N>::PER_SM)
     return;
   }
   if (tid == 0) {
-    sh.abort = 0;
+    sh.abort = sh.any_far = 0;
     sh.bad[0] = sh.bad[1] = 0;
     for (int i = 0; i < RING; ++i) {
       mbar_init(smem_u32(&sh.full[i]), 1);
@@ -629,7 +736,8 @@ __global__ void __launch_bounds__(AbCfg<N>::THREADS, AbCfg<N>::PER_SM)
       // (all warps decide together whether to go on: a wait may fail in one of them)
       if (named_barrier_any(1, SM_THREADS, !more && *abort != 0) || !more) break;
       const AtUnit& x = sh.queue[k % AB_QUEUE];  // (its members are read where they are needed, not kept in registers)
-      const int nrow = min(R - x.r0, N), nt = x.nt, ncache = x.ncache;
+      int nrow = min(R - x.r0, N), nt = x.nt;
+      const int ncache = x.ncache;
       if (nt == 0) {  // nothing to see
         for (int r = warp - 2; r < nrow; r += 4 * C::GROUPS) {
           const int row = x.r0 + r, h = row_head(dm.window, a.tdiv, row), t = row - h * dm.window;
@@ -654,7 +762,7 @@ __global__ void __launch_bounds__(AbCfg<N>::THREADS, AbCfg<N>::PER_SM)
 #pragma unroll
       for (int r = 0; r < GR / 2; ++r) z[r] = make_float2(0.f, 0.f);
       const bool active = first < nrow;  // (a group without rows passes the tiles on)
-      float qfac = 0.f, ks_next = 0.f, vs_next = 0.f, lv = AB_UNIT;  // lv: log2 of V's scale (a block of zeros keeps the one before)
+      float qfac = 0.f, ks_next = 0.f, vs_next = 0.f, lv = AB_UNIT;  // lv: log2 of V's scale (far ones and 0 keep the one before)
       if (i_first < ncache && block(i_first) < blocks)
         ks_next = __ldg(ksp + block(i_first)), vs_next = __ldg(vsp + block(i_first));
 #pragma unroll 1
@@ -662,7 +770,8 @@ __global__ void __launch_bounds__(AbCfg<N>::THREADS, AbCfg<N>::PER_SM)
         const uint32_t it = it0 + i, b = it & 1, sb = it % SBUF;
         const bool drafted = i >= ncache;
         const float ks = ks_next;
-        if (vs_next > 0.f) lv = log2_scale(vs_next);
+        const bool far = is_far(vs_next);
+        if (vs_next > 0.f && !far) lv = log2_scale(vs_next);
         if (i + TURNS < ncache && block(i + TURNS) < blocks)
           ks_next = __ldg(ksp + block(i + TURNS)), vs_next = __ldg(vsp + block(i + TURNS));
         // One warp looks, the others are held by the barrier (the looks of all took a third of the issue slots). A wait
@@ -673,6 +782,8 @@ __global__ void __launch_bounds__(AbCfg<N>::THREADS, AbCfg<N>::PER_SM)
           break;
         }
         tc_fence_after();
+        // (not before: with this tile's S the place's filling before V of it, at most that of its K, has been used)
+        if (far && !drafted) ok = drop_far<N>(sh, ring, 2 * it0 + place_v(i, nt), quarter, lane, a.status);
         const int nv = drafted ? x.nd : min(AB_TOK, nlive - i * AB_TOK);  // rows of the tile that hold tokens
         if (i < TURNS) qfac = sh.qfac[k % AB_QUEUE];  // (there with the first product)
         const float c = drafted ? sc.scale2 : qfac * ks;
@@ -846,9 +957,7 @@ __global__ void __launch_bounds__(AbCfg<N>::THREADS, AbCfg<N>::PER_SM)
       // all warps meet here whether or not a wait failed, and leave together if one did
       if (named_barrier_any(1, SM_THREADS, !ok)) break;
       tc_fence_after();
-      const uint64_t bad = (uint64_t)sh.bad[1] << 32 | sh.bad[0];
-      const bool parts = x.nsp > 1;
-      const int64_t slot = parts ? (int64_t)at_slot<__nv_bfloat16>(a, x, x.split) * a.srows : 0;
+      const auto slot = [&]() { return (int64_t)at_slot<__nv_bfloat16>(a, x, x.split) * a.srows; };
       if (tsm < nrow) {
         const int r = tsm, row = x.r0 + r, h = row_head(dm.window, a.tdiv, row), t = row - h * dm.window;
         float m = fmaxf(sh.ref[0][r], sh.ref[1][r]), sum = 0.f, share[TURNS];
@@ -857,20 +966,25 @@ __global__ void __launch_bounds__(AbCfg<N>::THREADS, AbCfg<N>::PER_SM)
           share[j] = sh.ref[j][r] == m ? 1.f : ex2(sh.ref[j][r] - m);
           sum += ((sh.sum[j][0][r] + sh.sum[j][1][r]) + (sh.sum[j][2][r] + sh.sum[j][3][r])) * share[j];
         }
-        const float unit = ex2(AB_UNIT) * (parts ? 1.f : (sum == 0.f ? 0.f : 1.f / sum));
+        const float unit = ex2(AB_UNIT) * (x.nsp > 1 ? 1.f : (sum == 0.f ? 0.f : 1.f / sum));
 #pragma unroll
         for (int j = 0; j < TURNS; ++j) sh.inv[j][r] = share[j] * unit;
         if (m > -INFINITY) m -= AB_UNIT;
-        if (parts) ((float2*)a.mlpart)[slot + r] = make_float2(m, sum);
+        sh.norm[r] = make_float2(m, x.nsp > 1 ? 1.f : (sum == 0.f ? 0.f : 1.f / sum));
+        if (x.nsp > 1) ((float2*)a.mlpart)[slot() + r] = make_float2(m, sum);
         else if (t < x.rows && a.lse != nullptr)
           a.lse[x.s * a.ls[0] + x.l * a.ls[1] + (x.g * dm.G + h) * a.ls[2] + t] = row_lse(m, sum);
       }
       named_barrier_sync(1, SM_THREADS);
+      if (sh.any_far != 0) add_far<N>(dm, a, sc, sh, k, (int)((it0 - x.nt) & 1));
+      nrow = min(R - x.r0, N), nt = x.nt;
+      const bool parts = x.nsp > 1;
       // a lane has one channel of some rows, four at a time (few instructions: a CTA comes here once or twice)
+      const uint64_t bad = (uint64_t)sh.bad[1] << 32 | sh.bad[0];
       const uint32_t o0 = tmem + AB_O + lanes;
       __nv_bfloat16* o = (__nv_bfloat16*)a.o + x.s * a.os[0] + x.l * a.os[1] + (int64_t)x.g * dm.G * a.os[2] + tok;
       const __nv_bfloat16* vd = (const __nv_bfloat16*)a.vd + x.s * a.vds[0] + x.l * a.vds[1] + x.g * a.vds[2] + tok;
-      float* po = parts ? a.opart + slot * D + tok : nullptr;
+      float* po = parts ? a.opart + slot() * D + tok : nullptr;
       const bool both = nt > 1;
       const int one = (int)((it0 - nt) & 1), rows = x.rows, row0 = x.r0;  // the first tile's team
 #pragma unroll 1
@@ -904,6 +1018,7 @@ __global__ void __launch_bounds__(AbCfg<N>::THREADS, AbCfg<N>::PER_SM)
       }
       named_barrier_sync(1, SM_THREADS);  // the masks, sums and bits are read, and the item
       if (bad != 0 && tsm == 0) sh.bad[0] = sh.bad[1] = 0;
+      if (tsm == 0) sh.any_far = 0;
       if (lane == 0) mbar_arrive(smem_u32(&sh.ofree)), done(k);
     }
   }

@@ -29,13 +29,6 @@ __device__ __forceinline__ uint32_t e4m3x2(float a, float b) {
 __device__ __forceinline__ uint32_t e4m3x4(const float* x, float by) {
   return e4m3x2(x[0] * by, x[1] * by) | e4m3x2(x[2] * by, x[3] * by) << 16;
 }
-// Two e4m3 bytes' values, exact.
-__device__ __forceinline__ float2 e4m3_values(uint32_t two) {
-  uint32_t h;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)two));
-  return make_float2(__half2float(__ushort_as_half((unsigned short)(h & 0xffff))),
-                     __half2float(__ushort_as_half((unsigned short)(h >> 16))));
-}
 
 template <typename T>
 struct ByPiece {  // 16 bytes of a row

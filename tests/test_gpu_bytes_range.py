@@ -77,7 +77,7 @@ def plain(t, q, kd=None, vd=None, tree=None):
 
 def far(vs):
     """Blocks whose V does not go through the tensor cores."""
-    return (vs > 0) & ((vs < 2.0 ** -40) | (vs > 2.0 ** 16))
+    return (vs > 0) & ((vs < 2.0 ** -32) | (vs > 2.0 ** 16))
 
 
 def check(t, q, *drafted):
@@ -124,3 +124,84 @@ def test_attend_a_larger_token_in_every_tile():
     v[:, :, :, ::128] = 0.0
     t.store(k, v)
     check(t, q)
+
+
+# -------------------------------------------------------------------- scales ----
+HEADS = [(1, 8, 2), (7, 8, 2), (30, 8, 2), (8, 4, 4)]  # queries, query and KV heads: 16, 32 and 64 rows at a time
+
+
+def filled(g, S, Hq, Hkv, n, change, lengths=None, spread=0.7):
+    """Slots whose V (float32) is what `change` makes of ordinary values."""
+    t = Slots(S, 1, Hq, Hkv, n)
+    k, v = spread * randn(g, S, 1, Hkv, n, D), randn(g, S, 1, Hkv, n, D) + 0.5
+    change(v)
+    t.store(k, v, lengths)
+    return t
+
+
+@pytest.mark.parametrize("T,Hq,Hkv", HEADS)
+@pytest.mark.parametrize("size", [2.0 ** -118, 2.0 ** -100, 2.0 ** -60, 2.0 ** -31, 2.0 ** 22, 2.0 ** 40, 2.0 ** 102])
+def test_attend_values_all_very_small_or_large(size, T, Hq, Hkv):
+    """The logarithm of the sum of exponentials has nothing to do with V; scales from the least one on."""
+    g = gen(720)
+    t = filled(g, 2, Hq, Hkv, 640, lambda v: v.mul_(size), [640, 70])
+    q = randn(g, 2, 1, Hq, T, D, dtype=BF16)
+    check(t, q)
+    kd, vd = (randn(g, 2, 1, Hkv, T, D, dtype=BF16) for _ in range(2))
+    check(t, q, kd, (vd * size).to(BF16))
+
+
+@pytest.mark.parametrize("T,Hq,Hkv", HEADS)
+@pytest.mark.parametrize("n", [64, 640])
+def test_attend_cached_values_that_are_not_finite(n, T, Hq, Hkv):
+    """An infinite value is read as one, in its channel alone; the others, and the sum of exponentials, are as without it."""
+    g = gen(721)
+
+    def change(v):
+        v[0, 0, 0, 5, 7], v[0, 0, -1, n - 1, 0] = math.inf, -math.inf
+        v[1, 0, 0, 63, 100], v[1, 0, -1, 1, 3], v[1, 0, -1, n - 2, 3] = math.nan, math.inf, -math.inf
+
+    t = filled(g, 3, Hq, Hkv, n, change)
+    q = randn(g, 3, 1, Hq, T, D, dtype=BF16)
+    check(t, q)
+    kd, vd = (randn(g, 3, 1, Hkv, T, D, dtype=BF16) for _ in range(2))
+    check(t, q, kd, vd, trees(g, 3, T))
+    o, _ = t.c.attend(q)
+    assert (o[0, 0, 0, :, 7] == math.inf).all() and (o[0, 0, -1, :, 0] == -math.inf).all()
+    assert o[1, 0, 0, :, 100].isnan().all() and o[1, 0, -1, :, 3].isnan().all()
+    assert (~o.isfinite()).sum() == 4 * T * (Hq // Hkv)
+
+
+@pytest.mark.parametrize("T,Hq,Hkv", HEADS)
+def test_attend_scales_that_differ_by_many_orders(T, Hq, Hkv):
+    """Blocks whose few large values stand in channels of their own, blocks of small ones and of zeros: each channel has
+    what its own values give."""
+    g, n = gen(722), 64 * 14
+
+    def change(v):
+        for block, size in ((1, 2.0 ** 60), (4, 2.0 ** 100), (7, 2.0 ** 118), (12, 2.0 ** 30)):
+            v[:, :, :, 64 * block + 3, block] = size
+        for block, size in ((2, 2.0 ** -118), (5, 2.0 ** -70), (9, 0.0), (10, 2.0 ** -45)):
+            v[:, :, :, 64 * block:64 * block + 64] *= size
+
+    t = filled(g, 2, Hq, Hkv, n, change, [n, 64 * 8 - 5])
+    q = randn(g, 2, 1, Hq, T, D, dtype=BF16)
+    check(t, q)
+    kd, vd = (randn(g, 2, 1, Hkv, T, D, dtype=BF16) for _ in range(2))
+    check(t, q, kd, vd, trees(g, 2, T))
+
+
+@pytest.mark.parametrize("T,Hq,Hkv", [(1, 4, 1), (40, 8, 1)])
+def test_attend_far_scales_in_several_splits(T, Hq, Hkv):
+    g, n = gen(723), 20032
+
+    def change(v):
+        v[:, :, :, 77, 5], v[:, :, :, 9000:9064, 6], v[:, :, :, n - 1, 7] = 2.0 ** 80, 2.0 ** 70, -math.inf
+        v[:, :, :, 12800:13056] *= 2.0 ** -90
+
+    t = filled(g, 1, Hq, Hkv, n, change, spread=0.4)
+    q = randn(g, 1, 1, Hq, T, D, dtype=BF16)
+    check(t, q)
+    again = [x.clone() for x in t.c.attend(q)]
+    for _ in range(3):
+        assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(t.c.attend(q), again))
