@@ -75,8 +75,9 @@ struct AbSmem {
   uint64_t rowmask[N];                     // drafted tokens that a row sees
   __align__(16) float4 top[2][N];                  // by a tile's parity: the four quarters' maxima of a row
   __align__(16) float base[4 * C::GROUPS][C::GR];  // a warp's own: its rows' maxima, then log2 vs - ref
+  __align__(16) float coef[4 * C::GROUPS][C::GR];  // and what their products are multiplied with
   float sum[2][4][N], ref[2][N], inv[2][N];        // by team
-  float qmax[C::LOADERS], qfac[AB_QUEUE];
+  float qfac[AB_QUEUE][N];                 // scale log2(e) 2^e of a row
   uint32_t tmem, bad[2];
   float2 norm[N];                          // a row's reference, and what exp2(logit - reference) is multiplied with
   float far[C::GROUPS][4][64];             // add_far's weights
@@ -631,7 +632,7 @@ __global__ void __launch_bounds__(AbCfg<N>::THREADS, AbCfg<N>::PER_SM)
     if (leader) umma_commit(smem_u32(&sh.drained));
     wait_for(smem_u32(&sh.drained), 0, a.status, nullptr);
   } else if (warp >= LOAD0) {
-    // ------------------ the rows as they are (for drafted tokens), then scaled to e4m3's range and split
+    // ------------------ the rows as they are (for drafted tokens), then each scaled to e4m3's range and split
     const int e0 = (warp - LOAD0) * 32 + lane, c = e0 & 15;  // 16 bytes: channels 8 c .. + 7
     constexpr int STEP = 2 * LOADERS, PIECES = N / STEP;
     const uint32_t mine = smem_u32(qb) + (c >> 3) * PART;
@@ -658,8 +659,9 @@ __global__ void __launch_bounds__(AbCfg<N>::THREADS, AbCfg<N>::PER_SM)
       }
       // the item before's last tile has met its rows
       const bool ok = busy == 0 || wait_for(smem_u32(&sh.rowsfree), (busy - 1) & 1, a.status, abort);
-      // (zeros behind the last row, as far as the softmax looks)
-      const int pieces = min(PIECES, (R - x.r0 + 7) / 8 * (8 / STEP));
+      // (zeros behind the last row, as far as the softmax looks: CH rows at a time)
+      constexpr int CH = N == 16 ? 8 : 16;
+      const int pieces = min(PIECES, (R - x.r0 + CH - 1) / CH * (CH / STEP));
 #pragma unroll 4
       for (int i = 0; i < pieces; ++i) {
         const int r = (e0 >> 4) + STEP * i;
@@ -672,33 +674,26 @@ __global__ void __launch_bounds__(AbCfg<N>::THREADS, AbCfg<N>::PER_SM)
         if (lane == 0) mbar_arrive(smem_u32(&sh.rowsasked));
       }
       cp_async_wait<0>();  // (a thread reads what it has copied itself)
-      float top = 0.f;     // of the finite ones
-#pragma unroll 2
-      for (int i = 0; i < pieces; ++i) {
-        const uint4 w = lds_u128(mine + sw128_off((e0 >> 4) + STEP * i, c & 7));
-        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float lo = fabsf(bf16lo(u[e])), hi = fabsf(bf16hi(u[e]));
-          if (lo < INFINITY) top = fmaxf(top, lo);
-          if (hi < INFINITY) top = fmaxf(top, hi);
-        }
-      }
-      top = warp_max(top);
-      if (lane == 0) sh.qmax[warp - LOAD0] = top;
       if (named_barrier_any(2, 32 * LOADERS, !ok)) break;
-#pragma unroll
-      for (int i = 0; i < LOADERS; ++i) top = fmaxf(top, sh.qmax[i]);
-      // the power of two that brings the largest to 224 .. 448
-      int e = top == 0.f ? 127 : (int)(__float_as_uint(top) >> 23) - 8 + ((__float_as_uint(top) & 0x7fffffu) > 0x600000u);
-      e = e < 1 ? 1 : e;
-      const float by = __uint_as_float((uint32_t)(254 - e) << 23);
-      if (e0 == 0) sh.qfac[k % AB_QUEUE] = sc.scale2 * __uint_as_float((uint32_t)e << 23);
-#pragma unroll 1
+#pragma unroll 2
       for (int i = 0; i < pieces; ++i) {
         const int r = (e0 >> 4) + STEP * i;
         const uint4 w = lds_u128(mine + sw128_off(r, c & 7));
         const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+        float top = 0.f;  // the row's largest finite one: 16 lanes have it
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float lo = fabsf(bf16lo(u[j])), hi = fabsf(bf16hi(u[j]));
+          if (lo < INFINITY) top = fmaxf(top, lo);
+          if (hi < INFINITY) top = fmaxf(top, hi);
+        }
+#pragma unroll
+        for (int off = 8; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+        // the power of two that brings it to 224 .. 448
+        int e = top == 0.f ? 127 : (int)(__float_as_uint(top) >> 23) - 8 + ((__float_as_uint(top) & 0x7fffffu) > 0x600000u);
+        e = e < 1 ? 1 : e;
+        const float by = __uint_as_float((uint32_t)(254 - e) << 23);
+        if (c == 0) sh.qfac[k % AB_QUEUE][r] = sc.scale2 * __uint_as_float((uint32_t)e << 23);
         uint32_t hi[2], lo[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -721,7 +716,7 @@ __global__ void __launch_bounds__(AbCfg<N>::THREADS, AbCfg<N>::PER_SM)
     // group: four warps, which have the tensor memory's four quarters of lanes
     const int gi = (warp - 2) >> 2, team = gi / CG, cg = gi % CG, quarter = warp & 3, tok = quarter * 32 + lane;
     const int first = GR * cg, tsm = tid - 64;  // the group's first row
-    const uint32_t bases = smem_u32(sh.base[warp - 2]);
+    const uint32_t bases = smem_u32(sh.base[warp - 2]), coefs = smem_u32(sh.coef[warp - 2]);
     // where the token's line of weights is, and its swizzle of the group's bytes in it (weight_off)
     const uint32_t line = smem_u32(ps) + team * WBUF + tok * (2 * N);
     const uint32_t swizzle = ((uint32_t)(tok * (2 * N)) >> 3 & (uint32_t)(2 * N - 16)) ^ (uint32_t)first;
@@ -785,8 +780,8 @@ __global__ void __launch_bounds__(AbCfg<N>::THREADS, AbCfg<N>::PER_SM)
         // (not before: with this tile's S the place's filling before V of it, at most that of its K, has been used)
         if (far && !drafted) ok = drop_far<N>(sh, ring, 2 * it0 + place_v(i, nt), quarter, lane, a.status);
         const int nv = drafted ? x.nd : min(AB_TOK, nlive - i * AB_TOK);  // rows of the tile that hold tokens
-        if (i < TURNS) qfac = sh.qfac[k % AB_QUEUE];  // (there with the first product)
-        const float c = drafted ? sc.scale2 : qfac * ks;
+        if (i < TURNS) qfac = sh.qfac[k % AB_QUEUE][first + mine];  // (there with the first product)
+        const float c = drafted ? sc.scale2 : qfac * ks;            // of row `mine`
         const float w_lv = drafted ? 0.f : lv;  // (drafted weights are bf16, and V as it is)
         const uint32_t scol = tmem + N * sb + first + lanes, tops = smem_u32(&sh.top[b][first + mine]);
         const bool seen = tok < nv, part = drafted || nv < AB_TOK;
@@ -832,7 +827,10 @@ __global__ void __launch_bounds__(AbCfg<N>::THREADS, AbCfg<N>::PER_SM)
               deep = fmaxf(deep, to - AB_DEEP);
             }
           }
-          if (lane < GR) sts_f32(bases + lane * 4, ref == -INFINITY ? 0.f : w_lv - ref);
+          if (lane < GR) {
+            sts_f32(bases + lane * 4, ref == -INFINITY ? 0.f : w_lv - ref);
+            sts_f32(coefs + lane * 4, c);
+          }
           __syncwarp();
           // the tile before's weights are read (and its sums in the accumulators, should they be rescaled)
           if (i >= TURNS) {
@@ -858,7 +856,7 @@ __global__ void __launch_bounds__(AbCfg<N>::THREADS, AbCfg<N>::PER_SM)
           }
           // The weights, and the lane's sums of what they are of Z.
           const float iv1 = ex2(AB_UNIT - w_lv);
-          const float2 cc = make_float2(c, c), iv = make_float2(iv1, iv1);
+          const float2 iv = make_float2(iv1, iv1);
 #pragma unroll
           for (int c0 = 0; c0 < GR; c0 += CH) {
             if (c0 > 0 && first + c0 >= nrow) break;
@@ -872,9 +870,9 @@ __global__ void __launch_bounds__(AbCfg<N>::THREADS, AbCfg<N>::PER_SM)
             float2 v[CH / 2];
 #pragma unroll
             for (int e = 0; e < CH / 2; e += 2) {
-              const float4 bs = lds_f32x4(bases + (c0 + 2 * e) * 4);
-              v[e] = fma2(make_float2(s1[2 * e], s1[2 * e + 1]), cc, make_float2(bs.x, bs.y));
-              v[e + 1] = fma2(make_float2(s1[2 * e + 2], s1[2 * e + 3]), cc, make_float2(bs.z, bs.w));
+              const float4 bs = lds_f32x4(bases + (c0 + 2 * e) * 4), cs = lds_f32x4(coefs + (c0 + 2 * e) * 4);
+              v[e] = fma2(make_float2(s1[2 * e], s1[2 * e + 1]), make_float2(cs.x, cs.y), make_float2(bs.x, bs.y));
+              v[e + 1] = fma2(make_float2(s1[2 * e + 2], s1[2 * e + 3]), make_float2(cs.z, cs.w), make_float2(bs.z, bs.w));
             }
 #pragma unroll
             for (int e = 0; e < CH / 2; ++e) v[e] = make_float2(ex2(v[e].x), ex2(v[e].y));

@@ -205,3 +205,28 @@ def test_attend_far_scales_in_several_splits(T, Hq, Hkv):
     again = [x.clone() for x in t.c.attend(q)]
     for _ in range(3):
         assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(t.c.attend(q), again))
+
+
+# ------------------------------------------------------------------- queries ----
+@pytest.mark.parametrize("T", [1, 6, 9, 40])
+def test_attend_rows_of_very_different_sizes(T):
+    """Heads and drafted tokens whose queries are small beside others of the same block of rows: a row's output has its own
+    rounding, whatever stands beside it."""
+    g, S, Hq, Hkv, n = gen(740 + T), 2, 8, 2, 320
+    t = filled(g, S, Hq, Hkv, n, lambda v: v, [320, 77], spread=1.0)
+    q = randn(g, S, 1, Hq, T, D, dtype=BF16)
+    alone = q.clone()
+    bits = torch.tensor([14, 0, 7, -1, 0, -30, 12, 20], dtype=F32, device=DEV)
+    q *= torch.exp2(bits).to(BF16)[:, None, None]
+    if T > 1:
+        q[:, :, :, 1::3] *= 2.0 ** -9
+        q[:, :, 1, 2::3], q[:, :, 4, 0] = 0.0, 2.0 ** -120
+    check(t, q)
+    kd, vd = (randn(g, S, 1, Hkv, T, D, dtype=BF16) for _ in range(2))
+    check(t, q, kd, vd, trees(g, S, T))
+    # rows that are the same give the same, to the last bit
+    rows = [1, 4] if T == 1 else [1]
+    at = [i for i in range(T) if i % 3 == 0 and (T == 1 or i > 0)]
+    one, two = (x.clone() for x in t.c.attend(alone)), t.c.attend(q)
+    for a, b in zip(one, two):
+        assert torch.equal(a[:, :, rows][:, :, :, at], b[:, :, rows][:, :, :, at])
