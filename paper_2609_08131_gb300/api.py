@@ -16,6 +16,7 @@ import torch
 from . import (
     JACAP_ATTEND_ZERO_BYTES,
     JACAP_BF16,
+    JACAP_ERR_WORKSPACE,
     JACAP_F32,
     JACAP_OK,
     jacap_append,
@@ -426,11 +427,14 @@ class Cache8:
     128] (torch.float8_e4m3fn; a slot's n x 128 bytes lie together) and ``k_scales``, ``v_scales`` [L, Hkv, S, n / 64]
     (float32), a power of two for each block of 64 tokens, by which ``store`` and ``append`` write the
     bytes. ``lengths`` int32 [S] on the device: live tokens of each slot, which they keep up to date. Owns the
-    workspace of its calls, which therefore come one after the other, and the outputs of ``attend``.
+    workspace of its calls, which therefore come one after the other, and the outputs of ``attend``, which takes up
+    to ``tokens`` queries per request and head (the workspace has their splits' sums: in MB 10 for 64 of them with
+    32 / 8 heads, 5 for 8, 1 for one).
 
     ``Cache8.empty`` makes the tensors; ``part`` is a handle of some layers or slots of the same tensors."""
 
-    def __init__(self, k, v, k_scales, v_scales, lengths, num_q_heads: int, scale: float | None = None):
+    def __init__(self, k, v, k_scales, v_scales, lengths, num_q_heads: int, scale: float | None = None,
+                 tokens: int = 64):
         dev = k.device
         if k.dim() != 5 or k.shape[-1] != 128 or k.shape[3] % 64 != 0 or k.shape[3] == 0 or k.numel() == 0:
             raise ValueError("k must be [L, Hkv, S, n, 128], n a multiple of 64")
@@ -456,11 +460,13 @@ class Cache8:
         c.head_dim, c.slot_tokens = 128, self.n
         c.strides[:] = one(k)
         c.scale_strides[:] = one(k_scales)
-        nbytes = jacap_bytes_workspace(c, 64)
+        self.tokens = int(tokens)
+        nbytes = jacap_bytes_workspace(c, self.tokens)
         if nbytes == 0:
-            wide = self.Hq % self.Hkv == 0 and self.Hq // self.Hkv > 8
+            wide = self.Hq % self.Hkv == 0 and self.Hq // self.Hkv > 8 or self.tokens > 64
             raise JacapError(2 if wide else 1, "jacap_bytes_workspace")
-        self.ws = torch.zeros(nbytes, dtype=torch.uint8, device=dev)
+        self.ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        self.ws[:JACAP_ATTEND_ZERO_BYTES + 4 * self.S].zero_()  # the status word and counters
         self._attn = jacap_attention()
         self._attn.scale = self.scale
         self._at = {}
@@ -470,22 +476,22 @@ class Cache8:
 
     @classmethod
     def empty(cls, num_seqs: int, num_layers: int, num_q_heads: int, num_kv_heads: int, slot_tokens: int,
-              device="cuda", scale: float | None = None):
+              device="cuda", scale: float | None = None, tokens: int = 64):
         """Empty slots of at least ``slot_tokens`` tokens (rounded up to blocks of 64)."""
         n = max(1, -(-int(slot_tokens) // 64)) * 64
         shape = (2, num_layers, num_kv_heads, num_seqs)
         rows = torch.zeros((*shape, n, 128), dtype=torch.uint8, device=device).view(torch.float8_e4m3fn)
         scales = torch.zeros((*shape, n // 64), dtype=torch.float32, device=device)
         lengths = torch.zeros(num_seqs, dtype=torch.int32, device=device)
-        return cls(rows[0], rows[1], scales[0], scales[1], lengths, num_q_heads, scale)
+        return cls(rows[0], rows[1], scales[0], scales[1], lengths, num_q_heads, scale, tokens)
 
-    def part(self, layers=slice(None), slots=slice(None)):
-        """A handle (with a workspace of its own) of the given layers and slots (slices) of these tensors: a layer's
-        attention in a model's loop, or the slots of the requests whose prompts have arrived. Where it takes all
-        slots its ``lengths`` are these."""
+    def part(self, layers=slice(None), slots=slice(None), tokens: int | None = None):
+        """A handle (with a workspace of its own, for up to ``tokens`` queries; None: as many as here) of the given
+        layers and slots (slices) of these tensors: a layer's attention in a model's loop, or the slots of the requests
+        whose prompts have arrived. Where it takes all slots its ``lengths`` are these."""
         at = (layers, slice(None), slots)
         return Cache8(self.k[at], self.v[at], self.k_scales[at], self.v_scales[at], self.lengths[slots],
-                      self.Hq, self.scale)
+                      self.Hq, self.scale, self.tokens if tokens is None else tokens)
 
     def _rows(self, k, v, names, tokens=None):
         """Checks rows [S, L, Hkv, t, 128]; their addresses, library type, number and strides."""
@@ -535,7 +541,7 @@ class Cache8:
     def attend(self, q, k_draft=None, v_draft=None, tree=None, lengths=None, draft_lens=None, stream=None):
         """Attention of each request's last queries over its slot and, if given, over drafted tokens that are
         not in it yet (``jacap_bytes_attend``): q [S, L, Hq, T, 128], k_draft and v_draft [S, L, Hkv, T, 128]
-        (bf16, T at most 64), tree int64 [S, T] (``tree_masks``; None: a chain), lengths int32 [S] (None: the slots'
+        (bf16, T at most the handle's ``tokens``), tree int64 [S, T] (``tree_masks``; None: a chain), lengths int32 [S] (None: the slots'
         own), draft_lens int32 [S] queries of each request (None: T; rows behind are left as they were). Returns (o
         [S, L, Hq, T, 128] bf16, lse [S, L, Hq, T] float32), which the next call of as many queries overwrites."""
         a, dev, bf16 = self._attn, self.device, torch.bfloat16
@@ -544,6 +550,8 @@ class Cache8:
         S, L, T = self.S, self.L, q.shape[3]
         if not 1 <= T <= 64:
             raise JacapError(2 if T > 64 else 1, "jacap_bytes_attend")
+        if T > self.tokens:
+            raise JacapError(JACAP_ERR_WORKSPACE, "jacap_bytes_attend")
         qp = _tensor("q", q, dev, bf16, (S, L, self.Hq, T, 128))
         if (k_draft is None) != (v_draft is None) or (tree is not None and k_draft is None):
             raise ValueError("k_draft and v_draft come together, and a tree with them")

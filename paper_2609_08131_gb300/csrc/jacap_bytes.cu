@@ -56,7 +56,7 @@ BytesPlan plan_of(const jacap_byte_cache* c, int tokens) {
   const int64_t tiles = (c->slot_tokens - 1) / 128 + 2, units = (int64_t)c->num_seqs * c->num_layers * c->num_kv_heads;
   p.nsplit = tiles < 2 * p.edge ? 1 : (int)((tiles - 1) / p.least + 2);  // a share's borders are anywhere in a unit
   // two slots for each border between CTAs: the split before and the one after
-  p.slots = (int)(2 * (std::min<int64_t>(units * p.nrb * p.nsplit, ATTEND_CTAS) - 1));
+  p.slots = (int)(2 * (std::min<int64_t>(units * p.nrb * p.nsplit, attend_bytes_ctas(p.block)) - 1));
   p.srows = std::min(p.rows, p.block);
   return p;
 }

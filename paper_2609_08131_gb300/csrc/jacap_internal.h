@@ -244,6 +244,7 @@ struct ByteScales {
   float scale2;        // scale log2 e
 };
 int attend_bytes_block(int rows);  // rows of a CTA
+int attend_bytes_ctas(int block);  // CTAs at most
 // maps: K, V, drafted K, drafted V
 cudaError_t launch_attend_bytes(const CUtensorMap* maps, const Dims& dm, const AttendArgs& a, const ByteScales& sc,
                                 int sms, cudaStream_t st);

@@ -1034,12 +1034,15 @@ static cudaError_t launch_n(const CUtensorMap* maps, const Dims& dm, const Atten
   auto kern = attend_bytes_kernel<N>;
   JACAP_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ab_smem<N>()));
   const int64_t items = (int64_t)dm.L * dm.Hkv * dm.S * a.nsplit * a.nrb;
-  const int places = AbCfg<N>::PER_SM * sms < ATTEND_CTAS ? AbCfg<N>::PER_SM * sms : ATTEND_CTAS;
+  const int places = min(AbCfg<N>::PER_SM * sms, attend_bytes_ctas(N));
   return launch_pdl(true, kern, (int)(items < places ? items : places), AbCfg<N>::THREADS, ab_smem<N>(), st, maps[0],
                     maps[1], maps[2], maps[3], dm, a, sc);
 }
 
 int attend_bytes_block(int rows) { return rows <= 16 ? 16 : (rows <= 32 ? 32 : 64); }
+// (so many have slots for their splits' sums: two CTAs of 16 rows run on an SM, one of more)
+int attend_bytes_ctas(int block) { return block == 16 ? ATTEND_CTAS : ATTEND_CTAS / 2; }
+static_assert(AbCfg<16>::PER_SM == 2 && AbCfg<32>::PER_SM == 1 && AbCfg<64>::PER_SM == 1, "attend_bytes_ctas");
 
 cudaError_t launch_attend_bytes(const CUtensorMap* maps, const Dims& dm, const AttendArgs& a, const ByteScales& sc,
                                 int sms, cudaStream_t st) {

@@ -1,0 +1,29 @@
+"""GPU tests of handles of a cache held in 8 bits: their workspaces, parts of a cache, and slots of any length."""
+
+import pytest
+import torch
+
+import paper_2609_08131_gb300.api as api
+from paper_2609_08131_gb300 import JACAP_ATTEND_ZERO_BYTES
+from test_gpu_bytes import BF16, D, DEV, gen, ints, randn, trees
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("T", [1, 5, 40])
+def test_a_workspace_of_few_queries_does_what_one_of_many_does(T):
+    """Only the status word and the counters start at zero; the rest may hold anything."""
+    g, S, Hq, Hkv, n = gen(800 + T), 3, 8, 2, 9088
+    many = api.Cache8.empty(S, 2, Hq, Hkv, n, device=DEV)
+    many.store(*(randn(g, S, 2, Hkv, 9000, D, dtype=BF16) for _ in range(2)), ints([9000, 70, 4000]))
+    few = many.part(tokens=T)
+    assert few.ws.numel() <= many.ws.numel()
+    few.ws[JACAP_ATTEND_ZERO_BYTES + 4 * S:].fill_(0xFF)
+    q, kd, vd = randn(g, S, 2, Hq, T, D, dtype=BF16), *(randn(g, S, 2, Hkv, T, D, dtype=BF16) for _ in range(2))
+    masks = trees(g, S, T)
+    for _ in range(2):
+        for a, b in zip(many.attend(q, kd, vd, masks), few.attend(q, kd, vd, masks)):
+            assert torch.equal(a, b)
+    few.append(kd, vd, taken=ints([T, 0, 1]))
+    assert many.lengths.tolist() == [9000 + T, 70, 4001]
+    many.check(), few.check()
