@@ -663,7 +663,7 @@ size_t jacap_bytes_workspace(const jacap_byte_cache* cache, int32_t tokens);
  * K and V, or what an eviction kept of them). Bytes of other rows and scales of other blocks are left as they were.
  *   k_rows, v_rows device, `dtype`: row (s, l, g, i), i < rows, at s row_strides[0] + l [1] +
  *                  g [2] + i [3] of k_rows ([4 .. 7] of v_rows): elements, multiples of 16 bytes, not negative
- *   rows           0 to slot_tokens
+ *   rows           0 to slot_tokens (0: k_rows and v_rows are not read and may be NULL)
  *   lengths        device int32 [num_seqs], 0 to rows, or NULL: rows
  *   lengths_out    device int32 [num_seqs] or NULL: the lengths (`lengths` itself works)
  */

@@ -505,7 +505,7 @@ class Cache8:
         return kp, vp, JACAP_BF16 if k.dtype == torch.bfloat16 else JACAP_F32, k.shape[3]
 
     def store(self, k, v, lengths=None, stream=None):
-        """Rows k, v [S, L, Hkv, t, 128] (float32 or bf16, t at most n; any strides of whole 16 bytes) into
+        """Rows k, v [S, L, Hkv, t, 128] (float32 or bf16, t 0 to n; any strides of whole 16 bytes) into
         the slots' rows from 0 on (``jacap_bytes_store``): lengths[s] (int32 [S] on the device; None: t) of each
         request, which become the slots' ``lengths``. Other rows keep their bytes."""
         kp, vp, dtype, t = self._rows(k, v, ("k", "v"))

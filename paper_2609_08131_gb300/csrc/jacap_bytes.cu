@@ -88,7 +88,8 @@ BytesCarve carve(const jacap_byte_cache* c, int tokens) {
 jacap_status byte_args(const jacap_byte_cache* c, jacap_dtype dtype, const void* k, const void* v,
                        const int64_t* strides, int tokens, void* ws, size_t ws_bytes, ByteArgs& a) {
   if (dtype != JACAP_F32 && dtype != JACAP_BF16) return JACAP_ERR_INVALID_ARG;
-  if (k == nullptr || v == nullptr || strides == nullptr || !aligned16(k) || !aligned16(v)) return JACAP_ERR_INVALID_ARG;
+  if (strides == nullptr || !aligned16(k) || !aligned16(v)) return JACAP_ERR_INVALID_ARG;
+  if (tokens > 0 && (k == nullptr || v == nullptr)) return JACAP_ERR_INVALID_ARG;  // (no rows have no address)
   const int64_t el16 = dtype == JACAP_BF16 ? 8 : 4;
   const int64_t count[4] = {c->num_seqs, c->num_layers, c->num_kv_heads, tokens};
   memset(&a, 0, sizeof(a));

@@ -1,10 +1,13 @@
 """Handles of a cache held in 8 bits, without a GPU: the workspace that they take, and what calls beyond it get."""
 
+import ctypes
+
 import pytest
 import torch
 
 import paper_2609_08131_gb300 as J
 from paper_2609_08131_gb300 import api
+from test_operators_cpu import BAD, P, PASSED, passed, refused
 
 ZEROED = J.JACAP_ATTEND_ZERO_BYTES
 
@@ -36,3 +39,19 @@ def test_numbers_of_queries_that_no_workspace_has(tokens, status):
     with pytest.raises(api.JacapError) as e:
         empty(tokens, S=1, n=64)
     assert e.value.status == status
+
+
+def store(rows, k, v):
+    c = empty(S=2, Hq=4, Hkv=2, n=128)
+    strides = (ctypes.c_int64 * 8)(*[512 * 128, 512 * 128, 256 * 128, 128] * 2)
+    return J.jacap_bytes_store(c._cache, J.JACAP_BF16, k, v, strides, rows, P, P, P, 1 << 20, None)
+
+
+@PASSED
+def test_no_rows_have_no_address():
+    passed(store(0, None, None))
+
+
+@pytest.mark.parametrize("k,v", [(None, P), (P, None)])
+def test_rows_have_one(k, v):
+    refused(store(1, k, v), BAD)

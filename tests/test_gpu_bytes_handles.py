@@ -27,3 +27,24 @@ def test_a_workspace_of_few_queries_does_what_one_of_many_does(T):
     few.append(kd, vd, taken=ints([T, 0, 1]))
     assert many.lengths.tolist() == [9000 + T, 70, 4001]
     many.check(), few.check()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, BF16])
+def test_a_store_of_no_rows_empties_the_slots(dtype):
+    g = gen(810)
+    c = api.Cache8.empty(2, 1, 4, 2, 128, device=DEV)
+    c.store(*(randn(g, 2, 1, 2, 100, D, dtype=BF16) for _ in range(2)))
+    before = [x.clone() for x in (c.k.view(torch.uint8), c.v.view(torch.uint8), c.k_scales, c.v_scales)]
+    none = torch.empty(2, 1, 2, 0, D, dtype=dtype, device=DEV)
+    c.store(none, none, ints([0, 0]))
+    assert c.lengths.tolist() == [0, 0]
+    assert all(torch.equal(a, b) for a, b in zip(before, (c.k.view(torch.uint8), c.v.view(torch.uint8), c.k_scales, c.v_scales)))
+    c.check()
+    c.append(*(randn(g, 2, 1, 2, 3, D, dtype=dtype) for _ in range(2)))
+    c.store(none, none)
+    assert c.lengths.tolist() == [0, 0]
+    o, lse = c.attend(randn(g, 2, 1, 4, 1, D, dtype=BF16))
+    assert (o == 0).all() and (lse == -float("inf")).all()
+    c.store(none, none, ints([0, 1]))  # a length that there is no row for
+    with pytest.raises(api.JacapError):
+        c.check()
