@@ -48,3 +48,24 @@ def test_a_store_of_no_rows_empties_the_slots(dtype):
     c.store(none, none, ints([0, 1]))  # a length that there is no row for
     with pytest.raises(api.JacapError):
         c.check()
+
+
+def test_rows_at_the_very_end_of_slots_whose_offsets_pass_32_bits():
+    """5.4 GB: the last block of the last slot has what a small cache's has, and nothing else is touched."""
+    S, L, Hkv, n, g = 2, 2, 8, 655360, gen(820)
+    c = api.Cache8.empty(S, L, 8, Hkv, n, device=DEV, tokens=1)
+    small = api.Cache8.empty(1, 1, 8, Hkv, 64, device=DEV, tokens=1)
+    k, v = (randn(g, 1, 1, Hkv, 3, D, dtype=BF16) for _ in range(2))
+    x, y = (torch.zeros(S, L, Hkv, 3, D, dtype=BF16, device=DEV) for _ in range(2))
+    x[1:, 1:], y[1:, 1:] = k, v
+    small.append(k, v, lengths=ints([61]))
+    c.append(x, y, lengths=ints([n - 3] * S))
+    assert c.lengths.tolist() == [n] * S
+    for big, little in ((c.k.view(torch.uint8), small.k.view(torch.uint8)), (c.v.view(torch.uint8), small.v.view(torch.uint8)),
+                        (c.k_scales, small.k_scales), (c.v_scales, small.v_scales)):
+        last = big[1, :, 1]
+        at = slice(-64, None) if big.dim() == 5 else slice(-1, None)
+        assert torch.equal(last[:, at], little[0, :, 0]) and (little != 0).any()
+        last[:, at].zero_()
+        assert not any(big[l, h].any() for l in range(L) for h in range(Hkv))
+    c.check(), small.check()
