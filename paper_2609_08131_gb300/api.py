@@ -488,7 +488,8 @@ class Cache8:
     def part(self, layers=slice(None), slots=slice(None), tokens: int | None = None):
         """A handle (with a workspace of its own, for up to ``tokens`` queries; None: as many as here) of the given
         layers and slots (slices) of these tensors: a layer's attention in a model's loop, or the slots of the requests
-        whose prompts have arrived. Where it takes all slots its ``lengths`` are these."""
+        whose prompts have arrived. Where it takes all slots its ``lengths`` are these, so that every layer's ``append``
+        or ``store`` sets them: appends layer by layer take a copy from before the step as their ``lengths``."""
         at = (layers, slice(None), slots)
         return Cache8(self.k[at], self.v[at], self.k_scales[at], self.v_scales[at], self.lengths[slots],
                       self.Hq, self.scale, self.tokens if tokens is None else tokens)

@@ -69,3 +69,23 @@ def test_rows_at_the_very_end_of_slots_whose_offsets_pass_32_bits():
         last[:, at].zero_()
         assert not any(big[l, h].any() for l in range(L) for h in range(Hkv))
     c.check(), small.check()
+
+
+def test_a_step_entered_layer_by_layer():
+    g, S, L, Hkv, T = gen(830), 3, 3, 2, 4
+    whole, by_layer = (api.Cache8.empty(S, L, 4, Hkv, 128, device=DEV) for _ in range(2))
+    k0, v0 = (randn(g, S, L, Hkv, 62, D, dtype=BF16) for _ in range(2))
+    path, taken = ints([[0, 2, 3, -1], [1, -1, -1, -1], [-1] * 4]), ints([3, 1, 0])
+    k, v = (3 * randn(g, S, L, Hkv, T, D, dtype=BF16) for _ in range(2))
+    for c in (whole, by_layer):
+        c.store(k0, v0, ints([62, 0, 30]))
+    whole.append(k, v, path, taken)
+    before = by_layer.lengths.clone()
+    for l in range(L):
+        at = slice(l, l + 1)
+        by_layer.part(layers=at).append(k[:, at], v[:, at], path, taken, lengths=before)
+    assert by_layer.lengths.tolist() == whole.lengths.tolist() == [65, 1, 30]
+    for name in ("k", "v"):
+        assert torch.equal(getattr(whole, name).view(torch.uint8), getattr(by_layer, name).view(torch.uint8))
+        assert torch.equal(getattr(whole, name + "_scales"), getattr(by_layer, name + "_scales"))
+    by_layer.check()
