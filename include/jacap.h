@@ -710,14 +710,17 @@ jacap_status jacap_bytes_attend(const jacap_byte_cache* cache, const jacap_atten
 
 /*
  * Which of a request's drafted tokens the target model accepts, and the token that it
- * draws after them, such that the tokens are distributed as the target's own. From the
+ * draws after them, such that the tokens are distributed as the target's own (where the drafted tokens that follow the
+ * same node were drawn independently of each other from its row of q, not without replacement). From the
  * root (what follows the cached tokens) the walk tries the drafted tokens that follow the node it
  * is at, by their index: with r the target's probabilities there and Z their sum, Z = 1, drafted
  * token t = (x, its random number u_t) is accepted if u_t Z q(x) < r(x), and the walk goes to it;
  * else r becomes max(r - Z q, 0) and Z the sum of that. Where no drafted token is left, the next
  * token is the least y with r(0) + .. + r(y) > u_T (r(0) + .. + r(V - 1)) (the target's own probabilities in r's
  * place where r is all zero). Without q each drafted token counts as given: q is 1 at x, and a rejection takes
- * x out of r. Sums and comparisons have 45 bits or more.
+ * x out of r and r(x) out of Z, which is the sum of r as far as the target's probabilities sum to 1 (rows rounded to bf16
+ * may be off by some 2^-9, and then the siblings of a token with nearly all of a row are accepted that much too seldom or
+ * too often). Sums and comparisons have 45 bits or more (products below 2^-100 fewer).
  *   num_seqs, tokens, vocab  S; T, 1 to 64 (else JACAP_ERR_UNSUPPORTED); V, at least 1
  *   tokens_in      device int32 [S][T] the drafted tokens (one outside [0, V) is rejected, counts as no
  *                  token and is reported)

@@ -616,8 +616,8 @@ class DraftVerifier:
     def run(self, tokens, p, u, q=None, tree=None, draft_lens=None, stream=None):
         """tokens int32 [S, T], the drafted ones; p [S, T + 1, V] (float32 or bf16) the target's probabilities
         after the cached tokens and after each drafted one; u float32 [S, T + 1] random numbers in [0, 1); q [S,
-        T (or T + 1), V], as p, the probabilities that the tokens following row t - 1 were drawn from (None: they
-        were chosen, not drawn); tree int64 [S, T] (``tree_masks``; None: a chain); draft_lens int32 [S] drafted
+        T (or T + 1), V], as p, the probabilities that the tokens following row t - 1 were drawn from, independently
+        of each other where several follow it (None: they were chosen, not drawn; then p's rows should sum to 1); tree int64 [S, T] (``tree_masks``; None: a chain); draft_lens int32 [S] drafted
         tokens of each request (None: T). Returns (path, taken, next): the accepted tokens' indices in order,
         then -1, their number, and the token drawn after them."""
         h, dev, S, T, V = self._how, self.device, self.S, self.T, self.V

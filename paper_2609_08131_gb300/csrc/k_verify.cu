@@ -1,7 +1,8 @@
 // k_verify.cu - which of a request's drafted tokens the target model accepts, from given random numbers.
 // At a node of the tree, r_0 = p (the target's probabilities after it), Z_0 = 1, and for its drafted tokens x in turn
 //   x is accepted if u Z_j q(x) < r_j(x), else r_{j+1} = max(r_j - Z_j q, 0), Z_{j+1} = sum r_{j+1}
-// (without q: r_j loses x); where none is left, the next token is the least y whose partial sum of r_j passes u_T sum r_j.
+// (without q: r_j loses x, and Z_j r_j(x), with no sum over the row; where p does not sum to 1 Z is not quite r's); where
+// none is left, the next token is the least y whose partial sum of r_j passes u_T sum r_j.
 // As a value that is 0 stays 0, r_j = max(p - c_j q, 0) with c_j = Z_0 + .. + Z_{j-1}: one step, however many rejections.
 //
 // The tests need p and q at the drafted tokens alone, which all are fetched at once; rows are read only where a
