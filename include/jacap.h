@@ -650,11 +650,12 @@ typedef struct {
 } jacap_byte_cache;
 
 /*
- * Bytes of the workspace of the calls on such a cache, with attention of up to `tokens` (1 to
- * 64) queries per request and head; 0 for a cache that is refused. Its first JACAP_ATTEND_ZERO_BYTES +
- * 4 num_seqs bytes are zeroed once before the first call: a status word, and counters that every call leaves at zero. Calls that share one (of several
- * `tokens` too) come one after the other. A length, count or path entry outside its range is clamped and
- * reported in the word (JACAP_ERR_INVALID_ARG), which stays set until it is zeroed.
+ * Bytes of the workspace of the calls on such a cache, with attention of up to `tokens` (1 to 64)
+ * queries per request and head; 0 for a cache that is refused. Its first JACAP_ATTEND_ZERO_BYTES +
+ * 4 num_seqs bytes are zeroed once before the first call: a status word, and counters that every
+ * call leaves at zero. Calls that share one (of several `tokens` too) come one after the other. A
+ * length, count or path entry outside its range is clamped and reported in the word
+ * (JACAP_ERR_INVALID_ARG), which stays set until it is zeroed.
  */
 size_t jacap_bytes_workspace(const jacap_byte_cache* cache, int32_t tokens);
 

@@ -542,9 +542,10 @@ class Cache8:
     def attend(self, q, k_draft=None, v_draft=None, tree=None, lengths=None, draft_lens=None, stream=None):
         """Attention of each request's last queries over its slot and, if given, over drafted tokens that are
         not in it yet (``jacap_bytes_attend``): q [S, L, Hq, T, 128], k_draft and v_draft [S, L, Hkv, T, 128]
-        (bf16, T at most the handle's ``tokens``), tree int64 [S, T] (``tree_masks``; None: a chain), lengths int32 [S] (None: the slots'
-        own), draft_lens int32 [S] queries of each request (None: T; rows behind are left as they were). Returns (o
-        [S, L, Hq, T, 128] bf16, lse [S, L, Hq, T] float32), which the next call of as many queries overwrites."""
+        (bf16, T at most the handle's ``tokens``), tree int64 [S, T] (``tree_masks``; None: a chain), lengths
+        int32 [S] (None: the slots' own), draft_lens int32 [S] queries of each request (None: T; rows behind
+        are left as they were). Returns (o [S, L, Hq, T, 128] bf16, lse [S, L, Hq, T] float32), which the next
+        call of as many queries overwrites."""
         a, dev, bf16 = self._attn, self.device, torch.bfloat16
         if not isinstance(q, torch.Tensor) or q.dim() != 5:
             raise ValueError("q must be [S, L, Hq, T, 128]")
@@ -616,8 +617,9 @@ class DraftVerifier:
     def run(self, tokens, p, u, q=None, tree=None, draft_lens=None, stream=None):
         """tokens int32 [S, T], the drafted ones; p [S, T + 1, V] (float32 or bf16) the target's probabilities
         after the cached tokens and after each drafted one; u float32 [S, T + 1] random numbers in [0, 1); q [S,
-        T (or T + 1), V], as p, the probabilities that the tokens following row t - 1 were drawn from, independently
-        of each other where several follow it (None: they were chosen, not drawn; then p's rows should sum to 1); tree int64 [S, T] (``tree_masks``; None: a chain); draft_lens int32 [S] drafted
+        T (or T + 1), V], as p, the probabilities that the tokens following row t - 1 were drawn from,
+        independently of each other where several follow it (None: they were chosen, not drawn; then p's rows
+        should sum to 1); tree int64 [S, T] (``tree_masks``; None: a chain); draft_lens int32 [S] drafted
         tokens of each request (None: T). Returns (path, taken, next): the accepted tokens' indices in order,
         then -1, their number, and the token drawn after them."""
         h, dev, S, T, V = self._how, self.device, self.S, self.T, self.V

@@ -4,42 +4,44 @@
 //   l_i = scale ks_b q_r . k8_i,   o_r = sum_i exp(l_i - M) vs_b v8_i / Z,   Z = sum_i exp(l_i - M),
 // b being token i's block; drafted tokens as in k_attend.cu.
 //
-// The tensor cores multiply the cache's bytes as they lie in memory, so that nothing is converted per token:
-// what meets them is split into two parts of 8 bits instead, hi = e4m3(x) and lo = e5m2(x - hi). A bf16 value has
-// eight significant bits: e4m3 keeps four, what is left is at most half of their last step and three bits of it remain,
-// as many as e5m2 has, so that x = hi + lo exactly (from e4m3's lowest normal value, 2^-6, on; below that to 2^-14), and
+// The tensor cores multiply the cache's bytes as they lie in memory, so that nothing is converted per token: what
+// meets them is split into two parts of 8 bits instead, hi = e4m3(x) and lo = e5m2(x - hi). A bf16 value has eight
+// significant bits: e4m3 keeps four, what is left is at most half of their last step and three bits of it remain, as
+// many as e5m2 has, so that x = hi + lo exactly (from e4m3's lowest normal value, 2^-6, on; below that to 2^-14), and
 //   q . k8 = hi . k8 + lo . k8
-// are two products into one accumulator. The softmax weights are split alike, which rounds them to
-// eight bits, as they would be for a product in bf16. (e5m2, not e4m3 again, because of its lowest step, 2^-16: with e4m3
-// weights below 2^-10 would be lost, and with them the output of rows whose largest weight meets a value near zero.)
+// are two products into one accumulator. The softmax weights are split alike, which rounds them to eight bits, as
+// they would be for a product in bf16. (e5m2, not e4m3 again, because of its lowest step, 2^-16: with e4m3 weights
+// below 2^-10 would be lost, and with them the output of rows whose largest weight meets a value near zero.)
 //
-// S is computed transposed, S^T = K8 Q^T: tokens are the 128 lanes of tensor memory and rows its columns (16, 32 or 64
-// per CTA, padded), so that one query row costs a small product, not one of 128 rows. A softmax warp
-// has 32 tokens, a lane one token of all rows: the maximum over a tile is a warp's reduction and an
-// exchange of 4 values per row; the sums stay with the lanes until the item's end. O^T = V8^T P^T
-// accumulates with channels as lanes.
+// S is computed transposed, S^T = K8 Q^T: tokens are the 128 lanes of tensor memory and rows its columns (16, 32 or
+// 64 per CTA, padded), so that one query row costs a small product, not one of 128 rows. A softmax warp has 32
+// tokens, a lane one token of all rows: the maximum over a tile is a warp's reduction and an exchange of 4 values per
+// row; the sums stay with the lanes until the item's end. O^T = V8^T P^T accumulates with channels as lanes.
 //
-// A weight is w = exp2(l log2 e + log2 vs_b - ref_r), which takes in V's scale, and fits e4m3 (448) as ref_r follows the
-// rows' maxima: a tile whose largest weight would pass 2^8.75, or not reach 2^0.25, moves ref_r so that it is
-// 2^4.5, and the accumulators are rescaled. (Downwards too, so that weights that are small beside one seen before, but not
-// beside their neighbours, keep their bits; 2^-40 below the largest one seen it stops.) Where one of a tile's four
-// quarters has none above 2^-6 of the largest (a prompt's first token may have nearly all of the weight, and a value
-// near zero), the largest is put to 2^8.5 instead, so that the others keep eight bits down to 2^-14.5 of it. Z takes w / vs_b.
+// A weight is w = exp2(l log2 e + log2 vs_b - ref_r), which takes in V's scale, and fits e4m3 (448) as ref_r follows
+// the rows' maxima: a tile whose largest weight would pass 2^8.75, or not reach 2^0.25, moves ref_r so that it is
+// 2^4.5, and the accumulators are rescaled. (Downwards too, so that weights that are small beside one seen before,
+// but not beside their neighbours, keep their bits; 2^-40 below the largest one seen it stops.) Where one of a tile's
+// four quarters has none above 2^-6 of the largest (a prompt's first token may have nearly all of the weight, and a
+// value near zero), the largest is put to 2^8.5 instead, so that the others keep eight bits down to 2^-14.5 of it. Z
+// takes w / vs_b.
 //
-// That holds while V's scales are of ordinary size. Beside a block of 2^120 (of a value that is infinite) or 2^-126 the
-// other blocks' weights, or its own part of Z, would leave float32's range, and eight bits long before. So a block whose
-// scale is outside 2^-32 .. 2^16 (values all below 1e-7, or one above 2.9e7) counts in Z with the scale of an ordinary one,
-// and its part of the output is not left to the tensor cores but added at the item's end, one by one (add_far).
+// That holds while V's scales are of ordinary size. Beside a block of 2^120 (of a value that is infinite) or 2^-126
+// the other blocks' weights, or its own part of Z, would leave float32's range, and eight bits long before. So a
+// block whose scale is outside 2^-32 .. 2^16 (values all below 1e-7, or one above 2.9e7) counts in Z with the scale
+// of an ordinary one, and its part of the output is not left to the tensor cores but added at the item's end, one by
+// one (add_far).
 //
-// CTAs and splits are those of k_attend.cu: persistent CTAs with even shares of all tiles (128 tokens: 16 KB of K, 16 of
-// V); a split's sums are joined by the CTA that finishes its unit's last one. More than 64 rows: K and V
-// are read again for each 64. (Turning the tiles to bf16 in shared memory for products of 128 rows and more takes 151 us
-// for 128 rows of 8 heads over 31290 tokens, this 58 us; 256 rows 123 and 87 us; only 512 rows gain, 134 and 149 us.)
+// CTAs and splits are those of k_attend.cu: persistent CTAs with even shares of all tiles (128 tokens: 16 KB of K, 16
+// of V); a split's sums are joined by the CTA that finishes its unit's last one. More than 64 rows: K and V are read
+// again for each 64. (Turning the tiles to bf16 in shared memory for products of 128 rows and more takes 151 us for
+// 128 rows of 8 heads over 31290 tokens, this 58 us; 256 rows 123 and 87 us; only 512 rows gain, 134 and 149 us.)
 //
-// Measured, 32 query heads of 8 KV heads: 16 slots of about 2100 tokens 22 us (69 MB, 10 us at a copy's rate; start, end and
-// join take some 9 us), a chain of 8 over 131011 tokens 63 us (268 MB, 4.2 TB/s, floor 39.5 us), 48 slots of 28 / 4 heads
-// 56 us (278 MB, 5 TB/s, floor 41 us). With 16 and 32 rows the loads' latency and the softmax chain bound it, with 64 the
-// chain: 16 trees of 64 over 46 to 16383 tokens, 40 / 8 heads, 313 us, 55 % of the issue slots, tensor pipe 20 %.
+// Measured, 32 query heads of 8 KV heads: 16 slots of about 2100 tokens 22 us (69 MB, 10 us at a copy's rate; start,
+// end and join take some 9 us), a chain of 8 over 131011 tokens 63 us (268 MB, 4.2 TB/s, floor 39.5 us), 48 slots of
+// 28 / 4 heads 56 us (278 MB, 5 TB/s, floor 41 us). With 16 and 32 rows the loads' latency and the softmax chain
+// bound it, with 64 the chain: 16 trees of 64 over 46 to 16383 tokens, 40 / 8 heads, 313 us, 55 % of the issue slots,
+// tensor pipe 20 %.
 #include "k_attend_body.cuh"
 
 namespace jacap {
@@ -47,8 +49,8 @@ namespace jacap {
 constexpr int AB_TOK = 128, AB_TILE = AB_TOK * D;  // bytes of a tile of K or V; a drafted one: 64 tokens of bf16
 constexpr int AB_QUEUE = 5;  // items published and not yet done with by all
 // A CTA of N rows. Warps: 0 TMA producer, 1 MMA, then two teams of CG softmax groups (four warps, GR rows each), then
-// those that fetch rows. A softmax is a chain of some 2000 to 4600 cycles, of which a warp waits most: the teams take turns
-// at the tiles, each with accumulators and references of its own, which meet at an item's end.
+// those that fetch rows. A softmax is a chain of some 2000 to 4600 cycles, of which a warp waits most: the teams take
+// turns at the tiles, each with accumulators and references of its own, which meet at an item's end.
 constexpr int AB_TURNS = 2, AB_SBUF = 4;  // teams, and tiles' S at a time
 template <int N>
 struct AbCfg {
@@ -111,8 +113,8 @@ __device__ __forceinline__ float warp_max(float x) {  // (without NaN)
   asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
   return r;
 }
-// Four values' parts, hi = e4m3(x) and lo = e5m2(x - hi), packed (a's in the low bytes). The difference is taken in 16 bits
-// (eleven significant ones, exact from there on), two at a time.
+// Four values' parts, hi = e4m3(x) and lo = e5m2(x - hi), packed (a's in the low bytes). The difference is taken in
+// 16 bits (eleven significant ones, exact from there on), two at a time.
 __device__ __forceinline__ void split_f8(float a, float b, float c, float d, uint32_t& hi, uint32_t& lo) {
   asm("{\n\t.reg .b16 h0, h1, l0, l1;\n\t.reg .b32 v0, v1, x0, x1;\n\t"
       "cvt.rn.satfinite.e4m3x2.f32 h0, %3, %2;\n\tcvt.rn.satfinite.e4m3x2.f32 h1, %5, %4;\n\t"
@@ -290,8 +292,8 @@ __device__ __noinline__ void join_rows(const Dims& dm, const AttendArgs& a, cons
   }
 }
 
-// mbar_wait with few instructions between two looks (which the hardware holds back for a while by itself): the warps that
-// wait share the issue slots with those that do not.
+// mbar_wait with few instructions between two looks (which the hardware holds back for a while by itself): the warps
+// that wait share the issue slots with those that do not.
 __device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, uint32_t* status, volatile int* abort) {
   if (mbar_try_wait(bar, parity)) return true;
   const unsigned long long t0 = globaltimer();
@@ -308,9 +310,9 @@ __device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, uint32_t
   }
 }
 
-// What such blocks of the item add to rows c0 .. c0 + 3 (of `nrow`), one channel (that of the thread) each. All of the
-// group's 128 threads: two rows' logits of a token each, then the sums over the block's tokens. An infinite value is added
-// as it is, whatever its weight.
+// What such blocks of the item add to rows c0 .. c0 + 3 (of `nrow`), one channel (that of the thread) each. All of
+// the group's 128 threads: two rows' logits of a token each, then the sums over the block's tokens. An infinite value
+// is added as it is, whatever its weight.
 __device__ __forceinline__ float4 far_values(const Dims& dm, const AttendArgs& a, const ByteScales& sc, const AtUnit& x,
                                           int c0, int nrow, const float2* norm, float (*w)[64], int bar, int tok) {
   const int64_t scales = x.l * sc.strides[0] + x.g * sc.strides[1] + x.s * sc.strides[2];
@@ -358,7 +360,8 @@ __device__ __forceinline__ float4 far_values(const Dims& dm, const AttendArgs& a
   return make_float4(y[0], y[1], y[2], y[3]);
 }
 
-// Such a block's rows of V's tile (place n of the ring) are zeros to the tensor cores: a warp's 32. False: the wait failed.
+// Such a block's rows of V's tile (place n of the ring) are zeros to the tensor cores: a warp's 32. False: the wait
+// failed.
 template <int N>
 __device__ __noinline__ bool drop_far(AbSmem<N>& sh, uint8_t* ring, uint32_t n, int quarter, int lane, uint32_t* status) {
   constexpr int RING = AbCfg<N>::RING;
@@ -371,7 +374,8 @@ __device__ __noinline__ bool drop_far(AbSmem<N>& sh, uint8_t* ring, uint32_t n, 
 }
 
 // An item with such blocks, whose first tile was team `one`'s: what both teams have of a row, normalised, and the far
-// values come to be that team's sums, with a factor of 1, and the other's have one of 0. All threads of the softmax groups.
+// values come to be that team's sums, with a factor of 1, and the other's have one of 0. All threads of the softmax
+// groups.
 template <int N>
 __device__ __noinline__ void add_far(const Dims& dm, const AttendArgs& a, const ByteScales& sc, AbSmem<N>& sh, uint32_t k,
                                      int one) {
@@ -427,7 +431,8 @@ __global__ void __launch_bounds__(AbCfg<N>::THREADS, AbCfg<N>::PER_SM)
   AbSmem<N>& sh = *(AbSmem<N>*)(ps + 2 * WBUF);
   static_assert(4 * PART + 2 * WBUF + sizeof(AbSmem<N>) >= 8192, "what a drafted tile's product reads behind the ring");
 
-  // (numbers that are a warp's own, and known to be: the tensor instructions take their operands from uniform registers)
+  // (numbers that are a warp's own, and known to be: the tensor instructions take their operands from uniform
+  // registers)
   const auto uniform = [](int x) { return __reduce_max_sync(0xffffffffu, x); };
   const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
   const int R = dm.G * dm.window;
@@ -493,8 +498,8 @@ __global__ void __launch_bounds__(AbCfg<N>::THREADS, AbCfg<N>::PER_SM)
       uint32_t published = 0, st = 0, pass = 0;  // items; the ring's place, and how often it was filled
       AtUnit x, next;
       bool ok = true, first = true;
-      // Item x; the item after it is published a few loads later, so that its rows are on their way long before they are
-      // needed. (One place for each step, as a CTA runs most of its instructions for the first time.)
+      // Item x; the item after it is published a few loads later, so that its rows are on their way long before they
+      // are needed. (One place for each step, as a CTA runs most of its instructions for the first time.)
       for (int tk = 0, tv = 0, end = 0, when = 0; ok;) {  // next tile of K and of V, tiles
         if (tk + tv == when) {
           share.next(next, N);
@@ -539,10 +544,10 @@ __global__ void __launch_bounds__(AbCfg<N>::THREADS, AbCfg<N>::PER_SM)
       }
     }
   } else if (warp == 1) {
-    // ------------------------------------------------ MMA issuer ----------
-    // (All lanes go through it, so that what they compute is uniform; one issues, some 70 cycles a product whatever N
-    // is. Both parts of the weights in one product of twice the columns, and of the rows with 32, gained nothing: an issue
-    // that ends sooner waits longer for the weights.)
+    // ------------------------------------------------ MMA issuer ---------- (All lanes go through it, so that what
+    // they compute is uniform; one issues, some 70 cycles a product whatever N is. Both parts of the weights in one
+    // product of twice the columns, and of the rows with 32, gained nothing: an issue that ends sooner waits longer
+    // for the weights.)
     const bool leader = elect_one();
     constexpr uint32_t IDESC_S[2] = {idesc_e4m3_f32(128, N, 0, 0, false), idesc_e4m3_f32(128, N, 0, 0, true)};  // hi, lo
     constexpr uint32_t IDESC_O[2] = {idesc_e4m3_f32(128, N, 1, 1, false), idesc_e4m3_f32(128, N, 1, 1, true)};
@@ -573,7 +578,8 @@ __global__ void __launch_bounds__(AbCfg<N>::THREADS, AbCfg<N>::PER_SM)
 #pragma unroll 1
       for (int i = 0; ok && i < nt + TURNS; ++i) {
         if (i < nt) {
-          // S^T = K Q^T of tile i goes where that of the tile SBUF before was, which was read before its product was issued
+          // S^T = K Q^T of tile i goes where that of the tile SBUF before was, which was read before its product was
+          // issued
           if (!(ok = landed())) break;
           const uint32_t b = (it + i) % SBUF, d = tmem + N * b;
           const uint64_t kd = kd0 + (uint64_t)(st * (AB_TILE >> 4));
