@@ -274,6 +274,7 @@ __device__ __noinline__ void join_rows(const Dims& dm, const AttendArgs& a, cons
       if (j0 > 0) w = ml(j0 + lane, r);
       // (a split that saw nothing has the reference -inf and the sum 0, one of NaN only -inf and NaN)
       const float f = w.x == m ? (w.x == -INFINITY && w.y == 0.f ? 0.f : 1.f) : ex2(w.x - m);
+      const float fo = fmaxf(f, 0x1p-149f);  // (what is not finite stays so, whatever its split's weight)
       float z = w.y * f;
 #pragma unroll
       for (int off = 16; off >= 1; off >>= 1) z += __shfl_xor_sync(0xffffffffu, z, off);
@@ -282,8 +283,7 @@ __device__ __noinline__ void join_rows(const Dims& dm, const AttendArgs& a, cons
 #pragma unroll 4
       for (int j = 0; j < n; ++j) {
         const float4 v = __ldcg((const float4*)(a.opart + (at(j0 + j) + r) * D) + lane);
-        const float fj = __shfl_sync(0xffffffffu, f, j);
-        if (fj == 0.f) continue;
+        const float fj = __shfl_sync(0xffffffffu, fo, j);
         y.x = fmaf(v.x, fj, y.x), y.y = fmaf(v.y, fj, y.y), y.z = fmaf(v.z, fj, y.z), y.w = fmaf(v.w, fj, y.w);
       }
     }

@@ -207,6 +207,32 @@ def test_attend_far_scales_in_several_splits(T, Hq, Hkv):
         assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(t.c.attend(q), again))
 
 
+
+@pytest.mark.parametrize("T,Hq,Hkv,n", [(1, 4, 1, 20032), (6, 8, 2, 9000), (40, 8, 1, 20032), (1, 8, 2, 300)])
+def test_attend_values_that_are_not_finite_at_tokens_of_hardly_any_weight(T, Hq, Hkv, n):
+    """As plain sums have them: whichever splits there are, and however small their weight beside another's."""
+    g = gen(724)
+    t = Slots(1, 1, Hq, Hkv, n)
+    q, k = toward(g, 1, 1, Hq, Hkv, n, T)
+    v = randn(g, 1, 1, Hkv, n, D)
+    k[:, :, :, 0] = 300.0 / math.sqrt(D)  # e^300 of the others' weight
+    v[:, :, :, n // 2, 3], v[:, :, :, n - 1, 5], v[:, :, :, 7, 8], v[:, :, :, n - 2, 100] = (math.inf, -math.inf, math.inf,
+                                                                                            math.nan)
+    t.store(k, v)
+    kd, vd = (randn(g, 1, 1, Hkv, T, D, dtype=BF16) * 0.3 for _ in range(2))
+    for drafted in ((None, None), (kd, vd)):
+        if drafted[0] is not None:
+            vd[:, :, :, 0, 60], vd[:, :, :, 0, 61] = math.inf, math.nan  # of the first drafted token, which all see
+        o, lse = t.c.attend(q, *drafted)
+        assert lse.isfinite().all()
+        for c, want in ((3, math.inf), (5, -math.inf), (8, math.inf)):
+            assert (o[..., c] == want).all()
+        assert o[..., 100].isnan().all()
+        if drafted[0] is not None:
+            assert (o[..., 60] == math.inf).all() and o[..., 61].isnan().all()
+        assert (~o.isfinite()).sum() == o[..., 0].numel() * (4 if drafted[0] is None else 6)
+
+
 # ------------------------------------------------------------------- queries ----
 @pytest.mark.parametrize("T", [1, 6, 9, 40])
 def test_attend_rows_of_very_different_sizes(T):
