@@ -30,17 +30,18 @@
 // the other blocks' weights, or its own part of Z, would leave float32's range, and eight bits long before. So a
 // block whose scale is outside 2^-32 .. 2^16 (values all below 1e-7, or one above 2.9e7) counts in Z with the scale
 // of an ordinary one, and its part of the output is not left to the tensor cores but added at the item's end, one by
-// one (add_far).
+// one (add_far): one such block in every slot and head makes 16 slots' 24 us 35, a chain's 64 us 109 and the trees'
+// 322 us 796.
 //
 // CTAs and splits are those of k_attend.cu: persistent CTAs with even shares of all tiles (128 tokens: 16 KB of K, 16
 // of V); a split's sums are joined by the CTA that finishes its unit's last one. More than 64 rows: K and V are read
 // again for each 64. (Turning the tiles to bf16 in shared memory for products of 128 rows and more takes 151 us for
 // 128 rows of 8 heads over 31290 tokens, this 58 us; 256 rows 123 and 87 us; only 512 rows gain, 134 and 149 us.)
 //
-// Measured, 32 query heads of 8 KV heads: 16 slots of about 2100 tokens 22 us (69 MB, 10 us at a copy's rate; start,
-// end and join take some 9 us), a chain of 8 over 131011 tokens 63 us (268 MB, 4.2 TB/s, floor 39.5 us), 48 slots of
-// 28 / 4 heads 56 us (278 MB, 5 TB/s, floor 41 us). With 16 and 32 rows the loads' latency and the softmax chain
-// bound it, with 64 the chain: 16 trees of 64 over 46 to 16383 tokens, 40 / 8 heads, 313 us, 55 % of the issue slots,
+// Measured, 32 query heads of 8 KV heads: 16 slots of about 2100 tokens 24.5 us (69 MB, 10 us at a copy's rate; start,
+// end and join take some 9 us), a chain of 8 over 131011 tokens 64 us (268 MB, 4.2 TB/s, floor 39.5 us), 48 slots of
+// 28 / 4 heads 57 us (278 MB, 4.9 TB/s, floor 41 us). With 16 and 32 rows the loads' latency and the softmax chain
+// bound it, with 64 the chain: 16 trees of 64 over 46 to 16383 tokens, 40 / 8 heads, 321 us, 55 % of the issue slots,
 // tensor pipe 20 %.
 #include "k_attend_body.cuh"
 
