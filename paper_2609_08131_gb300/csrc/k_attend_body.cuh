@@ -256,9 +256,9 @@ struct AtShares {
   AtDivisor by;               // per
   int l, g, rb, s;
 
-  // Virtual tiles of request s0 + lane (as at_unit counts them, at least one, and its start), and of requests s0 .. s0 +
-  // lane. (Not inlined: a CTA's first instructions come from L2, at some 40 cycles each, and these come twice.)
-  static __device__ __noinline__ uint2 count(const Dims& dm, const AttendArgs& a, const int32_t* cu, int s0, int lane) {
+  // Virtual tiles of request s0 + lane (as at_unit counts them, at least one, and its start), and of requests s0 ..
+  // s0 + lane. (Inlined at both places: as a function 16 slots took 37.5 us instead of 36.8, in bytes 24.5, not 24.2.)
+  static __device__ __forceinline__ uint2 count(const Dims& dm, const AttendArgs& a, const int32_t* cu, int s0, int lane) {
     uint32_t own = 0;
     if (s0 + lane < dm.S) {
       const AtLive x = at_live(dm, a, cu, s0 + lane);
