@@ -841,7 +841,7 @@ __global__ void __launch_bounds__(AbCfg<N>::THREADS, AbCfg<N>::PER_SM)
           __syncwarp();
           // the tile before's weights are read (and its sums in the accumulators, should they be rescaled)
           if (i >= TURNS) {
-            ok = wait_for(smem_u32(&sh.pvdone[b]), ((it - TURNS) >> 1) & 1, a.status, abort);
+            ok = wait_for(smem_u32(&sh.pvdone[b]), ((it - TURNS) >> 1) & 1, a.status, abort) && ok;
             tc_fence_after();
             if (__any_sync(0xffffffffu, f != 1.f)) {  // (the same in all warps of the group)
 #pragma unroll
