@@ -702,7 +702,7 @@ jacap_status jacap_bytes_append(const jacap_byte_cache* cache, jacap_dtype dtype
  * their product with V (those of less than 2^-6 of the largest of 128 neighbouring tokens, V's
  * scale included, to 2^-14 of that or, where it is more, 2^-58 of the row's largest).
  * Blocks whose V's scale is below 2^-32 or above 2^16 are added to the output in float32, one value after the other
- * (slower; sums with finite values from 2^95 on may become infinite): an infinite value makes its own channel infinite
+ * (slower; sums with finite values from 2^110 on may become infinite): an infinite value makes its own channel infinite
  * and nothing else.
  */
 jacap_status jacap_bytes_attend(const jacap_byte_cache* cache, const jacap_attention* attn, int32_t tokens,

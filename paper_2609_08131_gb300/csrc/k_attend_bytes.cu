@@ -382,7 +382,22 @@ __device__ __noinline__ void add_far(const Dims& dm, const AttendArgs& a, const 
                                      int one) {
   const int warp = threadIdx.x >> 5, gi = (warp - 2) >> 2, tok = (warp & 3) * 32 + (threadIdx.x & 31);
   const AtUnit& x = sh.queue[k % AB_QUEUE];
-  const int nrow = min(dm.G * dm.window - x.r0, N);
+  const int nrow = min(dm.G * dm.window - x.r0, N), r = threadIdx.x - 64;
+  if (x.nsp > 1) {
+    // A split's reference may be 2^40 below a weight of an earlier tile: the large values want its sum between 1 and 2.
+    if (r < nrow) {  // (the thread has written them)
+      float2* ml = (float2*)a.mlpart + (int64_t)at_slot<__nv_bfloat16>(a, x, x.split) * a.srows + r;
+      const float2 z = *ml;
+      if (z.y > 0.f && z.y < INFINITY) {
+        const int e = min((int)(__float_as_uint(z.y) >> 23) - 127, 126);
+        const float by = __uint_as_float((uint32_t)(127 - e) << 23);
+        *ml = make_float2(z.x + (float)e, z.y * by);
+        sh.norm[r].x = z.x + (float)e;
+        sh.inv[0][r] *= by, sh.inv[1][r] *= by;
+      }
+    }
+    named_barrier_sync(1, 128 * AbCfg<N>::GROUPS);
+  }
   const uint32_t o0 = sh.tmem + AB_SBUF * N + ((uint32_t)((warp & 3) * 32) << 16);
 #pragma unroll 1
   for (int c0 = 4 * gi; c0 < nrow; c0 += 4 * AbCfg<N>::GROUPS) {

@@ -208,6 +208,22 @@ def test_attend_far_scales_in_several_splits(T, Hq, Hkv):
 
 
 
+@pytest.mark.parametrize("T,Hq,Hkv", HEADS)
+@pytest.mark.parametrize("n", [170, 426, 1300])
+@pytest.mark.parametrize("size", [2.0 ** 60, 2.0 ** 85, 2.0 ** 105])
+def test_attend_large_values_before_tokens_of_hardly_any_weight(size, n, T, Hq, Hkv):
+    """A tile whose weights are far below those of the tiles before it, in the same split: the large value stays finite."""
+    g = gen(725)
+    t = Slots(1, 1, Hq, Hkv, n)
+    q, k = toward(g, 1, 1, Hq, Hkv, n, T)
+    v = randn(g, 1, 1, Hkv, n, D)
+    k[:, :, :, n - 91] = 60.0 / math.sqrt(D)
+    v[:, :, :, n - 91, 9] = size
+    t.store(k, v)
+    check(t, q)
+    check(t, q, *(randn(g, 1, 1, Hkv, T, D, dtype=BF16) * 0.3 for _ in range(2)))
+
+
 @pytest.mark.parametrize("T,Hq,Hkv,n", [(1, 4, 1, 20032), (6, 8, 2, 9000), (40, 8, 1, 20032), (1, 8, 2, 300)])
 def test_attend_values_that_are_not_finite_at_tokens_of_hardly_any_weight(T, Hq, Hkv, n):
     """As plain sums have them: whichever splits there are, and however small their weight beside another's."""
