@@ -38,11 +38,11 @@
 // again for each 64. (Turning the tiles to bf16 in shared memory for products of 128 rows and more takes 151 us for
 // 128 rows of 8 heads over 31290 tokens, this 58 us; 256 rows 123 and 87 us; only 512 rows gain, 134 and 149 us.)
 //
-// Measured, 32 query heads of 8 KV heads: 16 slots of about 2100 tokens 24.3 us (69 MB, 10 us at a copy's rate; start,
-// end and join take some 9 us), a chain of 8 over 131011 tokens 63 us (268 MB, 4.3 TB/s, floor 39.5 us), 48 slots of
-// 28 / 4 heads 57 us (278 MB, 4.9 TB/s, floor 41 us). With 16 and 32 rows the loads' latency and the softmax chain
-// bound it, with 64 the chain: 16 trees of 64 over 46 to 16383 tokens, 40 / 8 heads, 321 us, 55 % of the issue slots,
-// tensor pipe 20 %.
+// Measured, 32 query heads of 8 KV heads: 16 slots of about 2100 tokens 24.4 us (69 MB, 10 us at a copy's rate;
+// start, end and join take some 9 us), a chain of 8 over 131011 tokens 63.6 us (268 MB, 4.2 TB/s, floor 39.5 us), 48
+// slots of 28 / 4 heads 57 us (278 MB, 4.9 TB/s, floor 41 us). With 16 and 32 rows the loads' latency and the softmax
+// chain bound it, with 64 the chain: 16 trees of 64 over 46 to 16383 tokens, 40 / 8 heads, 321 us, 55 % of the issue
+// slots, tensor pipe 20 %.
 #include "k_attend_body.cuh"
 
 namespace jacap {
